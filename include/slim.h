@@ -374,6 +374,125 @@ int slim_static_reset(void *stream);
 int slim_static_selftest_timeout(void *stream);
 
 /*
+ * Norm of every query and key head and rotation by position (what stands between a layer's projections and its
+ * attention), in one pass.  For a token and head x (128 bf16 values), in fp32, rounded to bf16 once at the end:
+ *   n_d = x_d * w_d / sqrt(mean(x^2) + eps)            (n = x where the weight is NULL)
+ *   a_i = position[axis[i]] * inv_freq[i],  i < rotary_dim / 2
+ *   (n_f, n_s) -> (n_f cos a_i - n_s sin a_i, n_f sin a_i + n_s cos a_i)
+ * for the pair (f, s) = (i, i + rotary_dim / 2), or (2 i, 2 i + 1) with interleaved != 0.  Dimensions from rotary_dim on
+ * are not rotated.  Angles are formed in fp64 (positions up to 2^31 keep fp32 accuracy).
+ *
+ *   inv_freq   device double [rotary_dim / 2], radians per position (any scaling of the frequencies is the caller's)
+ *   axis       device uint8 [rotary_dim / 2]: which of the token's positions turns pair i (time, height, width of an
+ *              image or video token); NULL with n_axes == 1.  Entries from n_axes on count as n_axes - 1.
+ *   q_weight, k_weight  device bf16 [128], 16-byte aligned, or NULL: no norm for that side
+ *   eps        > 0 where a weight is given
+ *   rotary_dim multiple of 16, 0 (no rotation) to 128;  n_axes 1 to 4
+ * The struct is host memory and is read during the call only.
+ */
+typedef struct slim_norm_rope {
+    const double  *inv_freq;
+    const uint8_t *axis;
+    const void    *q_weight;
+    const void    *k_weight;
+    float          eps;
+    int32_t        rotary_dim;
+    int32_t        n_axes;
+    int32_t        interleaved;
+} slim_norm_rope_t;
+
+/*
+ *   q, k       device bf16, token t's heads at t * q_stride (k_stride) elements, [heads][128] from there (the rows of a
+ *              fused projection); 16-byte aligned, strides multiples of 8 and at least heads * 128
+ *   q_out, k_out  device bf16 [n_tokens][Hq or Hkv][128], 16-byte aligned; may be the input itself where that is
+ *              contiguous, and must not overlap it otherwise
+ *   positions  device int32 [n_axes][n_tokens]; NULL only with rotary_dim == 0
+ *   Hq or Hkv may be 0 (its pointers are then ignored).  The results serve as q and k_new of the other calls.
+ */
+int slim_norm_rope(const slim_norm_rope_t *nr, const void *q, int64_t q_stride, void *q_out,
+                   const void *k, int64_t k_stride, void *k_out, const int32_t *positions,
+                   int32_t n_tokens, int32_t Hq, int32_t Hkv, void *stream);
+
+/*
+ * slim_norm_rope and slim_kv_append in one pass (Section 2.2: K and V go to the cache as they are produced): the queries
+ * are written to q_out, the normed and rotated keys and the values (as they are) are quantised straight into the cache.
+ * The keys are quantised from their fp32 values, without a rounding to bf16 in between.
+ *
+ *   v          device bf16 like k;  cu_new, start_pos  as for slim_kv_append
+ *   positions  device int32 [n_axes][n_tokens], or NULL: every axis holds the token's cache position.  (After an
+ *              eviction a token's position is no longer its cache position: pass it.)
+ *   n_tokens   rows of q, k and v; those from cu_new[B] on are neither read into anything nor written
+ */
+int slim_norm_rope_append(const slim_cache_t *cache, const slim_norm_rope_t *nr, const void *q, int64_t q_stride, void *q_out,
+                          const void *k, int64_t k_stride, const void *v, int64_t v_stride, const int32_t *positions,
+                          const int32_t *cu_new, const int32_t *start_pos, int32_t B, int32_t n_tokens, int32_t Hq, void *stream);
+
+/*
+ * Decode attention of a batch in which groups of sequences share a prefix: the page table rows of a group's sequences
+ * begin with the same pages.  The result is that of slim_attn_decode (with k_new / v_new, both or neither, that of
+ * slim_decode_step), but the prefix's keys and values are read and multiplied once for the whole group.
+ *
+ *   cu_group   device int32 [n_groups + 1]: group g is the sequences cu_group[g] .. cu_group[g + 1] - 1; the groups cover
+ *              all B sequences (a sequence that shares nothing may be a group of its own)
+ *   shared_len device int32 [B]: tokens of the prefix, the same for a group's sequences; counted in whole pages (a
+ *              length inside a page is cut to the pages before it), 0: nothing shared
+ *   kv_len     device int32 [B]: all cached tokens of a sequence, prefix included; may be less than the prefix
+ *   max_group, max_shared, max_tail  upper bounds on a group's sequences, on shared_len and on kv_len - shared_len
+ *              (they size the launch and the workspace)
+ *   workspace  at least slim_shared_workspace_bytes(...) bytes; header as for slim_attn_decode
+ * A new token that would fall into the prefix is not appended (the page belongs to all of the group).
+ */
+int slim_attn_decode_shared(const slim_cache_t *cache, const void *q, const void *k_new, const void *v_new, void *out,
+                            const int32_t *cu_group, const int32_t *shared_len, const int32_t *kv_len,
+                            int32_t n_groups, int32_t B, int32_t max_group, int32_t max_shared, int32_t max_tail,
+                            int32_t Hq, float sm_scale, void *workspace, size_t workspace_bytes, void *stream);
+size_t slim_shared_workspace_bytes(int32_t B, int32_t Hq, int32_t Hkv, int32_t n_groups, int32_t max_group,
+                                   int32_t max_shared, int32_t max_tail);
+
+/*
+ * slim_attn_decode (with k_new / v_new, both or neither, slim_decode_step) that also accumulates every cached token's
+ * attention weight, the measure that slim_kv_evict goes by.  For kv head g and token j < kv_len[b]:
+ *   weight_out[b][g][j] = decay * weight_in[b][g][j] + sum over the query heads of g of softmax_j(...)
+ * where tokens j >= weighed[b] (new since the last call) and a NULL weight_in count as 0 before.
+ *
+ *   weight_in, weight_out  device fp32 [B][Hkv][weight_stride], weight_stride >= max_kv; may be the same array; entries
+ *              from kv_len[b] on are left as they are
+ *   weighed    device int32 [B], or NULL: kv_len[b] - 1
+ *   workspace  at least slim_weights_workspace_bytes(...) bytes (the scores lie there between the two kernels); header
+ *              as for slim_attn_decode
+ */
+int slim_attn_decode_weights(const slim_cache_t *cache, const void *q, const void *k_new, const void *v_new, void *out,
+                             const float *weight_in, float *weight_out, int32_t weight_stride, const int32_t *weighed,
+                             const int32_t *kv_len, int32_t B, int32_t max_kv, int32_t Hq, float sm_scale, float decay,
+                             void *workspace, size_t workspace_bytes, void *stream);
+size_t slim_weights_workspace_bytes(int32_t B, int32_t Hq, int32_t Hkv, int32_t max_kv);
+
+/*
+ * Eviction: every (sequence, kv head) with more than `budget` cached tokens keeps `budget` of them: first the protected
+ * ones (position < n_sink, or among the last n_recent positions seen), then those of the largest weight, equal ones by
+ * the lower slot; NaN counts as minus infinity.  The kept tokens end up in slots 0 .. budget - 1, those that already
+ * were there in their slots, the others in the freed ones, both in ascending order (attention does not depend on the
+ * order of the keys).  Afterwards the sequence's length is min(kv_len[b], budget) - the caller's to note, and its pages
+ * behind that are the caller's to reuse; slots from the budget on keep what they held.
+ *
+ *   weight_in, weight_out  device fp32 [B][Hkv][stride]: the kept tokens' weights follow them to their new slots;
+ *              entries from min(kv_len[b], budget) on are left as they are.  May be the same array.
+ *   pos_in, pos_out  device int32 [B][Hkv][stride]: the token position of every slot, in the same way.  pos_in is read
+ *              for the first placed[b] slots (what an earlier eviction arranged); the slots behind them hold the
+ *              sequence's last tokens in order: slot s holds position seen[b] - kv_len[b] + s.  May be the same array.
+ *   placed     device int32 [B], or NULL: 0 (pos_in may then be NULL)
+ *   seen       device int32 [B]: tokens the sequence has had in all, or NULL: kv_len[b]
+ *   stride     >= max_kv;  budget >= 1;  n_sink, n_recent >= 0, n_sink + n_recent <= budget
+ *   workspace  device, 16-byte aligned, at least slim_evict_workspace_bytes(...) bytes; needs no initialisation
+ * The pages of a sequence that is cut must not be shared with another one.
+ */
+int slim_kv_evict(const slim_cache_t *cache, const float *weight_in, float *weight_out, const int32_t *pos_in,
+                  int32_t *pos_out, int32_t stride, const int32_t *kv_len, const int32_t *placed, const int32_t *seen,
+                  int32_t B, int32_t max_kv, int32_t budget, int32_t n_sink, int32_t n_recent,
+                  void *workspace, size_t workspace_bytes, void *stream);
+size_t slim_evict_workspace_bytes(int32_t B, int32_t Hkv, int32_t max_kv, int32_t budget);
+
+/*
  * Device-side waits are bounded.  The attention kernels wait on hardware barriers (TMA copies, tensor-core
  * completion); every such wait gives up after a fixed number of tries, and a kernel whose wait ran out
  * stores SLIM_ERR_TIMEOUT in the first word of its workspace and finishes with undefined output instead of

@@ -29,6 +29,8 @@ EXPORTS = (
     "slim_static_selftest_timeout", "slim_attn_decode_partial", "slim_attn_merge_partials", "slim_decode_step", "slim_decode_step_host", "slim_step_staging_bytes", "slim_read_status", "slim_selftest_timeout", "slim_workspace_bytes",
     "slim_cache_code_bytes", "slim_cache_scale_bytes", "slim_strerror", "slim_last_cuda_error",
     "slim_version",
+    "slim_norm_rope", "slim_norm_rope_append", "slim_attn_decode_shared", "slim_shared_workspace_bytes",
+    "slim_attn_decode_weights", "slim_weights_workspace_bytes", "slim_kv_evict", "slim_evict_workspace_bytes",
 )
 
 
@@ -43,6 +45,20 @@ class SlimCacheStruct(ctypes.Structure):
         ("num_kv_heads", ctypes.c_int32),
         ("head_dim", ctypes.c_int32),
         ("max_pages_per_seq", ctypes.c_int32),
+    ]
+
+
+class SlimNormRopeStruct(ctypes.Structure):
+    """Mirror of slim_norm_rope_t."""
+    _fields_ = [
+        ("inv_freq", ctypes.c_void_p),
+        ("axis", ctypes.c_void_p),
+        ("q_weight", ctypes.c_void_p),
+        ("k_weight", ctypes.c_void_p),
+        ("eps", ctypes.c_float),
+        ("rotary_dim", ctypes.c_int32),
+        ("n_axes", ctypes.c_int32),
+        ("interleaved", ctypes.c_int32),
     ]
 
 
@@ -100,6 +116,23 @@ def lib():
         L.slim_decode_step_host.restype = ctypes.c_int
         L.slim_step_staging_bytes.argtypes = [I, I, I]
         L.slim_step_staging_bytes.restype = Z
+        NP, J = ctypes.POINTER(SlimNormRopeStruct), ctypes.c_int64
+        L.slim_norm_rope.argtypes = [NP, P, J, P, P, J, P, P, I, I, I, P]
+        L.slim_norm_rope.restype = ctypes.c_int
+        L.slim_norm_rope_append.argtypes = [CP, NP, P, J, P, P, J, P, J, P, P, P, I, I, I, P]
+        L.slim_norm_rope_append.restype = ctypes.c_int
+        L.slim_attn_decode_shared.argtypes = [CP, P, P, P, P, P, P, P, I, I, I, I, I, I, F, P, Z, P]
+        L.slim_attn_decode_shared.restype = ctypes.c_int
+        L.slim_shared_workspace_bytes.argtypes = [I, I, I, I, I, I, I]
+        L.slim_shared_workspace_bytes.restype = Z
+        L.slim_attn_decode_weights.argtypes = [CP, P, P, P, P, P, P, I, P, P, I, I, I, F, F, P, Z, P]
+        L.slim_attn_decode_weights.restype = ctypes.c_int
+        L.slim_weights_workspace_bytes.argtypes = [I, I, I, I]
+        L.slim_weights_workspace_bytes.restype = Z
+        L.slim_kv_evict.argtypes = [CP, P, P, P, P, I, P, P, P, I, I, I, I, I, P, Z, P]
+        L.slim_kv_evict.restype = ctypes.c_int
+        L.slim_evict_workspace_bytes.argtypes = [I, I, I, I]
+        L.slim_evict_workspace_bytes.restype = Z
         L.slim_read_status.argtypes = [P, P]
         L.slim_read_status.restype = ctypes.c_int
         L.slim_selftest_timeout.argtypes = [P, P]
@@ -283,6 +316,137 @@ def slim_decode_step_host(cache, q_host, k_new_host, v_new_host, out_host, stagi
                                      _ptr(out_host), _ptr(staging), _nbytes(staging), _ptr(kv_len), B, max_kv, Hq,
                                      sm_scale, _ptr(workspace), _nbytes(workspace), _stream(stream))
     _check(rc, "slim_decode_step_host")
+
+
+# ------------------------------------------------------------------ norm, rotation, shared prefixes, weights, eviction
+def _addr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _cuda_stream(stream):
+    return (torch.cuda.current_stream() if stream is None else stream).cuda_stream
+
+
+class NormRope:
+    """slim_norm_rope_t over the tensors it names: inv_freq fp64 [rotary_dim / 2] radians per position, axis uint8
+    [rotary_dim / 2] (which of a token's n_axes positions turns each pair), norm weights bf16 [128] or None."""
+
+    def __init__(self, inv_freq=None, q_weight=None, k_weight=None, eps=1e-6, axis=None, n_axes=1, interleaved=False):
+        half = 0 if inv_freq is None else inv_freq.numel()
+        if half and inv_freq.dtype != torch.float64:
+            raise TypeError("inv_freq must be float64 (angles of far positions are formed in it)")
+        if axis is not None and (axis.dtype != torch.uint8 or axis.numel() != half):
+            raise TypeError("axis must be uint8, one entry per frequency")
+        for w in (q_weight, k_weight):
+            if w is not None and (w.dtype != torch.bfloat16 or w.numel() != HEAD_DIM):
+                raise TypeError(f"norm weights must be bfloat16 [{HEAD_DIM}]")
+        # contiguous copies where needed; kept here because the struct holds bare addresses
+        self.tensors = [None if t is None else t.contiguous() for t in (inv_freq if half else None, axis, q_weight, k_weight)]
+        self.n_axes = n_axes
+        self.struct = SlimNormRopeStruct(*[_addr(t) for t in self.tensors], eps, 2 * half, n_axes, 1 if interleaved else 0)
+
+
+def _heads(t, where):
+    """Token stride and heads of bf16 [tokens, heads, 128] whose tokens may lie apart (views of a fused projection)."""
+    n, heads, d = t.shape
+    stride = t.stride()
+    if t.dtype != torch.bfloat16 or d != HEAD_DIM or stride[2] != 1 or (heads > 1 and stride[1] != HEAD_DIM):
+        raise SlimError(SLIM_ERR_INVALID_ARG, f"{where}: rows must be bfloat16 [tokens, heads, 128], heads contiguous")
+    return (stride[0] if n > 1 else heads * HEAD_DIM), heads
+
+
+def _rows_out(out, like, where):
+    if out.dtype != torch.bfloat16 or out.shape != like.shape or not out.is_contiguous():
+        raise SlimError(SLIM_ERR_INVALID_ARG, f"{where}: the output must be contiguous bfloat16 of the input's shape")
+
+
+def _positions(positions, nr, n, where):
+    if positions is not None and (positions.dtype != torch.int32 or positions.numel() != nr.n_axes * n or not positions.is_contiguous()):
+        raise SlimError(SLIM_ERR_INVALID_ARG, f"{where}: positions must be contiguous int32 [n_axes, tokens]")
+
+
+def slim_norm_rope(nr, q, q_out, k, k_out, positions, stream=None):
+    """Norm and rotation of q and k (bf16 [tokens, heads, 128], either may be None) into q_out and k_out."""
+    n = (q if q is not None else k).shape[0]
+    qs = hq = ks = hkv = 0
+    if q is not None:
+        qs, hq = _heads(q, "slim_norm_rope")
+        _rows_out(q_out, q, "slim_norm_rope")
+    if k is not None:
+        ks, hkv = _heads(k, "slim_norm_rope")
+        _rows_out(k_out, k, "slim_norm_rope")
+        if k.shape[0] != n:
+            raise SlimError(SLIM_ERR_INVALID_ARG, "slim_norm_rope: q and k differ in tokens")
+    _positions(positions, nr, n, "slim_norm_rope")
+    rc = lib().slim_norm_rope(ctypes.byref(nr.struct), _addr(q), qs, _addr(q_out), _addr(k), ks, _addr(k_out), _addr(positions), n, hq, hkv,
+                              _cuda_stream(stream))
+    _check(rc, "slim_norm_rope")
+
+
+def slim_norm_rope_append(cache, nr, q, q_out, k, v, positions, cu_new, start_pos, B, stream=None):
+    """Norm and rotation of q into q_out; keys (normed, rotated) and values quantised into the cache.  positions None:
+    the tokens' cache positions."""
+    where = "slim_norm_rope_append"
+    n = k.shape[0]
+    ks, hkv = _heads(k, where)
+    vs, hv = _heads(v, where)
+    qs = hq = 0
+    if q is not None:
+        qs, hq = _heads(q, where)
+        _rows_out(q_out, q, where)
+    if hkv != cache.Hkv or hv != hkv or v.shape[0] != n or (q is not None and q.shape[0] != n):
+        raise SlimError(SLIM_ERR_INVALID_ARG, f"{where}: q, k, v and the cache differ in tokens or kv heads")
+    _positions(positions, nr, n, where)
+    rc = lib().slim_norm_rope_append(ctypes.byref(cache.struct), ctypes.byref(nr.struct), _addr(q), qs, _addr(q_out), _addr(k), ks, _addr(v), vs,
+                                     _addr(positions), _addr(cu_new), _addr(start_pos), B, n, hq, _cuda_stream(stream))
+    _check(rc, where)
+
+
+def slim_attn_decode_shared(cache, q, out, cu_group, shared_len, kv_len, n_groups, B, max_group, max_shared, max_tail, Hq, sm_scale,
+                            workspace, stream=None, k_new=None, v_new=None):
+    """Decode attention of a batch whose groups of sequences share a prefix of shared_len tokens (the same pages)."""
+    rc = lib().slim_attn_decode_shared(ctypes.byref(cache.struct), _addr(q), _addr(k_new), _addr(v_new), _addr(out), _addr(cu_group),
+                                       _addr(shared_len), _addr(kv_len), n_groups, B, max_group, max_shared, max_tail, Hq, sm_scale,
+                                       _addr(workspace), _nbytes(workspace), _cuda_stream(stream))
+    _check(rc, "slim_attn_decode_shared")
+
+
+def slim_attn_decode_weights(cache, q, out, weight_in, weight_out, weighed, kv_len, B, max_kv, Hq, sm_scale, decay, workspace, stream=None,
+                             k_new=None, v_new=None):
+    """slim_attn_decode that also accumulates attention weights: fp32 [B, Hkv, stride], weight_in may be weight_out or None."""
+    rc = lib().slim_attn_decode_weights(ctypes.byref(cache.struct), _addr(q), _addr(k_new), _addr(v_new), _addr(out), _addr(weight_in),
+                                        _addr(weight_out), weight_out.shape[-1], _addr(weighed), _addr(kv_len), B, max_kv, Hq, sm_scale, decay,
+                                        _addr(workspace), _nbytes(workspace), _cuda_stream(stream))
+    _check(rc, "slim_attn_decode_weights")
+
+
+def slim_kv_evict(cache, weight_in, weight_out, pos_in, pos_out, kv_len, placed, seen, B, max_kv, budget, n_sink, n_recent, workspace,
+                  stream=None):
+    """Keeps `budget` tokens of every (sequence, kv head); weights fp32 and positions int32 [B, Hkv, stride] follow them.
+    The lengths afterwards are min(kv_len, budget)."""
+    rc = lib().slim_kv_evict(ctypes.byref(cache.struct), _addr(weight_in), _addr(weight_out), _addr(pos_in), _addr(pos_out), weight_out.shape[-1],
+                             _addr(kv_len), _addr(placed), _addr(seen), B, max_kv, budget, n_sink, n_recent, _addr(workspace),
+                             _nbytes(workspace), _cuda_stream(stream))
+    _check(rc, "slim_kv_evict")
+
+
+def _scratch(n, device):
+    return torch.zeros(max(16, n), dtype=torch.uint8, device=device)
+
+
+def shared_workspace(B, Hq, Hkv, n_groups, max_group, max_shared, max_tail, device="cuda"):
+    """A zeroed torch uint8 buffer of the size slim_attn_decode_shared needs."""
+    return _scratch(lib().slim_shared_workspace_bytes(B, Hq, Hkv, n_groups, max_group, max_shared, max_tail), device)
+
+
+def weights_workspace(B, Hq, Hkv, max_kv, device="cuda"):
+    """A zeroed torch uint8 buffer of the size slim_attn_decode_weights needs."""
+    return _scratch(lib().slim_weights_workspace_bytes(B, Hq, Hkv, max_kv), device)
+
+
+def evict_workspace(B, Hkv, max_kv, budget, device="cuda"):
+    """A torch uint8 buffer of the size slim_kv_evict needs."""
+    return _scratch(lib().slim_evict_workspace_bytes(B, Hkv, max_kv, budget), device)
 
 
 def slim_read_status(workspace, stream=None):

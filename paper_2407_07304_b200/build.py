@@ -6,7 +6,8 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libslim.so")
-SOURCES = ["slim_abi.cu", "slim_append.cu", "slim_decode.cu", "slim_decode_stream.cu", "slim_tmap.cu", "slim_prefill_tc.cu", "slim_prefill_row.cu"]
+SOURCES = ["slim_abi.cu", "slim_append.cu", "slim_norm_rope.cu", "slim_decode.cu", "slim_decode_stream.cu", "slim_decode_shared.cu",
+           "slim_decode_weights.cu", "slim_evict.cu", "slim_tmap.cu", "slim_prefill_tc.cu", "slim_prefill_row.cu"]
 
 
 def _nvcc():
@@ -30,7 +31,7 @@ def build(force=False, verbose=False):
     if not force and not _stale():
         return LIB
     cmd = [_nvcc(), "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-           "-shared", "-Xcompiler", "-fPIC", "-o", LIB]
+           "-shared", "-Xcompiler", "-fPIC", "-t", "0", "-o", LIB]   # -t 0: the sources side by side
     if verbose:
         cmd += ["-Xptxas", "-v"]
     cmd += [os.path.join(CSRC, s) for s in SOURCES]

@@ -1,4 +1,6 @@
 // C ABI of the library (declared in include/slim.h): argument validation and dispatch.
+#include <math.h>
+
 #include "slim_common.cuh"
 #include "slim_tcgen05.cuh"
 
@@ -31,6 +33,21 @@ int launch_prefill_tc(const slim_cache_t *c, const void *q, void *out, const int
 int launch_prefill_row(const slim_cache_t *c, const void *q, void *out, const int32_t *cu_q, const int32_t *kv_len,
                        int B, int max_q, int Hq, float sm_scale, void *workspace, cudaStream_t stream);
 size_t prefill_workspace_bytes();
+int launch_norm_rope(const slim_cache_t *c, const slim_norm_rope_t *nr, const void *q, int64_t q_stride, void *q_out, const void *k,
+                     int64_t k_stride, void *k_out, const void *v, int64_t v_stride, const int32_t *positions, const int32_t *cu_new,
+                     const int32_t *start_pos, int B, int n_tokens, int Hq, int Hkv, cudaStream_t stream);
+int launch_decode_shared(const slim_cache_t *c, const void *q, const void *k_new, const void *v_new, void *out, const int32_t *cu_group,
+                         const int32_t *shared_len, const int32_t *kv_len, int n_groups, int B, int max_group, int max_shared,
+                         int max_tail, int Hq, float sm_scale, void *workspace, cudaStream_t stream);
+size_t shared_workspace_bytes(int B, int Hq, int Hkv, int n_groups, int max_group, int max_shared, int max_tail);
+int launch_decode_weights(const slim_cache_t *c, const void *q, const void *k_new, const void *v_new, void *out, const float *w_in,
+                          float *w_out, int w_stride, const int32_t *weighed, const int32_t *kv_len, int B, int max_kv, int Hq,
+                          float sm_scale, float decay, void *workspace, cudaStream_t stream);
+size_t weights_workspace_bytes(int B, int Hq, int Hkv, int max_kv);
+int launch_evict(const slim_cache_t *c, const float *w_in, float *w_out, const int32_t *pos_in, int32_t *pos_out, int stride,
+                 const int32_t *kv_len, const int32_t *placed, const int32_t *seen, int B, int max_kv, int budget, int n_sink,
+                 int n_recent, void *workspace, cudaStream_t stream);
+size_t evict_workspace_bytes(int B, int Hkv, int max_kv, int budget);
 
 static int check_cache(const slim_cache_t *c)
 {
@@ -280,6 +297,162 @@ SLIM_EXPORT int slim_decode_step_host(const slim_cache_t *cache, const void *q_h
     return SLIM_OK;
 }
 
+// Shared validation of the two norm and rotation calls.
+static bool misaligned(const void *ptr, uintptr_t bytes) { return ((uintptr_t)ptr & (bytes - 1)) != 0; }
+static int check_norm_rope(const slim_norm_rope_t *nr, int32_t n_tokens, int32_t Hq, int32_t Hkv)
+{
+    if (nr == nullptr || n_tokens < 0 || Hq < 0 || Hkv < 0 || Hq + (long long)Hkv == 0) return SLIM_ERR_INVALID_ARG;
+    if (nr->rotary_dim < 0 || nr->n_axes < 1) return SLIM_ERR_INVALID_ARG;
+    if (nr->rotary_dim > SLIM_HEAD_DIM || nr->rotary_dim % 16 != 0 || nr->n_axes > 4) return SLIM_ERR_UNSUPPORTED;
+    if (nr->rotary_dim > 0 && (nr->inv_freq == nullptr || misaligned(nr->inv_freq, 8))) return SLIM_ERR_INVALID_ARG;
+    if (nr->rotary_dim > 0 && nr->n_axes > 1 && nr->axis == nullptr) return SLIM_ERR_INVALID_ARG;
+    if (misaligned(nr->q_weight, 16) || misaligned(nr->k_weight, 16)) return SLIM_ERR_INVALID_ARG;
+    if ((nr->q_weight != nullptr || nr->k_weight != nullptr) && !(nr->eps > 0.f && nr->eps < INFINITY)) return SLIM_ERR_INVALID_ARG;
+    return SLIM_OK;
+}
+static bool bad_rows(const void *rows, int64_t stride, int32_t heads)
+{
+    return rows == nullptr || misaligned(rows, 16) || stride % 8 != 0 || stride < (int64_t)heads * SLIM_HEAD_DIM;
+}
+
+SLIM_EXPORT int slim_norm_rope(const slim_norm_rope_t *nr, const void *q, int64_t q_stride, void *q_out, const void *k, int64_t k_stride,
+                               void *k_out, const int32_t *positions, int32_t n_tokens, int32_t Hq, int32_t Hkv, void *stream)
+{
+    const int rc = check_norm_rope(nr, n_tokens, Hq, Hkv);
+    if (rc != SLIM_OK) return rc;
+    if (n_tokens == 0) return SLIM_OK;
+    if (Hq > 0 && (bad_rows(q, q_stride, Hq) || q_out == nullptr || misaligned(q_out, 16))) return SLIM_ERR_INVALID_ARG;
+    if (Hkv > 0 && (bad_rows(k, k_stride, Hkv) || k_out == nullptr || misaligned(k_out, 16))) return SLIM_ERR_INVALID_ARG;
+    if (positions == nullptr && nr->rotary_dim > 0) return SLIM_ERR_INVALID_ARG;
+    return launch_norm_rope(nullptr, nr, q, q_stride, q_out, k, k_stride, k_out, nullptr, 0, positions, nullptr, nullptr, 0, n_tokens,
+                            Hq, Hkv, (cudaStream_t)stream);
+}
+
+SLIM_EXPORT int slim_norm_rope_append(const slim_cache_t *cache, const slim_norm_rope_t *nr, const void *q, int64_t q_stride, void *q_out,
+                                      const void *k, int64_t k_stride, const void *v, int64_t v_stride, const int32_t *positions,
+                                      const int32_t *cu_new, const int32_t *start_pos, int32_t B, int32_t n_tokens, int32_t Hq,
+                                      void *stream)
+{
+    int rc = check_cache(cache);
+    if (rc != SLIM_OK) return rc;
+    rc = check_norm_rope(nr, n_tokens, Hq, cache->num_kv_heads);
+    if (rc != SLIM_OK) return rc;
+    if (B < 0) return SLIM_ERR_INVALID_ARG;
+    if (B == 0 || n_tokens == 0) return SLIM_OK;
+    if (Hq > 0 && (bad_rows(q, q_stride, Hq) || q_out == nullptr || misaligned(q_out, 16))) return SLIM_ERR_INVALID_ARG;
+    if (bad_rows(k, k_stride, cache->num_kv_heads) || bad_rows(v, v_stride, cache->num_kv_heads)) return SLIM_ERR_INVALID_ARG;
+    if (cu_new == nullptr || start_pos == nullptr) return SLIM_ERR_INVALID_ARG;
+    if (B > 65535) return SLIM_ERR_UNSUPPORTED;
+    return launch_norm_rope(cache, nr, q, q_stride, q_out, k, k_stride, nullptr, v, v_stride, positions, cu_new, start_pos, B, n_tokens,
+                            Hq, cache->num_kv_heads, (cudaStream_t)stream);
+}
+
+// What the calls below share of check_decode, whose workspace has another size.
+static int check_heads(const slim_cache_t *cache, int32_t B, int32_t Hq)
+{
+    const int rc = check_cache(cache);
+    if (rc != SLIM_OK) return rc;
+    if (B < 0 || Hq <= 0) return SLIM_ERR_INVALID_ARG;
+    if (Hq % cache->num_kv_heads != 0 || Hq / cache->num_kv_heads > 16) return SLIM_ERR_UNSUPPORTED;
+    if (B > 65535 || cache->num_kv_heads > 65535) return SLIM_ERR_UNSUPPORTED;
+    return SLIM_OK;
+}
+static int check_step_rows(const void *q, const void *k_new, const void *v_new, const void *out, const int32_t *kv_len)
+{
+    if (q == nullptr || out == nullptr || kv_len == nullptr) return SLIM_ERR_INVALID_ARG;
+    if (misaligned(q, 16) || misaligned(out, 16)) return SLIM_ERR_INVALID_ARG;
+    if ((k_new == nullptr) != (v_new == nullptr) || misaligned(k_new, 16) || misaligned(v_new, 16)) return SLIM_ERR_INVALID_ARG;
+    return SLIM_OK;
+}
+static int check_scratch(const void *workspace, size_t bytes, size_t need)
+{
+    if (need > 0 && (workspace == nullptr || bytes < need)) return SLIM_ERR_WORKSPACE;
+    return misaligned(workspace, 16) ? SLIM_ERR_INVALID_ARG : SLIM_OK;
+}
+static bool beyond_pages(const slim_cache_t *cache, int32_t tokens)
+{
+    return (long long)tokens > (long long)cache->max_pages_per_seq * SLIM_PAGE_TOKENS;
+}
+
+SLIM_EXPORT int slim_attn_decode_shared(const slim_cache_t *cache, const void *q, const void *k_new, const void *v_new, void *out,
+                                        const int32_t *cu_group, const int32_t *shared_len, const int32_t *kv_len, int32_t n_groups,
+                                        int32_t B, int32_t max_group, int32_t max_shared, int32_t max_tail, int32_t Hq, float sm_scale,
+                                        void *workspace, size_t workspace_bytes, void *stream)
+{
+    int rc = check_heads(cache, B, Hq);
+    if (rc != SLIM_OK) return rc;
+    if (n_groups < 0 || max_group < 0 || max_shared < 0 || max_tail < 0) return SLIM_ERR_INVALID_ARG;
+    if (B == 0) return SLIM_OK;
+    if (n_groups == 0 || max_group == 0 || max_group > B || cu_group == nullptr || shared_len == nullptr) return SLIM_ERR_INVALID_ARG;
+    if (n_groups > 65535) return SLIM_ERR_UNSUPPORTED;
+    if (beyond_pages(cache, max_shared) || beyond_pages(cache, max_tail)) return SLIM_ERR_INVALID_ARG;
+    rc = check_step_rows(q, k_new, v_new, out, kv_len);
+    if (rc != SLIM_OK) return rc;
+    rc = check_scratch(workspace, workspace_bytes,
+                       slim_shared_workspace_bytes(B, Hq, cache->num_kv_heads, n_groups, max_group, max_shared, max_tail));
+    if (rc != SLIM_OK) return rc;
+    return launch_decode_shared(cache, q, k_new, v_new, out, cu_group, shared_len, kv_len, n_groups, B, max_group, max_shared, max_tail, Hq,
+                                sm_scale, workspace, (cudaStream_t)stream);
+}
+
+SLIM_EXPORT size_t slim_shared_workspace_bytes(int32_t B, int32_t Hq, int32_t Hkv, int32_t n_groups, int32_t max_group,
+                                               int32_t max_shared, int32_t max_tail)
+{
+    if (B <= 0 || Hq <= 0 || Hkv <= 0 || Hq % Hkv != 0 || n_groups <= 0 || max_group <= 0 || max_shared < 0 || max_tail < 0) return 0;
+    return shared_workspace_bytes(B, Hq, Hkv, n_groups, max_group, max_shared, max_tail);
+}
+
+SLIM_EXPORT int slim_attn_decode_weights(const slim_cache_t *cache, const void *q, const void *k_new, const void *v_new, void *out,
+                                         const float *weight_in, float *weight_out, int32_t weight_stride, const int32_t *weighed,
+                                         const int32_t *kv_len, int32_t B, int32_t max_kv, int32_t Hq, float sm_scale, float decay,
+                                         void *workspace, size_t workspace_bytes, void *stream)
+{
+    int rc = check_heads(cache, B, Hq);
+    if (rc != SLIM_OK) return rc;
+    if (max_kv < 0 || weight_stride < max_kv) return SLIM_ERR_INVALID_ARG;
+    if (B == 0) return SLIM_OK;
+    if (beyond_pages(cache, max_kv)) return SLIM_ERR_INVALID_ARG;
+    rc = check_step_rows(q, k_new, v_new, out, kv_len);
+    if (rc != SLIM_OK) return rc;
+    if (weight_out == nullptr || misaligned(weight_out, 4) || misaligned(weight_in, 4)) return SLIM_ERR_INVALID_ARG;
+    rc = check_scratch(workspace, workspace_bytes, slim_weights_workspace_bytes(B, Hq, cache->num_kv_heads, max_kv));
+    if (rc != SLIM_OK) return rc;
+    return launch_decode_weights(cache, q, k_new, v_new, out, weight_in, weight_out, weight_stride, weighed, kv_len, B, max_kv, Hq, sm_scale,
+                                 decay, workspace, (cudaStream_t)stream);
+}
+
+SLIM_EXPORT size_t slim_weights_workspace_bytes(int32_t B, int32_t Hq, int32_t Hkv, int32_t max_kv)
+{
+    if (B <= 0 || Hq <= 0 || Hkv <= 0 || max_kv < 0) return 0;
+    return weights_workspace_bytes(B, Hq, Hkv, max_kv);
+}
+
+SLIM_EXPORT int slim_kv_evict(const slim_cache_t *cache, const float *weight_in, float *weight_out, const int32_t *pos_in, int32_t *pos_out,
+                              int32_t stride, const int32_t *kv_len, const int32_t *placed, const int32_t *seen, int32_t B, int32_t max_kv,
+                              int32_t budget, int32_t n_sink, int32_t n_recent, void *workspace, size_t workspace_bytes, void *stream)
+{
+    int rc = check_cache(cache);
+    if (rc != SLIM_OK) return rc;
+    if (B < 0 || max_kv < 0 || stride < max_kv || budget < 1 || n_sink < 0 || n_recent < 0 || (long long)n_sink + n_recent > budget)
+        return SLIM_ERR_INVALID_ARG;
+    if (B == 0 || max_kv == 0) return SLIM_OK;
+    if (B > 65535 || cache->num_kv_heads > 65535) return SLIM_ERR_UNSUPPORTED;
+    if (beyond_pages(cache, max_kv)) return SLIM_ERR_INVALID_ARG;
+    if (weight_in == nullptr || weight_out == nullptr || pos_out == nullptr || kv_len == nullptr) return SLIM_ERR_INVALID_ARG;
+    if (pos_in == nullptr && placed != nullptr) return SLIM_ERR_INVALID_ARG;
+    if (misaligned(weight_in, 4) || misaligned(weight_out, 4) || misaligned(pos_in, 4) || misaligned(pos_out, 4)) return SLIM_ERR_INVALID_ARG;
+    rc = check_scratch(workspace, workspace_bytes, slim_evict_workspace_bytes(B, cache->num_kv_heads, max_kv, budget));
+    if (rc != SLIM_OK) return rc;
+    return launch_evict(cache, weight_in, weight_out, pos_in, pos_out, stride, kv_len, placed, seen, B, max_kv, budget, n_sink, n_recent,
+                        workspace, (cudaStream_t)stream);
+}
+
+SLIM_EXPORT size_t slim_evict_workspace_bytes(int32_t B, int32_t Hkv, int32_t max_kv, int32_t budget)
+{
+    if (B <= 0 || Hkv <= 0 || max_kv < 0 || budget < 1) return 0;
+    return evict_workspace_bytes(B, Hkv, max_kv, budget);
+}
+
 SLIM_EXPORT size_t slim_workspace_bytes(int32_t phase, int32_t B, int32_t Hq, int32_t Hkv, int32_t max_q,
                                         int32_t max_kv)
 {
@@ -344,4 +517,4 @@ SLIM_EXPORT const char *slim_strerror(int code)
 
 SLIM_EXPORT int slim_last_cuda_error(void) { return g_last_cuda_error; }
 
-SLIM_EXPORT int slim_version(void) { return 100; }
+SLIM_EXPORT int slim_version(void) { return 200; }

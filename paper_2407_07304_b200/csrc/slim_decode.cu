@@ -24,6 +24,21 @@ __device__ __forceinline__ int merge_row_partials(int len, int cap_tokens)
     return (L == 0) ? 0 : (L - 1 + kChunkTok - 1) / kChunkTok + 1;
 }
 
+// The same for a row whose first tokens are a shared prefix: the prefix's slots (every one of them is filled, those without
+// a key with weight 0), then the tail's partials.  Without a prefix cap_tokens bounds the whole row, with one the tail.
+struct MergeRows {
+    const int32_t *kv_len, *shared_len;   // shared_len null: no prefix
+    int slot0, max_pages, cap_tokens;
+    __device__ __forceinline__ int partials(int b) const
+    {
+        const int len = __ldg(kv_len + b);
+        if (shared_len == nullptr) return merge_row_partials(len, cap_tokens);
+        const int start = min(max(__ldg(shared_len + b), 0) / kPageTokens, max_pages) * kPageTokens;
+        const int tail = merge_row_partials(len - start, min(max_pages * kPageTokens - start, cap_tokens));
+        return (tail == 0 && min(len, start) <= 0) ? 0 : slot0 + tail;
+    }
+};
+
 // Second pass: log-sum-exp merge of a row's chunk partials,
 //   M = max m_c;  l = sum l_c 2^(m_c - M);  o = sum O_c 2^(m_c - M) / l.
 // One block per (sequence, query head) row: GROUPS groups of 128 threads (thread = head dim), group g takes
@@ -33,8 +48,8 @@ __device__ __forceinline__ int merge_row_partials(int len, int cap_tokens)
 template <int kMergeGroups>
 __global__ void __launch_bounds__(kMergeGroups * kHeadDim)
 slim_decode_merge_kernel(const float *__restrict__ part_o, const float *__restrict__ part_ml,
-                         const int32_t *__restrict__ kv_len, __nv_bfloat16 *__restrict__ out, float *__restrict__ raw,
-                         int B, int Hq, int n_slots, int cap_tokens)
+                         const MergeRows rows, __nv_bfloat16 *__restrict__ out, float *__restrict__ raw,
+                         int B, int Hq, int n_slots)
 {
     constexpr int kMergeThreads = kMergeGroups * kHeadDim;
     __shared__ float w_s[kHeadDim];
@@ -43,9 +58,7 @@ slim_decode_merge_kernel(const float *__restrict__ part_o, const float *__restri
     const int row = blockIdx.x;            // b * Hq + h
     const int tid = threadIdx.x, d = tid & (kHeadDim - 1), g = tid >> 7;
     pdl_wait();   // the split pass before this kernel must have finished writing the partials
-    const int b = row / Hq;
-    const int len = kv_len[b];
-    const int nc = merge_row_partials(len, cap_tokens);
+    const int nc = rows.partials(row / Hq);
     const float2 *ml = reinterpret_cast<const float2 *>(part_ml) + (size_t)row * n_slots;
     const float *po = part_o + (size_t)row * n_slots * kHeadDim;
     // ---- the row's maximum
@@ -130,17 +143,16 @@ constexpr int kMergeWarpBatch = 16;
 constexpr int kMergeWarpsPerBlock = 8;
 __global__ void __launch_bounds__(kMergeWarpsPerBlock * 32)
 slim_decode_merge_warp_kernel(const float *__restrict__ part_o, const float *__restrict__ part_ml,
-                              const int32_t *__restrict__ kv_len, __nv_bfloat16 *__restrict__ out, float *__restrict__ raw,
-                              int B, int Hq, int n_slots, int cap_tokens)
+                              const MergeRows rows, __nv_bfloat16 *__restrict__ out, float *__restrict__ raw,
+                              int B, int Hq, int n_slots)
 {
     const int lane = threadIdx.x & 31;
     const int row = blockIdx.x * kMergeWarpsPerBlock + (threadIdx.x >> 5);   // b * Hq + h
     pdl_wait();   // the split pass before this kernel must have finished writing the partials
     if (row >= B * Hq) return;
-    const int len = __ldg(kv_len + row / Hq);
+    const int nc = rows.partials(row / Hq);
     const float2 *ml = reinterpret_cast<const float2 *>(part_ml) + (size_t)row * n_slots;
     const float4 *po = reinterpret_cast<const float4 *>(part_o + (size_t)row * n_slots * kHeadDim) + lane;
-    const int nc = merge_row_partials(len, cap_tokens);
     float4 o[kMergeWarpBatch];
 #pragma unroll
     for (int u = 0; u < kMergeWarpBatch; ++u)
@@ -186,15 +198,14 @@ slim_decode_merge_warp_kernel(const float *__restrict__ part_o, const float *__r
 template <int kWarps>
 __global__ void __launch_bounds__(kWarps * 32, 1)
 slim_decode_merge_block_kernel(const float *__restrict__ part_o, const float *__restrict__ part_ml,
-                               const int32_t *__restrict__ kv_len, __nv_bfloat16 *__restrict__ out, float *__restrict__ raw,
-                               int B, int Hq, int n_slots, int cap_tokens)
+                               const MergeRows rows, __nv_bfloat16 *__restrict__ out, float *__restrict__ raw,
+                               int B, int Hq, int n_slots)
 {
     __shared__ float4 acc_s[kWarps][32];
     __shared__ float m_s[kWarps], l_s[kWarps];
     const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
     const int row = blockIdx.x;   // b * Hq + h
     pdl_wait();   // the split pass before this kernel must have finished writing the partials
-    const int len = __ldg(kv_len + row / Hq);
     const int c_base = w * kMergeWarpBatch;
     const float2 *ml = reinterpret_cast<const float2 *>(part_ml) + (size_t)row * n_slots;
     const float4 *po = reinterpret_cast<const float4 *>(part_o + (size_t)row * n_slots * kHeadDim) + lane;
@@ -203,11 +214,11 @@ slim_decode_merge_block_kernel(const float *__restrict__ part_o, const float *__
     for (int u = 0; u < kMergeWarpBatch; ++u)
         o[u] = ld_cg_now(po + (size_t)min(c_base + u, n_slots - 1) * (kHeadDim / 4));   // n_slots >= 32 here; slots past nc are not used
     float2 v = (lane < kMergeWarpBatch && c_base + lane < n_slots) ? __ldcg(ml + c_base + lane) : make_float2(-INFINITY, 0.f);
-    const int nc = merge_row_partials(len, cap_tokens);
+    const int nc = rows.partials(row / Hq);
     const bool mine = lane < kMergeWarpBatch && c_base + lane < nc;
     if (!mine) v = make_float2(-INFINITY, 0.f);
     const float Mw = warp_max(v.x);
-    const float wgt = mine ? exp2f(v.x - Mw) : 0.f;
+    const float wgt = (v.x != -INFINITY) ? exp2f(v.x - Mw) : 0.f;   // (a prefix slot without keys: weight 0)
     const float lw = warp_sum(v.y * wgt);
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
@@ -263,11 +274,10 @@ size_t decode_workspace_bytes(int B, int Hq, int Hkv, int max_kv)
     return kDecodeHeaderBytes + (size_t)B * Hq * slots * (kHeadDim + 2) * sizeof(float);
 }
 
-static DecodeParams make_params(const slim_cache_t *c, const void *q, const int32_t *kv_len, int B, int max_kv,
-                                int Hq, float sm_scale, void *workspace, int &C)
+DecodeParams make_decode_params(const slim_cache_t *c, const void *q, const int32_t *kv_len, int B, int max_kv,
+                                int Hq, float sm_scale, void *workspace)
 {
     const int Hkv = c->num_kv_heads;
-    C = kChunkTok;
     DecodeParams p;
     p.codes = c->codes;
     p.scales = c->scales;
@@ -279,7 +289,7 @@ static DecodeParams make_params(const slim_cache_t *c, const void *q, const int3
     p.G = Hq / Hkv;
     p.max_pages_per_seq = c->max_pages_per_seq;
     p.num_pages = c->num_pages;
-    p.n_chunks = (max_kv + C - 1) / C;
+    p.n_chunks = (max_kv + kChunkTok - 1) / kChunkTok;
     p.n_slots = p.n_chunks + 1;
     p.scale_log2e = sm_scale * kLog2e;
     p.status = static_cast<int *>(workspace);
@@ -288,14 +298,17 @@ static DecodeParams make_params(const slim_cache_t *c, const void *q, const int3
     p.k_new = p.v_new = nullptr;
     p.out = nullptr;
     p.counters = nullptr;
+    p.scores = nullptr;
+    p.score_stride = 0;
+    p.shared_len = nullptr;
+    p.slot0 = 0;
     return p;
 }
 
 int launch_decode_split(const slim_cache_t *c, const void *q, const void *k_new, const void *v_new, const int32_t *kv_len,
                         int B, int max_kv, int Hq, float sm_scale, void *workspace, cudaStream_t stream)
 {
-    int C;
-    DecodeParams p = make_params(c, q, kv_len, B, max_kv, Hq, sm_scale, workspace, C);
+    DecodeParams p = make_decode_params(c, q, kv_len, B, max_kv, Hq, sm_scale, workspace);
     if (p.n_chunks == 0) return SLIM_OK;
     p.k_new = static_cast<const __nv_bfloat16 *>(k_new);
     p.v_new = static_cast<const __nv_bfloat16 *>(v_new);
@@ -310,46 +323,60 @@ int launch_decode_merge(const slim_cache_t *c, void *out, const int32_t *kv_len,
 // kernel merges them itself when its blocks finish (one warp per pair); otherwise the merge kernel follows.
 constexpr int kInKernelMergeMaxPartials = 32;   // G * chunks of a (sequence, kv head) that one warp merges at the end of a block
 
-int launch_decode(const slim_cache_t *c, const void *q, const void *k_new, const void *v_new, void *out,
-                  const int32_t *kv_len, int B, int max_kv, int Hq, float sm_scale, void *workspace, cudaStream_t stream)
+int launch_decode_params(const slim_cache_t *c, DecodeParams &p, int B, void *out, cudaStream_t stream)
 {
-    int C;
-    DecodeParams p = make_params(c, q, kv_len, B, max_kv, Hq, sm_scale, workspace, C);
-    if (p.n_chunks == 0) return launch_decode_merge(c, out, kv_len, B, max_kv, Hq, workspace, stream);   // rows of zeros
-    p.k_new = static_cast<const __nv_bfloat16 *>(k_new);
-    p.v_new = static_cast<const __nv_bfloat16 *>(v_new);
+    if (p.n_chunks == 0) return launch_merge_rows(p, B, out, nullptr, stream);   // rows of zeros
     const bool in_kernel = (long long)B * p.Hkv <= kDecodeCounterRows && p.G * p.n_slots <= kInKernelMergeMaxPartials;
     if (in_kernel) {
         p.out = static_cast<__nv_bfloat16 *>(out);
-        p.counters = reinterpret_cast<int *>(static_cast<char *>(workspace) + kDecodeStatusBytes);
+        p.counters = reinterpret_cast<int *>(reinterpret_cast<char *>(p.status) + kDecodeStatusBytes);
     }
     const int rc = launch_decode_split_stream(c, p, B, stream);
     if (rc != SLIM_OK || in_kernel) return rc;
-    return launch_decode_merge(c, out, kv_len, B, max_kv, Hq, workspace, stream);
+    return launch_merge_rows(p, B, out, nullptr, stream);
+}
+
+int launch_decode(const slim_cache_t *c, const void *q, const void *k_new, const void *v_new, void *out,
+                  const int32_t *kv_len, int B, int max_kv, int Hq, float sm_scale, void *workspace, cudaStream_t stream)
+{
+    DecodeParams p = make_decode_params(c, q, kv_len, B, max_kv, Hq, sm_scale, workspace);
+    p.k_new = static_cast<const __nv_bfloat16 *>(k_new);
+    p.v_new = static_cast<const __nv_bfloat16 *>(v_new);
+    return launch_decode_params(c, p, B, out, stream);
 }
 
 int launch_decode_merge(const slim_cache_t *c, void *out, const int32_t *kv_len, int B, int max_kv, int Hq,
                         const void *workspace, cudaStream_t stream, float *raw)
 {
-    int C;
-    const DecodeParams p = make_params(c, nullptr, kv_len, B, max_kv, Hq, 1.f, const_cast<void *>(workspace), C);
-    const int rows = B * Hq;
-    const int cap = (int)std::min<long long>((long long)c->max_pages_per_seq * kPageTokens, (long long)p.n_chunks * C);
+    const DecodeParams p = make_decode_params(c, nullptr, kv_len, B, max_kv, Hq, 1.f, const_cast<void *>(workspace));
+    return launch_merge_rows(p, B, out, raw, stream);
+}
+
+int launch_merge_rows(const DecodeParams &p, int B, void *out, float *raw, cudaStream_t stream)
+{
+    const int rows = B * p.Hq;
+    MergeRows r;
+    r.kv_len = p.kv_len;
+    r.shared_len = p.shared_len;
+    r.slot0 = p.slot0;
+    r.max_pages = p.max_pages_per_seq;
+    const long long chunk_tokens = (long long)p.n_chunks * kChunkTok;
+    r.cap_tokens = (int)std::min<long long>((long long)p.max_pages_per_seq * kPageTokens, chunk_tokens);
     const float *po = p.part_o, *pm = p.part_ml;
     __nv_bfloat16 *o = static_cast<__nv_bfloat16 *>(out);
+    const int Hq = p.Hq;
     if (p.n_slots >= 32 && p.n_slots <= 16 * kMergeWarpBatch) {
         if (p.n_slots <= 4 * kMergeWarpBatch)
-            SLIM_CUDA_TRY(launch_pdl(slim_decode_merge_block_kernel<4>, dim3(rows), dim3(128), 0, stream, po, pm, kv_len, o, raw, B, Hq, p.n_slots, cap));
+            SLIM_CUDA_TRY(launch_pdl(slim_decode_merge_block_kernel<4>, dim3(rows), dim3(128), 0, stream, po, pm, r, o, raw, B, Hq, p.n_slots));
         else if (p.n_slots <= 8 * kMergeWarpBatch)
-            SLIM_CUDA_TRY(launch_pdl(slim_decode_merge_block_kernel<8>, dim3(rows), dim3(256), 0, stream, po, pm, kv_len, o, raw, B, Hq, p.n_slots, cap));
+            SLIM_CUDA_TRY(launch_pdl(slim_decode_merge_block_kernel<8>, dim3(rows), dim3(256), 0, stream, po, pm, r, o, raw, B, Hq, p.n_slots));
         else
-            SLIM_CUDA_TRY(launch_pdl(slim_decode_merge_block_kernel<16>, dim3(rows), dim3(512), 0, stream, po, pm, kv_len, o, raw, B, Hq, p.n_slots, cap));
+            SLIM_CUDA_TRY(launch_pdl(slim_decode_merge_block_kernel<16>, dim3(rows), dim3(512), 0, stream, po, pm, r, o, raw, B, Hq, p.n_slots));
     } else if (p.n_slots >= 32) {
-        SLIM_CUDA_TRY(launch_pdl(slim_decode_merge_kernel<4>, dim3(rows), dim3(4 * kHeadDim), 0, stream, po, pm, kv_len, o, raw, B, Hq, p.n_slots, cap));
+        SLIM_CUDA_TRY(launch_pdl(slim_decode_merge_kernel<4>, dim3(rows), dim3(4 * kHeadDim), 0, stream, po, pm, r, o, raw, B, Hq, p.n_slots));
     } else {
         const int blocks = (rows + kMergeWarpsPerBlock - 1) / kMergeWarpsPerBlock;
-        SLIM_CUDA_TRY(launch_pdl(slim_decode_merge_warp_kernel, dim3(blocks), dim3(kMergeWarpsPerBlock * 32), 0, stream, po, pm, kv_len, o, raw, B, Hq,
-                                 p.n_slots, cap));
+        SLIM_CUDA_TRY(launch_pdl(slim_decode_merge_warp_kernel, dim3(blocks), dim3(kMergeWarpsPerBlock * 32), 0, stream, po, pm, r, o, raw, B, Hq, p.n_slots));
     }
     return SLIM_OK;
 }
@@ -359,8 +386,7 @@ int launch_decode_merge(const slim_cache_t *c, void *out, const int32_t *kv_len,
 int launch_decode_partial(const slim_cache_t *c, const void *q, float *partial, const int32_t *kv_len, int B, int max_kv, int Hq,
                           float sm_scale, void *workspace, cudaStream_t stream)
 {
-    int C;
-    DecodeParams p = make_params(c, q, kv_len, B, max_kv, Hq, sm_scale, workspace, C);
+    DecodeParams p = make_decode_params(c, q, kv_len, B, max_kv, Hq, sm_scale, workspace);
     if (p.n_chunks > 0) {
         const int rc = launch_decode_split_stream(c, p, B, stream);
         if (rc != SLIM_OK) return rc;

@@ -25,7 +25,20 @@ struct DecodeParams {
     int n_chunks;             // 256-token chunks that max_kv tokens need
     int n_slots;              // partial slots per row: n_chunks + 1 (the last token of a row has a partial of its own)
     float scale_log2e;        // sm_scale * log2(e)
+    // scores kept for the attention weights (optional): [B][Hq][score_stride], in log2 units, position by position
+    float *scores;
+    int score_stride;
+    // tokens behind a shared prefix (optional): the prefix's length per sequence, and the partial slots in front of
+    // the tail's that the prefix kernel fills
+    const int32_t *shared_len;
+    int slot0;
 };
+
+// The length of the prefix that sequence b shares: whole pages, never beyond the page table.
+__device__ __forceinline__ int decode_shared_tokens(const DecodeParams &p, int b)
+{
+    return min(max(__ldg(p.shared_len + b), 0) / kPageTokens, p.max_pages_per_seq) * kPageTokens;
+}
 
 // Workspace header in front of the partials: the status word (16 bytes), then the counters of the in-kernel
 // merge.  The header has one size for every shape, so a workspace zeroed once stays valid when the shapes of the
@@ -34,6 +47,16 @@ constexpr size_t kDecodeStatusBytes = 16;
 constexpr int kDecodeCounterRows = 16384;   // (sequence, kv head) pairs the in-kernel merge can count
 constexpr size_t kDecodeHeaderBytes = kDecodeStatusBytes + (size_t)kDecodeCounterRows * sizeof(int);
 
+// Parameters of a split pass over `workspace` (slim_decode.cu); what is optional is left out.
+DecodeParams make_decode_params(const slim_cache_t *c, const void *q, const int32_t *kv_len, int B, int max_kv, int Hq,
+                                float sm_scale, void *workspace);
+size_t decode_workspace_bytes(int B, int Hq, int Hkv, int max_kv);
 int launch_decode_split_stream(const slim_cache_t *c, const DecodeParams &p, int B, cudaStream_t stream);
+// The split pass and, where it did not merge its own partials, the merge kernel (p.out and p.counters are set here).
+int launch_decode_params(const slim_cache_t *c, DecodeParams &p, int B, void *out, cudaStream_t stream);
+int launch_decode(const slim_cache_t *c, const void *q, const void *k_new, const void *v_new, void *out, const int32_t *kv_len, int B,
+                  int max_kv, int Hq, float sm_scale, void *workspace, cudaStream_t stream);
+// The merge kernel: out (bf16 rows) or, where raw is given, the rows' merged partials.
+int launch_merge_rows(const DecodeParams &p, int B, void *out, float *raw, cudaStream_t stream);
 
 }  // namespace slim

@@ -129,21 +129,46 @@ __device__ __forceinline__ float st_ordered_float(int i)
     return __int_as_float(i ^ ((i >> 31) & 0x7FFFFFFF));
 }
 
-// A sequence's cached tokens, never beyond the page table or the launch's max_kv.
+// What a launch does beside the plain split pass (a template argument, so that the plain kernel carries none of it).
+constexpr int kStPlain = 0;
+constexpr int kStScores = 1;   // every score also goes to p.scores (slim_attn_decode_weights turns them into attention weights)
+constexpr int kStTail = 2;     // only the tokens behind a shared prefix (slim_attn_decode_shared); the prefix kernel runs beside this one
+
+// The cached tokens of a sequence that this launch attends over start at position st_start: 0, or the end of the
+// prefix that the sequence shares (whole pages).
+template <int kWhat>
+__device__ __forceinline__ int st_start(const DecodeParams &p, int b)
+{
+    if (kWhat != kStTail) return 0;
+    return decode_shared_tokens(p, b);
+}
+
+// A sequence's cached tokens (from st_start on), never beyond the page table or the launch's max_kv.
+template <int kWhat>
 __device__ __forceinline__ int st_clamped_len(const DecodeParams &p, int b)
 {
-    const int cap = min(p.max_pages_per_seq * kPageTokens, p.n_chunks * kStChunk);
-    return min(max(__ldg(p.kv_len + b), 0), cap);
+    const int start = st_start<kWhat>(p, b);
+    const int cap = min(p.max_pages_per_seq * kPageTokens - start, p.n_chunks * kStChunk);
+    return min(max(__ldg(p.kv_len + b) - start, 0), cap);
 }
 
 // The tokens of a sequence that the chunks cover: all but the last one, which is attended from registers.
+template <int kWhat>
 __device__ __forceinline__ int st_chunk_len(const DecodeParams &p, int b)
 {
-    return max(st_clamped_len(p, b) - 1, 0);
+    return max(st_clamped_len<kWhat>(p, b) - 1, 0);
+}
+
+// Where the partial of a row's chunk lies: the tail's chunks follow the slots of the prefix kernel.
+template <int kWhat>
+__device__ __forceinline__ size_t st_slot(const DecodeParams &p, size_t row, int chunk)
+{
+    return row * p.n_slots + (kWhat == kStTail ? p.slot0 : 0) + chunk;
 }
 
 // Steps (sequence, kv head, chunk) to the next chunk in the order the work is cut in; sequences without
 // chunks are skipped.  Only called while another chunk exists, so a sequence with chunks is always found.
+template <int kWhat>
 __device__ __forceinline__ void st_next_chunk(const DecodeParams &p, int B, int &b, int &head, int &chunk, int &len, int &nc)
 {
     if (++chunk == nc) {
@@ -152,7 +177,7 @@ __device__ __forceinline__ void st_next_chunk(const DecodeParams &p, int B, int 
             head = 0;
             do {
                 ++b;
-                len = (b < B) ? st_chunk_len(p, b) : kStChunk;   // b < B always holds inside a block's range
+                len = (b < B) ? st_chunk_len<kWhat>(p, b) : kStChunk;   // b < B always holds inside a block's range
                 nc = (len + kStChunk - 1) / kStChunk;
             } while (nc == 0);
         }
@@ -173,11 +198,12 @@ __device__ __forceinline__ long long st_div(long long a, int b)
 // of the G query heads the token's partial - score s' = s + log2(sv), weight P = 1, so m = s', l = 1 / sv and
 // O = the V codes - goes to slot `slot` of the row; with to_out (a sequence of one token in a launch that merges
 // its own partials) the result code * sv is written straight to the output instead.
-template <bool kAppend>
+template <bool kAppend, int kWhat>
 __device__ __forceinline__ void st_last_token(const DecodeParams &p, int b, int head, int L, int slot, int lane, bool to_out)
 {
     const int kv = lane >> 4, l = lane & 15;
-    const int pos = L - 1;
+    const int start = st_start<kWhat>(p, b);
+    const int pos = start + L - 1;
     const int page_raw = __ldg(p.block_table + (size_t)b * p.max_pages_per_seq + (pos >> 7));
     const bool page_ok = page_raw >= 0 && page_raw < p.num_pages;
     const int page = page_ok ? page_raw : 0;
@@ -186,7 +212,7 @@ __device__ __forceinline__ void st_last_token(const DecodeParams &p, int b, int 
     const size_t scale_off = scale_block_offset(page, head, kv, p.Hkv) + row_in_page;
     uint2 pk;
     float scale;
-    if (kAppend && __ldg(p.kv_len + b) == L) {   // (the same for every lane of the warp)
+    if (kAppend && __ldg(p.kv_len + b) - start == L) {   // (the same for every lane of the warp)
         const __nv_bfloat16 *src = (kv ? p.v_new : p.k_new) + ((size_t)b * p.Hkv + head) * kHeadDim;
         pk = quantize_row16(__ldg(reinterpret_cast<const uint4 *>(src) + l), scale);
         if (page_ok) {
@@ -240,13 +266,14 @@ __device__ __forceinline__ void st_last_token(const DecodeParams &p, int b, int 
 #pragma unroll
             for (int o = 8; o > 0; o >>= 1) dot += __shfl_xor_sync(0xffffffffu, dot, o);   // lanes 0-15: q . k codes
             const float s = __shfl_sync(0xffffffffu, dot, 0);
-            const size_t ps = (row0 + h0 + i) * p.n_slots + slot;
+            const size_t ps = st_slot<kWhat>(p, row0 + h0 + i, slot);
             if (kv == 1) {
                 float4 *dst = reinterpret_cast<float4 *>(p.part_o + ps * kHeadDim + 8 * l);
                 dst[0] = make_float4(c[0], c[1], c[2], c[3]);
                 dst[1] = make_float4(c[4], c[5], c[6], c[7]);
             }
             if (lane == 0) *reinterpret_cast<float2 *>(p.part_ml + ps * 2) = make_float2(fmaf(s, ks, lsv), rsv);
+            if (kWhat == kStScores && lane == 0) p.scores[(row0 + h0 + i) * p.score_stride + pos] = s * ks;
         }
     }
 }
@@ -304,7 +331,7 @@ __device__ __forceinline__ void st_merge_rows(const DecodeParams &p, int b, int 
     }
 }
 
-template <int NH, bool kAppend, bool kMerge>
+template <int NH, bool kAppend, bool kMerge, int kWhat>
 __global__ void __launch_bounds__(StSmem<NH, kAppend>::kThreads, 1)
 slim_decode_stream_kernel(const __grid_constant__ CUtensorMap map_tile, const __grid_constant__ CUtensorMap map_tail,
                           const DecodeParams p, const int B)
@@ -344,10 +371,11 @@ slim_decode_stream_kernel(const __grid_constant__ CUtensorMap map_tile, const __
         }
     };
     auto page_ids = [&](int bb, int cc) {
-        const int32_t *bt = p.block_table + (size_t)bb * p.max_pages_per_seq + cc * 2;
+        const int first = cc * 2 + (kWhat == kStTail ? st_start<kWhat>(p, bb) / kPageTokens : 0);
+        const int32_t *bt = p.block_table + (size_t)bb * p.max_pages_per_seq + first;
         int2 r;
-        r.x = (cc * 2 < p.max_pages_per_seq) ? __ldg(bt) : 0;
-        r.y = (cc * 2 + 1 < p.max_pages_per_seq) ? __ldg(bt + 1) : 0;
+        r.x = (first < p.max_pages_per_seq) ? __ldg(bt) : 0;
+        r.y = (first + 1 < p.max_pages_per_seq) ? __ldg(bt + 1) : 0;
         return r;
     };
     const uint64_t stream_policy = tc::policy_evict_first();   // cache rows are read once per launch
@@ -366,7 +394,7 @@ slim_decode_stream_kernel(const __grid_constant__ CUtensorMap map_tile, const __
             const int2 cpg = w_pg;
             // ---- the next chunk's coordinates and page ids, requested before this chunk's copies are issued
             if (n + 1 < n_end) {
-                st_next_chunk(p, B, w_b, w_head, w_chunk, w_len, w_nc);
+                st_next_chunk<kWhat>(p, B, w_b, w_head, w_chunk, w_len, w_nc);
                 w_pg = page_ids(min(w_b, B - 1), w_chunk);
             }
             int page[2] = {cpg.x, cpg.y};
@@ -450,8 +478,9 @@ slim_decode_stream_kernel(const __grid_constant__ CUtensorMap map_tile, const __
     if (warp == kPW) tc::tmem_alloc(smem_u32(tmem_slot), L::kTmemCols);
     if (warp == kPW || warp == kPW + 1) {
         // Up to here the block may run beside the kernel before it in the stream (the same step's
-        // slim_kv_append); from here on it reads what earlier kernels may have written.
-        pdl_wait();
+        // slim_kv_append); from here on it reads what earlier kernels may have written.  (The tail launch follows the
+        // prefix kernel, which writes nothing that is read here and has itself waited for everything before it.)
+        if (kWhat != kStTail) pdl_wait();
         // ---- this block's contiguous range of chunks, in (sequence, kv head, chunk) order.  The work is cut
         //      by 128-token tiles (what a chunk costs) and the cut points are moved up to chunk starts.  The first
         //      producer warp finds where the range starts, the second where it ends, at the same time.
@@ -466,11 +495,11 @@ slim_decode_stream_kernel(const __grid_constant__ CUtensorMap map_tile, const __
         cut.b = cut.head = cut.chunk = cut.len = 0;
         cut.nc = 1;
         const int which = warp - kPW;   // 0: the range's start, 1: its end
-        const int len_first = (lane < B) ? st_chunk_len(p, lane) : 0;   // tokens of the first 32 sequences that chunks cover
+        const int len_first = (lane < B) ? st_chunk_len<kWhat>(p, lane) : 0;   // tokens of the first 32 sequences that chunks cover
         const int len_u = __shfl_sync(0xffffffffu, len_first, 0);
         bool uniform = __all_sync(0xffffffffu, lane >= B || len_first == len_u);
         for (int base = 32; base < B && uniform; base += 32)
-            uniform = __all_sync(0xffffffffu, base + lane >= B || st_chunk_len(p, base + lane) == len_u);
+            uniform = __all_sync(0xffffffffu, base + lane >= B || st_chunk_len<kWhat>(p, base + lane) == len_u);
         if (uniform) {
             // every sequence has the same length (a batch decoded in lockstep): the cut has a closed form
             const int nt = (len_u + kStTile - 1) / kStTile, nc = (len_u + kStChunk - 1) / kStChunk;
@@ -495,7 +524,7 @@ slim_decode_stream_kernel(const __grid_constant__ CUtensorMap map_tile, const __
             auto scan_block = [&](int base) {
                 Scan r;
                 const int b = base + lane;
-                r.len = (base == 0) ? len_first : ((b < B) ? st_chunk_len(p, b) : 0);
+                r.len = (base == 0) ? len_first : ((b < B) ? st_chunk_len<kWhat>(p, b) : 0);
                 r.nt = (r.len + kStTile - 1) / kStTile;
                 r.nc = (r.len + kStChunk - 1) / kStChunk;
                 r.it = r.nt;
@@ -543,7 +572,7 @@ slim_decode_stream_kernel(const __grid_constant__ CUtensorMap map_tile, const __
             if (which == 0) {
                 // one step from the chunk before the cut: a cut at the end of a run moves to the next run with chunks
                 int b0 = cut.b, head0 = cut.head, chunk0 = cut.chunk - 1, nc0 = cut.nc, len0 = cut.len;
-                st_next_chunk(p, B, b0, head0, chunk0, len0, nc0);
+                st_next_chunk<kWhat>(p, B, b0, head0, chunk0, len0, nc0);
                 range[1] = min(b0, B - 1);   // (beyond the last sequence only when the range is empty)
                 range[2] = head0;
                 range[3] = chunk0;
@@ -674,20 +703,20 @@ slim_decode_stream_kernel(const __grid_constant__ CUtensorMap map_tile, const __
             //      last chunk; those pairs are dealt to the block's consumer warps in turn, from the last warp down (the
             //      first group takes the block's first chunk).  A sequence of one token has no chunk: its pairs are
             //      dealt to the blocks by index.
-            pdl_wait();
+            if (kWhat != kStTail) pdl_wait();
             if (cnt > 0) {
                 int b = range[1], head = range[2];
                 int L = range[5] + 1;   // the chunks cover all of the sequence's tokens but the last
                 int nc = range[4];
                 int last = nc - 1 - range[3];   // list index of the pair's last chunk
                 for (int r = 0; last < cnt; ++r) {
-                    if (kPW - 1 - r % kPW == warp) st_last_token<kAppend>(p, b, head, L, nc, lane, false);
+                    if (kPW - 1 - r % kPW == warp) st_last_token<kAppend, kWhat>(p, b, head, L, nc, lane, false);
                     // the next pair with chunks
                     if (++head == p.Hkv) {
                         head = 0;
                         do {
                             ++b;
-                            L = (b < B) ? st_clamped_len(p, b) : 0;
+                            L = (b < B) ? st_clamped_len<kWhat>(p, b) : 0;
                         } while (b < B && L < 2);
                         if (b >= B) break;
                         nc = (L - 1 + kStChunk - 1) / kStChunk;
@@ -698,7 +727,7 @@ slim_decode_stream_kernel(const __grid_constant__ CUtensorMap map_tile, const __
             const long long pairs = (long long)B * p.Hkv;
             for (long long pr = blockIdx.x + (long long)warp * gridDim.x; pr < pairs; pr += (long long)kPW * gridDim.x) {
                 const int b = (int)st_div(pr, p.Hkv), head = (int)(pr - (long long)b * p.Hkv);
-                if (st_clamped_len(p, b) == 1) st_last_token<kAppend>(p, b, head, 1, 0, lane, kMerge);
+                if (st_clamped_len<kWhat>(p, b) == 1) st_last_token<kAppend, kWhat>(p, b, head, 1, 0, lane, kMerge);
             }
         }
         for (int n = g; n < cnt; n += kStGroups) {
@@ -789,6 +818,8 @@ slim_decode_stream_kernel(const __grid_constant__ CUtensorMap map_tile, const __
                         // 65536 hi + 256 mid + lo; each plane's sum is below 2^22 in magnitude
                         const float x = fmaf((float)(int)r[h], 65536.f, (float)(((int)r[NH + h] << 8) + (int)r[2 * NH + h]));
                         s[t][h] = (valid[t] && h < p.G) ? fmaf(x, sk[t] * rowscale[h], lsv[t]) : -INFINITY;
+                        if (kWhat == kStScores && valid[t] && h < p.G && record_ok)
+                            p.scores[((size_t)b * p.Hq + h0 + h) * p.score_stride + chunk * kStChunk + t * kStTile + gtid] = x * (sk[t] * rowscale[h]);
                         mloc[h] = fmaxf(mloc[h], s[t][h]);
                     }
                 } else {
@@ -849,7 +880,7 @@ slim_decode_stream_kernel(const __grid_constant__ CUtensorMap map_tile, const __
 #pragma unroll
                 for (int h = 0; h < NH; ++h) {
                     if (h < p.G && record_ok) {
-                        const size_t ps = ((size_t)b * p.Hq + h0 + h) * p.n_slots + chunk;
+                        const size_t ps = st_slot<kWhat>(p, (size_t)b * p.Hq + h0 + h, chunk);
                         p.part_o[ps * kHeadDim + gtid] = (float)(((int)r[h] << 8) + (int)r[NH + h]) * (1.f / kStPFix);
                     }
                 }
@@ -869,7 +900,7 @@ slim_decode_stream_kernel(const __grid_constant__ CUtensorMap map_tile, const __
 #pragma unroll
                 for (int o = kLanesPerHead / 2; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
                 if (seg == 0 && h < p.G && record_ok) {
-                    const size_t ps = ((size_t)b * p.Hq + h0 + h) * p.n_slots + chunk;
+                    const size_t ps = st_slot<kWhat>(p, (size_t)b * p.Hq + h0 + h, chunk);
                     const float4 mw = *reinterpret_cast<const float4 *>(red_m + h * 4);
                     p.part_ml[ps * 2] = fmaxf(fmaxf(mw.x, mw.y), fmaxf(mw.z, mw.w));
                     p.part_ml[ps * 2 + 1] = l;
@@ -916,7 +947,7 @@ slim_decode_stream_kernel(const __grid_constant__ CUtensorMap map_tile, const __
                         int len;
                         do {
                             ++b;
-                            len = (b < B) ? st_chunk_len(p, b) : kStChunk;   // b < B always holds inside the range
+                            len = (b < B) ? st_chunk_len<kWhat>(p, b) : kStChunk;   // b < B always holds inside the range
                         } while (len == 0);
                         nc = (len + kStChunk - 1) / kStChunk;
                     }
@@ -925,7 +956,7 @@ slim_decode_stream_kernel(const __grid_constant__ CUtensorMap map_tile, const __
             // sequences without tokens have no partial and therefore no merge: their rows are zero (a sequence of one
             // token was written by the warp that attended it)
             for (int b = blockIdx.x; b < B; b += gridDim.x) {
-                if (st_clamped_len(p, b) != 0) continue;
+                if (st_clamped_len<kWhat>(p, b) != 0) continue;
                 uint4 *dst = reinterpret_cast<uint4 *>(p.out + (size_t)b * p.Hq * kHeadDim);
                 for (int i = tid; i < p.Hq * (kHeadDim / 8); i += kPW * 32) dst[i] = make_uint4(0, 0, 0, 0);
             }
@@ -943,20 +974,45 @@ slim_decode_stream_kernel(const __grid_constant__ CUtensorMap map_tile, const __
         __syncwarp();
         tc::fence_after_sync();
         tc::tmem_dealloc(*tmem_slot, L::kTmemCols);   // (this warp allocated it; the block's last barrier lies behind)
+        // the merge kernel waits for this launch only: it must not end before the prefix kernel has
+        if (kWhat == kStTail) pdl_wait();
     }
 }
 
-template <int NH, bool kAppend, bool kMerge>
+template <int NH, bool kAppend, bool kMerge, int kWhat>
 static int launch_stream(dim3 grid, cudaStream_t stream, const CUtensorMap &map_tile, const CUtensorMap &map_tail,
                          const DecodeParams &p, int B)
 {
     constexpr int bytes = (int)StSmem<NH, kAppend>::kBytes;
-    const int rc = allow_dynamic_smem(reinterpret_cast<const void *>(slim_decode_stream_kernel<NH, kAppend, kMerge>), bytes);
+    const int rc = allow_dynamic_smem(reinterpret_cast<const void *>(slim_decode_stream_kernel<NH, kAppend, kMerge, kWhat>), bytes);
     if (rc != SLIM_OK) return rc;
-    SLIM_CUDA_TRY(launch_pdl(slim_decode_stream_kernel<NH, kAppend, kMerge>, grid, dim3(StSmem<NH, kAppend>::kThreads), bytes, stream, map_tile,
+    SLIM_CUDA_TRY(launch_pdl(slim_decode_stream_kernel<NH, kAppend, kMerge, kWhat>, grid, dim3(StSmem<NH, kAppend>::kThreads), bytes, stream, map_tile,
                              map_tail, p, B));
     SLIM_CUDA_TRY(cudaGetLastError());
     return SLIM_OK;
+}
+
+template <int NH, int kWhat>
+static int launch_stream_form(dim3 grid, cudaStream_t stream, const CUtensorMap &map_tile, const CUtensorMap &map_tail,
+                              const DecodeParams &p, int B)
+{
+    const bool append = p.k_new != nullptr;
+    if constexpr (kWhat != kStTail) {   // (a tail's partials are merged with the prefix's by the merge kernel)
+        if (p.counters != nullptr) {
+            if (append) return launch_stream<NH, true, true, kWhat>(grid, stream, map_tile, map_tail, p, B);
+            return launch_stream<NH, false, true, kWhat>(grid, stream, map_tile, map_tail, p, B);
+        }
+    }
+    if (append) return launch_stream<NH, true, false, kWhat>(grid, stream, map_tile, map_tail, p, B);
+    return launch_stream<NH, false, false, kWhat>(grid, stream, map_tile, map_tail, p, B);
+}
+
+template <int kWhat>
+static int launch_stream_what(dim3 grid, cudaStream_t stream, const CUtensorMap &map_tile, const CUtensorMap &map_tail,
+                              const DecodeParams &p, int B)
+{
+    if (p.G <= 8) return launch_stream_form<8, kWhat>(grid, stream, map_tile, map_tail, p, B);
+    return launch_stream_form<16, kWhat>(grid, stream, map_tile, map_tail, p, B);
 }
 
 int launch_decode_split_stream(const slim_cache_t *c, const DecodeParams &p, int B, cudaStream_t stream)
@@ -970,23 +1026,10 @@ int launch_decode_split_stream(const slim_cache_t *c, const DecodeParams &p, int
     rc = sm_count(&sms);
     if (rc != SLIM_OK) return rc;
     const long long max_items = (long long)p.n_chunks * p.Hkv * B;
-    const unsigned grid = (unsigned)(max_items < sms ? max_items : sms);
-    const dim3 blocks(grid);
-    const bool append = p.k_new != nullptr, merge = p.counters != nullptr;
-    if (p.G <= 8) {
-        if (merge) {
-            if (append) return launch_stream<8, true, true>(blocks, stream, map_tile, map_tail, p, B);
-            return launch_stream<8, false, true>(blocks, stream, map_tile, map_tail, p, B);
-        }
-        if (append) return launch_stream<8, true, false>(blocks, stream, map_tile, map_tail, p, B);
-        return launch_stream<8, false, false>(blocks, stream, map_tile, map_tail, p, B);
-    }
-    if (merge) {
-        if (append) return launch_stream<16, true, true>(blocks, stream, map_tile, map_tail, p, B);
-        return launch_stream<16, false, true>(blocks, stream, map_tile, map_tail, p, B);
-    }
-    if (append) return launch_stream<16, true, false>(blocks, stream, map_tile, map_tail, p, B);
-    return launch_stream<16, false, false>(blocks, stream, map_tile, map_tail, p, B);
+    const dim3 grid((unsigned)(max_items < sms ? max_items : sms));
+    if (p.shared_len != nullptr) return launch_stream_what<kStTail>(grid, stream, map_tile, map_tail, p, B);
+    if (p.scores != nullptr) return launch_stream_what<kStScores>(grid, stream, map_tile, map_tail, p, B);
+    return launch_stream_what<kStPlain>(grid, stream, map_tile, map_tail, p, B);
 }
 
 }  // namespace slim

@@ -114,6 +114,78 @@ class LayerRun:
         return codes[0], scales[0], codes[1], scales[1]
 
 
+class RotatedRun:
+    """One attention layer of a serving loop on a cache of bounded size: projections in, attention out.
+
+    The queries and keys of every token are normed, rotated by position and the keys and values quantised into the cache
+    in one call; every decode step accumulates the tokens' attention weights; evict() cuts each sequence back to `budget`
+    tokens by those weights (the first n_sink and the last n_recent always stay).  Slots stop telling positions then, so
+    positions are counted here (`seen`) and kept per slot (`positions`)."""
+
+    def __init__(self, B, Hq, Hkv, max_tokens, inv_freq, q_weight=None, k_weight=None, eps=1e-6, interleaved=False, budget=None, n_sink=4,
+                 n_recent=32, decay=1.0, device="cuda"):
+        self.B, self.Hq, self.Hkv, self.device = B, Hq, Hkv, torch.device(device)
+        self.pages = (max_tokens + PAGE_TOKENS - 1) // PAGE_TOKENS
+        self.max_tokens = self.pages * PAGE_TOKENS
+        self.budget, self.n_sink, self.n_recent, self.decay = budget, n_sink, n_recent, decay
+        self.sm_scale = slim.HEAD_DIM ** -0.5
+        self.cache = slim.SlimCache(B, Hkv, self.pages, device=device)
+        on = lambda t: None if t is None else t.to(self.device)  # noqa: E731
+        self.rope = slim.NormRope(on(inv_freq), on(q_weight), on(k_weight), eps, interleaved=interleaved)
+        self.weights = torch.zeros((B, Hkv, self.max_tokens), dtype=torch.float32, device=device)
+        self.positions = torch.zeros((B, Hkv, self.max_tokens), dtype=torch.int32, device=device)
+        self.lens, self.seen, self.placed = [0] * B, [0] * B, [0] * B
+        self.weighed = [0] * B        # tokens that the weights cover
+        self.ws_prefill = slim.workspace(slim.PHASE_PREFILL, B, Hq, Hkv, self.max_tokens, self.max_tokens, device=device)
+        self.ws_decode = slim.weights_workspace(B, Hq, Hkv, self.max_tokens, device=device)
+        self.ws_evict = None if budget is None else slim.evict_workspace(B, Hkv, self.max_tokens, budget, device=device)
+        self.q_last = None            # the last call's normed and rotated queries
+
+    def _i32(self, values):
+        return torch.tensor(values, dtype=torch.int32, device=self.device)
+
+    def _append(self, qkv, counts):
+        """qkv bf16 [tokens, Hq + 2 Hkv, 128]: the next counts[b] tokens of every sequence, as the fused projection leaves them."""
+        if any(n + c > self.max_tokens for n, c in zip(self.lens, counts)):
+            raise ValueError("the cache is full: evict first")
+        q, k, v = qkv[:, :self.Hq], qkv[:, self.Hq:self.Hq + self.Hkv], qkv[:, self.Hq + self.Hkv:]
+        cu = [0]
+        for c in counts:
+            cu.append(cu[-1] + c)
+        positions = self._i32([s + t for s, c in zip(self.seen, counts) for t in range(c)]).view(1, -1)
+        self.q_last = torch.empty((qkv.shape[0], self.Hq, slim.HEAD_DIM), dtype=torch.bfloat16, device=self.device)
+        slim.slim_norm_rope_append(self.cache, self.rope, q, self.q_last, k, v, positions, self._i32(cu), self._i32(self.lens), self.B)
+        self.lens = [n + c for n, c in zip(self.lens, counts)]
+        self.seen = [n + c for n, c in zip(self.seen, counts)]
+        return cu
+
+    def prompt(self, qkv, counts):
+        """Causal attention of the next counts[b] tokens of every sequence; per sequence bf16 [counts[b], Hq, 128]."""
+        cu = self._append(qkv, counts)
+        out = torch.empty_like(self.q_last)
+        slim.slim_attn_prefill(self.cache, self.q_last, out, self._i32(cu), self._i32(self.lens), self.B, max(counts), max(self.lens), self.Hq,
+                               self.sm_scale, self.ws_prefill)
+        return [out[cu[b]:cu[b + 1]] for b in range(self.B)]
+
+    def step(self, qkv):
+        """One new token per sequence (bf16 [B, Hq + 2 Hkv, 128]): appended, attended, every cached token's weight accumulated."""
+        self._append(qkv, [1] * self.B)
+        out = torch.empty_like(self.q_last)
+        slim.slim_attn_decode_weights(self.cache, self.q_last, out, self.weights, self.weights, self._i32(self.weighed), self._i32(self.lens), self.B,
+                                      max(self.lens), self.Hq, self.sm_scale, self.decay, self.ws_decode)
+        self.weighed = list(self.lens)
+        return out
+
+    def evict(self):
+        """Cuts every sequence back to the budget.  The weights must cover every cached token: call it after a step."""
+        if self.budget is None or self.weighed != self.lens:
+            raise ValueError("no budget, or tokens that no step has weighed")
+        slim.slim_kv_evict(self.cache, self.weights, self.weights, self.positions, self.positions, self._i32(self.lens), self._i32(self.placed),
+                           self._i32(self.seen), self.B, max(self.lens), self.budget, self.n_sink, self.n_recent, self.ws_evict)
+        self.lens = [min(n, self.budget) for n in self.lens]
+        self.weighed, self.placed = list(self.lens), list(self.lens)
+
+
 def run_workload(w: Workload, device="cuda", decode_steps=None, block_table=None, num_pages=None, one_call_step=False):
     """The workload's full call sequence.  Returns (LayerRun, prefill outputs per sequence or None,
     {decode step: output [B, Hq, 128]}); decode_steps limits which steps' outputs are kept.  With one_call_step
