@@ -10,34 +10,11 @@
 
 #include "slim_common.cuh"
 #include "slim_decode_params.cuh"
+#include "slim_merge.cuh"
 
 namespace slim {
 
-constexpr int kChunkTok = 256;   // tokens per partial result (two pages)
 static_assert(kDecodeHeaderBytes == SLIM_WORKSPACE_HEADER_BYTES, "the header size promised in slim.h");
-
-// Partials of a row of `len` cached tokens (never more than cap_tokens): one per 256-token chunk of the
-// tokens before the last one, then the last token's own.
-__device__ __forceinline__ int merge_row_partials(int len, int cap_tokens)
-{
-    const int L = min(max(len, 0), cap_tokens);
-    return (L == 0) ? 0 : (L - 1 + kChunkTok - 1) / kChunkTok + 1;
-}
-
-// The same for a row whose first tokens are a shared prefix: the prefix's slots (every one of them is filled, those without
-// a key with weight 0), then the tail's partials.  Without a prefix cap_tokens bounds the whole row, with one the tail.
-struct MergeRows {
-    const int32_t *kv_len, *shared_len;   // shared_len null: no prefix
-    int slot0, max_pages, cap_tokens;
-    __device__ __forceinline__ int partials(int b) const
-    {
-        const int len = __ldg(kv_len + b);
-        if (shared_len == nullptr) return merge_row_partials(len, cap_tokens);
-        const int start = min(max(__ldg(shared_len + b), 0) / kPageTokens, max_pages) * kPageTokens;
-        const int tail = merge_row_partials(len - start, min(max_pages * kPageTokens - start, cap_tokens));
-        return (tail == 0 && min(len, start) <= 0) ? 0 : slot0 + tail;
-    }
-};
 
 // Second pass: log-sum-exp merge of a row's chunk partials,
 //   M = max m_c;  l = sum l_c 2^(m_c - M);  o = sum O_c 2^(m_c - M) / l.
@@ -117,14 +94,6 @@ slim_decode_merge_kernel(const float *__restrict__ part_o, const float *__restri
     }
 }
 
-// A row's merged partial (what slim_attn_decode_partial returns): O relative to M, then M and l; a lane owns four dims.
-__device__ __forceinline__ void store_raw_partial(float *raw, int row, int lane, float4 o, float M, float l)
-{
-    float *dst = raw + (size_t)row * SLIM_PARTIAL_FLOATS;
-    reinterpret_cast<float4 *>(dst)[lane] = o;
-    if (lane == 0) *reinterpret_cast<float2 *>(dst + kHeadDim) = make_float2(M, l);
-}
-
 // A 16-byte load past the L1 cache that the compiler keeps where it is written (the merge kernels request a
 // row's partials before the values that decide which of them count have arrived).
 __device__ __forceinline__ float4 ld_cg_now(const float4 *ptr)
@@ -134,62 +103,16 @@ __device__ __forceinline__ float4 ld_cg_now(const float4 *ptr)
     return v;
 }
 
-// The same merge for rows of fewer than 32 chunks: one warp per (sequence, query head) row, a lane owns four head
-// dims, lane c owns chunk c's (m, l).  Once the row's length has arrived, the (m, l) pairs and the first sixteen
-// partial outputs of the row are requested together, so a row costs two round trips to memory instead of one per
-// step of the reduction.  (Asking for the sixteen slots before the length is known, as the block-per-row kernel below
-// does, read half as much again on ragged batches and was 0.5 us slower on the 64 / 8-head workload.)
-constexpr int kMergeWarpBatch = 16;
+// Rows of fewer than 32 chunks: one warp per row (slim_merge.cuh).
 constexpr int kMergeWarpsPerBlock = 8;
 __global__ void __launch_bounds__(kMergeWarpsPerBlock * 32)
 slim_decode_merge_warp_kernel(const float *__restrict__ part_o, const float *__restrict__ part_ml,
                               const MergeRows rows, __nv_bfloat16 *__restrict__ out, float *__restrict__ raw,
                               int B, int Hq, int n_slots)
 {
-    const int lane = threadIdx.x & 31;
     const int row = blockIdx.x * kMergeWarpsPerBlock + (threadIdx.x >> 5);   // b * Hq + h
     pdl_wait();   // the split pass before this kernel must have finished writing the partials
-    if (row >= B * Hq) return;
-    const int nc = rows.partials(row / Hq);
-    const float2 *ml = reinterpret_cast<const float2 *>(part_ml) + (size_t)row * n_slots;
-    const float4 *po = reinterpret_cast<const float4 *>(part_o + (size_t)row * n_slots * kHeadDim) + lane;
-    float4 o[kMergeWarpBatch];
-#pragma unroll
-    for (int u = 0; u < kMergeWarpBatch; ++u)
-        o[u] = (u < nc) ? __ldcg(po + (size_t)u * (kHeadDim / 4)) : make_float4(0.f, 0.f, 0.f, 0.f);
-    float2 v = (lane < nc) ? __ldcg(ml + lane) : make_float2(-INFINITY, 0.f);
-    if (lane >= nc) v = make_float2(-INFINITY, 0.f);
-    const float M = warp_max(v.x);
-    const float w = (lane < nc) ? exp2f(v.x - M) : 0.f;
-    const float l = warp_sum(v.y * w);
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int c0 = 0; c0 < nc; c0 += kMergeWarpBatch) {
-        if (c0 > 0) {
-#pragma unroll
-            for (int u = 0; u < kMergeWarpBatch; ++u)
-                o[u] = (c0 + u < nc) ? __ldcg(po + (size_t)(c0 + u) * (kHeadDim / 4)) : make_float4(0.f, 0.f, 0.f, 0.f);
-        }
-#pragma unroll
-        for (int u = 0; u < kMergeWarpBatch; ++u) {
-            const float wj = __shfl_sync(0xffffffffu, w, (c0 + u) & 31);
-            if (c0 + u < nc) {
-                acc.x = fmaf(o[u].x, wj, acc.x);
-                acc.y = fmaf(o[u].y, wj, acc.y);
-                acc.z = fmaf(o[u].z, wj, acc.z);
-                acc.w = fmaf(o[u].w, wj, acc.w);
-            }
-        }
-    }
-    if (raw != nullptr) {
-        store_raw_partial(raw, row, lane, nc > 0 ? acc : make_float4(0.f, 0.f, 0.f, 0.f), nc > 0 ? M : -INFINITY, nc > 0 ? l : 0.f);
-        return;
-    }
-    const float inv = (nc > 0 && l > 0.f) ? 1.f / l : 0.f;
-    __nv_bfloat162 lo = __floats2bfloat162_rn(acc.x * inv, acc.y * inv), hi = __floats2bfloat162_rn(acc.z * inv, acc.w * inv);
-    uint2 packed;
-    packed.x = *reinterpret_cast<uint32_t *>(&lo);
-    packed.y = *reinterpret_cast<uint32_t *>(&hi);
-    *reinterpret_cast<uint2 *>(out + (size_t)row * kHeadDim + lane * 4) = packed;
+    if (row < B * Hq) merge_row_by_warp(part_o, part_ml, rows, out, raw, row, row / Hq, n_slots, threadIdx.x & 31);
 }
 
 // Rows of 32 to 16 * kWarps chunks: one block per row, warp w owns the sixteen chunk slots [16 w, 16 w + 16) and
@@ -298,8 +221,8 @@ DecodeParams make_decode_params(const slim_cache_t *c, const void *q, const int3
     p.k_new = p.v_new = nullptr;
     p.out = nullptr;
     p.counters = nullptr;
-    p.scores = nullptr;
-    p.score_stride = 0;
+    p.shares = nullptr;
+    p.share_stride = 0;
     p.shared_len = nullptr;
     p.slot0 = 0;
     return p;
@@ -323,17 +246,12 @@ int launch_decode_merge(const slim_cache_t *c, void *out, const int32_t *kv_len,
 // kernel merges them itself when its blocks finish (one warp per pair); otherwise the merge kernel follows.
 constexpr int kInKernelMergeMaxPartials = 32;   // G * chunks of a (sequence, kv head) that one warp merges at the end of a block
 
-int launch_decode_params(const slim_cache_t *c, DecodeParams &p, int B, void *out, cudaStream_t stream)
+bool merge_in_split_kernel(DecodeParams &p, int B, void *out)
 {
-    if (p.n_chunks == 0) return launch_merge_rows(p, B, out, nullptr, stream);   // rows of zeros
-    const bool in_kernel = (long long)B * p.Hkv <= kDecodeCounterRows && p.G * p.n_slots <= kInKernelMergeMaxPartials;
-    if (in_kernel) {
-        p.out = static_cast<__nv_bfloat16 *>(out);
-        p.counters = reinterpret_cast<int *>(reinterpret_cast<char *>(p.status) + kDecodeStatusBytes);
-    }
-    const int rc = launch_decode_split_stream(c, p, B, stream);
-    if (rc != SLIM_OK || in_kernel) return rc;
-    return launch_merge_rows(p, B, out, nullptr, stream);
+    if ((long long)B * p.Hkv > kDecodeCounterRows || p.G * p.n_slots > kInKernelMergeMaxPartials) return false;
+    p.out = static_cast<__nv_bfloat16 *>(out);
+    p.counters = reinterpret_cast<int *>(reinterpret_cast<char *>(p.status) + kDecodeStatusBytes);
+    return true;
 }
 
 int launch_decode(const slim_cache_t *c, const void *q, const void *k_new, const void *v_new, void *out,
@@ -342,7 +260,11 @@ int launch_decode(const slim_cache_t *c, const void *q, const void *k_new, const
     DecodeParams p = make_decode_params(c, q, kv_len, B, max_kv, Hq, sm_scale, workspace);
     p.k_new = static_cast<const __nv_bfloat16 *>(k_new);
     p.v_new = static_cast<const __nv_bfloat16 *>(v_new);
-    return launch_decode_params(c, p, B, out, stream);
+    if (p.n_chunks == 0) return launch_merge_rows(p, B, out, nullptr, stream);   // rows of zeros
+    const bool in_kernel = merge_in_split_kernel(p, B, out);
+    const int rc = launch_decode_split_stream(c, p, B, stream);
+    if (rc != SLIM_OK || in_kernel) return rc;
+    return launch_merge_rows(p, B, out, nullptr, stream);
 }
 
 int launch_decode_merge(const slim_cache_t *c, void *out, const int32_t *kv_len, int B, int max_kv, int Hq,
@@ -355,13 +277,7 @@ int launch_decode_merge(const slim_cache_t *c, void *out, const int32_t *kv_len,
 int launch_merge_rows(const DecodeParams &p, int B, void *out, float *raw, cudaStream_t stream)
 {
     const int rows = B * p.Hq;
-    MergeRows r;
-    r.kv_len = p.kv_len;
-    r.shared_len = p.shared_len;
-    r.slot0 = p.slot0;
-    r.max_pages = p.max_pages_per_seq;
-    const long long chunk_tokens = (long long)p.n_chunks * kChunkTok;
-    r.cap_tokens = (int)std::min<long long>((long long)p.max_pages_per_seq * kPageTokens, chunk_tokens);
+    const MergeRows r = merge_rows(p);
     const float *po = p.part_o, *pm = p.part_ml;
     __nv_bfloat16 *o = static_cast<__nv_bfloat16 *>(out);
     const int Hq = p.Hq;

@@ -25,9 +25,10 @@ struct DecodeParams {
     int n_chunks;             // 256-token chunks that max_kv tokens need
     int n_slots;              // partial slots per row: n_chunks + 1 (the last token of a row has a partial of its own)
     float scale_log2e;        // sm_scale * log2(e)
-    // scores kept for the attention weights (optional): [B][Hq][score_stride], in log2 units, position by position
-    float *scores;
-    int score_stride;
+    // kept for the attention weights (optional): [B][Hq][share_stride], position by position a token's share of the
+    // denominator l of its partial, 2^(s - m)
+    float *shares;
+    int share_stride;
     // tokens behind a shared prefix (optional): the prefix's length per sequence, and the partial slots in front of
     // the tail's that the prefix kernel fills
     const int32_t *shared_len;
@@ -52,8 +53,8 @@ DecodeParams make_decode_params(const slim_cache_t *c, const void *q, const int3
                                 float sm_scale, void *workspace);
 size_t decode_workspace_bytes(int B, int Hq, int Hkv, int max_kv);
 int launch_decode_split_stream(const slim_cache_t *c, const DecodeParams &p, int B, cudaStream_t stream);
-// The split pass and, where it did not merge its own partials, the merge kernel (p.out and p.counters are set here).
-int launch_decode_params(const slim_cache_t *c, DecodeParams &p, int B, void *out, cudaStream_t stream);
+// Whether the split kernel merges its own partials (few per pair); p.out and p.counters are set then.
+bool merge_in_split_kernel(DecodeParams &p, int B, void *out);
 int launch_decode(const slim_cache_t *c, const void *q, const void *k_new, const void *v_new, void *out, const int32_t *kv_len, int B,
                   int max_kv, int Hq, float sm_scale, void *workspace, cudaStream_t stream);
 // The merge kernel: out (bf16 rows) or, where raw is given, the rows' merged partials.

@@ -131,7 +131,7 @@ __device__ __forceinline__ float st_ordered_float(int i)
 
 // What a launch does beside the plain split pass (a template argument, so that the plain kernel carries none of it).
 constexpr int kStPlain = 0;
-constexpr int kStScores = 1;   // every score also goes to p.scores (slim_attn_decode_weights turns them into attention weights)
+constexpr int kStShares = 1;   // every token's share of its partial's denominator also goes to p.shares (slim_attn_decode_weights)
 constexpr int kStTail = 2;     // only the tokens behind a shared prefix (slim_attn_decode_shared); the prefix kernel runs beside this one
 
 // The cached tokens of a sequence that this launch attends over start at position st_start: 0, or the end of the
@@ -273,7 +273,7 @@ __device__ __forceinline__ void st_last_token(const DecodeParams &p, int b, int 
                 dst[1] = make_float4(c[4], c[5], c[6], c[7]);
             }
             if (lane == 0) *reinterpret_cast<float2 *>(p.part_ml + ps * 2) = make_float2(fmaf(s, ks, lsv), rsv);
-            if (kWhat == kStScores && lane == 0) p.scores[(row0 + h0 + i) * p.score_stride + pos] = s * ks;
+            if (kWhat == kStShares && lane == 0) p.shares[(row0 + h0 + i) * p.share_stride + pos] = rsv;
         }
     }
 }
@@ -818,8 +818,6 @@ slim_decode_stream_kernel(const __grid_constant__ CUtensorMap map_tile, const __
                         // 65536 hi + 256 mid + lo; each plane's sum is below 2^22 in magnitude
                         const float x = fmaf((float)(int)r[h], 65536.f, (float)(((int)r[NH + h] << 8) + (int)r[2 * NH + h]));
                         s[t][h] = (valid[t] && h < p.G) ? fmaf(x, sk[t] * rowscale[h], lsv[t]) : -INFINITY;
-                        if (kWhat == kStScores && valid[t] && h < p.G && record_ok)
-                            p.scores[((size_t)b * p.Hq + h0 + h) * p.score_stride + chunk * kStChunk + t * kStTile + gtid] = x * (sk[t] * rowscale[h]);
                         mloc[h] = fmaxf(mloc[h], s[t][h]);
                     }
                 } else {
@@ -850,6 +848,7 @@ slim_decode_stream_kernel(const __grid_constant__ CUtensorMap map_tile, const __
                         if (t < n_tiles) {
                             const float e = st_exp2(s[t][h] - M);
                             lloc = fmaf(e, rsv[t], lloc);
+                            if (kWhat == kStShares) s[t][h] = e * rsv[t];   // the token's share of the chunk's denominator
                             const uint32_t bits = __float_as_uint(fmaf(e, kStPFix, 8388608.f));   // 2^23 + round(e * 65535)
                             unsigned char *pt = grp + L::kP + t * L::kPTileBytes;
                             pt[st_core_off(h, gtid)] = (unsigned char)((bits >> 8) & 0xFFu);
@@ -861,6 +860,16 @@ slim_decode_stream_kernel(const __grid_constant__ CUtensorMap map_tile, const __
             }
             tc::fence_proxy_async();
             tc::mbar_arrive(bar_ready_pv(g));         // P^T is in place (128 arrivals start the output MMAs)
+            if (kWhat == kStShares && record_ok) {
+                // (stored while the output MMAs run: ahead of them the stores cost 12 us of a 50 us launch)
+                float *dst = p.shares + ((size_t)b * p.Hq + h0) * p.share_stride + chunk * kStChunk + gtid;
+#pragma unroll
+                for (int h = 0; h < NH; ++h) {
+#pragma unroll
+                    for (int t = 0; t < 2; ++t)
+                        if (h < p.G && valid[t]) dst[(size_t)h * p.share_stride + t * kStTile] = s[t][h];
+                }
+            }
 
             wait(bar_mma_pv(g), mph);
             __syncwarp();
@@ -1028,7 +1037,7 @@ int launch_decode_split_stream(const slim_cache_t *c, const DecodeParams &p, int
     const long long max_items = (long long)p.n_chunks * p.Hkv * B;
     const dim3 grid((unsigned)(max_items < sms ? max_items : sms));
     if (p.shared_len != nullptr) return launch_stream_what<kStTail>(grid, stream, map_tile, map_tail, p, B);
-    if (p.scores != nullptr) return launch_stream_what<kStScores>(grid, stream, map_tile, map_tail, p, B);
+    if (p.shares != nullptr) return launch_stream_what<kStShares>(grid, stream, map_tile, map_tail, p, B);
     return launch_stream_what<kStPlain>(grid, stream, map_tile, map_tail, p, B);
 }
 

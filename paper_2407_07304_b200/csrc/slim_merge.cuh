@@ -1,0 +1,104 @@
+// The log-sum-exp merge of a row's partials by one warp, and what the merge kernels share.
+#pragma once
+#include "slim_common.cuh"
+#include "slim_decode_params.cuh"
+
+namespace slim {
+
+constexpr int kChunkTok = 256;   // tokens per partial result (two pages)
+
+// Partials of a row of `len` cached tokens (never more than cap_tokens): one per 256-token chunk of the
+// tokens before the last one, then the last token's own.
+__device__ __forceinline__ int merge_row_partials(int len, int cap_tokens)
+{
+    const int L = min(max(len, 0), cap_tokens);
+    return (L == 0) ? 0 : (L - 1 + kChunkTok - 1) / kChunkTok + 1;
+}
+
+// The same for a row whose first tokens are a shared prefix: the prefix's slots (every one of them is filled, those without
+// a key with weight 0), then the tail's partials.  Without a prefix cap_tokens bounds the whole row, with one the tail.
+struct MergeRows {
+    const int32_t *kv_len, *shared_len;   // shared_len null: no prefix
+    int slot0, max_pages, cap_tokens;
+    __device__ __forceinline__ int partials(int b) const
+    {
+        const int len = __ldg(kv_len + b);
+        if (shared_len == nullptr) return merge_row_partials(len, cap_tokens);
+        const int start = min(max(__ldg(shared_len + b), 0) / kPageTokens, max_pages) * kPageTokens;
+        const int tail = merge_row_partials(len - start, min(max_pages * kPageTokens - start, cap_tokens));
+        return (tail == 0 && min(len, start) <= 0) ? 0 : slot0 + tail;
+    }
+};
+
+inline MergeRows merge_rows(const DecodeParams &p)
+{
+    MergeRows r;
+    r.kv_len = p.kv_len;
+    r.shared_len = p.shared_len;
+    r.slot0 = p.slot0;
+    r.max_pages = p.max_pages_per_seq;
+    const long long pages = (long long)p.max_pages_per_seq * kPageTokens, chunks = (long long)p.n_chunks * kChunkTok;
+    r.cap_tokens = (int)(pages < chunks ? pages : chunks);
+    return r;
+}
+
+// A row's merged partial (what slim_attn_decode_partial returns): O relative to M, then M and l; a lane owns four dims.
+__device__ __forceinline__ void store_raw_partial(float *raw, int row, int lane, float4 o, float M, float l)
+{
+    float *dst = raw + (size_t)row * SLIM_PARTIAL_FLOATS;
+    reinterpret_cast<float4 *>(dst)[lane] = o;
+    if (lane == 0) *reinterpret_cast<float2 *>(dst + kHeadDim) = make_float2(M, l);
+}
+
+// The same merge for rows of fewer than 32 chunks: one warp per (sequence, query head) row, a lane owns four head
+// dims, lane c owns chunk c's (m, l).  Once the row's length has arrived, the (m, l) pairs and the first sixteen
+// partial outputs of the row are requested together, so a row costs two round trips to memory instead of one per
+// step of the reduction.  (Asking for the sixteen slots before the length is known, as the block-per-row kernel below
+// does, read half as much again on ragged batches and was 0.5 us slower on the 64 / 8-head workload.)
+constexpr int kMergeWarpBatch = 16;
+__device__ __forceinline__ void merge_row_by_warp(const float *part_o, const float *part_ml, const MergeRows &rows, __nv_bfloat16 *out,
+                                                  float *raw, int row, int b, int n_slots, int lane)
+{
+    const int nc = rows.partials(b);
+    const float2 *ml = reinterpret_cast<const float2 *>(part_ml) + (size_t)row * n_slots;
+    const float4 *po = reinterpret_cast<const float4 *>(part_o + (size_t)row * n_slots * kHeadDim) + lane;
+    float4 o[kMergeWarpBatch];
+#pragma unroll
+    for (int u = 0; u < kMergeWarpBatch; ++u)
+        o[u] = (u < nc) ? __ldcg(po + (size_t)u * (kHeadDim / 4)) : make_float4(0.f, 0.f, 0.f, 0.f);
+    float2 v = (lane < nc) ? __ldcg(ml + lane) : make_float2(-INFINITY, 0.f);
+    if (lane >= nc) v = make_float2(-INFINITY, 0.f);
+    const float M = warp_max(v.x);
+    const float w = (lane < nc) ? exp2f(v.x - M) : 0.f;
+    const float l = warp_sum(v.y * w);
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int c0 = 0; c0 < nc; c0 += kMergeWarpBatch) {
+        if (c0 > 0) {
+#pragma unroll
+            for (int u = 0; u < kMergeWarpBatch; ++u)
+                o[u] = (c0 + u < nc) ? __ldcg(po + (size_t)(c0 + u) * (kHeadDim / 4)) : make_float4(0.f, 0.f, 0.f, 0.f);
+        }
+#pragma unroll
+        for (int u = 0; u < kMergeWarpBatch; ++u) {
+            const float wj = __shfl_sync(0xffffffffu, w, (c0 + u) & 31);
+            if (c0 + u < nc) {
+                acc.x = fmaf(o[u].x, wj, acc.x);
+                acc.y = fmaf(o[u].y, wj, acc.y);
+                acc.z = fmaf(o[u].z, wj, acc.z);
+                acc.w = fmaf(o[u].w, wj, acc.w);
+            }
+        }
+    }
+    if (raw != nullptr) {
+        store_raw_partial(raw, row, lane, nc > 0 ? acc : make_float4(0.f, 0.f, 0.f, 0.f), nc > 0 ? M : -INFINITY, nc > 0 ? l : 0.f);
+        return;
+    }
+    const float inv = (nc > 0 && l > 0.f) ? 1.f / l : 0.f;
+    __nv_bfloat162 lo = __floats2bfloat162_rn(acc.x * inv, acc.y * inv), hi = __floats2bfloat162_rn(acc.z * inv, acc.w * inv);
+    uint2 packed;
+    packed.x = *reinterpret_cast<uint32_t *>(&lo);
+    packed.y = *reinterpret_cast<uint32_t *>(&hi);
+    *reinterpret_cast<uint2 *>(out + (size_t)row * kHeadDim + lane * 4) = packed;
+}
+
+}  // namespace slim

@@ -131,9 +131,9 @@ def test_workspace_sizes():
     # the scores: 4 bytes per query head and token, rounded up to whole chunks
     base = slim.slim_workspace_bytes(slim.PHASE_DECODE, 3, 8, 2, 1, 700)
     assert 3 * 8 * 768 * 4 <= L.slim_weights_workspace_bytes(3, 8, 2, 700) - base < 3 * 8 * 768 * 4 + 256
-    # a row of move lists per (sequence, kv head): never more than the budget, nor than what is cut
-    assert L.slim_evict_workspace_bytes(2, 3, 1000, 990) == 2 * 3 * (1 + 2 * 10) * 4
-    assert L.slim_evict_workspace_bytes(2, 3, 1000, 10) == 2 * 3 * (1 + 2 * 10) * 4
+    # three lists per (sequence, kv head): never more than the budget, nor than what is cut
+    assert L.slim_evict_workspace_bytes(2, 3, 1000, 990) == 2 * 3 * (1 + 3 * 10) * 4
+    assert L.slim_evict_workspace_bytes(2, 3, 1000, 10) == 2 * 3 * (1 + 3 * 10) * 4
     assert L.slim_evict_workspace_bytes(2, 3, 10, 1000) == 2 * 3 * 4
 
 

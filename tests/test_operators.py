@@ -483,6 +483,8 @@ EVICT_CASES = [
     ([300, 45, 1000], 2, 40, 3, 17, [0, 45, 77], False), ([1000, 700], 1, 999, 0, 999, None, False), ([513], 2, 512, 0, 0, None, True),
     ([4100, 2000], 2, 1024, 4, 256, [1024, 1024], False), ([9001], 2, 9000, 4, 64, [9000], True), ([20000, 12000], 1, 500, 0, 0, [500, 0], False),
     ([260] * 9, 5, 130, 0, 10, None, False), ([60001], 1, 3000, 16, 100, [3000], True), ([55000], 1, 54990, 0, 0, None, False),
+    ([16385, 70000], 1, 2000, 4, 300, [2000, 2000], True), ([66000], 1, 65990, 0, 0, None, False), ([65536], 1, 32768, 0, 0, [32768], False),
+    ([8193, 3], 2, 100, 1, 1, None, True),
 ]
 
 
