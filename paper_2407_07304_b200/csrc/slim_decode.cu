@@ -111,8 +111,14 @@ slim_decode_merge_warp_kernel(const float *__restrict__ part_o, const float *__r
                               int B, int Hq, int n_slots)
 {
     const int row = blockIdx.x * kMergeWarpsPerBlock + (threadIdx.x >> 5);   // b * Hq + h
+    const bool mine = row < B * Hq;
+    // Behind a shared prefix the lengths are read ahead of the wait (0.3 us of a step): this kernel starts only after every
+    // block of the prefix kernel has seen the end of everything before it in the stream.
+    int nc = (mine && rows.shared_len != nullptr) ? rows.partials(row / Hq) : 0;
     pdl_wait();   // the split pass before this kernel must have finished writing the partials
-    if (row < B * Hq) merge_row_by_warp(part_o, part_ml, rows, out, raw, row, row / Hq, n_slots, threadIdx.x & 31);
+    if (!mine) return;
+    if (rows.shared_len == nullptr) nc = rows.partials(row / Hq);
+    merge_row_by_warp(part_o, part_ml, nc, out, raw, row, n_slots, threadIdx.x & 31);
 }
 
 // Rows of 32 to 16 * kWarps chunks: one block per row, warp w owns the sixteen chunk slots [16 w, 16 w + 16) and
@@ -225,6 +231,7 @@ DecodeParams make_decode_params(const slim_cache_t *c, const void *q, const int3
     p.share_stride = 0;
     p.shared_len = nullptr;
     p.slot0 = 0;
+    p.max_blocks = 0;
     return p;
 }
 

@@ -33,6 +33,7 @@ struct DecodeParams {
     // the tail's that the prefix kernel fills
     const int32_t *shared_len;
     int slot0;
+    int max_blocks;   // of the split pass (0: one per SM)
 };
 
 // The length of the prefix that sequence b shares: whole pages, never beyond the page table.

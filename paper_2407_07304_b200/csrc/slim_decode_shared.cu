@@ -10,16 +10,22 @@
 //
 // Prefix kernel: a block owns up to 256 stacked rows of one (group, kv head) and one contiguous part of the prefix's 128-key
 // tiles; the number of parts fills the chip once.  The structure is that of the prefill kernel: TMA-staged INT8
-// tiles, dequantised in registers into fp16 operands code * scale / 2^e, scores and outputs on tcgen05 with
-// accumulators in tensor memory, thread = row in the softmax, rescaling only when the maximum grows by more than 2^8.
+// tiles, converted in registers into fp16 operands, scores and outputs on tcgen05 with accumulators in tensor memory, thread = row in the softmax, rescaling only when the maximum grows by more than 2^8.
+// K's operand is code * scale / 2^e rounded once: the fp16 scale goes in two parts.  (With the scale itself rounded to fp16
+// all 128 terms of a key's scores are off by up to 2^-11 in the same direction: half of the result's whole error.  Exact
+// codes as K's operand and the key's scale in the softmax cost 0.4 us per key tile of 256 rows.)  V's scale is rounded to
+// fp16: its errors are the tokens' own and average out over them.
 // With more than 128 rows the block's two softmax groups take 128 rows each and every key tile serves both; with at
 // most 128 rows both groups work on the same rows and take the key tiles in turn, so that the scores of one tile are
 // formed while the softmax of the other runs, and their two partials are merged through shared memory at the end.
 // The causal mask of the prefill kernel becomes a limit per row (a sequence may be shorter than the prefix).
 //
-// The tail kernel is launched as a programmatic dependent that does not wait for this one: its blocks start on the SMs
-// that the prefix blocks leave, and only their end waits for the prefix kernel (the merge kernel waits for the tail's).
+// The tail kernel is launched as a programmatic dependent that does not wait for this one: its blocks run beside the
+// prefix blocks, on the SMs left to them, and only their end waits for the prefix kernel (the merge kernel waits for the
+// tail's).
 #include <cuda.h>
+
+#include <type_traits>
 
 #include "slim_common.cuh"
 #include "slim_decode_params.cuh"
@@ -44,12 +50,17 @@ constexpr uint32_t kVf = kKf + 2 * 32768;       // two fp16 V tiles
 constexpr uint32_t kRaw = kVf + 2 * 32768;      // raw INT8 tiles: stage 0 K, stage 1 V
 constexpr uint32_t kRawScales = kRaw + 2 * 16384;
 constexpr uint32_t kMisc = kRawScales + 2 * 512;
-constexpr uint32_t kRowScale = kMisc + 512;     // float[2][128]; after the last key tile float2[128]: (m, l) of softmax group 1
-constexpr uint32_t kBytes = kRowScale + 1024;
+// where the softmax groups take the key tiles in turn: scales of a second raw stage (whose tiles lie in the unused second Q
+// tile), the rows' scales for group 1, and at the end, over the raw tiles, group 1's (m, l)
+constexpr uint32_t kRawScales1 = kMisc + 512;
+constexpr uint32_t kRowScale = kRawScales1 + 1024;
+constexpr uint32_t kMl = kRaw;
+constexpr uint32_t kBytes = kRowScale + 512;
 // kMisc: floats by key tile mod 4: [0,4) kexp, [4,8) log2 vexp, [8,12) 1 / vexp; byte 64: tensor-memory address;
 //        byte 72: failure flag; byte 76: tokens of the prefix that any sequence of the group has; byte 128..: mbarriers
-enum Bar { RAW_FULL = 0, RAW_EMPTY = 2, KF_FULL = 4, KF_EMPTY = 6, VF_FULL = 8, VF_EMPTY = 10,
-           S_FULL = 12, P_FULL = 14, O_DONE = 16, Q_FULL = 18, VEXP_FULL = 20, NUM_BARS = 24 };
+// (raw barriers: 2 * stage + kind, kind 0 K, 1 V)
+enum Bar { RAW_FULL = 0, RAW_EMPTY = 4, KF_FULL = 8, KF_EMPTY = 10, VF_FULL = 12, VF_EMPTY = 14,
+           S_FULL = 16, P_FULL = 18, O_DONE = 20, Q_FULL = 22, VEXP_FULL = 24, NUM_BARS = 28 };
 static_assert(128 + 8 * NUM_BARS <= 512, "mbarriers fit the misc area");
 static_assert(kBytes <= 232448, "shared memory budget of one block");
 }  // namespace shl
@@ -72,12 +83,18 @@ __device__ __forceinline__ float sh_max3(float a, float b, float c)
     asm("max.f32 %0, %1, %2, %3;\n" : "=f"(m) : "f"(a), "f"(b), "f"(c));
     return m;
 }
-__device__ __forceinline__ uint32_t sh_code_pair(uint32_t halves, uint32_t factor)
+template <bool kLow>
+__device__ __forceinline__ uint32_t sh_code_pair(uint32_t halves, uint32_t factor, uint32_t low)
 {
-    // halves: two fp16 numbers 1152 + code; (x - 1152) * factor
+    // halves: two fp16 numbers 1152 + code; code * (factor + low), rounded once, or code * factor
     uint32_t d, r;
     asm("sub.rn.f16x2 %0, %1, %2;\n" : "=r"(d) : "r"(halves), "r"(0x64806480u));
-    asm("mul.rn.f16x2 %0, %1, %2;\n" : "=r"(r) : "r"(d), "r"(factor));
+    if (kLow) {
+        asm("mul.rn.f16x2 %0, %1, %2;\n" : "=r"(r) : "r"(d), "r"(low));
+        asm("fma.rn.f16x2 %0, %1, %2, %3;\n" : "=r"(r) : "r"(d), "r"(factor), "r"(r));
+    } else {
+        asm("mul.rn.f16x2 %0, %1, %2;\n" : "=r"(r) : "r"(d), "r"(factor));
+    }
     return r;
 }
 
@@ -105,6 +122,12 @@ __device__ __forceinline__ void prefix_block(const CUtensorMap &codes_map, const
     int *known = reinterpret_cast<int *>(smem + shl::kMisc + 76);
     const uint32_t bar0 = sbase + shl::kMisc + 128;
     auto bar = [&](int which, int idx) { return bar0 + 8u * (uint32_t)(which + idx); };
+    // Raw stages per kind.  Where a tile is used by one group only, two: a tile takes the converters half as long as it
+    // takes to arrive.
+    constexpr int kRawStages = by_rows ? 1 : 2;
+    auto raw_tile = [&](int kv, int j) { return (kRawStages > 1 && (j & 1) ? shl::kQ + 32768u : shl::kRaw) + (uint32_t)kv * 16384u; };
+    auto raw_scales = [&](int kv, int j) { return (kRawStages > 1 && (j & 1) ? shl::kRawScales1 : shl::kRawScales) + (uint32_t)kv * 512u; };
+    auto raw_bar = [&](int which, int kv, int j) { return bar(which, 2 * (j % kRawStages) + kv); };
 
     // ---- the loader asks for the first raw tiles before the block's set-up is complete
     int raw_issued = 0;
@@ -113,10 +136,10 @@ __device__ __forceinline__ void prefix_block(const CUtensorMap &codes_map, const
     auto request_raw = [&](int i) {
         const int kv = i & 1, j = i >> 1;
         const int page = (page_next >= 0 && page_next < p.num_pages) ? page_next : 0;
-        const uint32_t full = bar(shl::RAW_FULL, kv);
+        const uint32_t full = raw_bar(shl::RAW_FULL, kv, j);
         tc::mbar_arrive_expect_tx(full, 16384 + 512);
-        tc::tma_load_2d(sbase + shl::kRaw + kv * 16384, &codes_map, 0, ((page * p.Hkv + head) * 2 + kv) * kPageTokens, full);
-        tc::bulk_load(sbase + shl::kRawScales + kv * 512, p.scales + scale_block_offset(page, head, kv, p.Hkv), 512, full);
+        tc::tma_load_2d(sbase + raw_tile(kv, j), &codes_map, 0, ((page * p.Hkv + head) * 2 + kv) * kPageTokens, full);
+        tc::bulk_load(sbase + raw_scales(kv, j), p.scales + scale_block_offset(page, head, kv, p.Hkv), 512, full);
         if (kv == 1 && j + 1 < T) {
             // the next key tile's page id, and its two tiles on their way into the L2
             if (by_rows || j0 + j + 1 < tiles) page_next = __ldg(bt + j + 1);
@@ -127,26 +150,41 @@ __device__ __forceinline__ void prefix_block(const CUtensorMap &codes_map, const
         ++raw_issued;
     };
     if (warp == 12 && lane == 0) {
-        for (int i = 0; i < 2; ++i) tc::mbar_init(bar(shl::RAW_FULL, i), 1);
+        for (int i = 0; i < 2 * kRawStages; ++i) tc::mbar_init(bar(shl::RAW_FULL, i), 1);
         tc::mbar_init_fence();
         page_next = __ldg(bt);
-        for (int i = 0; i < 2; ++i) request_raw(i);
+        for (int i = 0; i < 2 * kRawStages; ++i) request_raw(i);   // (T >= kRawStages)
     }
-    // ---- query rows, sixteen lanes per row: warp w of a group converts rows 32 (w & 3) + 2 i + (lane >> 4) of its tile
+    // ---- query rows, sixteen lanes per row: warp w of group t brings in and converts rows 32 (w & 3) + 2 i + (lane >> 4) of
+    //      its tile.  A row's 16-byte pieces go where their fp16 form will lie and are converted in place, so that both
+    //      loops stay rolled: unrolled over registers they are 15 KB of instructions that every block runs once, and
+    //      fetching those took longer than the rows.
     const bool has_q = warp < 8 && (warp < 4 || by_rows);
-    uint4 qv[16];
+    const int q_row = (warp & 3) * 32 + (lane >> 4), q_piece = lane & 15;
+    auto q_off = [&](int i) {   // (rows two apart: only the piece's slot depends on i beyond the stride)
+        const int rr = q_row + 2 * i;
+        return shl::kQ + (uint32_t)(warp >> 2) * 32768u + (uint32_t)(q_piece >> 3) * 16384u + (uint32_t)rr * 128u + (uint32_t)(((q_piece & 7) ^ (rr & 7)) << 4);
+    };
     if (has_q) {
-        const int t = warp >> 2;
-#pragma unroll
+        const int r0 = (warp >> 2) * kShTileRows + q_row;
+        int sq = (m0 + r0) / p.G, gq = m0 + r0 - sq * p.G;   // sequence and query head of row r0 + 2 i
+        const __nv_bfloat16 *src = p.q + ((size_t)seq0 * p.Hq + (size_t)head * p.G) * kHeadDim + q_piece * 8;
+#pragma unroll 4
         for (int i = 0; i < 16; ++i) {
-            const int r = t * kShTileRows + (warp & 3) * 32 + 2 * i + (lane >> 4);
-            qv[i] = make_uint4(0, 0, 0, 0);
-            if (r < rows) qv[i] = __ldg(reinterpret_cast<const uint4 *>(p.q + out_row(r) * kHeadDim) + (lane & 15));
+            if (r0 + 2 * i < rows)
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;\n" ::"r"(sbase + q_off(i)),
+                             "l"(src + ((size_t)sq * p.Hq + gq) * kHeadDim) : "memory");
+            else
+                *reinterpret_cast<uint4 *>(smem + q_off(i)) = make_uint4(0, 0, 0, 0);
+            gq += 2;
+            if (gq >= p.G) gq -= p.G, ++sq;
+            if (gq >= p.G) gq -= p.G, ++sq;   // (one query head per kv head)
         }
+        asm volatile("cp.async.commit_group;\n" ::: "memory");
     }
-    if (tid == 0) {
+    if (warp == 14 && lane == 0) {   // (a warp that has nothing else to do here)
         for (int t = 0; t < 2; ++t) {
-            tc::mbar_init(bar(shl::RAW_EMPTY, t), kShConvWarps);
+            for (int i = 0; i < kRawStages; ++i) tc::mbar_init(bar(shl::RAW_EMPTY, 2 * i + t), kShConvWarps);
             tc::mbar_init(bar(shl::KF_FULL, t), kShConvWarps);
             tc::mbar_init(bar(shl::KF_EMPTY, t), 1);
             tc::mbar_init(bar(shl::VF_FULL, t), kShConvWarps);
@@ -167,34 +205,6 @@ __device__ __forceinline__ void prefix_block(const CUtensorMap &codes_map, const
         for (int s = seq0 + lane; s < seq1; s += 32) most = max(most, min(__ldg(p.kv_len + s), decode_shared_tokens(p, s)));
         most = __reduce_max_sync(0xffffffffu, most);
         if (lane == 0) *known = most;
-    }
-    if (has_q) {
-        // Q rows -> fp16 (divided by a power of two near the row's absmax: the copy of bf16 is exact), A operand layout
-        const int t = warp >> 2;
-        float *row_scale = reinterpret_cast<float *>(smem + shl::kRowScale) + t * kShTileRows;
-        const int piece = lane & 15;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const int rr = (warp & 3) * 32 + 2 * i + (lane >> 4);
-            const uint32_t w[4] = {qv[i].x, qv[i].y, qv[i].z, qv[i].w};
-            float am = 0.f;
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-                am = fmaxf(am, fmaxf(fabsf(bf16_bits_to_float(w[k] & 0xFFFFu)), fabsf(bf16_bits_to_float(w[k] >> 16))));
-#pragma unroll
-            for (int o = 8; o > 0; o >>= 1) am = fmaxf(am, __shfl_xor_sync(0xffffffffu, am, o));
-            const float p2 = pow2_floor(am);
-            const float inv = pow2_recip(p2);
-            uint32_t hw[4];
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-                hw[k] = pack_half2(bf16_bits_to_float(w[k] & 0xFFFFu) * inv, bf16_bits_to_float(w[k] >> 16) * inv);
-            const uint32_t off = shl::kQ + (uint32_t)t * 32768u + (uint32_t)(piece >> 3) * 16384u + (uint32_t)rr * 128u +
-                                 (uint32_t)(((piece & 7) ^ (rr & 7)) << 4);
-            *reinterpret_cast<uint4 *>(smem + off) = make_uint4(hw[0], hw[1], hw[2], hw[3]);
-            if (piece == 0) row_scale[rr] = p2 * p.scale_log2e;
-        }
-        tc::fence_proxy_async();
     }
     tc::fence_before_sync();
     __syncthreads();
@@ -219,23 +229,69 @@ __device__ __forceinline__ void prefix_block(const CUtensorMap &codes_map, const
         // =========================================================== softmax of group t: thread = row
         const int t = warp >> 2;
         const int r = tid & 127;
+        float *row_scale = reinterpret_cast<float *>(smem + shl::kRowScale);
+        float rs = 0.f;   // row scale: sm_scale * log2(e) * the power of two that the row was divided by
+        if (has_q) {
+            // Q rows -> fp16, divided by a power of two near the row's absmax (the copy of bf16 is exact): thread = row, the
+            // sixteen pieces in place
+            unsigned char *at = smem + shl::kQ + (uint32_t)t * 32768u + (uint32_t)r * 128u;
+            asm volatile("cp.async.wait_group 0;\n" ::: "memory");
+            __syncwarp();   // the row was brought in by lanes of this warp
+            uint32_t m2 = 0;
+#pragma unroll 8
+            for (int c = 0; c < 16; ++c) {
+                const uint4 w = *reinterpret_cast<const uint4 *>(at + (c >> 3) * 16384 + (((c & 7) ^ (r & 7)) << 4));
+                m2 = ap_max_bf16x2(m2, ap_max_bf16x2(ap_max_bf16x2(ap_abs_bf16x2(w.x), ap_abs_bf16x2(w.y)), ap_max_bf16x2(ap_abs_bf16x2(w.z), ap_abs_bf16x2(w.w))));
+            }
+            const float p2 = pow2_floor(fmaxf(__uint_as_float(m2 << 16), __uint_as_float(m2 & 0xFFFF0000u)));
+            const float inv = pow2_recip(p2);
+            const uint64_t inv2 = ap_pack(inv, inv);
+#pragma unroll 4
+            for (int c = 0; c < 16; ++c) {
+                uint4 *piece = reinterpret_cast<uint4 *>(at + (c >> 3) * 16384 + (((c & 7) ^ (r & 7)) << 4));
+                const uint4 raw = *piece;
+                const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
+                uint32_t hw[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    float x0, x1;
+                    ap_unpack(ap_mul2(ap_pack(__uint_as_float(w[k] << 16), __uint_as_float(w[k] & 0xFFFF0000u)), inv2), x0, x1);
+                    hw[k] = pack_half2(x0, x1);
+                }
+                *piece = make_uint4(hw[0], hw[1], hw[2], hw[3]);
+            }
+            rs = p2 * p.scale_log2e;
+            if (!by_rows) row_scale[r] = rs;
+            tc::fence_proxy_async();
+        }
+        if (!by_rows) {
+            // group 1 works on group 0's rows
+            tc::named_barrier(2, 256);
+            rs = row_scale[r];
+        }
         const int my_row = by_rows ? t * kShTileRows + r : r;      // row of the block
         const uint32_t lane_base = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t tS = tmem + lane_base + kShTmemS + (uint32_t)t * 128u;
         const uint32_t tO = tmem + lane_base + kShTmemO + (uint32_t)t * 128u;
-        tc::mbar_arrive(bar(shl::Q_FULL, t));                      // the rows were converted before the set-up's barrier
-        const float rs = reinterpret_cast<const float *>(smem + shl::kRowScale)[by_rows ? tid : r];
+        tc::mbar_arrive(bar(shl::Q_FULL, t));
         int limit = tiles * kShKeys;                               // keys that the row sees (rows of no sequence: their zero queries harm nothing)
         if (my_row < rows) {
             const int s = seq0 + (m0 + my_row) / p.G;
             limit = min(limit, min(__ldg(p.kv_len + s), decode_shared_tokens(p, s)));
         }
+        const bool warp_rows = my_row - lane < rows;
         float m_run = -INFINITY, l_run = 0.f;
         for (int n = 0; n < steps; ++n) {
             const int j = by_rows ? n : 2 * n + t;                 // key tile of the block's part
             wait(bar(shl::S_FULL, t), (uint32_t)n & 1u);
             __syncwarp();
             tc::fence_after_sync();
+            if (!warp_rows) {
+                // no row of the stack in this warp: whatever lies in its score rows serves as P, nothing reads the result
+                tc::fence_before_sync();
+                tc::mbar_arrive(bar(shl::P_FULL, t));
+                continue;
+            }
             wait(bar(shl::VEXP_FULL, j & 3), (uint32_t)(j >> 2) & 1u);
             const float c = fmaxf(rs * misc_f[j & 3], 1e-37f);     // row scale * kexp of this key tile (> 0)
             const float F = misc_f[4 + (j & 3)];                   // log2 vexp
@@ -318,7 +374,7 @@ __device__ __forceinline__ void prefix_block(const CUtensorMap &codes_map, const
         __syncwarp();
         tc::fence_after_sync();
         unsigned char *stage0 = smem + shl::kKf, *stage1 = smem + shl::kVf;
-        float2 *ml1 = reinterpret_cast<float2 *>(smem + shl::kRowScale);
+        float2 *ml1 = reinterpret_cast<float2 *>(smem + shl::kMl);
         float w_own = 1.f, w_other = 0.f;
         if (!by_rows) {
             if (t == 1) ml1[r] = make_float2(m_run, l_run);
@@ -370,14 +426,14 @@ __device__ __forceinline__ void prefix_block(const CUtensorMap &codes_map, const
             // coalesced: a warp writes one of its rows' 512 bytes per store
             const unsigned char *stage = t ? stage1 : stage0;
             __syncwarp();
-            if (my_row < rows && ok) *reinterpret_cast<float2 *>(p.part_ml + (out_row(my_row) * p.n_slots + split) * 2) = make_float2(m_run, l_run);
+            const size_t ps = my_row < rows ? out_row(my_row) * p.n_slots + split : 0;
+            if (my_row < rows && ok) *reinterpret_cast<float2 *>(p.part_ml + ps * 2) = make_float2(m_run, l_run);
+            const int n_out = ok ? min(32, rows - (my_row - lane)) : 0;   // rows of this warp
 #pragma unroll 4
-            for (int i = 0; i < 32; ++i) {
+            for (int i = 0; i < n_out; ++i) {
                 const int rr = (warp & 3) * 32 + i;
-                const int row = (by_rows ? t * kShTileRows : 0) + rr;
-                if (row >= rows) break;
-                const float4 x = *reinterpret_cast<const float4 *>(stage + rr * 512 + (((lane + rr) & 31) << 4));
-                if (ok) reinterpret_cast<float4 *>(p.part_o + (out_row(row) * p.n_slots + split) * kHeadDim)[lane] = x;
+                const size_t to = (size_t)__shfl_sync(0xffffffffu, (unsigned long long)ps, i);
+                reinterpret_cast<float4 *>(p.part_o + to * kHeadDim)[lane] = *reinterpret_cast<const float4 *>(stage + rr * 512 + (((lane + rr) & 31) << 4));
             }
         }
     } else if (warp < 12 || warp >= 14) {
@@ -387,13 +443,13 @@ __device__ __forceinline__ void prefix_block(const CUtensorMap &codes_map, const
         const int n_rows = main_cv ? 1 : 2, c_first = main_cv ? 0 : 6, c_last = main_cv ? 6 : 8;
         const bool announces = warp == 8 && lane == 0;
         const int kept = min(*known, tiles * kShKeys) - j0 * kShKeys;      // tokens of the block's part that exist
-        for (int i = 0; i < 2 * T; ++i) {
-            const int kv = i & 1, j = i >> 1;
-            const bool is_k = kv == 0;
+        auto convert = [&](auto kind, int j) {
+            constexpr int kv = decltype(kind)::value;
+            constexpr bool is_k = kv == 0;
             const int buf = j & 1;
-            wait(bar(shl::RAW_FULL, kv), (uint32_t)j & 1u);
-            const unsigned char *raw = smem + shl::kRaw + kv * 16384;
-            const float *scales = reinterpret_cast<const float *>(smem + shl::kRawScales + kv * 512);
+            wait(raw_bar(shl::RAW_FULL, kv, j), (uint32_t)(j / kRawStages) & 1u);
+            const unsigned char *raw = smem + raw_tile(kv, j);
+            const float *scales = reinterpret_cast<const float *>(smem + raw_scales(kv, j));
             const int n_valid = min(kShKeys, kept - j * kShKeys);
             float wm = 0.f;
             {
@@ -422,8 +478,11 @@ __device__ __forceinline__ void prefix_block(const CUtensorMap &codes_map, const
             for (int q = 0; q < 2; ++q) {
                 if (q >= n_rows) break;
                 const int r = r0 + 64 * q;
+                // scale / 2^e in [0, 2) as the sum of two fp16 numbers
                 const float f = ((r < n_valid) ? scales[r] : 0.f) * rex;
                 const uint32_t fac2 = pack_half2(f, f);
+                const float f_low = f - __half2float(__low2half(*reinterpret_cast<const __half2 *>(&fac2)));
+                const uint32_t low2 = pack_half2(f_low, f_low);
                 unsigned char *dstb = dst_tile + r * 128;
                 for (int c = c_first; c < c_last; ++c) {
                     const uint4 w4 = *reinterpret_cast<const uint4 *>(raw + r * 128 + ((c ^ (r & 7)) << 4));
@@ -432,8 +491,8 @@ __device__ __forceinline__ void prefix_block(const CUtensorMap &codes_map, const
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
                         const uint32_t x = w[k] ^ 0x80808080u;   // byte code ^ 0x80 under 0x64 is the fp16 number 1152 + code
-                        hh[2 * k] = sh_code_pair(__byte_perm(x, 0x64646464u, 0x4140), fac2);
-                        hh[2 * k + 1] = sh_code_pair(__byte_perm(x, 0x64646464u, 0x4342), fac2);
+                        hh[2 * k] = sh_code_pair<is_k>(__byte_perm(x, 0x64646464u, 0x4140), fac2, low2);
+                        hh[2 * k + 1] = sh_code_pair<is_k>(__byte_perm(x, 0x64646464u, 0x4342), fac2, low2);
                     }
                     const uint32_t hf = (uint32_t)(c >> 2) * 16384u;
                     const int oc = 2 * (c & 3);
@@ -445,14 +504,18 @@ __device__ __forceinline__ void prefix_block(const CUtensorMap &codes_map, const
             __syncwarp();
             if (lane == 0) {
                 tc::mbar_arrive(bar(is_k ? shl::KF_FULL : shl::VF_FULL, buf));
-                tc::mbar_arrive(bar(shl::RAW_EMPTY, kv));
+                tc::mbar_arrive(raw_bar(shl::RAW_EMPTY, kv, j));
             }
+        };
+        for (int j = 0; j < T; ++j) {
+            convert(std::integral_constant<int, 0>(), j);
+            convert(std::integral_constant<int, 1>(), j);
         }
     } else if (warp == 12) {
         // =========================================================== loader (one thread)
         if (lane == 0) {
-            for (int i = 2; i < 2 * T; ++i) {
-                wait(bar(shl::RAW_EMPTY, i & 1), ((uint32_t)(i >> 1) & 1u) ^ 1u);
+            for (int i = 2 * kRawStages; i < 2 * T; ++i) {
+                wait(raw_bar(shl::RAW_EMPTY, i & 1, i >> 1), ((uint32_t)((i >> 1) / kRawStages) & 1u) ^ 1u);
                 request_raw(i);
             }
         }
@@ -544,8 +607,8 @@ __device__ __forceinline__ void prefix_block(const CUtensorMap &codes_map, const
     __syncthreads();
     if (warp == 12 && lane == 0 && *fail != 0) {
         // a wait ran out somewhere: give the copies still in flight a bounded chance to land before the block exits
-        for (int i = max(0, raw_issued - 2); i < raw_issued; ++i)
-            tc::mbar_wait(bar(shl::RAW_FULL, i & 1), (uint32_t)(i >> 1) & 1u, 1u << 14);
+        for (int i = max(0, raw_issued - 2 * kRawStages); i < raw_issued; ++i)
+            tc::mbar_wait(raw_bar(shl::RAW_FULL, i & 1, i >> 1), (uint32_t)((i >> 1) / kRawStages) & 1u, 1u << 14);
         if (p.status != nullptr) atomicExch(p.status, SLIM_ERR_TIMEOUT);
     }
     if (warp == 13) {
@@ -560,10 +623,15 @@ __global__ void __launch_bounds__(kShThreads, 1)
 slim_decode_prefix_kernel(const __grid_constant__ CUtensorMap codes_map, const __grid_constant__ SharedParams sp)
 {
     extern __shared__ __align__(1024) unsigned char smem[];
-    pdl_launch_dependents();   // the tail's blocks may start on the SMs that this kernel does not use
+    // The tail's blocks may start on the SMs that this kernel does not use once all of its blocks are here, behind the
+    // wait: so the tail need not wait for what came before them in the stream.
+    pdl_wait();
+    pdl_launch_dependents();
     const DecodeParams &p = sp.d;
     const int head = (int)blockIdx.y % p.Hkv, m0 = (int)blockIdx.y / p.Hkv * kShRows;
-    const int seq0 = min(max(__ldg(sp.cu_group + blockIdx.z), 0), sp.B), seq1 = min(__ldg(sp.cu_group + blockIdx.z + 1), sp.B);
+    // (one group is all the sequences: nothing to look up)
+    const int seq0 = gridDim.z == 1 ? 0 : min(max(__ldg(sp.cu_group + blockIdx.z), 0), sp.B);
+    const int seq1 = gridDim.z == 1 ? sp.B : min(__ldg(sp.cu_group + blockIdx.z + 1), sp.B);
     const int R = (seq1 - seq0) * p.G;                       // stacked rows of the group and kv head
     if (m0 >= R) return;
     const int rows = min(kShRows, R - m0);
@@ -590,29 +658,45 @@ slim_decode_prefix_kernel(const __grid_constant__ CUtensorMap codes_map, const _
 
 // ---------------------------------------------------------------- host side
 struct SharedShape {
-    int row_blocks, splits, slots;
+    int row_blocks, splits, slots, tail_blocks;
 };
 
-// How the prefix is cut: parts so that the blocks (one per SM) fill the chip once, at least one key tile each.
-static SharedShape shared_shape(int Hq, int Hkv, int n_groups, int max_group, int max_shared, int max_tail)
+// How the work is divided over the SMs.  Prefix and tail blocks take an SM each and run side by side, so the number of
+// parts of the prefix is chosen for the earliest end of both, by what their blocks were measured to take (us):
+//   prefix block   10 + 2.6 per key tile of 256 rows; 13 + 1.4 where the softmax groups take the tiles in turn
+//   tail           6 + (2 per 256-token chunk, 4 with more than eight query heads per kv head) / blocks
+// The tails' lengths are device data: half of max_tail is taken for their mean.  (Prefixes of 2048 / 8192 / 16384 tokens
+// for 16 / 32 / 64 sequences: 38.6 / 47.9 / 67.1 us with the prefix on all SMs and the tail behind it, 30.9 / 34.8 / 53.7
+// side by side.)
+static SharedShape shared_shape(int B, int Hq, int Hkv, int n_groups, int max_group, int max_shared, int max_tail)
 {
     constexpr int kSms = 148;
     SharedShape s;
-    const long long rows = (long long)max_group * (Hq / Hkv);
+    const int G = Hq / Hkv;
+    const long long rows = (long long)max_group * G;
     s.row_blocks = (int)((rows + kShRows - 1) / kShRows);
-    const int tiles = max_shared / kShKeys, units = rows > kShTileRows ? tiles : (tiles + 1) / 2;
-    const long long per_split = (long long)Hkv * s.row_blocks * n_groups;
-    long long n = per_split > 0 ? kSms / per_split : 0;
-    if (n > units) n = units;
-    if (n < 1) n = 1;
-    s.splits = tiles > 0 ? (int)n : 0;
+    const bool by_rows = rows > kShTileRows;
+    const int tiles = max_shared / kShKeys, unit = by_rows ? 1 : 2, units = (tiles + unit - 1) / unit;
+    const long long per_part = (long long)Hkv * s.row_blocks * n_groups;
+    const double chunks = (double)B * Hkv * (max_tail + 255) / 512, tail_work = chunks * (G <= 8 ? 2.0 : 4.0);
+    s.splits = tiles > 0 ? 1 : 0;
+    s.tail_blocks = kSms;
+    double best = 1e30;
+    for (int n = 1; n <= units && n * per_part < kSms; ++n) {
+        const int tail_blocks = kSms - (int)(n * per_part);
+        const int part = unit * ((units + n - 1) / n);
+        const double prefix = by_rows ? 10.0 + 2.6 * part : 13.0 + 1.4 * part;
+        const double tail = max_tail > 0 ? 6.0 + tail_work / tail_blocks : 0.0;
+        const double end = prefix > tail ? prefix : tail;
+        if (end < best) best = end, s.splits = n, s.tail_blocks = tail_blocks;
+    }
     s.slots = s.splits + (max_tail + 255) / 256 + 1;
     return s;
 }
 
 size_t shared_workspace_bytes(int B, int Hq, int Hkv, int n_groups, int max_group, int max_shared, int max_tail)
 {
-    const SharedShape s = shared_shape(Hq, Hkv, n_groups, max_group, max_shared, max_tail);
+    const SharedShape s = shared_shape(B, Hq, Hkv, n_groups, max_group, max_shared, max_tail);
     return kDecodeHeaderBytes + (size_t)B * Hq * s.slots * (kHeadDim + 2) * sizeof(float);
 }
 
@@ -620,7 +704,7 @@ int launch_decode_shared(const slim_cache_t *c, const void *q, const void *k_new
                          const int32_t *shared_len, const int32_t *kv_len, int n_groups, int B, int max_group, int max_shared,
                          int max_tail, int Hq, float sm_scale, void *workspace, cudaStream_t stream)
 {
-    const SharedShape s = shared_shape(Hq, c->num_kv_heads, n_groups, max_group, max_shared, max_tail);
+    const SharedShape s = shared_shape(B, Hq, c->num_kv_heads, n_groups, max_group, max_shared, max_tail);
     // no prefix of a page or more: ordinary decode
     if (s.splits == 0) return launch_decode(c, q, k_new, v_new, out, kv_len, B, max_tail, Hq, sm_scale, workspace, stream);
     if ((long long)c->num_kv_heads * s.row_blocks > 65535) return SLIM_ERR_UNSUPPORTED;
@@ -630,6 +714,7 @@ int launch_decode_shared(const slim_cache_t *c, const void *q, const void *k_new
     p.shared_len = shared_len;
     p.slot0 = s.splits;
     p.n_slots = s.slots;
+    p.max_blocks = s.tail_blocks;
     p.part_ml = p.part_o + (size_t)B * Hq * p.n_slots * kHeadDim;
     SharedParams sp;
     sp.d = p;
@@ -641,10 +726,7 @@ int launch_decode_shared(const slim_cache_t *c, const void *q, const void *k_new
     rc = allow_dynamic_smem(reinterpret_cast<const void *>(slim_decode_prefix_kernel), (int)shl::kBytes);
     if (rc != SLIM_OK) return rc;
     const dim3 grid((unsigned)s.splits, (unsigned)(c->num_kv_heads * s.row_blocks), (unsigned)n_groups);
-    // launched without the programmatic attribute: it starts after everything before it in the stream, which is what
-    // allows the tail kernel not to wait at its start
-    slim_decode_prefix_kernel<<<grid, kShThreads, shl::kBytes, stream>>>(map, sp);
-    SLIM_CUDA_TRY(cudaGetLastError());
+    SLIM_CUDA_TRY(launch_pdl(slim_decode_prefix_kernel, grid, dim3(kShThreads), (size_t)shl::kBytes, stream, map, sp));
     if (p.n_chunks > 0) {
         rc = launch_decode_split_stream(c, p, B, stream);
         if (rc != SLIM_OK) return rc;

@@ -159,6 +159,14 @@ __device__ __forceinline__ int st_chunk_len(const DecodeParams &p, int b)
     return max(st_clamped_len<kWhat>(p, b) - 1, 0);
 }
 
+// The tiles that the work is cut by.  Tails are short and a chunk of them takes the consumers' time whatever it holds, so
+// there a chunk counts as two tiles.
+template <int kWhat>
+__device__ __forceinline__ int st_cut_tiles(int len, int n_chunks)
+{
+    return kWhat == kStTail ? 2 * n_chunks : (len + kStTile - 1) / kStTile;
+}
+
 // Where the partial of a row's chunk lies: the tail's chunks follow the slots of the prefix kernel.
 template <int kWhat>
 __device__ __forceinline__ size_t st_slot(const DecodeParams &p, size_t row, int chunk)
@@ -502,7 +510,7 @@ slim_decode_stream_kernel(const __grid_constant__ CUtensorMap map_tile, const __
             uniform = __all_sync(0xffffffffu, base + lane >= B || st_chunk_len<kWhat>(p, base + lane) == len_u);
         if (uniform) {
             // every sequence has the same length (a batch decoded in lockstep): the cut has a closed form
-            const int nt = (len_u + kStTile - 1) / kStTile, nc = (len_u + kStChunk - 1) / kStChunk;
+            const int nc = (len_u + kStChunk - 1) / kStChunk, nt = st_cut_tiles<kWhat>(len_u, nc);
             const long long pairs = (long long)B * p.Hkv;
             const long long x = st_div(pairs * nt * (blockIdx.x + which), (int)gridDim.x);
             cut.index = pairs * nc;
@@ -525,8 +533,8 @@ slim_decode_stream_kernel(const __grid_constant__ CUtensorMap map_tile, const __
                 Scan r;
                 const int b = base + lane;
                 r.len = (base == 0) ? len_first : ((b < B) ? st_chunk_len<kWhat>(p, b) : 0);
-                r.nt = (r.len + kStTile - 1) / kStTile;
                 r.nc = (r.len + kStChunk - 1) / kStChunk;
+                r.nt = st_cut_tiles<kWhat>(r.len, r.nc);
                 r.it = r.nt;
                 r.ic = r.nc;
 #pragma unroll
@@ -1034,6 +1042,7 @@ int launch_decode_split_stream(const slim_cache_t *c, const DecodeParams &p, int
     int sms = 0;
     rc = sm_count(&sms);
     if (rc != SLIM_OK) return rc;
+    if (p.max_blocks > 0 && p.max_blocks < sms) sms = p.max_blocks;
     const long long max_items = (long long)p.n_chunks * p.Hkv * B;
     const dim3 grid((unsigned)(max_items < sms ? max_items : sms));
     if (p.shared_len != nullptr) return launch_stream_what<kStTail>(grid, stream, map_tile, map_tail, p, B);

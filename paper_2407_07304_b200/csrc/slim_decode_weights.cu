@@ -35,7 +35,7 @@ slim_decode_weights_kernel(const DecodeParams p, const MergeRows rows, const flo
     pdl_launch_dependents();
     pdl_wait();
     if ((int)blockIdx.x == token_blocks) {
-        for (int h = warp; h < p.G; h += kDwThreads / 32) merge_row_by_warp(p.part_o, p.part_ml, rows, out, nullptr, row0 + h, b, p.n_slots, lane);
+        for (int h = warp; h < p.G; h += kDwThreads / 32) merge_row_by_warp(p.part_o, p.part_ml, rows.partials(b), out, nullptr, row0 + h, p.n_slots, lane);
         return;
     }
     const int len = min(max(__ldg(p.kv_len + b), 0), rows.cap_tokens);

@@ -56,10 +56,9 @@ __device__ __forceinline__ void store_raw_partial(float *raw, int row, int lane,
 // step of the reduction.  (Asking for the sixteen slots before the length is known, as the block-per-row kernel below
 // does, read half as much again on ragged batches and was 0.5 us slower on the 64 / 8-head workload.)
 constexpr int kMergeWarpBatch = 16;
-__device__ __forceinline__ void merge_row_by_warp(const float *part_o, const float *part_ml, const MergeRows &rows, __nv_bfloat16 *out,
-                                                  float *raw, int row, int b, int n_slots, int lane)
+__device__ __forceinline__ void merge_row_by_warp(const float *part_o, const float *part_ml, int nc, __nv_bfloat16 *out,
+                                                  float *raw, int row, int n_slots, int lane)
 {
-    const int nc = rows.partials(b);
     const float2 *ml = reinterpret_cast<const float2 *>(part_ml) + (size_t)row * n_slots;
     const float4 *po = reinterpret_cast<const float4 *>(part_o + (size_t)row * n_slots * kHeadDim) + lane;
     float4 o[kMergeWarpBatch];
