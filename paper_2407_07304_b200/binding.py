@@ -319,12 +319,15 @@ def slim_decode_step_host(cache, q_host, k_new_host, v_new_host, out_host, stagi
 
 
 # ------------------------------------------------------------------ norm, rotation, shared prefixes, weights, eviction
+# These calls are made for single tokens too, where the host's time per call is the step's: marshalling is kept short.
 def _addr(t):
     return None if t is None else t.data_ptr()
 
 
 def _cuda_stream(stream):
-    return (torch.cuda.current_stream() if stream is None else stream).cuda_stream
+    if stream is not None:
+        return stream.cuda_stream
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())   # torch.cuda.current_stream().cuda_stream without the object
 
 
 class NormRope:
@@ -344,61 +347,63 @@ class NormRope:
         self.tensors = [None if t is None else t.contiguous() for t in (inv_freq if half else None, axis, q_weight, k_weight)]
         self.n_axes = n_axes
         self.struct = SlimNormRopeStruct(*[_addr(t) for t in self.tensors], eps, 2 * half, n_axes, 1 if interleaved else 0)
+        self.ref = ctypes.byref(self.struct)
+
+
+def _bad_rows(where):
+    raise SlimError(SLIM_ERR_INVALID_ARG, f"{where}: rows must be bfloat16 [tokens, heads, 128] with contiguous heads, outputs contiguous and of "
+                                          "the same shape, positions contiguous int32 [n_axes, tokens]")
 
 
 def _heads(t, where):
     """Token stride and heads of bf16 [tokens, heads, 128] whose tokens may lie apart (views of a fused projection)."""
     n, heads, d = t.shape
-    stride = t.stride()
-    if t.dtype != torch.bfloat16 or d != HEAD_DIM or stride[2] != 1 or (heads > 1 and stride[1] != HEAD_DIM):
-        raise SlimError(SLIM_ERR_INVALID_ARG, f"{where}: rows must be bfloat16 [tokens, heads, 128], heads contiguous")
-    return (stride[0] if n > 1 else heads * HEAD_DIM), heads
-
-
-def _rows_out(out, like, where):
-    if out.dtype != torch.bfloat16 or out.shape != like.shape or not out.is_contiguous():
-        raise SlimError(SLIM_ERR_INVALID_ARG, f"{where}: the output must be contiguous bfloat16 of the input's shape")
-
-
-def _positions(positions, nr, n, where):
-    if positions is not None and (positions.dtype != torch.int32 or positions.numel() != nr.n_axes * n or not positions.is_contiguous()):
-        raise SlimError(SLIM_ERR_INVALID_ARG, f"{where}: positions must be contiguous int32 [n_axes, tokens]")
+    token, head, one = t.stride()
+    if t.dtype is not torch.bfloat16 or d != HEAD_DIM or one != 1 or (head != HEAD_DIM and heads > 1):
+        _bad_rows(where)
+    return (token if n > 1 else heads * HEAD_DIM), heads
 
 
 def slim_norm_rope(nr, q, q_out, k, k_out, positions, stream=None):
     """Norm and rotation of q and k (bf16 [tokens, heads, 128], either may be None) into q_out and k_out."""
-    n = (q if q is not None else k).shape[0]
-    qs = hq = ks = hkv = 0
+    where = "slim_norm_rope"
+    qa = qs = hq = qo = ka = ks = hkv = ko = 0
+    n = len(k) if q is None else len(q)
     if q is not None:
-        qs, hq = _heads(q, "slim_norm_rope")
-        _rows_out(q_out, q, "slim_norm_rope")
+        qs, hq = _heads(q, where)
+        qa, qo = q.data_ptr(), q_out.data_ptr()
+        if q_out.dtype is not torch.bfloat16 or q_out.shape != q.shape or not q_out.is_contiguous():
+            _bad_rows(where)
     if k is not None:
-        ks, hkv = _heads(k, "slim_norm_rope")
-        _rows_out(k_out, k, "slim_norm_rope")
-        if k.shape[0] != n:
-            raise SlimError(SLIM_ERR_INVALID_ARG, "slim_norm_rope: q and k differ in tokens")
-    _positions(positions, nr, n, "slim_norm_rope")
-    rc = lib().slim_norm_rope(ctypes.byref(nr.struct), _addr(q), qs, _addr(q_out), _addr(k), ks, _addr(k_out), _addr(positions), n, hq, hkv,
-                              _cuda_stream(stream))
-    _check(rc, "slim_norm_rope")
+        ks, hkv = _heads(k, where)
+        ka, ko = k.data_ptr(), k_out.data_ptr()
+        if k_out.dtype is not torch.bfloat16 or k_out.shape != k.shape or not k_out.is_contiguous() or len(k) != n:
+            _bad_rows(where)
+    if positions is not None and (positions.dtype is not torch.int32 or positions.numel() != nr.n_axes * n or not positions.is_contiguous()):
+        _bad_rows(where)
+    rc = (_lib or lib()).slim_norm_rope(nr.ref, qa, qs, qo, ka, ks, ko, _addr(positions), n, hq, hkv, _cuda_stream(stream))
+    if rc:
+        _check(rc, where)
 
 
 def slim_norm_rope_append(cache, nr, q, q_out, k, v, positions, cu_new, start_pos, B, stream=None):
     """Norm and rotation of q into q_out; keys (normed, rotated) and values quantised into the cache.  positions None:
     the tokens' cache positions."""
     where = "slim_norm_rope_append"
-    n = k.shape[0]
+    n = len(k)
     ks, hkv = _heads(k, where)
     vs, hv = _heads(v, where)
     qs = hq = 0
     if q is not None:
         qs, hq = _heads(q, where)
-        _rows_out(q_out, q, where)
-    if hkv != cache.Hkv or hv != hkv or v.shape[0] != n or (q is not None and q.shape[0] != n):
-        raise SlimError(SLIM_ERR_INVALID_ARG, f"{where}: q, k, v and the cache differ in tokens or kv heads")
-    _positions(positions, nr, n, where)
-    rc = lib().slim_norm_rope_append(ctypes.byref(cache.struct), ctypes.byref(nr.struct), _addr(q), qs, _addr(q_out), _addr(k), ks, _addr(v), vs,
-                                     _addr(positions), _addr(cu_new), _addr(start_pos), B, n, hq, _cuda_stream(stream))
+        if q_out.dtype is not torch.bfloat16 or q_out.shape != q.shape or not q_out.is_contiguous() or len(q) != n:
+            _bad_rows(where)
+    if hkv != cache.Hkv or hv != hkv or len(v) != n:
+        _bad_rows(where + " (q, k, v and the cache differ in tokens or kv heads)")
+    if positions is not None and (positions.dtype is not torch.int32 or positions.numel() != nr.n_axes * n or not positions.is_contiguous()):
+        _bad_rows(where)
+    rc = lib().slim_norm_rope_append(ctypes.byref(cache.struct), nr.ref, _addr(q), qs, _addr(q_out), k.data_ptr(), ks, v.data_ptr(), vs,
+                                     _addr(positions), cu_new.data_ptr(), start_pos.data_ptr(), B, n, hq, _cuda_stream(stream))
     _check(rc, where)
 
 

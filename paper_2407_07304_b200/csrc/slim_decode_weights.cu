@@ -24,7 +24,7 @@ constexpr int kDwBatch = 8;                                   // query heads who
 static_assert(kDwThreads == kChunkTok, "thread = position in the chunk");
 
 // grid = (token blocks [+ 1: merge], kv heads, sequences)
-__global__ void __launch_bounds__(kDwThreads)
+__global__ void __launch_bounds__(kDwThreads, 3)
 slim_decode_weights_kernel(const DecodeParams p, const MergeRows rows, const float *w_in, float *w_out, int w_stride, const int32_t *weighed,
                            float decay, int token_blocks, __nv_bfloat16 *out)
 {

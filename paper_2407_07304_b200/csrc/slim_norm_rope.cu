@@ -15,15 +15,18 @@
 // kernel: lane l holds the 16-byte pieces l, l + 4, l + 8, l + 12, so a load instruction of a warp covers eight rows
 // in whole 64-byte sectors, and the two halves of a 128- or 64-dimension rotation lie in the same lane.  Narrower
 // rotations in halves (rotary_dim other than 64 and 128) read the partner piece a second time, from the L1.
-// A block takes 64 consecutive rows (token-major: the token's query heads, key heads, value heads); the cosines and
-// sines of the one to three tokens it touches are computed once per block, by all its threads, while the rows are on
+// A block takes 32 consecutive rows (token-major: the token's query heads, key heads, value heads); the cosines and
+// sines of the few tokens that it touches are computed once per block, by all its threads, while the rows are on
 // their way, so no table of angles is read from memory.
 #include "slim_common.cuh"
 #include "slim_quant.cuh"
 
 namespace slim {
 
-constexpr int kNrThreads = 256;
+// (Blocks of 128 threads, nine per SM: 54 us for a prompt of 16384 tokens with 32 query heads on 2 kv heads, 5.4 TB/s;
+// 256 threads 61 us, 64 threads 58 us; several batches of rows per block, or the weights folded into the angles' table
+// with packed arithmetic, take registers and with them blocks, and were 5 to 25 % slower.)
+constexpr int kNrThreads = 128;
 constexpr int kNrLanes = 4;                             // lanes per row
 constexpr int kNrRows = kNrThreads / kNrLanes;          // rows per block
 
@@ -113,7 +116,7 @@ __device__ __forceinline__ void nr_unpack(const uint4 raw, float *x)
 }
 
 template <int kMode, bool kAppend>
-__global__ void __launch_bounds__(kNrThreads)
+__global__ void __launch_bounds__(kNrThreads, 9)
 slim_norm_rope_kernel(const NormRopeParams p)
 {
     extern __shared__ __align__(16) float nr_smem[];
@@ -151,7 +154,8 @@ slim_norm_rope_kernel(const NormRopeParams p)
 
     // ---- where the block's tokens go, then their angles
     if (kAppend) {
-        for (int t = warp; t < p.span; t += kNrThreads / 32) {
+        // (by the block's last warps, while the first ones compute angles)
+        for (int t = kNrThreads / 32 - 1 - warp; t < p.span; t += kNrThreads / 32) {
             int2 at = make_int2(-1, 0);
             if (tok0 + t < p.n_tokens && tok0 + t < __ldg(p.cu_new + p.B)) {   // tokens behind the last sequence go nowhere
                 const int b = nr_find_sequence(p.cu_new, p.B, tok0 + t, lane);
@@ -159,7 +163,7 @@ slim_norm_rope_kernel(const NormRopeParams p)
             }
             if (lane == 0) where_s[t] = at;
         }
-        __syncthreads();
+        if (p.positions == nullptr) __syncthreads();   // (the angles wait for the positions then)
     }
     for (int i = tid; i < p.span * p.half; i += kNrThreads) {
         const int t = i / p.half, k = i - t * p.half;
@@ -313,7 +317,7 @@ static int launch_mode(const NormRopeParams &p, bool interleaved, cudaStream_t s
     const long long rows = (long long)p.n_tokens * p.rows_per_token;
     if (rows > 0x7FFFFF00LL) return SLIM_ERR_UNSUPPORTED;   // the kernel indexes rows with 32-bit integers
     const unsigned blocks = (unsigned)((rows + kNrRows - 1) / kNrRows);
-    const size_t smem = (size_t)p.span * (2 * p.half * sizeof(float) + sizeof(int2));   // 33 KB at most (one row per token)
+    const size_t smem = (size_t)p.span * (2 * p.half * sizeof(float) + sizeof(int2));   // 17 KB at most (one row per token)
     if (interleaved)
         SLIM_CUDA_TRY(launch_pdl(slim_norm_rope_kernel<kNrAdjacent, kAppend>, dim3(blocks), dim3(kNrThreads), smem, stream, p));
     else if (p.half % 32 == 0)
@@ -347,7 +351,7 @@ int launch_norm_rope(const slim_cache_t *c, const slim_norm_rope_t *nr, const vo
     p.n_axes = nr->n_axes;
     p.eps = nr->eps;
     p.rows_per_token = Hq + (c != nullptr ? 2 : 1) * Hkv;
-    p.span = (kNrRows - 1 + p.rows_per_token - 1) / p.rows_per_token + 1;   // tokens that 64 consecutive rows touch at most
+    p.span = (kNrRows - 1 + p.rows_per_token - 1) / p.rows_per_token + 1;   // tokens that a block's consecutive rows touch at most
     if (c == nullptr) return launch_mode<false>(p, nr->interleaved != 0, stream);
     p.codes = c->codes;
     p.scales = c->scales;
