@@ -50,17 +50,15 @@ constexpr uint32_t kVf = kKf + 2 * 32768;       // two fp16 V tiles
 constexpr uint32_t kRaw = kVf + 2 * 32768;      // raw INT8 tiles: stage 0 K, stage 1 V
 constexpr uint32_t kRawScales = kRaw + 2 * 16384;
 constexpr uint32_t kMisc = kRawScales + 2 * 512;
-// where the softmax groups take the key tiles in turn: scales of a second raw stage (whose tiles lie in the unused second Q
-// tile), the rows' scales for group 1, and at the end, over the raw tiles, group 1's (m, l)
-constexpr uint32_t kRawScales1 = kMisc + 512;
-constexpr uint32_t kRowScale = kRawScales1 + 1024;
+// where the softmax groups take the key tiles in turn: the rows' scales for group 1, and at the end, over the raw tiles,
+// group 1's (m, l)
+constexpr uint32_t kRowScale = kMisc + 512;
 constexpr uint32_t kMl = kRaw;
 constexpr uint32_t kBytes = kRowScale + 512;
 // kMisc: floats by key tile mod 4: [0,4) kexp, [4,8) log2 vexp, [8,12) 1 / vexp; byte 64: tensor-memory address;
 //        byte 72: failure flag; byte 76: tokens of the prefix that any sequence of the group has; byte 128..: mbarriers
-// (raw barriers: 2 * stage + kind, kind 0 K, 1 V)
-enum Bar { RAW_FULL = 0, RAW_EMPTY = 4, KF_FULL = 8, KF_EMPTY = 10, VF_FULL = 12, VF_EMPTY = 14,
-           S_FULL = 16, P_FULL = 18, O_DONE = 20, Q_FULL = 22, VEXP_FULL = 24, NUM_BARS = 28 };
+enum Bar { RAW_FULL = 0, RAW_EMPTY = 2, KF_FULL = 4, KF_EMPTY = 6, VF_FULL = 8, VF_EMPTY = 10,
+           S_FULL = 12, P_FULL = 14, O_DONE = 16, Q_FULL = 18, VEXP_FULL = 20, NUM_BARS = 24 };
 static_assert(128 + 8 * NUM_BARS <= 512, "mbarriers fit the misc area");
 static_assert(kBytes <= 232448, "shared memory budget of one block");
 }  // namespace shl
@@ -122,12 +120,6 @@ __device__ __forceinline__ void prefix_block(const CUtensorMap &codes_map, const
     int *known = reinterpret_cast<int *>(smem + shl::kMisc + 76);
     const uint32_t bar0 = sbase + shl::kMisc + 128;
     auto bar = [&](int which, int idx) { return bar0 + 8u * (uint32_t)(which + idx); };
-    // Raw stages per kind.  Where a tile is used by one group only, two: a tile takes the converters half as long as it
-    // takes to arrive.
-    constexpr int kRawStages = by_rows ? 1 : 2;
-    auto raw_tile = [&](int kv, int j) { return (kRawStages > 1 && (j & 1) ? shl::kQ + 32768u : shl::kRaw) + (uint32_t)kv * 16384u; };
-    auto raw_scales = [&](int kv, int j) { return (kRawStages > 1 && (j & 1) ? shl::kRawScales1 : shl::kRawScales) + (uint32_t)kv * 512u; };
-    auto raw_bar = [&](int which, int kv, int j) { return bar(which, 2 * (j % kRawStages) + kv); };
 
     // ---- the loader asks for the first raw tiles before the block's set-up is complete
     int raw_issued = 0;
@@ -136,10 +128,10 @@ __device__ __forceinline__ void prefix_block(const CUtensorMap &codes_map, const
     auto request_raw = [&](int i) {
         const int kv = i & 1, j = i >> 1;
         const int page = (page_next >= 0 && page_next < p.num_pages) ? page_next : 0;
-        const uint32_t full = raw_bar(shl::RAW_FULL, kv, j);
+        const uint32_t full = bar(shl::RAW_FULL, kv);
         tc::mbar_arrive_expect_tx(full, 16384 + 512);
-        tc::tma_load_2d(sbase + raw_tile(kv, j), &codes_map, 0, ((page * p.Hkv + head) * 2 + kv) * kPageTokens, full);
-        tc::bulk_load(sbase + raw_scales(kv, j), p.scales + scale_block_offset(page, head, kv, p.Hkv), 512, full);
+        tc::tma_load_2d(sbase + shl::kRaw + kv * 16384, &codes_map, 0, ((page * p.Hkv + head) * 2 + kv) * kPageTokens, full);
+        tc::bulk_load(sbase + shl::kRawScales + kv * 512, p.scales + scale_block_offset(page, head, kv, p.Hkv), 512, full);
         if (kv == 1 && j + 1 < T) {
             // the next key tile's page id, and its two tiles on their way into the L2
             if (by_rows || j0 + j + 1 < tiles) page_next = __ldg(bt + j + 1);
@@ -150,10 +142,10 @@ __device__ __forceinline__ void prefix_block(const CUtensorMap &codes_map, const
         ++raw_issued;
     };
     if (warp == 12 && lane == 0) {
-        for (int i = 0; i < 2 * kRawStages; ++i) tc::mbar_init(bar(shl::RAW_FULL, i), 1);
+        for (int i = 0; i < 2; ++i) tc::mbar_init(bar(shl::RAW_FULL, i), 1);
         tc::mbar_init_fence();
         page_next = __ldg(bt);
-        for (int i = 0; i < 2 * kRawStages; ++i) request_raw(i);   // (T >= kRawStages)
+        for (int i = 0; i < 2; ++i) request_raw(i);
     }
     // ---- query rows, sixteen lanes per row: warp w of group t brings in and converts rows 32 (w & 3) + 2 i + (lane >> 4) of
     //      its tile.  A row's 16-byte pieces go where their fp16 form will lie and are converted in place, so that both
@@ -184,7 +176,7 @@ __device__ __forceinline__ void prefix_block(const CUtensorMap &codes_map, const
     }
     if (warp == 14 && lane == 0) {   // (a warp that has nothing else to do here)
         for (int t = 0; t < 2; ++t) {
-            for (int i = 0; i < kRawStages; ++i) tc::mbar_init(bar(shl::RAW_EMPTY, 2 * i + t), kShConvWarps);
+            tc::mbar_init(bar(shl::RAW_EMPTY, t), kShConvWarps);
             tc::mbar_init(bar(shl::KF_FULL, t), kShConvWarps);
             tc::mbar_init(bar(shl::KF_EMPTY, t), 1);
             tc::mbar_init(bar(shl::VF_FULL, t), kShConvWarps);
@@ -447,9 +439,9 @@ __device__ __forceinline__ void prefix_block(const CUtensorMap &codes_map, const
             constexpr int kv = decltype(kind)::value;
             constexpr bool is_k = kv == 0;
             const int buf = j & 1;
-            wait(raw_bar(shl::RAW_FULL, kv, j), (uint32_t)(j / kRawStages) & 1u);
-            const unsigned char *raw = smem + raw_tile(kv, j);
-            const float *scales = reinterpret_cast<const float *>(smem + raw_scales(kv, j));
+            wait(bar(shl::RAW_FULL, kv), (uint32_t)j & 1u);
+            const unsigned char *raw = smem + shl::kRaw + kv * 16384;
+            const float *scales = reinterpret_cast<const float *>(smem + shl::kRawScales + kv * 512);
             const int n_valid = min(kShKeys, kept - j * kShKeys);
             float wm = 0.f;
             {
@@ -504,7 +496,7 @@ __device__ __forceinline__ void prefix_block(const CUtensorMap &codes_map, const
             __syncwarp();
             if (lane == 0) {
                 tc::mbar_arrive(bar(is_k ? shl::KF_FULL : shl::VF_FULL, buf));
-                tc::mbar_arrive(raw_bar(shl::RAW_EMPTY, kv, j));
+                tc::mbar_arrive(bar(shl::RAW_EMPTY, kv));
             }
         };
         for (int j = 0; j < T; ++j) {
@@ -514,8 +506,8 @@ __device__ __forceinline__ void prefix_block(const CUtensorMap &codes_map, const
     } else if (warp == 12) {
         // =========================================================== loader (one thread)
         if (lane == 0) {
-            for (int i = 2 * kRawStages; i < 2 * T; ++i) {
-                wait(raw_bar(shl::RAW_EMPTY, i & 1, i >> 1), ((uint32_t)((i >> 1) / kRawStages) & 1u) ^ 1u);
+            for (int i = 2; i < 2 * T; ++i) {
+                wait(bar(shl::RAW_EMPTY, i & 1), ((uint32_t)(i >> 1) & 1u) ^ 1u);
                 request_raw(i);
             }
         }
@@ -607,8 +599,8 @@ __device__ __forceinline__ void prefix_block(const CUtensorMap &codes_map, const
     __syncthreads();
     if (warp == 12 && lane == 0 && *fail != 0) {
         // a wait ran out somewhere: give the copies still in flight a bounded chance to land before the block exits
-        for (int i = max(0, raw_issued - 2 * kRawStages); i < raw_issued; ++i)
-            tc::mbar_wait(raw_bar(shl::RAW_FULL, i & 1, i >> 1), (uint32_t)((i >> 1) / kRawStages) & 1u, 1u << 14);
+        for (int i = max(0, raw_issued - 2); i < raw_issued; ++i)
+            tc::mbar_wait(bar(shl::RAW_FULL, i & 1), (uint32_t)(i >> 1) & 1u, 1u << 14);
         if (p.status != nullptr) atomicExch(p.status, SLIM_ERR_TIMEOUT);
     }
     if (warp == 13) {

@@ -691,3 +691,137 @@ def test_results_repeat_bit_for_bit():
         if first is None:
             first = (out, o2, wt)
         assert all(torch.equal(x, y) for x, y in zip(first, (out, o2, wt)))
+
+
+def test_pages_behind_four_gigabytes():
+    """A pool of 4.6 GB of codes whose last pages are the ones in use: offsets beyond 2^32 in every call."""
+    slim = _slim()
+    n_pages, B, hq, hkv, mp = 140000, 2, 4, 1, 4
+    table = torch.arange(n_pages - B * mp, n_pages, dtype=torch.int32).view(B, mp)
+    table[1, :2] = table[0, :2]                              # a shared prefix of two pages
+    cache = slim.SlimCache(B, hkv, mp, block_table=table, num_pages=n_pages)
+    rows, inv, axis, pos, w = rope_inputs(21, 900, hq, hkv, 128, 1, True)
+    qo = torch.empty((900, hq, D), dtype=torch.bfloat16, device="cuda")
+    slim.slim_norm_rope_append(cache, slim.NormRope(inv, w[0], w[1]), rows[:, :hq], qo, rows[:, hq:hq + 1], rows[:, hq + 1:], pos, i32([0, 450, 900]),
+                               i32([0, 0]), B)
+    torch.cuda.synchronize()
+    assert (cache.codes_view()[n_pages - B * mp].abs().amax(-1) > 0).all() and not cache.codes_view()[:1000].any()
+    lens, q = [450, 300], qo[:2].contiguous()
+    want, probs, slack = attend(cache, q, lens, D ** -0.5)
+    out = torch.empty_like(q)
+    ws = slim.shared_workspace(B, hq, hkv, 1, B, 256, 256)
+    slim.slim_attn_decode_shared(cache, q, out, i32([0, 2]), i32([256, 256]), i32(lens), 1, B, B, 256, 256, hq, D ** -0.5, ws)
+    out2, wt = torch.empty_like(q), torch.zeros((B, hkv, 450), device="cuda")
+    slim.slim_attn_decode_weights(cache, q, out2, None, wt, None, i32(lens), B, 450, hq, D ** -0.5, 1.0, slim.weights_workspace(B, hq, hkv, 450))
+    torch.cuda.synchronize()
+    out_close(out, want, slack, "shared")
+    out_close(out2, want, slack, "weights")
+    assert (wt[0, 0].double() - probs[0].sum(0)).abs().max() < 1e-4
+    # the first sequence alone is cut (the second's prefix pages are not its own)
+    before = cache.codes_view()[table[0].long().cuda()].clone()
+    alone = slim.SlimCache(1, hkv, mp, block_table=table[:1], num_pages=n_pages)
+    alone.codes, alone.scales = cache.codes, cache.scales
+    alone.struct.codes, alone.struct.scales = cache.codes.data_ptr(), cache.scales.data_ptr()
+    po, wo = torch.zeros((1, hkv, 450), dtype=torch.int32, device="cuda"), torch.zeros((1, hkv, 450), device="cuda")
+    slim.slim_kv_evict(alone, wt[:1].contiguous(), wo, None, po, i32([450]), None, None, 1, 450, 200, 0, 0, slim.evict_workspace(1, hkv, 450, 200))
+    torch.cuda.synchronize()
+    src, p = evict_reference(wt[0, 0].cpu().numpy(), np.arange(450), 450, 200, 0, 0, 450, 0)
+    assert po[0, 0, :200].cpu().tolist() == p.tolist()
+    flat = before.permute(1, 2, 0, 3, 4).reshape(2, mp * PAGE, D)
+    after = cache.codes_view()[table[0].long().cuda()].permute(1, 2, 0, 3, 4).reshape(2, mp * PAGE, D)
+    assert torch.equal(after[:, :200], flat[:, torch.from_numpy(src).cuda()]) and torch.equal(after[:, 200:], flat[:, 200:])
+
+
+def test_one_workspace_for_calls_of_different_kinds():
+    """A zeroed workspace serves ordinary, shared and weighted decode of different shapes in turn, its header back at zero."""
+    slim = _slim()
+    cache, B, cu = shared_setup(4, [(3, 6)], 8, 2, 2)
+    q = torch.randn((B, 8, D), generator=gen(14)).to(torch.bfloat16).cuda()
+    lens = [384 + 30 * b for b in range(B)]
+    want, _, slack = attend(cache, q, lens, D ** -0.5)
+    n = max(w.numel() for w in (slim.shared_workspace(B, 8, 2, 1, B, 384, 256), slim.weights_workspace(B, 8, 2, 640), slim.workspace(slim.PHASE_DECODE, B, 8, 2, 1, 640)))
+    ws = torch.full((n,), 0xEE, dtype=torch.uint8, device="cuda")
+    ws[:slim.WORKSPACE_HEADER_BYTES] = 0
+    wt = torch.zeros((B, 2, 640), device="cuda")
+    for _ in range(2):
+        for call in ("shared", "weights", "decode", "shared", "decode", "weights"):
+            out = torch.full_like(q, 3.0)
+            if call == "shared":
+                slim.slim_attn_decode_shared(cache, q, out, i32(cu), i32([384] * B), i32(lens), 1, B, B, 384, 256, 8, D ** -0.5, ws)
+            elif call == "weights":
+                slim.slim_attn_decode_weights(cache, q, out, None, wt, None, i32(lens), B, 640, 8, D ** -0.5, 1.0, ws)
+            else:
+                slim.slim_attn_decode(cache, q, out, i32(lens), B, 640, 8, D ** -0.5, ws)
+            torch.cuda.synchronize()
+            out_close(out, want, slack, call)
+            assert slim.slim_read_status(ws) == slim.SLIM_OK and not ws[:slim.WORKSPACE_HEADER_BYTES].any()
+
+
+def test_two_streams_at_once():
+    """The same calls on two streams that nothing orders, each with buffers of its own: the results of calls in turn."""
+    slim = _slim()
+    sets = []
+    for k in range(2):
+        cache, B, cu = shared_setup(30 + k, [(6, 10)], 16, 4, 2)
+        own = slim.SlimCache(B, 4, 8)
+        fill(own, 40 + k)
+        q = torch.randn((B, 16, D), generator=gen(50 + k)).to(torch.bfloat16).cuda()
+        sets.append(dict(cache=cache, own=own, q=q, cu=i32(cu), shared=i32([768] * B), lens=i32([768 + 20 * b for b in range(B)]), B=B,
+                         w1=slim.shared_workspace(B, 16, 4, 1, B, 768, 256), w2=slim.weights_workspace(B, 16, 4, 1024), w3=slim.evict_workspace(B, 4, 1024, 700),
+                         codes=own.codes.clone(), scales=own.scales.clone()))
+
+    def calls(s):
+        o1, o2 = torch.empty_like(s["q"]), torch.empty_like(s["q"])
+        wt = torch.zeros((s["B"], 4, 1024), device="cuda")
+        wo, po = torch.zeros_like(wt), torch.zeros((s["B"], 4, 1024), dtype=torch.int32, device="cuda")
+        for _ in range(8):
+            slim.slim_attn_decode_shared(s["cache"], s["q"], o1, s["cu"], s["shared"], s["lens"], 1, s["B"], s["B"], 768, 256, 16, D ** -0.5, s["w1"])
+            slim.slim_attn_decode_weights(s["own"], s["q"], o2, None, wt, None, s["lens"], s["B"], 1024, 16, D ** -0.5, 1.0, s["w2"])
+        slim.slim_kv_evict(s["own"], wt, wo, None, po, s["lens"], None, None, s["B"], 1024, 700, 4, 32, s["w3"])
+        return o1, o2, wt, wo, po
+
+    turn = []
+    for s in sets:
+        turn.append(calls(s))
+        torch.cuda.synchronize()
+        s["after"] = s["own"].codes.clone()
+        s["own"].codes.copy_(s["codes"])
+        s["own"].scales.copy_(s["scales"])
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in sets]
+    both = []
+    for s, st in zip(sets, streams):
+        with torch.cuda.stream(st):
+            both.append(calls(s))
+    torch.cuda.synchronize()
+    for s, a, b in zip(sets, turn, both):
+        assert all(torch.equal(x, y) for x, y in zip(a, b)) and torch.equal(s["own"].codes, s["after"])
+
+
+def test_long_eviction_in_a_graph():
+    """The cluster form and its move kernel, captured and replayed."""
+    slim = _slim()
+    n, budget = 20000, 5000
+    w, _ = evict_inputs(5, [n], 2, n, None, [n], "ties")
+    cache = slim.SlimCache(1, 2, (n + PAGE - 1) // PAGE)
+    fill(cache, 6)
+    codes = cache.codes.clone()
+    wi, wo, po = w.cuda(), torch.zeros((1, 2, n), device="cuda"), torch.zeros((1, 2, n), dtype=torch.int32, device="cuda")
+    lens, ws = i32([n]), slim.evict_workspace(1, 2, n, budget)
+    call = lambda: slim.slim_kv_evict(cache, wi, wo, None, po, lens, None, None, 1, n, budget, 4, 100, ws)  # noqa: E731
+    call()
+    torch.cuda.synchronize()
+    a = (cache.codes.clone(), wo.clone(), po.clone())
+    assert a[2][0, 0, :budget].cpu().tolist() == evict_reference(w[0, 0].numpy(), np.arange(n), n, budget, 4, 100, n, 0)[1].tolist()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        call()
+    for _ in range(2):
+        cache.codes.copy_(codes)
+        wo.zero_()
+        po.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(a, (cache.codes, wo, po)))
