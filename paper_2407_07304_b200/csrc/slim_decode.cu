@@ -22,10 +22,10 @@ static_assert(kDecodeHeaderBytes == SLIM_WORKSPACE_HEADER_BYTES, "the header siz
 // the chunks c = g mod GROUPS, so that a long sequence's hundreds of chunks are read with many independent
 // loads in flight (four groups); short rows use one group.  The chunk weights go through shared memory 128
 // at a time.
-template <int kMergeGroups>
+template <int kMergeGroups, class Rows>
 __global__ void __launch_bounds__(kMergeGroups * kHeadDim)
 slim_decode_merge_kernel(const float *__restrict__ part_o, const float *__restrict__ part_ml,
-                         const MergeRows rows, __nv_bfloat16 *__restrict__ out, float *__restrict__ raw,
+                         const Rows rows, __nv_bfloat16 *__restrict__ out, float *__restrict__ raw,
                          int B, int Hq, int n_slots)
 {
     constexpr int kMergeThreads = kMergeGroups * kHeadDim;
@@ -35,7 +35,7 @@ slim_decode_merge_kernel(const float *__restrict__ part_o, const float *__restri
     const int row = blockIdx.x;            // b * Hq + h
     const int tid = threadIdx.x, d = tid & (kHeadDim - 1), g = tid >> 7;
     pdl_wait();   // the split pass before this kernel must have finished writing the partials
-    const int nc = rows.partials(row / Hq);
+    const int nc = rows.partials(row / Hq, rows.length(row / Hq));
     const float2 *ml = reinterpret_cast<const float2 *>(part_ml) + (size_t)row * n_slots;
     const float *po = part_o + (size_t)row * n_slots * kHeadDim;
     // ---- the row's maximum
@@ -105,29 +105,30 @@ __device__ __forceinline__ float4 ld_cg_now(const float4 *ptr)
 
 // Rows of fewer than 32 chunks: one warp per row (slim_merge.cuh).
 constexpr int kMergeWarpsPerBlock = 8;
+template <class Rows>
 __global__ void __launch_bounds__(kMergeWarpsPerBlock * 32)
 slim_decode_merge_warp_kernel(const float *__restrict__ part_o, const float *__restrict__ part_ml,
-                              const MergeRows rows, __nv_bfloat16 *__restrict__ out, float *__restrict__ raw,
+                              const Rows rows, __nv_bfloat16 *__restrict__ out, float *__restrict__ raw,
                               int B, int Hq, int n_slots)
 {
     const int row = blockIdx.x * kMergeWarpsPerBlock + (threadIdx.x >> 5);   // b * Hq + h
-    const bool mine = row < B * Hq;
     // Behind a shared prefix the lengths are read ahead of the wait (0.3 us of a step): this kernel starts only after every
     // block of the prefix kernel has seen the end of everything before it in the stream.
-    int nc = (mine && rows.shared_len != nullptr) ? rows.partials(row / Hq) : 0;
+    int nc = 0;
+    if (Rows::kShared && row < B * Hq) nc = rows.partials(row / Hq, rows.length(row / Hq));
     pdl_wait();   // the split pass before this kernel must have finished writing the partials
-    if (!mine) return;
-    if (rows.shared_len == nullptr) nc = rows.partials(row / Hq);
+    if (row >= B * Hq) return;
+    if (!Rows::kShared) nc = rows.partials(row / Hq, rows.length(row / Hq));
     merge_row_by_warp(part_o, part_ml, nc, out, raw, row, n_slots, threadIdx.x & 31);
 }
 
 // Rows of 32 to 16 * kWarps chunks: one block per row, warp w owns the sixteen chunk slots [16 w, 16 w + 16) and
 // merges them as the kernel above does - all of its partials requested at once, before the row's length is known -
 // into (M_w, l_w, o_w); the warps' results are then merged by the same identity through shared memory.
-template <int kWarps>
+template <int kWarps, class Rows>
 __global__ void __launch_bounds__(kWarps * 32, 1)
 slim_decode_merge_block_kernel(const float *__restrict__ part_o, const float *__restrict__ part_ml,
-                               const MergeRows rows, __nv_bfloat16 *__restrict__ out, float *__restrict__ raw,
+                               const Rows rows, __nv_bfloat16 *__restrict__ out, float *__restrict__ raw,
                                int B, int Hq, int n_slots)
 {
     __shared__ float4 acc_s[kWarps][32];
@@ -135,6 +136,7 @@ slim_decode_merge_block_kernel(const float *__restrict__ part_o, const float *__
     const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
     const int row = blockIdx.x;   // b * Hq + h
     pdl_wait();   // the split pass before this kernel must have finished writing the partials
+    const int len = rows.length(row / Hq);
     const int c_base = w * kMergeWarpBatch;
     const float2 *ml = reinterpret_cast<const float2 *>(part_ml) + (size_t)row * n_slots;
     const float4 *po = reinterpret_cast<const float4 *>(part_o + (size_t)row * n_slots * kHeadDim) + lane;
@@ -143,7 +145,7 @@ slim_decode_merge_block_kernel(const float *__restrict__ part_o, const float *__
     for (int u = 0; u < kMergeWarpBatch; ++u)
         o[u] = ld_cg_now(po + (size_t)min(c_base + u, n_slots - 1) * (kHeadDim / 4));   // n_slots >= 32 here; slots past nc are not used
     float2 v = (lane < kMergeWarpBatch && c_base + lane < n_slots) ? __ldcg(ml + c_base + lane) : make_float2(-INFINITY, 0.f);
-    const int nc = rows.partials(row / Hq);
+    const int nc = rows.partials(row / Hq, len);
     const bool mine = lane < kMergeWarpBatch && c_base + lane < nc;
     if (!mine) v = make_float2(-INFINITY, 0.f);
     const float Mw = warp_max(v.x);
@@ -281,27 +283,34 @@ int launch_decode_merge(const slim_cache_t *c, void *out, const int32_t *kv_len,
     return launch_merge_rows(p, B, out, raw, stream);
 }
 
-int launch_merge_rows(const DecodeParams &p, int B, void *out, float *raw, cudaStream_t stream)
+template <class Rows>
+static int launch_merge(const DecodeParams &p, const Rows &r, int B, void *out, float *raw, cudaStream_t stream)
 {
     const int rows = B * p.Hq;
-    const MergeRows r = merge_rows(p);
     const float *po = p.part_o, *pm = p.part_ml;
     __nv_bfloat16 *o = static_cast<__nv_bfloat16 *>(out);
     const int Hq = p.Hq;
     if (p.n_slots >= 32 && p.n_slots <= 16 * kMergeWarpBatch) {
         if (p.n_slots <= 4 * kMergeWarpBatch)
-            SLIM_CUDA_TRY(launch_pdl(slim_decode_merge_block_kernel<4>, dim3(rows), dim3(128), 0, stream, po, pm, r, o, raw, B, Hq, p.n_slots));
+            SLIM_CUDA_TRY(launch_pdl(slim_decode_merge_block_kernel<4, Rows>, dim3(rows), dim3(128), 0, stream, po, pm, r, o, raw, B, Hq, p.n_slots));
         else if (p.n_slots <= 8 * kMergeWarpBatch)
-            SLIM_CUDA_TRY(launch_pdl(slim_decode_merge_block_kernel<8>, dim3(rows), dim3(256), 0, stream, po, pm, r, o, raw, B, Hq, p.n_slots));
+            SLIM_CUDA_TRY(launch_pdl(slim_decode_merge_block_kernel<8, Rows>, dim3(rows), dim3(256), 0, stream, po, pm, r, o, raw, B, Hq, p.n_slots));
         else
-            SLIM_CUDA_TRY(launch_pdl(slim_decode_merge_block_kernel<16>, dim3(rows), dim3(512), 0, stream, po, pm, r, o, raw, B, Hq, p.n_slots));
+            SLIM_CUDA_TRY(launch_pdl(slim_decode_merge_block_kernel<16, Rows>, dim3(rows), dim3(512), 0, stream, po, pm, r, o, raw, B, Hq, p.n_slots));
     } else if (p.n_slots >= 32) {
-        SLIM_CUDA_TRY(launch_pdl(slim_decode_merge_kernel<4>, dim3(rows), dim3(4 * kHeadDim), 0, stream, po, pm, r, o, raw, B, Hq, p.n_slots));
+        SLIM_CUDA_TRY(launch_pdl(slim_decode_merge_kernel<4, Rows>, dim3(rows), dim3(4 * kHeadDim), 0, stream, po, pm, r, o, raw, B, Hq, p.n_slots));
     } else {
         const int blocks = (rows + kMergeWarpsPerBlock - 1) / kMergeWarpsPerBlock;
-        SLIM_CUDA_TRY(launch_pdl(slim_decode_merge_warp_kernel, dim3(blocks), dim3(kMergeWarpsPerBlock * 32), 0, stream, po, pm, r, o, raw, B, Hq, p.n_slots));
+        SLIM_CUDA_TRY(launch_pdl(slim_decode_merge_warp_kernel<Rows>, dim3(blocks), dim3(kMergeWarpsPerBlock * 32), 0, stream, po, pm, r, o, raw, B, Hq, p.n_slots));
     }
     return SLIM_OK;
+}
+
+int launch_merge_rows(const DecodeParams &p, int B, void *out, float *raw, cudaStream_t stream)
+{
+    const int cap = merge_cap_tokens(p);
+    if (p.shared_len != nullptr) return launch_merge(p, SharedRows{p.kv_len, p.shared_len, p.slot0, p.max_pages_per_seq, cap}, B, out, raw, stream);
+    return launch_merge(p, PlainRows{p.kv_len, cap}, B, out, raw, stream);
 }
 
 // Decode attention over a part of every sequence's keys: split pass, then the merge pass leaves each row's merged

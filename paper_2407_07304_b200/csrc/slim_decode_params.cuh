@@ -4,7 +4,8 @@
 
 namespace slim {
 
-struct DecodeParams {
+// The plain split pass.  (It is passed by value with every launch: 32 bytes more of it cost a decode step 0.5 us.)
+struct SplitParams {
     const int8_t *codes;
     const float *scales;
     const int32_t *block_table;
@@ -25,6 +26,10 @@ struct DecodeParams {
     int n_chunks;             // 256-token chunks that max_kv tokens need
     int n_slots;              // partial slots per row: n_chunks + 1 (the last token of a row has a partial of its own)
     float scale_log2e;        // sm_scale * log2(e)
+};
+
+// What the other forms of the pass take beside it.
+struct DecodeParams : SplitParams {
     // kept for the attention weights (optional): [B][Hq][share_stride], position by position a token's share of the
     // denominator l of its partial, 2^(s - m)
     float *shares;

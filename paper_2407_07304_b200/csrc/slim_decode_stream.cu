@@ -43,6 +43,8 @@
 // Every wait is bounded; a wait that runs out raises the status word and the block drains and exits.
 #include <cuda.h>
 
+#include <type_traits>
+
 #include "slim_common.cuh"
 #include "slim_decode_params.cuh"
 #include "slim_quant.cuh"
@@ -134,18 +136,21 @@ constexpr int kStPlain = 0;
 constexpr int kStShares = 1;   // every token's share of its partial's denominator also goes to p.shares (slim_attn_decode_weights)
 constexpr int kStTail = 2;     // only the tokens behind a shared prefix (slim_attn_decode_shared); the prefix kernel runs beside this one
 
+template <int kWhat>
+using StParams = std::conditional_t<kWhat == kStPlain, SplitParams, DecodeParams>;
+
 // The cached tokens of a sequence that this launch attends over start at position st_start: 0, or the end of the
 // prefix that the sequence shares (whole pages).
 template <int kWhat>
-__device__ __forceinline__ int st_start(const DecodeParams &p, int b)
+__device__ __forceinline__ int st_start(const StParams<kWhat> &p, int b)
 {
-    if (kWhat != kStTail) return 0;
-    return decode_shared_tokens(p, b);
+    if constexpr (kWhat == kStTail) return decode_shared_tokens(p, b);
+    else return 0;
 }
 
 // A sequence's cached tokens (from st_start on), never beyond the page table or the launch's max_kv.
 template <int kWhat>
-__device__ __forceinline__ int st_clamped_len(const DecodeParams &p, int b)
+__device__ __forceinline__ int st_clamped_len(const StParams<kWhat> &p, int b)
 {
     const int start = st_start<kWhat>(p, b);
     const int cap = min(p.max_pages_per_seq * kPageTokens - start, p.n_chunks * kStChunk);
@@ -154,7 +159,7 @@ __device__ __forceinline__ int st_clamped_len(const DecodeParams &p, int b)
 
 // The tokens of a sequence that the chunks cover: all but the last one, which is attended from registers.
 template <int kWhat>
-__device__ __forceinline__ int st_chunk_len(const DecodeParams &p, int b)
+__device__ __forceinline__ int st_chunk_len(const StParams<kWhat> &p, int b)
 {
     return max(st_clamped_len<kWhat>(p, b) - 1, 0);
 }
@@ -169,15 +174,16 @@ __device__ __forceinline__ int st_cut_tiles(int len, int n_chunks)
 
 // Where the partial of a row's chunk lies: the tail's chunks follow the slots of the prefix kernel.
 template <int kWhat>
-__device__ __forceinline__ size_t st_slot(const DecodeParams &p, size_t row, int chunk)
+__device__ __forceinline__ size_t st_slot(const StParams<kWhat> &p, size_t row, int chunk)
 {
-    return row * p.n_slots + (kWhat == kStTail ? p.slot0 : 0) + chunk;
+    if constexpr (kWhat == kStTail) return row * p.n_slots + p.slot0 + chunk;
+    else return row * p.n_slots + chunk;
 }
 
 // Steps (sequence, kv head, chunk) to the next chunk in the order the work is cut in; sequences without
 // chunks are skipped.  Only called while another chunk exists, so a sequence with chunks is always found.
 template <int kWhat>
-__device__ __forceinline__ void st_next_chunk(const DecodeParams &p, int B, int &b, int &head, int &chunk, int &len, int &nc)
+__device__ __forceinline__ void st_next_chunk(const StParams<kWhat> &p, int B, int &b, int &head, int &chunk, int &len, int &nc)
 {
     if (++chunk == nc) {
         chunk = 0;
@@ -207,7 +213,7 @@ __device__ __forceinline__ long long st_div(long long a, int b)
 // O = the V codes - goes to slot `slot` of the row; with to_out (a sequence of one token in a launch that merges
 // its own partials) the result code * sv is written straight to the output instead.
 template <bool kAppend, int kWhat>
-__device__ __forceinline__ void st_last_token(const DecodeParams &p, int b, int head, int L, int slot, int lane, bool to_out)
+__device__ __forceinline__ void st_last_token(const StParams<kWhat> &p, int b, int head, int L, int slot, int lane, bool to_out)
 {
     const int kv = lane >> 4, l = lane & 15;
     const int start = st_start<kWhat>(p, b);
@@ -281,7 +287,9 @@ __device__ __forceinline__ void st_last_token(const DecodeParams &p, int b, int 
                 dst[1] = make_float4(c[4], c[5], c[6], c[7]);
             }
             if (lane == 0) *reinterpret_cast<float2 *>(p.part_ml + ps * 2) = make_float2(fmaf(s, ks, lsv), rsv);
-            if (kWhat == kStShares && lane == 0) p.shares[(row0 + h0 + i) * p.share_stride + pos] = rsv;
+            if constexpr (kWhat == kStShares) {
+                if (lane == 0) p.shares[(row0 + h0 + i) * p.share_stride + pos] = rsv;
+            }
         }
     }
 }
@@ -289,7 +297,7 @@ __device__ __forceinline__ void st_last_token(const DecodeParams &p, int b, int 
 // Log-sum-exp merge of the nc partials (the chunks' and the last token's) of the G query heads of (sequence b, kv head `head`) by one warp:
 //   M = max m_c;  l = sum l_c 2^(m_c - M);  o = sum O_c 2^(m_c - M) / l   (a lane owns four head dims).
 // The caller has made sure that every partial of the pair is visible; they are read past the L1 cache.
-__device__ __forceinline__ void st_merge_rows(const DecodeParams &p, int b, int head, int nc, int lane)
+__device__ __forceinline__ void st_merge_rows(const SplitParams &p, int b, int head, int nc, int lane)
 {
     constexpr int kBatch = 12;   // partial outputs requested before the first of them is used
     for (int h = 0; h < p.G; ++h) {
@@ -342,7 +350,7 @@ __device__ __forceinline__ void st_merge_rows(const DecodeParams &p, int b, int 
 template <int NH, bool kAppend, bool kMerge, int kWhat>
 __global__ void __launch_bounds__(StSmem<NH, kAppend>::kThreads, 1)
 slim_decode_stream_kernel(const __grid_constant__ CUtensorMap map_tile, const __grid_constant__ CUtensorMap map_tail,
-                          const DecodeParams p, const int B)
+                          const StParams<kWhat> p, const int B)
 {
     using L = StSmem<NH, kAppend>;
     constexpr int NS = L::NS, NP = L::NP;
@@ -868,14 +876,14 @@ slim_decode_stream_kernel(const __grid_constant__ CUtensorMap map_tile, const __
             }
             tc::fence_proxy_async();
             tc::mbar_arrive(bar_ready_pv(g));         // P^T is in place (128 arrivals start the output MMAs)
-            if (kWhat == kStShares && record_ok) {
+            if constexpr (kWhat == kStShares) {
                 // (stored while the output MMAs run: ahead of them the stores cost 12 us of a 50 us launch)
                 float *dst = p.shares + ((size_t)b * p.Hq + h0) * p.share_stride + chunk * kStChunk + gtid;
 #pragma unroll
                 for (int h = 0; h < NH; ++h) {
 #pragma unroll
                     for (int t = 0; t < 2; ++t)
-                        if (h < p.G && valid[t]) dst[(size_t)h * p.share_stride + t * kStTile] = s[t][h];
+                        if (h < p.G && valid[t] && record_ok) dst[(size_t)h * p.share_stride + t * kStTile] = s[t][h];
                 }
             }
 
@@ -1004,7 +1012,7 @@ static int launch_stream(dim3 grid, cudaStream_t stream, const CUtensorMap &map_
     const int rc = allow_dynamic_smem(reinterpret_cast<const void *>(slim_decode_stream_kernel<NH, kAppend, kMerge, kWhat>), bytes);
     if (rc != SLIM_OK) return rc;
     SLIM_CUDA_TRY(launch_pdl(slim_decode_stream_kernel<NH, kAppend, kMerge, kWhat>, grid, dim3(StSmem<NH, kAppend>::kThreads), bytes, stream, map_tile,
-                             map_tail, p, B));
+                             map_tail, static_cast<const StParams<kWhat> &>(p), B));
     SLIM_CUDA_TRY(cudaGetLastError());
     return SLIM_OK;
 }

@@ -25,7 +25,7 @@ static_assert(kDwThreads == kChunkTok, "thread = position in the chunk");
 
 // grid = (token blocks [+ 1: merge], kv heads, sequences)
 __global__ void __launch_bounds__(kDwThreads, 3)
-slim_decode_weights_kernel(const DecodeParams p, const MergeRows rows, const float *w_in, float *w_out, int w_stride, const int32_t *weighed,
+slim_decode_weights_kernel(const DecodeParams p, const PlainRows rows, const float *w_in, float *w_out, int w_stride, const int32_t *weighed,
                            float decay, int token_blocks, __nv_bfloat16 *out)
 {
     __shared__ float factor[kDwMaxGroup][kDwChunks + 1];      // per query head: the block's chunks, then the row's last token
@@ -35,7 +35,7 @@ slim_decode_weights_kernel(const DecodeParams p, const MergeRows rows, const flo
     pdl_launch_dependents();
     pdl_wait();
     if ((int)blockIdx.x == token_blocks) {
-        for (int h = warp; h < p.G; h += kDwThreads / 32) merge_row_by_warp(p.part_o, p.part_ml, rows.partials(b), out, nullptr, row0 + h, p.n_slots, lane);
+        for (int h = warp; h < p.G; h += kDwThreads / 32) merge_row_by_warp(p.part_o, p.part_ml, rows.partials(b, rows.length(b)), out, nullptr, row0 + h, p.n_slots, lane);
         return;
     }
     const int len = min(max(__ldg(p.kv_len + b), 0), rows.cap_tokens);
@@ -136,7 +136,7 @@ int launch_decode_weights(const slim_cache_t *c, const void *q, const void *k_ne
     }
     const int token_blocks = (max_kv + kDwBlockTokens - 1) / kDwBlockTokens;
     const dim3 grid((unsigned)(token_blocks + (merge_here ? 1 : 0)), (unsigned)p.Hkv, (unsigned)B);
-    SLIM_CUDA_TRY(launch_pdl(slim_decode_weights_kernel, grid, dim3(kDwThreads), 0, stream, p, merge_rows(p), w_in, w_out, w_stride, weighed, decay,
+    SLIM_CUDA_TRY(launch_pdl(slim_decode_weights_kernel, grid, dim3(kDwThreads), 0, stream, p, PlainRows{kv_len, merge_cap_tokens(p)}, w_in, w_out, w_stride, weighed, decay,
                              token_blocks, static_cast<__nv_bfloat16 *>(out)));
     return SLIM_OK;
 }

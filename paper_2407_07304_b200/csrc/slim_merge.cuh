@@ -15,31 +15,36 @@ __device__ __forceinline__ int merge_row_partials(int len, int cap_tokens)
     return (L == 0) ? 0 : (L - 1 + kChunkTok - 1) / kChunkTok + 1;
 }
 
-// The same for a row whose first tokens are a shared prefix: the prefix's slots (every one of them is filled, those without
-// a key with weight 0), then the tail's partials.  Without a prefix cap_tokens bounds the whole row, with one the tail.
-struct MergeRows {
-    const int32_t *kv_len, *shared_len;   // shared_len null: no prefix
+// How many partials the merge kernels find for a sequence.  (They are passed by value with every launch: the plain form
+// stays as small as it can be.)
+struct PlainRows {
+    const int32_t *kv_len;
+    int cap_tokens;
+    static constexpr bool kShared = false;
+    __device__ __forceinline__ int length(int b) const { return __ldg(kv_len + b); }
+    __device__ __forceinline__ int partials(int b, int len) const { return merge_row_partials(len, cap_tokens); }
+};
+
+// Behind a shared prefix: the prefix's slots (every one of them is filled, those without a key with weight 0), then the
+// tail's partials; cap_tokens bounds the tail.
+struct SharedRows {
+    const int32_t *kv_len, *shared_len;
     int slot0, max_pages, cap_tokens;
-    __device__ __forceinline__ int partials(int b) const
+    static constexpr bool kShared = true;
+    __device__ __forceinline__ int length(int b) const { return __ldg(kv_len + b); }
+    __device__ __forceinline__ int partials(int b, int len) const
     {
-        const int len = __ldg(kv_len + b);
-        if (shared_len == nullptr) return merge_row_partials(len, cap_tokens);
         const int start = min(max(__ldg(shared_len + b), 0) / kPageTokens, max_pages) * kPageTokens;
         const int tail = merge_row_partials(len - start, min(max_pages * kPageTokens - start, cap_tokens));
         return (tail == 0 && min(len, start) <= 0) ? 0 : slot0 + tail;
     }
 };
 
-inline MergeRows merge_rows(const DecodeParams &p)
+// Tokens that a launch attends over at most (behind the prefix, where there is one).
+inline int merge_cap_tokens(const DecodeParams &p)
 {
-    MergeRows r;
-    r.kv_len = p.kv_len;
-    r.shared_len = p.shared_len;
-    r.slot0 = p.slot0;
-    r.max_pages = p.max_pages_per_seq;
     const long long pages = (long long)p.max_pages_per_seq * kPageTokens, chunks = (long long)p.n_chunks * kChunkTok;
-    r.cap_tokens = (int)(pages < chunks ? pages : chunks);
-    return r;
+    return (int)(pages < chunks ? pages : chunks);
 }
 
 // A row's merged partial (what slim_attn_decode_partial returns): O relative to M, then M and l; a lane owns four dims.
