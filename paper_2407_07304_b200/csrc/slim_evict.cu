@@ -236,6 +236,7 @@ slim_evict_select_kernel(const EvictParams p)
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
         const int s = base + tid + i * kThreads;
+        if (base + i * kThreads >= r.len) break;   // (the same for the block: short rows leave the rest of it out)
         const int pos = (s < r.placed) ? pos_raw[i] : r.seen - r.len + s;
         if (!cut) {
             // nothing leaves: weights and positions as they are
@@ -251,22 +252,27 @@ slim_evict_select_kernel(const EvictParams p)
     }
     __syncthreads();
     const int s0 = base + tid * kPer;           // the thread's first slot
+    const bool any = s0 < r.len;                // the thread has slots of the row
     uint32_t key[kPer];                         // 0 behind the row's end (no token's key is 0)
     uint32_t lo = 0xFFFFFFFFu, hi = 0;          // smallest and largest key of the tokens that are not protected
     int safe = 0;                               // protected tokens
 #pragma unroll
-    for (int i4 = 0; i4 < kPer; i4 += 4) {
-        const float4 w4 = *reinterpret_cast<const float4 *>(&sm.w[S::at(tid * kPer) + i4]);
-        const int4 p4 = *reinterpret_cast<const int4 *>(&sm.pos[S::at(tid * kPer) + i4]);
-        const float w[4] = {w4.x, w4.y, w4.z, w4.w};
-        const int pos[4] = {p4.x, p4.y, p4.z, p4.w};
+    for (int i = 0; i < kPer; ++i) key[i] = 0u;
+    if (any) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const uint32_t k = (s0 + i4 + i < r.len) ? r.key_of(p, pos[i], w[i]) : 0u;
-            key[i4 + i] = k;
-            if (k == 0xFFFFFFFFu) ++safe;
-            else if (k != 0u) lo = min(lo, k), hi = max(hi, k);
-        }
+        for (int i4 = 0; i4 < kPer; i4 += 4) {
+            const float4 w4 = *reinterpret_cast<const float4 *>(&sm.w[S::at(tid * kPer) + i4]);
+            const int4 p4 = *reinterpret_cast<const int4 *>(&sm.pos[S::at(tid * kPer) + i4]);
+            const float w[4] = {w4.x, w4.y, w4.z, w4.w};
+            const int pos[4] = {p4.x, p4.y, p4.z, p4.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t k = (s0 + i4 + i < r.len) ? r.key_of(p, pos[i], w[i]) : 0u;
+                key[i4 + i] = k;
+                if (k == 0xFFFFFFFFu) ++safe;
+                else if (k != 0u) lo = min(lo, k), hi = max(hi, k);
+                }
+    }
     }
     lo = __reduce_min_sync(0xffffffffu, lo);
     hi = __reduce_max_sync(0xffffffffu, hi);
@@ -299,9 +305,11 @@ slim_evict_select_kernel(const EvictParams p)
             // the tokens above lo, by equal steps of (lo, hi]
             const uint32_t width = hi - lo;     // 0: all of them are at lo
             const int shift = (width > kEvBins) ? 32 - __clz((int)((width - 1) >> 11)) : 0;
+            if (any) {
 #pragma unroll
-            for (int i = 0; i < kPer; ++i)
-                if (key[i] > lo && key[i] <= hi) atomicAdd(&sm.hist[(key[i] - lo - 1) >> shift], 1u);
+                for (int i = 0; i < kPer; ++i)
+                    if (key[i] > lo && key[i] <= hi) atomicAdd(&sm.hist[(key[i] - lo - 1) >> shift], 1u);
+            }
             sync_row();
             const uint32_t *hist = sm.hist;
             if constexpr (kCluster) {
@@ -359,9 +367,11 @@ slim_evict_select_kernel(const EvictParams p)
             }
             if (inside <= kEvList) {
                 // listed per block, then (in a cluster) all the blocks' lists in every block
+                if (any) {
 #pragma unroll
-                for (int i = 0; i < kPer; ++i)
-                    if (key[i] >= first_key && key[i] <= last_key) sm.list[atomicAdd(&sm.n_list, 1)] = key[i];
+                    for (int i = 0; i < kPer; ++i)
+                        if (key[i] >= first_key && key[i] <= last_key) sm.list[atomicAdd(&sm.n_list, 1)] = key[i];
+                }
                 sync_row();
                 const uint32_t *all = sm.list;
                 if constexpr (kCluster) {
@@ -397,8 +407,10 @@ slim_evict_select_kernel(const EvictParams p)
     }
 
     unsigned keep = 0;   // bit i: slot s0 + i is kept
+    if (any) {
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) keep |= (key[i] != 0u && key[i] >= last) ? 1u << i : 0u;
+        for (int i = 0; i < kPer; ++i) keep |= (key[i] != 0u && key[i] >= last) ? 1u << i : 0u;
+    }
     // Exclusive prefix, over the row's threads, of a value per thread.
     auto row_prefix = [&](int v, int *block_value) {
         int incl = v;
@@ -469,16 +481,18 @@ slim_evict_select_kernel(const EvictParams p)
     // ---- the moving slots' weights and positions to the freed slots
     {
         int to[kPer];
+        if (mv != 0u) {
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) {
-            const int at = move0 + __popc(mv & ((1u << i) - 1u));
-            to[i] = !((mv >> i) & 1u) ? -1 : kMove ? freed[at] : __ldcg(freed + at);
-        }
+            for (int i = 0; i < kPer; ++i) {
+                const int at = move0 + __popc(mv & ((1u << i) - 1u));
+                to[i] = !((mv >> i) & 1u) ? -1 : kMove ? freed[at] : __ldcg(freed + at);
+            }
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) {
-            if (to[i] >= 0) {
-                r.w_out[to[i]] = sm.w[S::at(tid * kPer) + i];
-                r.pos_out[to[i]] = sm.pos[S::at(tid * kPer) + i];
+            for (int i = 0; i < kPer; ++i) {
+                if (to[i] >= 0) {
+                    r.w_out[to[i]] = sm.w[S::at(tid * kPer) + i];
+                    r.pos_out[to[i]] = sm.pos[S::at(tid * kPer) + i];
+                }
             }
         }
     }
@@ -490,6 +504,7 @@ slim_evict_select_kernel(const EvictParams p)
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
         const int s = tid + i * kThreads;
+        if (base + i * kThreads >= p.budget) break;
         if (base + s < p.budget && ((sm.kept[s / kPer] >> (s % kPer)) & 1u)) {
             r.w_out[base + s] = sm.w[S::at(s)];
             r.pos_out[base + s] = sm.pos[S::at(s)];
