@@ -343,8 +343,10 @@ class NormRope:
         for w in (q_weight, k_weight):
             if w is not None and (w.dtype != torch.bfloat16 or w.numel() != HEAD_DIM):
                 raise TypeError(f"norm weights must be bfloat16 [{HEAD_DIM}]")
-        # contiguous copies where needed; kept here because the struct holds bare addresses
-        self.tensors = [None if t is None else t.contiguous() for t in (inv_freq if half else None, axis, q_weight, k_weight)]
+        # kept here because the struct holds bare addresses
+        self.tensors = (inv_freq if half else None, axis, q_weight, k_weight)
+        if any(t is not None and not t.is_contiguous() for t in self.tensors):
+            raise TypeError("frequencies, axes and norm weights must be contiguous")
         self.n_axes = n_axes
         self.struct = SlimNormRopeStruct(*[_addr(t) for t in self.tensors], eps, 2 * half, n_axes, 1 if interleaved else 0)
         self.ref = ctypes.byref(self.struct)

@@ -236,7 +236,7 @@ __device__ __forceinline__ void prefix_block(const CUtensorMap &codes_map, const
                 m2 = ap_max_bf16x2(m2, ap_max_bf16x2(ap_max_bf16x2(ap_abs_bf16x2(w.x), ap_abs_bf16x2(w.y)), ap_max_bf16x2(ap_abs_bf16x2(w.z), ap_abs_bf16x2(w.w))));
             }
             const float p2 = pow2_floor(fmaxf(__uint_as_float(m2 << 16), __uint_as_float(m2 & 0xFFFF0000u)));
-            const float inv = pow2_recip(p2);
+            const float inv = copysignf(pow2_recip(p2), p.scale_log2e);   // (the factor c below is positive: a negative scale turns the row)
             const uint64_t inv2 = ap_pack(inv, inv);
 #pragma unroll 4
             for (int c = 0; c < 16; ++c) {
@@ -252,7 +252,7 @@ __device__ __forceinline__ void prefix_block(const CUtensorMap &codes_map, const
                 }
                 *piece = make_uint4(hw[0], hw[1], hw[2], hw[3]);
             }
-            rs = p2 * p.scale_log2e;
+            rs = p2 * fabsf(p.scale_log2e);
             if (!by_rows) row_scale[r] = rs;
             tc::fence_proxy_async();
         }

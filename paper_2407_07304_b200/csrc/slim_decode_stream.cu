@@ -877,7 +877,7 @@ slim_decode_stream_kernel(const __grid_constant__ CUtensorMap map_tile, const __
             tc::fence_proxy_async();
             tc::mbar_arrive(bar_ready_pv(g));         // P^T is in place (128 arrivals start the output MMAs)
             if constexpr (kWhat == kStShares) {
-                // (stored while the output MMAs run: ahead of them the stores cost 12 us of a 50 us launch)
+                // (stored while the output MMAs run: 43 us for the 64 / 8-head workload against 51 us with stores ahead of them)
                 float *dst = p.shares + ((size_t)b * p.Hq + h0) * p.share_stride + chunk * kStChunk + gtid;
 #pragma unroll
                 for (int h = 0; h < NH; ++h) {

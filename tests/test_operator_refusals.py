@@ -146,6 +146,8 @@ def test_binding_refuses_tensors():
         slim.NormRope(f, axis=torch.zeros(63, dtype=torch.uint8))
     with pytest.raises(TypeError):
         slim.NormRope(f, q_weight=torch.ones(128))
+    with pytest.raises(TypeError):
+        slim.NormRope(f, q_weight=torch.ones((128, 2), dtype=torch.bfloat16)[:, 0])
     nr = slim.NormRope(f)
     pos = torch.zeros(3, dtype=torch.int32)
     q = torch.zeros((3, 4, 128), dtype=torch.bfloat16)

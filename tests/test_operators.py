@@ -237,7 +237,7 @@ def attend(cache, q, lens, sm_scale):
         s = torch.einsum("hgd,hnd->hgn", q[b].double().view(cache.Hkv, G, D), k) * sm_scale
         p = torch.softmax(s, -1)
         out[b] = torch.einsum("hgn,hnd->hgd", p, v).reshape(Hq, D)
-        moved = torch.einsum("hgd,hnd->hgn", q[b].double().view(cache.Hkv, G, D) ** 2, k ** 2).amax(-1).sqrt() * sm_scale
+        moved = torch.einsum("hgd,hnd->hgn", q[b].double().view(cache.Hkv, G, D) ** 2, k ** 2).amax(-1).sqrt() * abs(sm_scale)
         top[b] = (torch.einsum("hgn,hnd->hgd", p, v.abs()).amax(-1) * (2.0 ** -9 + 16 * 2.0 ** -11 / 3 ** 0.5 * moved)).reshape(Hq, 1)
         probs.append(p.reshape(Hq, n))
     return out, probs, top
@@ -388,6 +388,54 @@ def test_decode_shared_growing_and_falling_maxima():
             if best.values[0] - best.values[1] > 20:
                 v = vv[0, best.indices[0]]
                 assert ((out[b, 0].double() - v).abs() <= v.abs() * 2.0 ** -8 + v.abs().max() * 2.0 ** -9).all()
+
+
+@pytest.mark.parametrize("sm_scale", [-0.05, 0.0, 1e-3, 0.4])
+def test_decode_shared_and_weights_any_scale(sm_scale):
+    slim = _slim()
+    for groups in ([(3, 4)], [(3, 40)]):                    # 16 and 160 rows per kv head
+        cache, B, cu = shared_setup(12, groups, 8, 2, 2)
+        q = torch.randn((B, 8, D), generator=gen(4)).to(torch.bfloat16).cuda()
+        lens = [384 + (37 * b) % 200 for b in range(B)]
+        out, out2 = torch.empty_like(q), torch.empty_like(q)
+        ws = slim.shared_workspace(B, 8, 2, 1, B, 384, 200)
+        slim.slim_attn_decode_shared(cache, q, out, i32(cu), i32([384] * B), i32(lens), 1, B, B, 384, 200, 8, sm_scale, ws)
+        wt = torch.zeros((B, 2, 600), device="cuda")
+        slim.slim_attn_decode_weights(cache, q, out2, None, wt, None, i32(lens), B, 600, 8, sm_scale, 1.0, slim.weights_workspace(B, 8, 2, 600))
+        torch.cuda.synchronize()
+        want, probs, slack = attend(cache, q, lens, sm_scale)
+        out_close(out, want, slack, "shared")
+        out_close(out2, want, slack, "weights")
+        for b in range(B):
+            assert (wt[b, :, :lens[b]].double() - probs[b].view(2, 4, -1).sum(1)).abs().max() < 1e-4
+
+
+def test_decode_shared_and_weights_zero_rows():
+    """Keys and values of zero (scale 0), a whole tile of them, zero queries."""
+    slim = _slim()
+    cache, B, cu = shared_setup(13, [(3, 30)], 8, 2, 3)
+    codes, scales = cache.codes_view(), cache.scales_view()
+    pre = cache.block_table[0, :3].long()
+    codes[pre[1]] = 0
+    scales[pre[1]] = 0.0                                    # every key and value of the second tile
+    tail = cache.block_table[:, 3].long()
+    codes[tail, :, :, 5:20] = 0
+    scales[tail, :, :, 5:20] = 0.0
+    q = torch.randn((B, 8, D), generator=gen(4)).to(torch.bfloat16).cuda()
+    q[3] = 0
+    q[4, 1] = 0
+    lens = [384 + (23 * b) % 300 for b in range(B)]
+    out, out2 = torch.empty_like(q), torch.empty_like(q)
+    ws = slim.shared_workspace(B, 8, 2, 1, B, 384, 300)
+    slim.slim_attn_decode_shared(cache, q, out, i32(cu), i32([384] * B), i32(lens), 1, B, B, 384, 300, 8, D ** -0.5, ws)
+    wt = torch.zeros((B, 2, 700), device="cuda")
+    slim.slim_attn_decode_weights(cache, q, out2, None, wt, None, i32(lens), B, 700, 8, D ** -0.5, 1.0, slim.weights_workspace(B, 8, 2, 700))
+    torch.cuda.synchronize()
+    want, probs, slack = attend(cache, q, lens, D ** -0.5)
+    out_close(out, want, slack, "shared")
+    out_close(out2, want, slack, "weights")
+    for b in range(B):
+        assert (wt[b, :, :lens[b]].double() - probs[b].view(2, 4, -1).sum(1)).abs().max() < 1e-5
 
 
 # ================================================================== attention weights
