@@ -359,20 +359,16 @@ __device__ __forceinline__ void prefix_block(const CUtensorMap &codes_map, const
             tc::mbar_arrive(bar(shl::P_FULL, t));
         }
 
-        // ---- epilogue: both groups' last products are complete, so the operand buffers are free: 64 KB for each group's
-        //      rows, 16-byte piece c of row r in piece slot (c + r) mod 32 (no bank conflicts either way)
-        wait(bar(shl::O_DONE, 0), (uint32_t)(steps - 1) & 1u);
-        wait(bar(shl::O_DONE, 1), (uint32_t)(steps - 1) & 1u);
+        // ---- epilogue: the rows go out through the operand buffers, 64 KB for each group, 16-byte piece c of row r in piece
+        //      slot (c + r) mod 32 (no bank conflicts either way).  Behind group 0's last product all scores are complete, so
+        //      the K buffers are free; behind group 1's, the block's last, the V buffers too.
+        wait(bar(shl::O_DONE, t), (uint32_t)(steps - 1) & 1u);
         __syncwarp();
         tc::fence_after_sync();
         unsigned char *stage0 = smem + shl::kKf, *stage1 = smem + shl::kVf;
         float2 *ml1 = reinterpret_cast<float2 *>(smem + shl::kMl);
-        float w_own = 1.f, w_other = 0.f;
-        if (!by_rows) {
-            if (t == 1) ml1[r] = make_float2(m_run, l_run);
-            // group 1 stages its rows first, group 0 adds them to its own
-        }
-        if (by_rows || t == 1) {
+        if (!by_rows && t == 1) ml1[r] = make_float2(m_run, l_run);   // group 1 stages its rows first, group 0 adds them to its own
+        if ((by_rows || t == 1) && warp_rows) {
             unsigned char *stage = (by_rows && t == 0) ? stage0 : stage1;
 #pragma unroll
             for (int c4 = 0; c4 < 4; ++c4) {
@@ -386,12 +382,12 @@ __device__ __forceinline__ void prefix_block(const CUtensorMap &codes_map, const
         }
         if (!by_rows) {
             tc::named_barrier(1, 256);
-            if (t == 0) {
+            if (t == 0 && warp_rows) {
                 const float2 other = ml1[r];
                 const float M = fmaxf(m_run, other.x);
                 const bool use_other = other.x != -INFINITY;
-                w_own = (m_run == -INFINITY) ? 0.f : exp2f(m_run - M);
-                w_other = use_other ? exp2f(other.x - M) : 0.f;
+                const float w_own = (m_run == -INFINITY) ? 0.f : exp2f(m_run - M);
+                const float w_other = use_other ? exp2f(other.x - M) : 0.f;
                 l_run = l_run * w_own + (use_other ? other.y * w_other : 0.f);
                 m_run = M;
 #pragma unroll
@@ -419,8 +415,9 @@ __device__ __forceinline__ void prefix_block(const CUtensorMap &codes_map, const
             const unsigned char *stage = t ? stage1 : stage0;
             __syncwarp();
             const size_t ps = my_row < rows ? out_row(my_row) * p.n_slots + split : 0;
-            if (my_row < rows && ok) *reinterpret_cast<float2 *>(p.part_ml + ps * 2) = make_float2(m_run, l_run);
-            const int n_out = ok ? min(32, rows - (my_row - lane)) : 0;   // rows of this warp
+            const bool all_ok = __all_sync(0xffffffffu, ok);   // (after a wait that ran out nothing is written, by no lane of the warp)
+            if (my_row < rows && all_ok) *reinterpret_cast<float2 *>(p.part_ml + ps * 2) = make_float2(m_run, l_run);
+            const int n_out = all_ok ? min(32, rows - (my_row - lane)) : 0;   // rows of this warp
 #pragma unroll 4
             for (int i = 0; i < n_out; ++i) {
                 const int rr = (warp & 3) * 32 + i;
