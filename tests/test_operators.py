@@ -281,6 +281,8 @@ SHARED_CASES = [
     ([(4, 2), (0, 3), (11, 9), (1, 1)], 6, 3, [1, 60, 300]), ([(20, 64)], 8, 1, [2]), ([(2, 4)], 4, 2, [-1, -128, -255, -256]),
     ([(3, 70)], 15, 5, [-384, -383, 1, 0, -1, 44, -129]), ([(33, 17)], 32, 32, [127, 128, 129]), ([(40, 8)], 64, 4, [700, 1]),
     ([(2, 129)], 1, 1, [9]),
+    # more prefix blocks than SMs: nine groups of 32 kv heads; thirteen row blocks of one kv head; 65 groups of one
+    ([(2, 2)] * 9, 32, 32, [3, 140]), ([(4, 200)], 16, 1, [5, 1, 260]), ([(1, 1), (2, 1)] * 32 + [(0, 1)], 4, 4, [2, 130, 0]),
 ]
 
 
