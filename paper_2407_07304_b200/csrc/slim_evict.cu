@@ -518,7 +518,7 @@ slim_evict_select_long_kernel(const EvictParams p)
 {
     constexpr int kThreads = 1024, kWarps = 32;
     __shared__ __align__(16) uint32_t hist[4][256];
-    __shared__ int warp_n[32];
+    __shared__ int warp_n[32], all_moves;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int b = blockIdx.y, head = blockIdx.x, row = b * p.Hkv + head;
     pdl_launch_dependents();
@@ -577,8 +577,8 @@ slim_evict_select_long_kernel(const EvictParams p)
         move_n += __popc(__ballot_sync(0xffffffffu, s >= p.budget && kept));
     });
     int free_at = block_prefix(free_n), move_at = block_prefix(move_n);
-    const int move0 = move_at;
     int32_t *freed = p.moves + (size_t)row * 3 * p.cap, *freed_row = freed + p.cap, *moving_row = freed_row + p.cap;
+    // the lists, and the slots that stay: what is written here in place of an input is what stands there, so the walk's keys hold
     walk([&](int s, bool in, bool kept) {
         const unsigned fr = __ballot_sync(0xffffffffu, in && s < p.budget && !kept), mv = __ballot_sync(0xffffffffu, s >= p.budget && kept);
         if (in && s < p.budget && !kept) {
@@ -586,18 +586,18 @@ slim_evict_select_long_kernel(const EvictParams p)
             freed[at] = s;
             freed_row[at] = r.cache_row(p, head, s);
         }
-        if (s >= p.budget && kept) moving_row[move_at + __popc(mv & lower)] = r.cache_row(p, head, s);
+        if (s >= p.budget && kept) moving_row[move_at + __popc(mv & lower)] = s;   // (the slot, until the lists are complete)
+        if (s < p.budget && kept) r.keep(s, s);
         free_at += __popc(fr);
         move_at += __popc(mv);
     });
-    if (warp == kWarps - 1 && lane == 0) p.n_moves[row] = move_at;
-    __syncthreads();   // every key has been read: the outputs may be the inputs
-    int at = move0;
-    walk([&](int s, bool in, bool kept) {
-        const unsigned mv = __ballot_sync(0xffffffffu, s >= p.budget && kept);
-        if (kept) r.keep(s < p.budget ? s : __ldcg(freed + at + __popc(mv & lower)), s);
-        at += __popc(mv);
-    });
+    if (warp == kWarps - 1 && lane == 0) all_moves = p.n_moves[row] = move_at;
+    __syncthreads();   // every key has been read: from here on freed slots are overwritten where the outputs are the inputs
+    for (int i = tid, n = all_moves; i < n; i += kThreads) {
+        const int s = __ldcg(moving_row + i);
+        r.keep(__ldcg(freed + i), s);
+        moving_row[i] = r.cache_row(p, head, s);
+    }
 }
 
 // The rows of every (sequence, kv head): sixteen lanes per row, four rows in flight.

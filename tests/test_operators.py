@@ -875,3 +875,26 @@ def test_long_eviction_in_a_graph():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(x, y) for x, y in zip(a, (cache.codes, wo, po)))
+
+
+@pytest.mark.parametrize("lens,budget", [([70000], 30000), ([66001, 90000], 45000)])
+def test_long_eviction_with_one_side_in_place(lens, budget):
+    """Weights in place and positions written anew (a sequence's first eviction), or the other way round: no walk over a
+    row may take what another thread has just moved into a freed slot for the token that was there."""
+    slim = _slim()
+    B, top = len(lens), max(lens)
+    w, _ = evict_inputs(top + budget, lens, 1, top, None, lens, "ties")
+    cache = slim.SlimCache(B, 1, (top + PAGE - 1) // PAGE)
+    ws = slim.evict_workspace(B, 1, top, budget)
+    want = [evict_reference(w[b, 0].numpy(), np.arange(n), n, budget, 4, 300, n, 0) for b, n in enumerate(lens)]
+    placed = i32(lens)
+    for weights_in_place in (True, False) * 4:
+        wi = w.cuda()
+        pi = torch.arange(top, dtype=torch.int32, device="cuda").repeat(B, 1, 1).contiguous()
+        wo, po = (wi, torch.zeros_like(pi)) if weights_in_place else (torch.zeros_like(wi), pi)
+        slim.slim_kv_evict(cache, wi, wo, None if weights_in_place else pi, po, i32(lens), None if weights_in_place else placed, None, B, top, budget, 4, 300, ws)
+        torch.cuda.synchronize()
+        for b in range(B):
+            src, p = want[b]
+            assert torch.equal(po[b, 0, :budget].cpu(), torch.from_numpy(p.astype(np.int32)))
+            assert torch.equal(wo[b, 0, :budget].cpu(), w[b, 0, torch.from_numpy(src)])
