@@ -437,8 +437,9 @@ int slim_norm_rope_append(const slim_cache_t *cache, const slim_norm_rope_t *nr,
  *   shared_len device int32 [B]: tokens of the prefix, the same for a group's sequences; counted in whole pages (a
  *              length inside a page is cut to the pages before it), 0: nothing shared
  *   kv_len     device int32 [B]: all cached tokens of a sequence, prefix included; may be less than the prefix
- *   max_group, max_shared, max_tail  upper bounds on a group's sequences, on shared_len and on kv_len - shared_len
- *              (they size the launch and the workspace)
+ *   max_group, max_shared, max_tail  upper bounds on a group's sequences, on shared_len and on the tokens of a sequence
+ *              behind its prefix, the prefix counted as above: a page that is shared in part belongs to the tail.  (They
+ *              size the launch and the workspace; tokens beyond them are not attended.)
  *   workspace  at least slim_shared_workspace_bytes(...) bytes; header as for slim_attn_decode
  * A new token that would fall into the prefix is not appended (the page belongs to all of the group).
  */

@@ -418,11 +418,23 @@ def slim_attn_decode_shared(cache, q, out, cu_group, shared_len, kv_len, n_group
     _check(rc, "slim_attn_decode_shared")
 
 
+def _slots(where, B, Hkv, weight_out, *others):
+    """Room per slot of those [B, Hkv, stride] arrays (fp32 weights, int32 positions): one stride serves them all."""
+    shape = weight_out.shape
+    if len(shape) != 3 or shape[0] < B or shape[1] != Hkv:
+        raise SlimError(SLIM_ERR_INVALID_ARG, f"{where}: weights and positions are [B, Hkv, stride]")
+    for t, dtype in ((weight_out, torch.float32), *others):
+        if t is not None and (t.dtype is not dtype or t.shape != shape or not t.is_contiguous()):
+            raise SlimError(SLIM_ERR_INVALID_ARG, f"{where}: weights must be float32, positions int32, all contiguous and of one shape")
+    return shape[2]
+
+
 def slim_attn_decode_weights(cache, q, out, weight_in, weight_out, weighed, kv_len, B, max_kv, Hq, sm_scale, decay, workspace, stream=None,
                              k_new=None, v_new=None):
     """slim_attn_decode that also accumulates attention weights: fp32 [B, Hkv, stride], weight_in may be weight_out or None."""
+    stride = _slots("slim_attn_decode_weights", B, cache.Hkv, weight_out, (weight_in, torch.float32))
     rc = lib().slim_attn_decode_weights(ctypes.byref(cache.struct), _addr(q), _addr(k_new), _addr(v_new), _addr(out), _addr(weight_in),
-                                        _addr(weight_out), weight_out.shape[-1], _addr(weighed), _addr(kv_len), B, max_kv, Hq, sm_scale, decay,
+                                        _addr(weight_out), stride, _addr(weighed), _addr(kv_len), B, max_kv, Hq, sm_scale, decay,
                                         _addr(workspace), _nbytes(workspace), _cuda_stream(stream))
     _check(rc, "slim_attn_decode_weights")
 
@@ -431,7 +443,8 @@ def slim_kv_evict(cache, weight_in, weight_out, pos_in, pos_out, kv_len, placed,
                   stream=None):
     """Keeps `budget` tokens of every (sequence, kv head); weights fp32 and positions int32 [B, Hkv, stride] follow them.
     The lengths afterwards are min(kv_len, budget)."""
-    rc = lib().slim_kv_evict(ctypes.byref(cache.struct), _addr(weight_in), _addr(weight_out), _addr(pos_in), _addr(pos_out), weight_out.shape[-1],
+    stride = _slots("slim_kv_evict", B, cache.Hkv, weight_out, (weight_in, torch.float32), (pos_in, torch.int32), (pos_out, torch.int32))
+    rc = lib().slim_kv_evict(ctypes.byref(cache.struct), _addr(weight_in), _addr(weight_out), _addr(pos_in), _addr(pos_out), stride,
                              _addr(kv_len), _addr(placed), _addr(seen), B, max_kv, budget, n_sink, n_recent, _addr(workspace),
                              _nbytes(workspace), _cuda_stream(stream))
     _check(rc, "slim_kv_evict")

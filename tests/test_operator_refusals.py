@@ -161,5 +161,27 @@ def test_binding_refuses_tensors():
         slim.slim_norm_rope(nr, q, q, q[:2], q[:2], pos, stream=_NoStream)
 
 
+def test_binding_refuses_weights_and_positions():
+    """One stride serves all of a call's arrays, so they must be of one shape."""
+    import torch
+    c = slim.SlimCache(2, 4, 2, device="cpu")
+    w, pos, lens = torch.zeros((2, 4, 256)), torch.zeros((2, 4, 256), dtype=torch.int32), torch.zeros(2, dtype=torch.int32)
+    evict = lambda wi, wo, pi, po, B=2: slim.slim_kv_evict(c, wi, wo, pi, po, lens, lens, lens, B, 256, 128, 0, 0, None, stream=_NoStream)  # noqa: E731
+    weigh = lambda wi, wo, B=2: slim.slim_attn_decode_weights(c, w, w, wi, wo, None, lens, B, 256, 4, 1.0, 1.0, None, stream=_NoStream)  # noqa: E731
+    for wi, wo, pi, po in ((w.half(), w, pos, pos), (w, w.double(), pos, pos), (w, w, pos.long(), pos), (w, w, pos, pos[..., :255]), (w[..., :128], w, pos, pos),
+                           (w, w, pos[:, :2], pos), (w, w.transpose(0, 1), pos, pos), (w, w.view(-1), pos, pos), (w.expand(2, 4, 256)[..., :1].expand(2, 4, 256), w, pos, pos)):
+        with pytest.raises(slim.SlimError) as e:
+            evict(wi, wo, pi, po)
+        assert e.value.code == INVALID
+    for wi, wo in ((w.half(), w), (None, w.double()), (w[..., :128], w), (None, w[:, :2]), (None, w[..., ::2])):
+        with pytest.raises(slim.SlimError) as e:
+            weigh(wi, wo)
+        assert e.value.code == INVALID
+    for call in (lambda: evict(w, w, pos, pos, B=3), lambda: weigh(w, w, B=3)):
+        with pytest.raises(slim.SlimError) as e:
+            call()
+        assert e.value.code == INVALID
+
+
 class _NoStream:
     cuda_stream = 0
