@@ -898,3 +898,36 @@ def test_long_eviction_with_one_side_in_place(lens, budget):
             src, p = want[b]
             assert torch.equal(po[b, 0, :budget].cpu(), torch.from_numpy(p.astype(np.int32)))
             assert torch.equal(wo[b, 0, :budget].cpu(), w[b, 0, torch.from_numpy(src)])
+
+
+@pytest.mark.parametrize("into", [1, 64, 127])
+def test_decode_shared_prefix_that_ends_inside_a_page(into):
+    """Counted in whole pages: the page that is shared in part is the tails' (a call of the same bounds gives the same bits)."""
+    slim = _slim()
+    hq, hkv = 16, 2
+    cache, B, cu = shared_setup(into, [(3, 4), (0, 1), (1, 2)], hq, hkv, 4)
+    pre = [384] * 4 + [0] + [128] * 2
+    lens = [n + 130 + 7 * b for b, n in enumerate(pre)]
+    max_tail = max(n - p for n, p in zip(lens, pre))
+    q = torch.randn((B, hq, D), generator=gen(into)).to(torch.bfloat16).cuda()
+    outs = []
+    for extra in (0, into):
+        out = torch.full_like(q, 5.0)
+        ws = slim.shared_workspace(B, hq, hkv, 3, 4, 384 + extra, max_tail)
+        slim.slim_attn_decode_shared(cache, q, out, i32(cu), i32([p + extra for p in pre]), i32(lens), 3, B, 4, 384 + extra, max_tail, hq, D ** -0.5, ws)
+        torch.cuda.synchronize()
+        assert slim.slim_read_status(ws) == 0
+        outs.append(out)
+    assert torch.equal(*outs) and not (outs[0] == 5.0).all(-1).any()
+
+
+def test_decode_shared_prefix_of_less_than_a_page_is_decode():
+    slim = _slim()
+    hq, hkv, lens = 8, 4, [300, 77, 1]
+    cache, B, cu = shared_setup(4, [(1, 3)], hq, hkv, 3)
+    q = torch.randn((B, hq, D), generator=gen(9)).to(torch.bfloat16).cuda()
+    a, b = torch.full_like(q, 5.0), torch.full_like(q, 5.0)
+    slim.slim_attn_decode_shared(cache, q, a, i32(cu), i32([127] * 3), i32(lens), 1, B, 3, 127, 300, hq, D ** -0.5, slim.shared_workspace(B, hq, hkv, 1, 3, 127, 300))
+    slim.slim_attn_decode(cache, q, b, i32(lens), B, 300, hq, D ** -0.5, slim.workspace(slim.PHASE_DECODE, B, hq, hkv, 1, 300))
+    torch.cuda.synchronize()
+    assert torch.equal(a, b)
