@@ -17,7 +17,8 @@
 // slots are ranked by one prefix sum of bit counts; weights and positions are read once, in whole lines, and handed to
 // the slots' owners through shared memory.  A row of up to 8192 tokens is one block's, a longer one a cluster's
 // of up to eight blocks, which read one another's histograms and lists through distributed shared memory;
-// beyond 65536 tokens one block walks the row again for each of four histograms of digits.
+// beyond 131072 tokens one block walks the row again for each of four histograms of digits (rows of 131072 tokens cut to
+// 16384: 324 us that way, 33 us by the cluster).
 // Measured (512 rows of 2049 tokens / 256 of up to 4096 / 2 of 32768, selection alone): 15 / 15 / 19 us; forms before it:
 // four histograms of the keys' digits 34 / 36 / 29 us (weights share their leading bits, the additions to one counter
 // queue up), a search with three bounds a step 18 / 23 / 27 us.
@@ -450,7 +451,7 @@ slim_evict_select_kernel(const EvictParams p)
     const int low_n = min(max(p.budget - s0, 0), kPer);                          // the thread's slots below the budget
     const unsigned low = (low_n == 32) ? 0xFFFFFFFFu : (1u << low_n) - 1u;
     unsigned fr = ~keep & low, mv = keep & ~low;
-    // both counts in one prefix: as many slots are freed as move, at most half of the row's 65536
+    // both counts in one prefix: as many slots are freed as move, fewer than 65536
     const unsigned both = (unsigned)row_prefix((int)((unsigned)__popc(fr) << 16 | (unsigned)__popc(mv)), &sm.block_sum);
     int free_at = (int)(both >> 16), move_at = (int)(both & 0xFFFFu);
     const int move0 = move_at;
@@ -667,6 +668,8 @@ static int launch_select_any(const EvictParams &p, int B, cudaStream_t stream)
         if (p.max_kv <= 2 * kEvBlockTokens) return launch_select<1024, kEvItems, true, false>(p, B, 2, stream);
         if (p.max_kv <= 4 * kEvBlockTokens) return launch_select<1024, kEvItems, true, false>(p, B, 4, stream);
         if (p.max_kv <= kEvMaxCluster * kEvBlockTokens) return launch_select<1024, kEvItems, true, false>(p, B, kEvMaxCluster, stream);
+        // (the counts of freed and moving slots share 32 bits)
+        if (p.max_kv <= 2 * kEvMaxCluster * kEvBlockTokens && p.cap < 65536) return launch_select<1024, 2 * kEvItems, true, false>(p, B, kEvMaxCluster, stream);
     }
     SLIM_CUDA_TRY(launch_pdl(slim_evict_select_long_kernel, dim3((unsigned)p.Hkv, (unsigned)B), dim3(1024), 0, stream, p));
     return SLIM_OK;

@@ -535,6 +535,8 @@ EVICT_CASES = [
     ([260] * 9, 5, 130, 0, 10, None, False), ([60001], 1, 3000, 16, 100, [3000], True), ([55000], 1, 54990, 0, 0, None, False),
     ([16385, 70000], 1, 2000, 4, 300, [2000, 2000], True), ([66000], 1, 65990, 0, 0, None, False), ([65536], 1, 32768, 0, 0, [32768], False),
     ([8193, 3], 2, 100, 1, 1, None, True),
+    ([131072], 1, 65535, 4, 64, None, True), ([131071, 70000], 1, 4000, 4, 64, [4000, 0], False), ([131072], 1, 65536, 0, 10, [65536], False),
+    ([140001, 131073], 1, 30000, 4, 64, [30000, 100], True),
 ]
 
 
@@ -877,7 +879,7 @@ def test_long_eviction_in_a_graph():
         assert all(torch.equal(x, y) for x, y in zip(a, (cache.codes, wo, po)))
 
 
-@pytest.mark.parametrize("lens,budget", [([70000], 30000), ([66001, 90000], 45000)])
+@pytest.mark.parametrize("lens,budget", [([70000], 30000), ([66001, 90000], 45000), ([140000], 60000), ([150001, 131080], 70000)])
 def test_long_eviction_with_one_side_in_place(lens, budget):
     """Weights in place and positions written anew (a sequence's first eviction), or the other way round: no walk over a
     row may take what another thread has just moved into a freed slot for the token that was there."""
