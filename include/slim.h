@@ -457,7 +457,7 @@ size_t slim_shared_workspace_bytes(int32_t B, int32_t Hq, int32_t Hkv, int32_t n
  * where tokens j >= weighed[b] (new since the last call) and a NULL weight_in count as 0 before.
  *
  *   weight_in, weight_out  device fp32 [B][Hkv][weight_stride], weight_stride >= max_kv; may be the same array; entries
- *              from kv_len[b] on are left as they are
+ *              from min(kv_len[b], max_kv) on are neither read nor written
  *   weighed    device int32 [B], or NULL: kv_len[b] - 1
  *   workspace  at least slim_weights_workspace_bytes(...) bytes (the scores lie there between the two kernels); header
  *              as for slim_attn_decode

@@ -26,7 +26,7 @@ static_assert(kDwThreads == kChunkTok, "thread = position in the chunk");
 // grid = (token blocks [+ 1: merge], kv heads, sequences)
 __global__ void __launch_bounds__(kDwThreads, 3)
 slim_decode_weights_kernel(const DecodeParams p, const PlainRows rows, const float *w_in, float *w_out, int w_stride, const int32_t *weighed,
-                           float decay, int token_blocks, __nv_bfloat16 *out)
+                           float decay, int max_kv, int token_blocks, __nv_bfloat16 *out)
 {
     __shared__ float factor[kDwMaxGroup][kDwChunks + 1];      // per query head: the block's chunks, then the row's last token
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -39,8 +39,11 @@ slim_decode_weights_kernel(const DecodeParams p, const PlainRows rows, const flo
         return;
     }
     const int len = min(max(__ldg(p.kv_len + b), 0), rows.cap_tokens);
+    // The attention takes whole chunks (a length beyond max_kv is cut at the end of max_kv's last chunk), but a row of weights
+    // has room for max_kv of them.
+    const int w_len = min(len, max_kv);
     const int first = (int)blockIdx.x * kDwBlockTokens;
-    if (first >= len) return;
+    if (first >= w_len) return;
     // ---- requested before anything is waited for: the first query heads' shares and the old weights
     const float *src = p.shares + (size_t)row0 * p.share_stride + first + tid;   // (a row's shares reach to the end of its last chunk)
     const int old_len = (w_in == nullptr) ? 0 : (weighed != nullptr) ? __ldg(weighed + b) : len - 1;
@@ -49,7 +52,7 @@ slim_decode_weights_kernel(const DecodeParams p, const PlainRows rows, const flo
 #pragma unroll
     for (int i = 0; i < kDwChunks; ++i) {
         const int j = first + tid + i * kChunkTok;
-        old[i] = (j < len && j < old_len) ? w_in[w_row + i * kChunkTok] : 0.f;
+        old[i] = (j < w_len && j < old_len) ? w_in[w_row + i * kChunkTok] : 0.f;
         sum[i] = 0.f;
     }
     auto fetch = [&](int h0) {
@@ -100,7 +103,7 @@ slim_decode_weights_kernel(const DecodeParams p, const PlainRows rows, const flo
     }
 #pragma unroll
     for (int i = 0; i < kDwChunks; ++i)
-        if (first + tid + i * kChunkTok < len) w_out[w_row + i * kChunkTok] = fmaf(decay, old[i], sum[i]);
+        if (first + tid + i * kChunkTok < w_len) w_out[w_row + i * kChunkTok] = fmaf(decay, old[i], sum[i]);
 }
 
 // The shares follow the split pass's workspace.
@@ -137,7 +140,7 @@ int launch_decode_weights(const slim_cache_t *c, const void *q, const void *k_ne
     const int token_blocks = (max_kv + kDwBlockTokens - 1) / kDwBlockTokens;
     const dim3 grid((unsigned)(token_blocks + (merge_here ? 1 : 0)), (unsigned)p.Hkv, (unsigned)B);
     SLIM_CUDA_TRY(launch_pdl(slim_decode_weights_kernel, grid, dim3(kDwThreads), 0, stream, p, PlainRows{kv_len, merge_cap_tokens(p)}, w_in, w_out, w_stride, weighed, decay,
-                             token_blocks, static_cast<__nv_bfloat16 *>(out)));
+                             max_kv, token_blocks, static_cast<__nv_bfloat16 *>(out)));
     return SLIM_OK;
 }
 

@@ -1,0 +1,66 @@
+"""Calls whose device-side lengths and groups pass the bounds given on the host: nothing behind the bounds is written, and no
+output depends on what the workspace held."""
+import pytest
+import torch
+
+from test_operators import D, attend, fill, gen, i32, rows_of
+
+pytestmark = pytest.mark.gpu
+
+
+def _slim():
+    from paper_2407_07304_b200 import binding
+    return binding
+
+
+@pytest.mark.parametrize("append", [False, True])
+@pytest.mark.parametrize("max_kv,lens,hq,hkv", [
+    (272, [300, 512, 272, 1000], 8, 2),      # lengths inside max_kv's last chunk, at its end, at max_kv, beyond the page table
+    (1, [2, 1, 256], 3, 3),                  # one entry of weight per row
+    (1025, [1026, 1280, 7], 16, 1),          # the last token block has room for one token
+])
+def test_weights_of_lengths_beyond_max_kv_stay_in_their_rows(max_kv, lens, hq, hkv, append):
+    """A row of weights holds max_kv entries; the attention takes whole chunks of 256 tokens.  With rows that lie back to back a
+    value too many lands in the next head's weights, and for the last row behind the array."""
+    slim = _slim()
+    B, mp, guard = len(lens), (max_kv + 255) // 256 * 2, 2048
+    g = gen(max_kv)
+    cache = slim.SlimCache(B, hkv, mp)
+    fill(cache, max_kv)
+    q = torch.randn((B, hq, D), generator=g).to(torch.bfloat16).cuda()
+    new = {}
+    if append:
+        new = dict(k_new=torch.randn((B, hkv, D), generator=g).to(torch.bfloat16).cuda(), v_new=torch.randn((B, hkv, D), generator=g).to(torch.bfloat16).cuda())
+    n = B * hkv * max_kv
+    held = torch.full((2, guard + n + guard), -3.0, device="cuda")
+    w_in, w_out = (h[guard:guard + n].view(B, hkv, max_kv) for h in held)
+    w_in.copy_(torch.rand((B, hkv, max_kv), generator=g))
+    weighed = i32([max_kv + 500] * B)                       # more than there is room for: every entry of the row counts
+    out = torch.empty_like(q)
+    ws = slim.weights_workspace(B, hq, hkv, max_kv)
+    slim.slim_attn_decode_weights(cache, q, out, w_in, w_out, weighed, i32(lens), B, max_kv, hq, D ** -0.5, 0.5, ws, **new)
+    torch.cuda.synchronize()
+    assert slim.slim_read_status(ws) == slim.SLIM_OK
+    assert (held[:, :guard] == -3.0).all() and (held[1, guard + n:] == -3.0).all()
+    # the same attention with rows of weights that have room for all of it
+    room = (max_kv + 255) // 256 * 256
+    wide_in, wide_out, ref = torch.zeros((B, hkv, room), device="cuda"), torch.full((B, hkv, room), -3.0, device="cuda"), torch.empty_like(q)
+    wide_in[..., :max_kv] = w_in
+    slim.slim_attn_decode_weights(cache, q, ref, wide_in, wide_out, weighed, i32([min(x, room) for x in lens]), B, room, hq, D ** -0.5, 0.5,
+                                  slim.weights_workspace(B, hq, hkv, room))
+    torch.cuda.synchronize()
+    assert torch.equal(out, ref)
+    for b, x in enumerate(lens):
+        m = min(x, max_kv)
+        assert torch.equal(w_out[b, :, :m], wide_out[b, :, :m]) and (w_out[b, :, m:] == -3.0).all()
+    _, probs, _ = attend(cache, q, [min(x, room) for x in lens], D ** -0.5)
+    for b, x in enumerate(lens):
+        m = min(x, max_kv)
+        k, _ = rows_of(cache, b, min(x, room))
+        p = probs[b].view(hkv, hq // hkv, -1).sum(1)[:, :m]
+        want = 0.5 * w_in[b, :, :m].double() + p
+        # a query element is held to 2^-21 of its row's largest power of two, twice for that power's spread: a score is off by
+        # 2^-20 max|q| sum|k| sm_scale at most; six fp32 roundings of scores and exponents up to 64 in log2 units; the
+        # denominator doubles it
+        ds = D ** -0.5 * 2.0 ** -20 * q[b].double().abs().max() * k.abs().sum(-1).max() + 6 * 64 * 2.0 ** -24
+        assert ((w_out[b, :, :m].double() - want).abs() <= 2 * ds * p + want * 2.0 ** -22 + 1e-30).all()
