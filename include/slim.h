@@ -433,7 +433,7 @@ int slim_norm_rope_append(const slim_cache_t *cache, const slim_norm_rope_t *nr,
  * slim_decode_step), but the prefix's keys and values are read and multiplied once for the whole group.
  *
  *   cu_group   device int32 [n_groups + 1]: group g is the sequences cu_group[g] .. cu_group[g + 1] - 1; the groups cover
- *              all B sequences (a sequence that shares nothing may be a group of its own)
+ *              all B sequences (a sequence that shares nothing may be a group of its own), so n_groups * max_group >= B
  *   shared_len device int32 [B]: tokens of the prefix, the same for a group's sequences; counted in whole pages (a
  *              length inside a page is cut to the pages before it), 0: nothing shared
  *   kv_len     device int32 [B]: all cached tokens of a sequence, prefix included; may be less than the prefix

@@ -384,6 +384,7 @@ SLIM_EXPORT int slim_attn_decode_shared(const slim_cache_t *cache, const void *q
     if (n_groups < 0 || max_group < 0 || max_shared < 0 || max_tail < 0) return SLIM_ERR_INVALID_ARG;
     if (B == 0) return SLIM_OK;
     if (n_groups == 0 || max_group == 0 || max_group > B || cu_group == nullptr || shared_len == nullptr) return SLIM_ERR_INVALID_ARG;
+    if ((long long)n_groups * max_group < B) return SLIM_ERR_INVALID_ARG;   // the groups cover all sequences
     if (n_groups > 65535) return SLIM_ERR_UNSUPPORTED;
     if (beyond_pages(cache, max_shared) || beyond_pages(cache, max_tail)) return SLIM_ERR_INVALID_ARG;
     rc = check_step_rows(q, k_new, v_new, out, kv_len);
