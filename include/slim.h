@@ -440,7 +440,8 @@ int slim_norm_rope_append(const slim_cache_t *cache, const slim_norm_rope_t *nr,
  *   max_group, max_shared, max_tail  upper bounds on a group's sequences, on shared_len and on the tokens of a sequence
  *              behind its prefix, the prefix counted as above: a page that is shared in part belongs to the tail.  (They
  *              size the launch and the workspace; tokens beyond them are not attended.)
- *   workspace  at least slim_shared_workspace_bytes(...) bytes; header as for slim_attn_decode
+ *   workspace  at least slim_shared_workspace_bytes(...) bytes, which never falls when an argument but Hkv grows: a workspace
+ *              made for the largest batch, groups and bounds serves every smaller call; header as for slim_attn_decode
  * A new token that would fall into the prefix is not appended (the page belongs to all of the group).
  */
 int slim_attn_decode_shared(const slim_cache_t *cache, const void *q, const void *k_new, const void *v_new, void *out,

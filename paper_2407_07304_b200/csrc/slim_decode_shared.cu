@@ -650,6 +650,8 @@ struct SharedShape {
     int row_blocks, splits, slots, tail_blocks;
 };
 
+constexpr int kShSms = 148;
+
 // How the work is divided over the SMs.  Prefix and tail blocks take an SM each and run side by side, so the number of
 // parts of the prefix is chosen for the earliest end of both, by what their blocks were measured to take (us):
 //   prefix block   10 + 2.6 per key tile of 256 rows; 13 + 1.4 where the softmax groups take the tiles in turn
@@ -659,7 +661,6 @@ struct SharedShape {
 // side by side.)
 static SharedShape shared_shape(int B, int Hq, int Hkv, int n_groups, int max_group, int max_shared, int max_tail)
 {
-    constexpr int kSms = 148;
     SharedShape s;
     const int G = Hq / Hkv;
     const long long rows = (long long)max_group * G;
@@ -669,10 +670,10 @@ static SharedShape shared_shape(int B, int Hq, int Hkv, int n_groups, int max_gr
     const long long per_part = (long long)Hkv * s.row_blocks * n_groups;
     const double chunks = (double)B * Hkv * (max_tail + 255) / 512, tail_work = chunks * (G <= 8 ? 2.0 : 4.0);
     s.splits = tiles > 0 ? 1 : 0;
-    s.tail_blocks = kSms;
+    s.tail_blocks = kShSms;
     double best = 1e30;
-    for (int n = 1; n <= units && n * per_part < kSms; ++n) {
-        const int tail_blocks = kSms - (int)(n * per_part);
+    for (int n = 1; n <= units && n * per_part < kShSms; ++n) {
+        const int tail_blocks = kShSms - (int)(n * per_part);
         const int part = unit * ((units + n - 1) / n);
         const double prefix = by_rows ? 10.0 + 2.6 * part : 13.0 + 1.4 * part;
         const double tail = max_tail > 0 ? 6.0 + tail_work / tail_blocks : 0.0;
@@ -683,10 +684,23 @@ static SharedShape shared_shape(int B, int Hq, int Hkv, int n_groups, int max_gr
     return s;
 }
 
+// Room for the partials of every call with at most these sequences, groups and bounds, so that a workspace made for the
+// largest serves the smaller ones too.  The division above does not grow with them (a shorter tail leaves more SMs to the
+// prefix, and so more parts), so the prefix's partials are bounded by what any division of such a call can have: one part, or
+// n parts with n * Hkv * row_blocks * n_groups < kShSms, never more than the prefix has units; and as B <= n_groups * max_group,
+//   n * B * Hq < kShSms * max_group * G / row_blocks <= kShSms * min(max_group * G, kShRows).
 size_t shared_workspace_bytes(int B, int Hq, int Hkv, int n_groups, int max_group, int max_shared, int max_tail)
 {
-    const SharedShape s = shared_shape(B, Hq, Hkv, n_groups, max_group, max_shared, max_tail);
-    return kDecodeHeaderBytes + (size_t)B * Hq * s.slots * (kHeadDim + 2) * sizeof(float);
+    const long long rows = (long long)B * Hq, stack = (long long)max_group * (Hq / Hkv);
+    const int tiles = max_shared / kShKeys, units = stack > kShTileRows ? tiles : (tiles + 1) / 2;
+    long long prefix = 0;
+    if (tiles > 0) {
+        prefix = kShSms * (stack < kShRows ? stack : kShRows);
+        if (prefix > rows * units) prefix = rows * units;
+        if (prefix < rows) prefix = rows;
+    }
+    const long long tail = rows * (((long long)max_tail + 255) / 256 + 1);
+    return kDecodeHeaderBytes + (size_t)(prefix + tail) * (kHeadDim + 2) * sizeof(float);
 }
 
 int launch_decode_shared(const slim_cache_t *c, const void *q, const void *k_new, const void *v_new, void *out, const int32_t *cu_group,

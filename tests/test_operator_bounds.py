@@ -3,7 +3,7 @@ output depends on what the workspace held."""
 import pytest
 import torch
 
-from test_operators import D, attend, fill, gen, i32, rows_of
+from test_operators import D, PAGE, attend, fill, gen, i32, rows_of, shared_setup
 
 pytestmark = pytest.mark.gpu
 
@@ -64,3 +64,20 @@ def test_weights_of_lengths_beyond_max_kv_stay_in_their_rows(max_kv, lens, hq, h
         # denominator doubles it
         ds = D ** -0.5 * 2.0 ** -20 * q[b].double().abs().max() * k.abs().sum(-1).max() + 6 * 64 * 2.0 ** -24
         assert ((w_out[b, :, :m].double() - want).abs() <= 2 * ds * p + want * 2.0 ** -22 + 1e-30).all()
+
+
+def test_one_workspace_from_the_first_step_to_the_longest_tail():
+    """A loop allocates for its longest tail and passes each step's own bounds: the same bits as with a workspace of the step's own."""
+    slim = _slim()
+    hq, hkv = 16, 2
+    cache, B, cu = shared_setup(71, [(24, 16)], hq, hkv, 17)
+    q = torch.randn((B, hq, D), generator=gen(71)).to(torch.bfloat16).cuda()
+    ws = slim.shared_workspace(B, hq, hkv, 1, B, 24 * PAGE, 2048)
+    ws[slim.WORKSPACE_HEADER_BYTES:] = 0xEE
+    for tail in (1, 2, 200, 256, 257, 700, 1024, 2048):
+        lens = i32([24 * PAGE + max(1, tail - b) for b in range(B)])
+        a, b = torch.full_like(q, 5.0), torch.full_like(q, 6.0)
+        for out, w in ((a, ws), (b, slim.shared_workspace(B, hq, hkv, 1, B, 24 * PAGE, tail))):
+            slim.slim_attn_decode_shared(cache, q, out, i32(cu), i32([24 * PAGE] * B), lens, 1, B, B, 24 * PAGE, tail, hq, D ** -0.5, w)
+        torch.cuda.synchronize()
+        assert torch.equal(a, b) and slim.slim_read_status(ws) == slim.SLIM_OK
