@@ -438,8 +438,10 @@ int slim_norm_rope_append(const slim_cache_t *cache, const slim_norm_rope_t *nr,
  *              length inside a page is cut to the pages before it), 0: nothing shared
  *   kv_len     device int32 [B]: all cached tokens of a sequence, prefix included; may be less than the prefix
  *   max_group, max_shared, max_tail  upper bounds on a group's sequences, on shared_len and on the tokens of a sequence
- *              behind its prefix, the prefix counted as above: a page that is shared in part belongs to the tail.  (They
- *              size the launch and the workspace; tokens beyond them are not attended.)
+ *              behind its prefix, the prefix counted as above: a page that is shared in part belongs to the tail.  They
+ *              size the launch and the workspace.  A shared_len beyond max_shared counts as max_shared: what follows is
+ *              the sequence's own (with max_shared below a page, all of it, as for slim_attn_decode).  Of the tokens
+ *              behind the prefix the first max_tail, rounded up to a multiple of 256, are attended.
  *   workspace  at least slim_shared_workspace_bytes(...) bytes, which never falls when an argument but Hkv grows: a workspace
  *              made for the largest batch, groups and bounds serves every smaller call; header as for slim_attn_decode
  * A new token that would fall into the prefix is not appended (the page belongs to all of the group).

@@ -232,6 +232,7 @@ DecodeParams make_decode_params(const slim_cache_t *c, const void *q, const int3
     p.shares = nullptr;
     p.share_stride = 0;
     p.shared_len = nullptr;
+    p.max_shared_pages = 0;
     p.slot0 = 0;
     p.max_blocks = 0;
     return p;
@@ -309,7 +310,7 @@ static int launch_merge(const DecodeParams &p, const Rows &r, int B, void *out, 
 int launch_merge_rows(const DecodeParams &p, int B, void *out, float *raw, cudaStream_t stream)
 {
     const int cap = merge_cap_tokens(p);
-    if (p.shared_len != nullptr) return launch_merge(p, SharedRows{p.kv_len, p.shared_len, p.slot0, p.max_pages_per_seq, cap}, B, out, raw, stream);
+    if (p.shared_len != nullptr) return launch_merge(p, SharedRows{p.kv_len, p.shared_len, p.slot0, p.max_pages_per_seq, p.max_shared_pages, cap}, B, out, raw, stream);
     return launch_merge(p, PlainRows{p.kv_len, cap}, B, out, raw, stream);
 }
 

@@ -37,14 +37,20 @@ struct DecodeParams : SplitParams {
     // tokens behind a shared prefix (optional): the prefix's length per sequence, and the partial slots in front of
     // the tail's that the prefix kernel fills
     const int32_t *shared_len;
+    int max_shared_pages;   // the launch's bound on the prefix, never beyond the page table
     int slot0;
     int max_blocks;   // of the split pass (0: one per SM)
 };
 
-// The length of the prefix that sequence b shares: whole pages, never beyond the page table.
+// The length of the prefix that sequence b shares: whole pages, never more than the launch was made for (what is shared
+// beyond that counts as the sequence's own).
+__device__ __forceinline__ int shared_tokens(const int32_t *shared_len, int max_shared_pages, int b)
+{
+    return min(max(__ldg(shared_len + b), 0) / kPageTokens, max_shared_pages) * kPageTokens;
+}
 __device__ __forceinline__ int decode_shared_tokens(const DecodeParams &p, int b)
 {
-    return min(max(__ldg(p.shared_len + b), 0) / kPageTokens, p.max_pages_per_seq) * kPageTokens;
+    return shared_tokens(p.shared_len, p.max_shared_pages, b);
 }
 
 // Workspace header in front of the partials: the status word (16 bytes), then the counters of the in-kernel

@@ -715,6 +715,7 @@ int launch_decode_shared(const slim_cache_t *c, const void *q, const void *k_new
     p.k_new = static_cast<const __nv_bfloat16 *>(k_new);
     p.v_new = static_cast<const __nv_bfloat16 *>(v_new);
     p.shared_len = shared_len;
+    p.max_shared_pages = max_shared / kPageTokens;
     p.slot0 = s.splits;
     p.n_slots = s.slots;
     p.max_blocks = s.tail_blocks;

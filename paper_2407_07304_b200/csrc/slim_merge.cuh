@@ -29,12 +29,12 @@ struct PlainRows {
 // tail's partials; cap_tokens bounds the tail.
 struct SharedRows {
     const int32_t *kv_len, *shared_len;
-    int slot0, max_pages, cap_tokens;
+    int slot0, max_pages, max_shared_pages, cap_tokens;
     static constexpr bool kShared = true;
     __device__ __forceinline__ int length(int b) const { return __ldg(kv_len + b); }
     __device__ __forceinline__ int partials(int b, int len) const
     {
-        const int start = min(max(__ldg(shared_len + b), 0) / kPageTokens, max_pages) * kPageTokens;
+        const int start = shared_tokens(shared_len, max_shared_pages, b);
         const int tail = merge_row_partials(len - start, min(max_pages * kPageTokens - start, cap_tokens));
         return (tail == 0 && min(len, start) <= 0) ? 0 : slot0 + tail;
     }

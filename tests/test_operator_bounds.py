@@ -3,7 +3,7 @@ output depends on what the workspace held."""
 import pytest
 import torch
 
-from test_operators import D, PAGE, attend, fill, gen, i32, rows_of, shared_setup
+from test_operators import D, PAGE, attend, fill, gen, i32, out_close, rows_of, shared_setup
 
 pytestmark = pytest.mark.gpu
 
@@ -81,3 +81,49 @@ def test_one_workspace_from_the_first_step_to_the_longest_tail():
             slim.slim_attn_decode_shared(cache, q, out, i32(cu), i32([24 * PAGE] * B), lens, 1, B, B, 24 * PAGE, tail, hq, D ** -0.5, w)
         torch.cuda.synchronize()
         assert torch.equal(a, b) and slim.slim_read_status(ws) == slim.SLIM_OK
+
+
+@pytest.mark.parametrize("hq,hkv,n", [(16, 2, 4), (4, 4, 1), (16, 1, 20)])
+def test_decode_shared_prefix_beyond_its_bound_is_the_sequences_own(hq, hkv, n):
+    """A shared_len beyond max_shared counts as max_shared: the bits of a call whose lengths say so."""
+    slim = _slim()
+    cache, B, cu = shared_setup(n, [(9, n), (2, 1)], hq, hkv, 3)
+    lens = [9 * PAGE + 5 + 11 * b for b in range(n)] + [400]
+    q = torch.randn((B, hq, D), generator=gen(n)).to(torch.bfloat16).cuda()
+    for bound in (4 * PAGE, 4 * PAGE + 17):
+        tail = max(lens) - 4 * PAGE
+        outs = []
+        for shared in ([9 * PAGE] * n + [2 * PAGE], [4 * PAGE] * n + [2 * PAGE]):
+            out = torch.full_like(q, 5.0)
+            ws = slim.shared_workspace(B, hq, hkv, 2, n, bound, tail)
+            ws[slim.WORKSPACE_HEADER_BYTES:] = 0xEE
+            slim.slim_attn_decode_shared(cache, q, out, i32(cu), i32(shared), i32(lens), 2, B, n, bound, tail, hq, D ** -0.5, ws)
+            torch.cuda.synchronize()
+            assert slim.slim_read_status(ws) == slim.SLIM_OK
+            outs.append(out)
+        assert torch.equal(*outs)
+        want, _, slack = attend(cache, q, lens, D ** -0.5)
+        out_close(outs[0], want, slack, bound)
+
+
+@pytest.mark.parametrize("append", [False, True])
+def test_decode_shared_tails_beyond_their_bound_are_cut(append):
+    """max_tail, rounded up to a multiple of 256 tokens, is what is attended behind the prefix; a new token behind it is not appended."""
+    slim = _slim()
+    hq, hkv, pre = 16, 2, 3 * PAGE
+    cache, B, cu = shared_setup(3, [(3, 5)], hq, hkv, 8)
+    lens = [pre + x for x in (700, 257, 256, 41, 512)]
+    q = torch.randn((B, hq, D), generator=gen(3)).to(torch.bfloat16).cuda()
+    new, before = {}, cache.codes.clone()
+    if append:
+        new = dict(k_new=torch.randn((B, hkv, D), generator=gen(4)).to(torch.bfloat16).cuda(), v_new=torch.randn((B, hkv, D), generator=gen(5)).to(torch.bfloat16).cuda())
+    out = torch.full_like(q, 5.0)
+    ws = slim.shared_workspace(B, hq, hkv, 1, B, pre, 40)
+    slim.slim_attn_decode_shared(cache, q, out, i32(cu), i32([pre] * B), i32(lens), 1, B, B, pre, 40, hq, D ** -0.5, ws, **new)
+    torch.cuda.synchronize()
+    assert slim.slim_read_status(ws) == slim.SLIM_OK
+    want, _, slack = attend(cache, q, [min(x, pre + 256) for x in lens], D ** -0.5)
+    out_close(out, want, slack, "cut")
+    for b, x in enumerate(lens):
+        same = torch.equal(cache.codes_view()[cache.block_table[b, 3:].long()], before.view_as(cache.codes_view())[cache.block_table[b, 3:].long()])
+        assert same == (not append or x > pre + 256)
