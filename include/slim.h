@@ -441,7 +441,8 @@ int slim_norm_rope_append(const slim_cache_t *cache, const slim_norm_rope_t *nr,
  *              behind its prefix, the prefix counted as above: a page that is shared in part belongs to the tail.  They
  *              size the launch and the workspace.  A shared_len beyond max_shared counts as max_shared: what follows is
  *              the sequence's own (with max_shared below a page, all of it, as for slim_attn_decode).  Of the tokens
- *              behind the prefix the first max_tail, rounded up to a multiple of 256, are attended.
+ *              behind the prefix the first max_tail, rounded up to a multiple of 256, are attended.  A sequence beyond
+ *              max_group of its group, or in no group, attends over what lies behind its prefix only.
  *   workspace  at least slim_shared_workspace_bytes(...) bytes, which never falls when an argument but Hkv grows: a workspace
  *              made for the largest batch, groups and bounds serves every smaller call; header as for slim_attn_decode
  * A new token that would fall into the prefix is not appended (the page belongs to all of the group).

@@ -54,7 +54,7 @@ slim_decode_merge_kernel(const float *__restrict__ part_o, const float *__restri
         __syncthreads();                   // the previous round's weights (and the maxima) have been used
         if (tid < n) {
             const float2 v = ml[c0 + tid];
-            const float w = exp2f(v.x - M);
+            const float w = (v.x != -INFINITY) ? exp2f(v.x - M) : 0.f;
             w_s[tid] = w;
             lsum = fmaf(v.y, w, lsum);
         }

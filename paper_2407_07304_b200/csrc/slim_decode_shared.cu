@@ -66,7 +66,7 @@ static_assert(kBytes <= 232448, "shared memory budget of one block");
 struct SharedParams {
     DecodeParams d;            // d.slot0 = parts of the prefix
     const int32_t *cu_group;   // [n_groups + 1]: the sequences of each group
-    int B;
+    int B, max_group;
 };
 
 __device__ __forceinline__ float sh_exp2(float x)
@@ -619,8 +619,26 @@ slim_decode_prefix_kernel(const __grid_constant__ CUtensorMap codes_map, const _
     const DecodeParams &p = sp.d;
     const int head = (int)blockIdx.y % p.Hkv, m0 = (int)blockIdx.y / p.Hkv * kShRows;
     // (one group is all the sequences: nothing to look up)
-    const int seq0 = gridDim.z == 1 ? 0 : min(max(__ldg(sp.cu_group + blockIdx.z), 0), sp.B);
-    const int seq1 = gridDim.z == 1 ? sp.B : min(__ldg(sp.cu_group + blockIdx.z + 1), sp.B);
+    const bool one = gridDim.z == 1;
+    const int seq0 = one ? 0 : min(max(__ldg(sp.cu_group + blockIdx.z), 0), sp.B);
+    const int seq_end = one ? sp.B : min(max(__ldg(sp.cu_group + blockIdx.z + 1), 0), sp.B);
+    const int seq1 = min(seq_end, seq0 + sp.max_group);      // (the launch has row blocks for max_group sequences)
+    // what the merge finds for rows r0 .. r1 - 1 of the stack that begins at sequence s0: no keys, weight 0
+    auto leave_empty = [&](int s0, int r0, int r1) {
+        const int lane = threadIdx.x & 31;
+        for (int r = r0 + (threadIdx.x >> 5); r < r1; r += kShThreads / 32) {
+            const int s = r / p.G;
+            const size_t ps = ((size_t)(s0 + s) * p.Hq + (size_t)head * p.G + (r - s * p.G)) * p.n_slots + blockIdx.x;
+            reinterpret_cast<float4 *>(p.part_o + ps * kHeadDim)[lane] = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (lane == 0) *reinterpret_cast<float2 *>(p.part_ml + ps * 2) = make_float2(-INFINITY, 0.f);
+        }
+    };
+    if (m0 == 0 && !one) {
+        // sequences beyond max_group of their group, and those of no group: the merge must not find what an earlier call left
+        leave_empty(seq1, 0, (seq_end - seq1) * p.G);
+        if (blockIdx.z == 0) leave_empty(0, 0, seq0 * p.G);
+        if (blockIdx.z == gridDim.z - 1) leave_empty(max(seq_end, seq0), 0, (sp.B - max(seq_end, seq0)) * p.G);
+    }
     const int R = (seq1 - seq0) * p.G;                       // stacked rows of the group and kv head
     if (m0 >= R) return;
     const int rows = min(kShRows, R - m0);
@@ -631,14 +649,7 @@ slim_decode_prefix_kernel(const __grid_constant__ CUtensorMap codes_map, const _
     const long long units = (tiles + unit - 1) / unit;
     const int j0 = unit * (int)(units * split / p.slot0), T = unit * (int)(units * (split + 1) / p.slot0) - j0;
     if (T <= 0) {
-        // a part without keys: weight 0 in the merge
-        for (int r = threadIdx.x >> 5; r < rows; r += kShThreads / 32) {
-            const int s = (m0 + r) / p.G;
-            const size_t ps = ((size_t)(seq0 + s) * p.Hq + (size_t)head * p.G + (m0 + r - s * p.G)) * p.n_slots + split;
-            const int lane = threadIdx.x & 31;
-            reinterpret_cast<float4 *>(p.part_o + ps * kHeadDim)[lane] = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (lane == 0) *reinterpret_cast<float2 *>(p.part_ml + ps * 2) = make_float2(-INFINITY, 0.f);
-        }
+        leave_empty(seq0, m0, m0 + rows);   // a part without keys
         return;
     }
     if (by_rows) prefix_block<true>(codes_map, sp, smem, seq0, seq1, head, m0, rows, j0, T, tiles);
@@ -724,6 +735,7 @@ int launch_decode_shared(const slim_cache_t *c, const void *q, const void *k_new
     sp.d = p;
     sp.cu_group = cu_group;
     sp.B = B;
+    sp.max_group = max_group;
     CUtensorMap map;
     int rc = codes_tensor_map(c, kShKeys, &map);
     if (rc != SLIM_OK) return rc;

@@ -73,7 +73,7 @@ __device__ __forceinline__ void merge_row_by_warp(const float *part_o, const flo
     float2 v = (lane < nc) ? __ldcg(ml + lane) : make_float2(-INFINITY, 0.f);
     if (lane >= nc) v = make_float2(-INFINITY, 0.f);
     const float M = warp_max(v.x);
-    const float w = (lane < nc) ? exp2f(v.x - M) : 0.f;
+    const float w = (v.x != -INFINITY) ? exp2f(v.x - M) : 0.f;   // (slots without keys: weight 0, also where no slot has any)
     const float l = warp_sum(v.y * w);
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
     for (int c0 = 0; c0 < nc; c0 += kMergeWarpBatch) {

@@ -127,3 +127,48 @@ def test_decode_shared_tails_beyond_their_bound_are_cut(append):
     for b, x in enumerate(lens):
         same = torch.equal(cache.codes_view()[cache.block_table[b, 3:].long()], before.view_as(cache.codes_view())[cache.block_table[b, 3:].long()])
         assert same == (not append or x > pre + 256)
+
+
+@pytest.mark.parametrize("hq,hkv,pre_pages,tail", [
+    (16, 2, 4, 300),        # partials merged by a warp per row
+    (1, 1, 2, 1),
+    (4, 2, 4, 40 * 256),    # by a block per row
+    (2, 2, 2, 300 * 256),   # by the general kernel
+])
+def test_decode_shared_group_beyond_max_group_attends_its_tails(hq, hkv, pre_pages, tail):
+    """More sequences in a group than max_group, and sequences in no group: no prefix for them, and nothing that the workspace
+    held before; the others as ever."""
+    slim = _slim()
+    n, most, pre = 5, 3, pre_pages * PAGE
+    B = 3 * n
+    mp = pre_pages + (tail + PAGE - 1) // PAGE
+    table = torch.arange(pre_pages + mp, dtype=torch.int32)
+    # (long tails may lie in the same pages: nothing is appended)
+    table = torch.cat([table[:pre_pages], table[pre_pages:pre_pages + mp - pre_pages]]).repeat(B, 1)
+    cache = slim.SlimCache(B, hkv, mp, block_table=table, num_pages=pre_pages + mp)
+    fill(cache, pre_pages)
+    q = torch.randn((B, hq, D), generator=gen(hq)).to(torch.bfloat16).cuda()
+    lens = [pre + (0, 1, 130, tail, max(1, tail - 1))[b % 5] for b in range(B)]
+    lens = [min(x, pre + tail) for x in lens]
+    cu = i32([2, 2 + n, 2 * n, 2 * n + 3, B - 2, B - 2, B - 2])            # five groups of at most max_group, one of five; the first and last two sequences in none
+    groups = 6
+    outs = []
+    for junk in (0xFF, 0x41):                               # NaN, and a large number
+        out = torch.full_like(q, 5.0)
+        ws = slim.shared_workspace(B, hq, hkv, groups, most, pre, tail)
+        ws[slim.WORKSPACE_HEADER_BYTES:] = junk
+        slim.slim_attn_decode_shared(cache, q, out, cu, i32([pre] * B), i32(lens), groups, B, most, pre, tail, hq, D ** -0.5, ws)
+        torch.cuda.synchronize()
+        assert slim.slim_read_status(ws) == slim.SLIM_OK
+        outs.append(out)
+    assert torch.equal(*outs)
+    alone = {0, 1, B - 2, B - 1, 2 + most, 2 + most + 1}    # no group, or beyond the first group's three
+    want, _, slack = attend(cache, q, lens, D ** -0.5)
+    behind = slim.SlimCache(B, hkv, mp - pre_pages, block_table=table[:, pre_pages:], num_pages=cache.num_pages)
+    behind.codes, behind.scales = cache.codes, cache.scales
+    own, _, own_slack = attend(behind, q, [x - pre for x in lens], D ** -0.5)
+    for b in alone:
+        want[b], slack[b] = own[b], own_slack[b]
+        if lens[b] == pre:
+            assert (outs[0][b] == 0).all()
+    out_close(outs[0], want, slack, "groups")
