@@ -39,6 +39,16 @@ __host__ __device__ inline size_t scale_block_offset(int page, int head, int kv,
 __device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;\n" ::: "memory"); }
 __device__ __forceinline__ void pdl_launch_dependents() { asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory"); }
 
+// What a kernel that must not wait for the one before it goes by: a thread of that kernel raises the flag behind its own
+// pdl_wait(), and whoever sees the flag raised also sees what was written before that wait returned.
+__device__ __forceinline__ void flag_raise(int *flag) { asm volatile("st.release.gpu.global.b32 [%0], 1;\n" ::"l"(flag) : "memory"); }
+__device__ __forceinline__ bool flag_raised(const int *flag)
+{
+    int v;
+    asm volatile("ld.acquire.gpu.global.b32 %0, [%1];\n" : "=r"(v) : "l"(flag) : "memory");
+    return v != 0;
+}
+
 template <typename... KArgs, typename... Args>
 inline cudaError_t launch_pdl(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t stream, Args... args)
 {

@@ -35,6 +35,7 @@ slim_decode_merge_kernel(const float *__restrict__ part_o, const float *__restri
     const int row = blockIdx.x;            // b * Hq + h
     const int tid = threadIdx.x, d = tid & (kHeadDim - 1), g = tid >> 7;
     pdl_wait();   // the split pass before this kernel must have finished writing the partials
+    rows.done(row == 0 && tid == 0);
     const int nc = rows.partials(row / Hq, rows.length(row / Hq));
     const float2 *ml = reinterpret_cast<const float2 *>(part_ml) + (size_t)row * n_slots;
     const float *po = part_o + (size_t)row * n_slots * kHeadDim;
@@ -112,13 +113,10 @@ slim_decode_merge_warp_kernel(const float *__restrict__ part_o, const float *__r
                               int B, int Hq, int n_slots)
 {
     const int row = blockIdx.x * kMergeWarpsPerBlock + (threadIdx.x >> 5);   // b * Hq + h
-    // Behind a shared prefix the lengths are read ahead of the wait (0.3 us of a step): this kernel starts only after every
-    // block of the prefix kernel has seen the end of everything before it in the stream.
-    int nc = 0;
-    if (Rows::kShared && row < B * Hq) nc = rows.partials(row / Hq, rows.length(row / Hq));
     pdl_wait();   // the split pass before this kernel must have finished writing the partials
+    rows.done(row == 0 && (threadIdx.x & 31) == 0);
     if (row >= B * Hq) return;
-    if (!Rows::kShared) nc = rows.partials(row / Hq, rows.length(row / Hq));
+    const int nc = rows.partials(row / Hq, rows.length(row / Hq));
     merge_row_by_warp(part_o, part_ml, nc, out, raw, row, n_slots, threadIdx.x & 31);
 }
 
@@ -136,6 +134,7 @@ slim_decode_merge_block_kernel(const float *__restrict__ part_o, const float *__
     const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
     const int row = blockIdx.x;   // b * Hq + h
     pdl_wait();   // the split pass before this kernel must have finished writing the partials
+    rows.done(row == 0 && threadIdx.x == 0);
     const int len = rows.length(row / Hq);
     const int c_base = w * kMergeWarpBatch;
     const float2 *ml = reinterpret_cast<const float2 *>(part_ml) + (size_t)row * n_slots;
@@ -233,6 +232,7 @@ DecodeParams make_decode_params(const slim_cache_t *c, const void *q, const int3
     p.share_stride = 0;
     p.shared_len = nullptr;
     p.max_shared_pages = 0;
+    p.begun = nullptr;
     p.slot0 = 0;
     p.max_blocks = 0;
     return p;
@@ -310,7 +310,7 @@ static int launch_merge(const DecodeParams &p, const Rows &r, int B, void *out, 
 int launch_merge_rows(const DecodeParams &p, int B, void *out, float *raw, cudaStream_t stream)
 {
     const int cap = merge_cap_tokens(p);
-    if (p.shared_len != nullptr) return launch_merge(p, SharedRows{p.kv_len, p.shared_len, p.slot0, p.max_pages_per_seq, p.max_shared_pages, cap}, B, out, raw, stream);
+    if (p.shared_len != nullptr) return launch_merge(p, SharedRows{p.kv_len, p.shared_len, p.begun, p.slot0, p.max_pages_per_seq, p.max_shared_pages, cap}, B, out, raw, stream);
     return launch_merge(p, PlainRows{p.kv_len, cap}, B, out, raw, stream);
 }
 

@@ -38,6 +38,7 @@ struct DecodeParams : SplitParams {
     // the tail's that the prefix kernel fills
     const int32_t *shared_len;
     int max_shared_pages;   // the launch's bound on the prefix, never beyond the page table
+    int *begun;             // in the workspace's header: raised once everything before the prefix kernel is visible, lowered by the merge
     int slot0;
     int max_blocks;   // of the split pass (0: one per SM)
 };
@@ -53,9 +54,9 @@ __device__ __forceinline__ int decode_shared_tokens(const DecodeParams &p, int b
     return shared_tokens(p.shared_len, p.max_shared_pages, b);
 }
 
-// Workspace header in front of the partials: the status word (16 bytes), then the counters of the in-kernel
-// merge.  The header has one size for every shape, so a workspace zeroed once stays valid when the shapes of the
-// calls that use it change.
+// Workspace header in front of the partials: the status word (16 bytes; the second int of them is the shared decode's
+// flag), then the counters of the in-kernel merge.  The header has one size for every shape, so a workspace zeroed once
+// stays valid when the shapes of the calls that use it change.
 constexpr size_t kDecodeStatusBytes = 16;
 constexpr int kDecodeCounterRows = 16384;   // (sequence, kv head) pairs the in-kernel merge can count
 constexpr size_t kDecodeHeaderBytes = kDecodeStatusBytes + (size_t)kDecodeCounterRows * sizeof(int);

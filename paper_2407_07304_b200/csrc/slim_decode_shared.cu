@@ -613,8 +613,10 @@ slim_decode_prefix_kernel(const __grid_constant__ CUtensorMap codes_map, const _
 {
     extern __shared__ __align__(1024) unsigned char smem[];
     // The tail's blocks may start on the SMs that this kernel does not use once all of its blocks are here, behind the
-    // wait: so the tail need not wait for what came before them in the stream.
+    // wait.  They must not wait for this kernel's end, so the flag tells them that what came before it in the stream has
+    // ended, and makes it visible to them.
     pdl_wait();
+    if (threadIdx.x == kShThreads - 32 && blockIdx.x + blockIdx.y + blockIdx.z == 0) flag_raise(sp.d.begun);   // (a warp with nothing else to do yet)
     pdl_launch_dependents();
     const DecodeParams &p = sp.d;
     const int head = (int)blockIdx.y % p.Hkv, m0 = (int)blockIdx.y / p.Hkv * kShRows;
@@ -727,6 +729,7 @@ int launch_decode_shared(const slim_cache_t *c, const void *q, const void *k_new
     p.v_new = static_cast<const __nv_bfloat16 *>(v_new);
     p.shared_len = shared_len;
     p.max_shared_pages = max_shared / kPageTokens;
+    p.begun = p.status + 1;
     p.slot0 = s.splits;
     p.n_slots = s.slots;
     p.max_blocks = s.tail_blocks;

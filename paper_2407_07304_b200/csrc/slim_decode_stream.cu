@@ -139,6 +139,22 @@ constexpr int kStTail = 2;     // only the tokens behind a shared prefix (slim_a
 template <int kWhat>
 using StParams = std::conditional_t<kWhat == kStPlain, SplitParams, DecodeParams>;
 
+// Waits until what earlier kernels of the stream wrote is visible.  The tail launch follows the prefix kernel, which writes
+// nothing that is read here and ends late: the flag that it raises behind its own wait stands for everything before it.  (It
+// is raised before the prefix kernel lets this one start; should it not be seen, the prefix kernel's end will do.)
+template <int kWhat>
+__device__ __forceinline__ void st_wait_earlier(const StParams<kWhat> &p)
+{
+    if constexpr (kWhat == kStTail) {
+        bool seen = false;
+        for (int i = 0; i < 64 && !seen; ++i) seen = __all_sync(0xffffffffu, flag_raised(p.begun));
+        if (!seen) pdl_wait();
+        asm volatile("fence.proxy.async.global;\n" ::: "memory");   // (the copies read it too)
+    } else {
+        pdl_wait();
+    }
+}
+
 // The cached tokens of a sequence that this launch attends over start at position st_start: 0, or the end of the
 // prefix that the sequence shares (whole pages).
 template <int kWhat>
@@ -494,9 +510,8 @@ slim_decode_stream_kernel(const __grid_constant__ CUtensorMap map_tile, const __
     if (warp == kPW) tc::tmem_alloc(smem_u32(tmem_slot), L::kTmemCols);
     if (warp == kPW || warp == kPW + 1) {
         // Up to here the block may run beside the kernel before it in the stream (the same step's
-        // slim_kv_append); from here on it reads what earlier kernels may have written.  (The tail launch follows the
-        // prefix kernel, which writes nothing that is read here and has itself waited for everything before it.)
-        if (kWhat != kStTail) pdl_wait();
+        // slim_kv_append); from here on it reads what earlier kernels may have written.
+        st_wait_earlier<kWhat>(p);
         // ---- this block's contiguous range of chunks, in (sequence, kv head, chunk) order.  The work is cut
         //      by 128-token tiles (what a chunk costs) and the cut points are moved up to chunk starts.  The first
         //      producer warp finds where the range starts, the second where it ends, at the same time.
@@ -719,7 +734,7 @@ slim_decode_stream_kernel(const __grid_constant__ CUtensorMap map_tile, const __
             //      last chunk; those pairs are dealt to the block's consumer warps in turn, from the last warp down (the
             //      first group takes the block's first chunk).  A sequence of one token has no chunk: its pairs are
             //      dealt to the blocks by index.
-            if (kWhat != kStTail) pdl_wait();
+            st_wait_earlier<kWhat>(p);
             if (cnt > 0) {
                 int b = range[1], head = range[2];
                 int L = range[5] + 1;   // the chunks cover all of the sequence's tokens but the last

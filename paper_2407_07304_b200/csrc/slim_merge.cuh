@@ -20,7 +20,7 @@ __device__ __forceinline__ int merge_row_partials(int len, int cap_tokens)
 struct PlainRows {
     const int32_t *kv_len;
     int cap_tokens;
-    static constexpr bool kShared = false;
+    __device__ __forceinline__ void done(bool) const {}
     __device__ __forceinline__ int length(int b) const { return __ldg(kv_len + b); }
     __device__ __forceinline__ int partials(int b, int len) const { return merge_row_partials(len, cap_tokens); }
 };
@@ -29,8 +29,13 @@ struct PlainRows {
 // tail's partials; cap_tokens bounds the tail.
 struct SharedRows {
     const int32_t *kv_len, *shared_len;
+    int *begun;
     int slot0, max_pages, max_shared_pages, cap_tokens;
-    static constexpr bool kShared = true;
+    // (both kernels before this one have ended: the workspace's header goes back to zero)
+    __device__ __forceinline__ void done(bool one_thread) const
+    {
+        if (one_thread) *begun = 0;
+    }
     __device__ __forceinline__ int length(int b) const { return __ldg(kv_len + b); }
     __device__ __forceinline__ int partials(int b, int len) const
     {
