@@ -430,7 +430,9 @@ int slim_norm_rope_append(const slim_cache_t *cache, const slim_norm_rope_t *nr,
 /*
  * Decode attention of a batch in which groups of sequences share a prefix: the page table rows of a group's sequences
  * begin with the same pages.  The result is that of slim_attn_decode (with k_new / v_new, both or neither, that of
- * slim_decode_step), but the prefix's keys and values are read and multiplied once for the whole group.
+ * slim_decode_step), but the prefix's keys and values are read and multiplied once for the whole group.  Scores are as exact
+ * as there; the prefix's probabilities and values are rounded to fp16 (2^-10 of each of a result's terms at most, where
+ * slim_attn_decode holds them to 2^-16).
  *
  *   cu_group   device int32 [n_groups + 1]: group g is the sequences cu_group[g] .. cu_group[g + 1] - 1; the groups cover
  *              all B sequences (a sequence that shares nothing may be a group of its own), so n_groups * max_group >= B

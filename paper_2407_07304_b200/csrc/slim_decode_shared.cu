@@ -11,10 +11,11 @@
 // Prefix kernel: a block owns up to 256 stacked rows of one (group, kv head) and one contiguous part of the prefix's 128-key
 // tiles; the number of parts fills the chip once.  The structure is that of the prefill kernel: TMA-staged INT8
 // tiles, converted in registers into fp16 operands, scores and outputs on tcgen05 with accumulators in tensor memory, thread = row in the softmax, rescaling only when the maximum grows by more than 2^8.
-// K's operand is code * scale / 2^e rounded once: the fp16 scale goes in two parts.  (With the scale itself rounded to fp16
-// all 128 terms of a key's scores are off by up to 2^-11 in the same direction: half of the result's whole error.  Exact
-// codes as K's operand and the key's scale in the softmax cost 0.4 us per key tile of 256 rows.)  V's scale is rounded to
-// fp16: its errors are the tokens' own and average out over them.
+// K's operand is the codes, exact in fp16, and so are the queries but for elements below 2^-17 of their row's largest; a key's
+// scale is multiplied in the softmax.  So a score is as exact as fp32 sums are, whatever its size: rounded to fp16, 128 terms
+// of a score of 350 move it by up to 0.1, and its weight by a tenth (with 2.6 us per key tile of 256 rows instead of 3.0).
+// P and V are rounded to fp16 (V's scale, then its product with the code): each of a result's terms is off by 2^-10 at most,
+// independently of one another, beside the 2^-8 of the result's own rounding to bf16.
 // With more than 128 rows the block's two softmax groups take 128 rows each and every key tile serves both; with at
 // most 128 rows both groups work on the same rows and take the key tiles in turn, so that the scores of one tile are
 // formed while the softmax of the other runs, and their two partials are merged through shared memory at the end.
@@ -48,14 +49,19 @@ constexpr uint32_t kQ = 0;                      // two fp16 Q tiles; a tile = tw
 constexpr uint32_t kKf = 65536;                 // two fp16 K tiles (even / odd key tiles)
 constexpr uint32_t kVf = kKf + 2 * 32768;       // two fp16 V tiles
 constexpr uint32_t kRaw = kVf + 2 * 32768;      // raw INT8 tiles: stage 0 K, stage 1 V
-constexpr uint32_t kRawScales = kRaw + 2 * 16384;
-constexpr uint32_t kMisc = kRawScales + 2 * 512;
-// where the softmax groups take the key tiles in turn: the rows' scales for group 1, and at the end, over the raw tiles,
-// group 1's (m, l)
-constexpr uint32_t kRowScale = kMisc + 512;
+constexpr uint32_t kRawScales = kRaw + 2 * 16384;   // of the raw V tile
+// The keys' scales stay until the softmax of their tile has read them, and the loader is ahead of it: with 128 rows per
+// group, when tile j is requested the products of tile j - 3 are done, which followed both groups' softmax of tile j - 4;
+// with the tiles taken in turn, those of tiles j - 3 and j - 4, which followed the softmax of tiles j - 5 and j - 6.
+constexpr uint32_t kKeyScales = kRawScales + 512;   // four key tiles
+constexpr uint32_t kMisc = kKeyScales + 4 * 512;
+// where the softmax groups take the key tiles in turn, the second Q tile is free: the keys' scales of eight key tiles, the
+// rows' scales for group 1; and at the end, over the raw tiles, group 1's (m, l)
+constexpr uint32_t kKeyScalesInTurn = kQ + 32768;
+constexpr uint32_t kRowScale = kKeyScalesInTurn + 8 * 512;
 constexpr uint32_t kMl = kRaw;
-constexpr uint32_t kBytes = kRowScale + 512;
-// kMisc: floats by key tile mod 4: [0,4) kexp, [4,8) log2 vexp, [8,12) 1 / vexp; byte 64: tensor-memory address;
+constexpr uint32_t kBytes = kMisc + 512;
+// kMisc: floats by key tile mod 4: [0,4) log2 vexp, [4,8) 1 / vexp; byte 64: tensor-memory address;
 //        byte 72: failure flag; byte 76: tokens of the prefix that any sequence of the group has; byte 128..: mbarriers
 enum Bar { RAW_FULL = 0, RAW_EMPTY = 2, KF_FULL = 4, KF_EMPTY = 6, VF_FULL = 8, VF_EMPTY = 10,
            S_FULL = 12, P_FULL = 14, O_DONE = 16, Q_FULL = 18, VEXP_FULL = 20, NUM_BARS = 24 };
@@ -81,18 +87,17 @@ __device__ __forceinline__ float sh_max3(float a, float b, float c)
     asm("max.f32 %0, %1, %2, %3;\n" : "=f"(m) : "f"(a), "f"(b), "f"(c));
     return m;
 }
-template <bool kLow>
-__device__ __forceinline__ uint32_t sh_code_pair(uint32_t halves, uint32_t factor, uint32_t low)
+// halves: two fp16 numbers 1152 + code -> the codes, exactly, or code * factor
+__device__ __forceinline__ uint32_t sh_code_pair(uint32_t halves)
 {
-    // halves: two fp16 numbers 1152 + code; code * (factor + low), rounded once, or code * factor
-    uint32_t d, r;
+    uint32_t d;
     asm("sub.rn.f16x2 %0, %1, %2;\n" : "=r"(d) : "r"(halves), "r"(0x64806480u));
-    if (kLow) {
-        asm("mul.rn.f16x2 %0, %1, %2;\n" : "=r"(r) : "r"(d), "r"(low));
-        asm("fma.rn.f16x2 %0, %1, %2, %3;\n" : "=r"(r) : "r"(d), "r"(factor), "r"(r));
-    } else {
-        asm("mul.rn.f16x2 %0, %1, %2;\n" : "=r"(r) : "r"(d), "r"(factor));
-    }
+    return d;
+}
+__device__ __forceinline__ uint32_t sh_value_pair(uint32_t halves, uint32_t factor)
+{
+    uint32_t r;
+    asm("mul.rn.f16x2 %0, %1, %2;\n" : "=r"(r) : "r"(sh_code_pair(halves)), "r"(factor));
     return r;
 }
 
@@ -120,6 +125,7 @@ __device__ __forceinline__ void prefix_block(const CUtensorMap &codes_map, const
     int *known = reinterpret_cast<int *>(smem + shl::kMisc + 76);
     const uint32_t bar0 = sbase + shl::kMisc + 128;
     auto bar = [&](int which, int idx) { return bar0 + 8u * (uint32_t)(which + idx); };
+    auto key_scales = [&](int j) { return by_rows ? shl::kKeyScales + (uint32_t)(j & 3) * 512u : shl::kKeyScalesInTurn + (uint32_t)(j & 7) * 512u; };
 
     // ---- the loader asks for the first raw tiles before the block's set-up is complete
     int raw_issued = 0;
@@ -131,7 +137,7 @@ __device__ __forceinline__ void prefix_block(const CUtensorMap &codes_map, const
         const uint32_t full = bar(shl::RAW_FULL, kv);
         tc::mbar_arrive_expect_tx(full, 16384 + 512);
         tc::tma_load_2d(sbase + shl::kRaw + kv * 16384, &codes_map, 0, ((page * p.Hkv + head) * 2 + kv) * kPageTokens, full);
-        tc::bulk_load(sbase + shl::kRawScales + kv * 512, p.scales + scale_block_offset(page, head, kv, p.Hkv), 512, full);
+        tc::bulk_load(sbase + (kv ? shl::kRawScales : key_scales(j)), p.scales + scale_block_offset(page, head, kv, p.Hkv), 512, full);
         if (kv == 1 && j + 1 < T) {
             // the next key tile's page id, and its two tiles on their way into the L2
             if (by_rows || j0 + j + 1 < tiles) page_next = __ldg(bt + j + 1);
@@ -272,6 +278,7 @@ __device__ __forceinline__ void prefix_block(const CUtensorMap &codes_map, const
             limit = min(limit, min(__ldg(p.kv_len + s), decode_shared_tokens(p, s)));
         }
         const bool warp_rows = my_row - lane < rows;
+        const float c = fmaxf(rs, 1e-37f);                         // (> 0)
         float m_run = -INFINITY, l_run = 0.f;
         for (int n = 0; n < steps; ++n) {
             const int j = by_rows ? n : 2 * n + t;                 // key tile of the block's part
@@ -285,9 +292,8 @@ __device__ __forceinline__ void prefix_block(const CUtensorMap &codes_map, const
                 continue;
             }
             wait(bar(shl::VEXP_FULL, j & 3), (uint32_t)(j >> 2) & 1u);
-            const float c = fmaxf(rs * misc_f[j & 3], 1e-37f);     // row scale * kexp of this key tile (> 0)
-            const float F = misc_f[4 + (j & 3)];                   // log2 vexp
-            const float vinv = misc_f[8 + (j & 3)];                // 1 / vexp
+            const float F = misc_f[j & 3];                         // log2 vexp
+            const float vinv = misc_f[4 + (j & 3)];                // 1 / vexp
             const int key0 = (j0 + j) * kShKeys;
             uint32_t v[128];
             {
@@ -300,6 +306,15 @@ __device__ __forceinline__ void prefix_block(const CUtensorMap &codes_map, const
                 tc::tmem_ld32(tS + 64, v2);
                 tc::tmem_ld32(tS + 96, v3);
                 tc::tmem_ld_wait();
+            }
+            const float4 *ks = reinterpret_cast<const float4 *>(smem + key_scales(j));
+#pragma unroll
+            for (int i = 0; i < 128; i += 4) {
+                const float4 k4 = ks[i / 4];
+                float x0, x1, x2, x3;
+                ap_unpack(ap_mul2(ap_pack(__uint_as_float(v[i]), __uint_as_float(v[i + 1])), ap_pack(k4.x, k4.y)), x0, x1);
+                ap_unpack(ap_mul2(ap_pack(__uint_as_float(v[i + 2]), __uint_as_float(v[i + 3])), ap_pack(k4.z, k4.w)), x2, x3);
+                v[i] = __float_as_uint(x0), v[i + 1] = __float_as_uint(x1), v[i + 2] = __float_as_uint(x2), v[i + 3] = __float_as_uint(x3);
             }
             if (__any_sync(0xffffffffu, key0 + kShKeys > limit)) {
 #pragma unroll
@@ -438,27 +453,25 @@ __device__ __forceinline__ void prefix_block(const CUtensorMap &codes_map, const
             const int buf = j & 1;
             wait(bar(shl::RAW_FULL, kv), (uint32_t)j & 1u);
             const unsigned char *raw = smem + shl::kRaw + kv * 16384;
-            const float *scales = reinterpret_cast<const float *>(smem + shl::kRawScales + kv * 512);
+            const float *scales = reinterpret_cast<const float *>(smem + shl::kRawScales);
             const int n_valid = min(kShKeys, kept - j * kShKeys);
-            float wm = 0.f;
-            {
+            float rex = 0.f;
+            if (is_k) {
+                wait(bar(shl::KF_EMPTY, buf), ((uint32_t)(j >> 1) & 1u) ^ 1u);
+            } else {
+                float wm = 0.f;
                 const float4 s4 = *reinterpret_cast<const float4 *>(scales + 4 * lane);
                 const float sv[4] = {s4.x, s4.y, s4.z, s4.w};
 #pragma unroll
                 for (int k = 0; k < 4; ++k)
                     if (4 * lane + k < n_valid) wm = fmaxf(wm, sv[k]);
                 wm = warp_max(wm);
-            }
-            const float ex = (wm > 0.f) ? pow2_floor(wm) : 1.f;
-            const float rex = pow2_recip(ex);
-            if (is_k) {
-                if (announces) misc_f[j & 3] = ex;
-                wait(bar(shl::KF_EMPTY, buf), ((uint32_t)(j >> 1) & 1u) ^ 1u);
-            } else {
+                const float ex = (wm > 0.f) ? pow2_floor(wm) : 1.f;
+                rex = pow2_recip(ex);
                 if (announces) {
-                    misc_f[4 + (j & 3)] = (float)((int)(__float_as_uint(ex) >> 23) - 127);
-                    misc_f[8 + (j & 3)] = rex;
-                    tc::mbar_arrive(bar(shl::VEXP_FULL, j & 3));
+                    misc_f[j & 3] = (float)((int)(__float_as_uint(ex) >> 23) - 127);
+                    misc_f[4 + (j & 3)] = rex;
+                    tc::mbar_arrive(bar(shl::VEXP_FULL, j & 3));   // (the keys' scales, too, have been seen to arrive)
                 }
                 wait(bar(shl::VF_EMPTY, buf), ((uint32_t)(j >> 1) & 1u) ^ 1u);
             }
@@ -467,11 +480,11 @@ __device__ __forceinline__ void prefix_block(const CUtensorMap &codes_map, const
             for (int q = 0; q < 2; ++q) {
                 if (q >= n_rows) break;
                 const int r = r0 + 64 * q;
-                // scale / 2^e in [0, 2) as the sum of two fp16 numbers
-                const float f = ((r < n_valid) ? scales[r] : 0.f) * rex;
-                const uint32_t fac2 = pack_half2(f, f);
-                const float f_low = f - __half2float(__low2half(*reinterpret_cast<const __half2 *>(&fac2)));
-                const uint32_t low2 = pack_half2(f_low, f_low);
+                uint32_t fac2 = 0;   // a value's scale / 2^e in [0, 2)
+                if (!is_k) {
+                    const float f = ((r < n_valid) ? scales[r] : 0.f) * rex;
+                    fac2 = pack_half2(f, f);
+                }
                 unsigned char *dstb = dst_tile + r * 128;
                 for (int c = c_first; c < c_last; ++c) {
                     const uint4 w4 = *reinterpret_cast<const uint4 *>(raw + r * 128 + ((c ^ (r & 7)) << 4));
@@ -480,8 +493,9 @@ __device__ __forceinline__ void prefix_block(const CUtensorMap &codes_map, const
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
                         const uint32_t x = w[k] ^ 0x80808080u;   // byte code ^ 0x80 under 0x64 is the fp16 number 1152 + code
-                        hh[2 * k] = sh_code_pair<is_k>(__byte_perm(x, 0x64646464u, 0x4140), fac2, low2);
-                        hh[2 * k + 1] = sh_code_pair<is_k>(__byte_perm(x, 0x64646464u, 0x4342), fac2, low2);
+                        const uint32_t h0 = __byte_perm(x, 0x64646464u, 0x4140), h1 = __byte_perm(x, 0x64646464u, 0x4342);
+                        hh[2 * k] = is_k ? sh_code_pair(h0) : sh_value_pair(h0, fac2);
+                        hh[2 * k + 1] = is_k ? sh_code_pair(h1) : sh_value_pair(h1, fac2);
                     }
                     const uint32_t hf = (uint32_t)(c >> 2) * 16384u;
                     const int oc = 2 * (c & 3);
@@ -667,7 +681,7 @@ constexpr int kShSms = 148;
 
 // How the work is divided over the SMs.  Prefix and tail blocks take an SM each and run side by side, so the number of
 // parts of the prefix is chosen for the earliest end of both, by what their blocks were measured to take (us):
-//   prefix block   10 + 2.6 per key tile of 256 rows; 13 + 1.4 where the softmax groups take the tiles in turn
+//   prefix block   10 + 3.0 per key tile of 256 rows; 13 + 1.4 where the softmax groups take the tiles in turn
 //   tail           6 + (2 per 256-token chunk, 4 with more than eight query heads per kv head) / blocks
 // The tails' lengths are device data: half of max_tail is taken for their mean.  (Prefixes of 2048 / 8192 / 16384 tokens
 // for 16 / 32 / 64 sequences: 38.6 / 47.9 / 67.1 us with the prefix on all SMs and the tail behind it, 30.9 / 34.8 / 53.7
@@ -688,7 +702,7 @@ static SharedShape shared_shape(int B, int Hq, int Hkv, int n_groups, int max_gr
     for (int n = 1; n <= units && n * per_part < kShSms; ++n) {
         const int tail_blocks = kShSms - (int)(n * per_part);
         const int part = unit * ((units + n - 1) / n);
-        const double prefix = by_rows ? 10.0 + 2.6 * part : 13.0 + 1.4 * part;
+        const double prefix = by_rows ? 10.0 + 3.0 * part : 13.0 + 1.4 * part;
         const double tail = max_tail > 0 ? 6.0 + tail_work / tail_blocks : 0.0;
         const double end = prefix > tail ? prefix : tail;
         if (end < best) best = end, s.splits = n, s.tail_blocks = tail_blocks;
