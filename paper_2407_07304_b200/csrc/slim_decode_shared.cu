@@ -682,7 +682,7 @@ constexpr int kShSms = 148;
 // How the work is divided over the SMs.  Prefix and tail blocks take an SM each and run side by side, so the number of
 // parts of the prefix is chosen for the earliest end of both, by what their blocks were measured to take (us):
 //   prefix block   10 + 3.0 per key tile of 256 rows; 13 + 1.4 where the softmax groups take the tiles in turn
-//   tail           6 + (2 per 256-token chunk, 4 with more than eight query heads per kv head) / blocks
+//   tail           7 + (2 per 256-token chunk, 4 with more than eight query heads per kv head) / blocks
 // The tails' lengths are device data: half of max_tail is taken for their mean.  (Prefixes of 2048 / 8192 / 16384 tokens
 // for 16 / 32 / 64 sequences: 38.6 / 47.9 / 67.1 us with the prefix on all SMs and the tail behind it, 30.9 / 34.8 / 53.7
 // side by side.)
@@ -703,7 +703,7 @@ static SharedShape shared_shape(int B, int Hq, int Hkv, int n_groups, int max_gr
         const int tail_blocks = kShSms - (int)(n * per_part);
         const int part = unit * ((units + n - 1) / n);
         const double prefix = by_rows ? 10.0 + 3.0 * part : 13.0 + 1.4 * part;
-        const double tail = max_tail > 0 ? 6.0 + tail_work / tail_blocks : 0.0;
+        const double tail = max_tail > 0 ? 7.0 + tail_work / tail_blocks : 0.0;
         const double end = prefix > tail ? prefix : tail;
         if (end < best) best = end, s.splits = n, s.tail_blocks = tail_blocks;
     }
