@@ -630,8 +630,12 @@ slim_decode_prefix_kernel(const __grid_constant__ CUtensorMap codes_map, const _
     // wait.  They must not wait for this kernel's end, so the flag tells them that what came before it in the stream has
     // ended, and makes it visible to them.
     pdl_wait();
-    if (threadIdx.x == kShThreads - 32 && blockIdx.x + blockIdx.y + blockIdx.z == 0) flag_raise(sp.d.begun);   // (a warp with nothing else to do yet)
-    pdl_launch_dependents();
+    if (blockIdx.x + blockIdx.y + blockIdx.z != 0) {
+        pdl_launch_dependents();
+    } else if (threadIdx.x == kShThreads - 32) {   // (a warp with nothing else to do yet; the tail starts behind this block's call, too)
+        flag_raise(sp.d.begun);
+        pdl_launch_dependents();
+    }
     const DecodeParams &p = sp.d;
     const int head = (int)blockIdx.y % p.Hkv, m0 = (int)blockIdx.y / p.Hkv * kShRows;
     // (one group is all the sequences: nothing to look up)

@@ -140,15 +140,13 @@ template <int kWhat>
 using StParams = std::conditional_t<kWhat == kStPlain, SplitParams, DecodeParams>;
 
 // Waits until what earlier kernels of the stream wrote is visible.  The tail launch follows the prefix kernel, which writes
-// nothing that is read here and ends late: the flag that it raises behind its own wait stands for everything before it.  (It
-// is raised before the prefix kernel lets this one start; should it not be seen, the prefix kernel's end will do.)
+// nothing that is read here and ends late: the flag that it raises behind its own wait, before it lets this launch start,
+// stands for everything before it.  Nothing waits for the flag: should it not be seen, the prefix kernel's end will do.
 template <int kWhat>
 __device__ __forceinline__ void st_wait_earlier(const StParams<kWhat> &p)
 {
     if constexpr (kWhat == kStTail) {
-        bool seen = false;
-        for (int i = 0; i < 64 && !seen; ++i) seen = __all_sync(0xffffffffu, flag_raised(p.begun));
-        if (!seen) pdl_wait();
+        if (!__all_sync(0xffffffffu, flag_raised(p.begun))) pdl_wait();
         asm volatile("fence.proxy.async.global;\n" ::: "memory");   // (the copies read it too)
     } else {
         pdl_wait();
