@@ -315,7 +315,6 @@ template <bool kAppend>
 static int launch_mode(const NormRopeParams &p, bool interleaved, cudaStream_t stream)
 {
     const long long rows = (long long)p.n_tokens * p.rows_per_token;
-    if (rows > 0x7FFFFF00LL) return SLIM_ERR_UNSUPPORTED;   // the kernel indexes rows with 32-bit integers
     const unsigned blocks = (unsigned)((rows + kNrRows - 1) / kNrRows);
     const size_t smem = (size_t)p.span * (2 * p.half * sizeof(float) + sizeof(int2));   // 17 KB at most (one row per token)
     if (interleaved)
@@ -332,6 +331,9 @@ int launch_norm_rope(const slim_cache_t *c, const slim_norm_rope_t *nr, const vo
                      int64_t k_stride, void *k_out, const void *v, int64_t v_stride, const int32_t *positions, const int32_t *cu_new,
                      const int32_t *start_pos, int B, int n_tokens, int Hq, int Hkv, cudaStream_t stream)
 {
+    // (the kernel indexes rows with 32-bit integers)
+    const long long per_token = Hq + (c != nullptr ? 2LL : 1LL) * Hkv;
+    if (per_token > 0x7FFFFF00LL / n_tokens) return SLIM_ERR_UNSUPPORTED;
     NormRopeParams p = {};
     p.src[0] = static_cast<const __nv_bfloat16 *>(q);
     p.src[1] = static_cast<const __nv_bfloat16 *>(k);
@@ -350,7 +352,7 @@ int launch_norm_rope(const slim_cache_t *c, const slim_norm_rope_t *nr, const vo
     p.half = nr->rotary_dim / 2;
     p.n_axes = nr->n_axes;
     p.eps = nr->eps;
-    p.rows_per_token = Hq + (c != nullptr ? 2 : 1) * Hkv;
+    p.rows_per_token = (int)per_token;
     p.span = (kNrRows - 1 + p.rows_per_token - 1) / p.rows_per_token + 1;   // tokens that a block's consecutive rows touch at most
     if (c == nullptr) return launch_mode<false>(p, nr->interleaved != 0, stream);
     p.codes = c->codes;
