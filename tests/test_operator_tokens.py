@@ -49,3 +49,44 @@ def test_decode_shared_scores_with_a_large_common_part(hq, hkv, n, offset):
     moved = 1.4427 * offset * (2.0 ** -16 + 3 * 2.0 ** -24)
     rms_close(ref, want, "decode", 1.25 * (1 + (moved / 1.65e-3) ** 2) ** 0.5)
     rms_close(out, want, "shared", 1.25 * (1 + (moved / 1.65e-3) ** 2) ** 0.5)
+
+
+TOKEN_CASES = [
+    # groups (prefix pages, sequences), hq, hkv, tails per sequence (cycled; negative: shorter than the prefix by that much)
+    ([(1, 1)], 8, 1, [1]), ([(3, 4)], 16, 2, [1, 2, 256, 257]), ([(9, 40)], 16, 1, [3, 515, 128]), ([(12, 3), (0, 2), (5, 7)], 24, 3, [1, 129, 300]),
+    ([(17, 16)], 8, 8, [0, 1, 255]), ([(4, 9)], 16, 2, [-1, -128, -200, -384, -511, 5]), ([(2, 33)], 28, 4, [-255, 1, 128, -129]),
+    ([(25, 5)], 64, 4, [513, 700]), ([(2, 2)] * 9, 32, 32, [3, 140]),
+]
+
+
+@pytest.mark.parametrize("append", [False, True])
+@pytest.mark.parametrize("case", TOKEN_CASES, ids=range(len(TOKEN_CASES)))
+def test_decode_shared_counts_every_token_once(case, append):
+    """Nearly equal scores, so that every token holds about 1 / n of the result: one left out, or counted twice, at the borders of
+    the prefix, its parts, pages and chunks moves the result by several times what the roundings may."""
+    groups, hq, hkv, tails = case
+    slim = _slim()
+    cache, B, cu = shared_setup(hq + len(groups), groups, hq, hkv, max(0, max(tails)) // PAGE + 2)
+    pre = [p * PAGE for p, n in groups for _ in range(n)]
+    lens = [max(1, pre[b] + tails[b % len(tails)]) for b in range(B)]
+    most, max_tail = max(n for _, n in groups), max(max(0, lens[b] - pre[b]) for b in range(B))
+    q = (torch.randn((B, hq, D), generator=gen(B)) * 0.05).to(torch.bfloat16).cuda()
+    out = torch.full_like(q, 5.0)
+    new = {}
+    if append:
+        new = dict(k_new=torch.randn((B, hkv, D), generator=gen(1)).to(torch.bfloat16).cuda(), v_new=torch.randn((B, hkv, D), generator=gen(2)).to(torch.bfloat16).cuda())
+    ws = slim.shared_workspace(B, hq, hkv, len(groups), most, max(pre), max_tail)
+    slim.slim_attn_decode_shared(cache, q, out, i32(cu), i32(pre), i32(lens), len(groups), B, most, max(pre), max_tail, hq, D ** -0.5, ws, **new)
+    torch.cuda.synchronize()
+    assert slim.slim_read_status(ws) == slim.SLIM_OK
+    want, probs, _ = attend(cache, q, lens, D ** -0.5)
+    rms_close(out, want, case)
+    # the check sees a single token: the exact result without it lies outside
+    for b in range(0, B, max(1, B // 6)):
+        best = (want[b].to(torch.bfloat16).double() - want[b]).norm()
+        _, v = rows_of(cache, b, lens[b])
+        for j in {0, 127, 128, 255, 256, pre[b] // 2 - 1, pre[b] // 2, pre[b] - 1, pre[b], pre[b] + 255, pre[b] + 256, lens[b] - 2, lens[b] - 1}:
+            if 0 <= j < lens[b] and lens[b] > 1:
+                p = probs[b][:, j, None]
+                without = (want[b] - p * v[:, j].repeat_interleave(hq // hkv, 0)) / (1 - p)
+                assert (without - want[b]).norm() > 3 * best, (b, j)
