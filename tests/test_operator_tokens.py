@@ -90,3 +90,32 @@ def test_decode_shared_counts_every_token_once(case, append):
                 p = probs[b][:, j, None]
                 without = (want[b] - p * v[:, j].repeat_interleave(hq // hkv, 0)) / (1 - p)
                 assert (without - want[b]).norm() > 3 * best, (b, j)
+
+
+@pytest.mark.parametrize("lens,hq,hkv", [([1], 1, 1), ([2, 1, 257, 256, 300], 6, 3), ([272], 32, 32), ([2049, 1030, 128], 16, 2), ([9000, 33], 16, 1)])
+def test_decode_weights_appends_like_the_other_calls(lens, hq, hkv):
+    """With k_new and v_new: codes and scales those of slim_kv_append on a copy of the cache, the output slim_decode_step's, the
+    weights those of a call without them over the copy."""
+    slim = _slim()
+    B, top = len(lens), max(lens)
+    mp = (top + PAGE - 1) // PAGE
+    table = torch.randperm(B * mp, generator=gen(top)).to(torch.int32).view(B, mp)
+    caches = [slim.SlimCache(B, hkv, mp, block_table=table) for _ in range(3)]
+    for c in caches:
+        fill(c, hq)
+    before = caches[0].codes.clone()
+    g = gen(top + 1)
+    q, kn, vn = (torch.randn((B, h, D), generator=g).to(torch.bfloat16).cuda() for h in (hq, hkv, hkv))
+    kn[0, 0] *= 20                                          # a new key that takes weight
+    out, step, plain = (torch.full_like(q, 5.0) for _ in range(3))
+    w, w_ref = (torch.full((B, hkv, top), -3.0, device="cuda") for _ in range(2))
+    n = i32(lens)
+    slim.slim_attn_decode_weights(caches[0], q, out, None, w, None, n, B, top, hq, D ** -0.5, 1.0, slim.weights_workspace(B, hq, hkv, top), k_new=kn, v_new=vn)
+    slim.slim_decode_step(caches[1], q, kn, vn, step, n, B, top, hq, D ** -0.5, slim.workspace(slim.PHASE_DECODE, B, hq, hkv, 1, top))
+    slim.slim_kv_append(caches[2], kn, vn, i32(list(range(B + 1))), n - 1, B, 1)
+    slim.slim_attn_decode_weights(caches[2], q, plain, None, w_ref, None, n, B, top, hq, D ** -0.5, 1.0, slim.weights_workspace(B, hq, hkv, top))
+    torch.cuda.synchronize()
+    assert not torch.equal(caches[0].codes, before)
+    for c in caches[1:]:
+        assert torch.equal(c.codes, caches[0].codes) and torch.equal(c.scales, caches[0].scales)
+    assert torch.equal(out, step) and torch.equal(out, plain) and torch.equal(w, w_ref)
