@@ -465,7 +465,8 @@ size_t slim_shared_workspace_bytes(int32_t B, int32_t Hq, int32_t Hkv, int32_t n
  *   weight_in, weight_out  device fp32 [B][Hkv][weight_stride], weight_stride >= max_kv; may be the same array; entries
  *              from min(kv_len[b], max_kv) on are neither read nor written
  *   weighed    device int32 [B], or NULL: kv_len[b] - 1
- *   workspace  at least slim_weights_workspace_bytes(...) bytes (the scores lie there between the two kernels); header
+ *   workspace  at least slim_weights_workspace_bytes(...) bytes (every token's share of its chunk's
+ *              denominator lies there between the two kernels); header
  *              as for slim_attn_decode
  */
 int slim_attn_decode_weights(const slim_cache_t *cache, const void *q, const void *k_new, const void *v_new, void *out,

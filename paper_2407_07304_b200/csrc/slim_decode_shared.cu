@@ -23,7 +23,8 @@
 //
 // The tail kernel is launched as a programmatic dependent that does not wait for this one: its blocks run beside the
 // prefix blocks, on the SMs left to them, and only their end waits for the prefix kernel (the merge kernel waits for the
-// tail's).
+// tail's).  What came before this kernel in the stream they see by a flag that it raises behind its own wait: about 1 us of
+// a call, against 8 to 14 us for a tail behind the prefix.
 #include <cuda.h>
 
 #include <type_traits>
@@ -105,7 +106,7 @@ __device__ __forceinline__ uint32_t sh_value_pair(uint32_t halves, uint32_t fact
 // by_rows: the softmax groups take 128 rows each; otherwise (at most 128 rows) they take the key tiles in turn, and T is
 // even: behind the end of the prefix (`tiles`) an odd part gets one more tile, the last one's page again, all of it
 // masked.  Two instances with equal step counts for both groups: with a flag at run time, or with counts T / 2 and
-// (T + 1) / 2, the compiler spills the softmax group's score row (1.5 KB per thread against 40 bytes).
+// (T + 1) / 2, the compiler spills the softmax group's score row (1.5 KB per thread against 100 bytes).
 template <bool by_rows>
 __device__ __forceinline__ void prefix_block(const CUtensorMap &codes_map, const SharedParams &sp, unsigned char *smem, int seq0, int seq1,
                                              int head, int m0, int rows, int j0, int T, int tiles)
@@ -687,9 +688,10 @@ constexpr int kShSms = 148;
 // parts of the prefix is chosen for the earliest end of both, by what their blocks were measured to take (us):
 //   prefix block   10 + 3.0 per key tile of 256 rows; 13 + 1.4 where the softmax groups take the tiles in turn
 //   tail           7 + (2 per 256-token chunk, 4 with more than eight query heads per kv head) / blocks
-// The tails' lengths are device data: half of max_tail is taken for their mean.  (Prefixes of 2048 / 8192 / 16384 tokens
-// for 16 / 32 / 64 sequences: 38.6 / 47.9 / 67.1 us with the prefix on all SMs and the tail behind it, 30.9 / 34.8 / 53.7
-// side by side.)
+// The tails' lengths are device data: half of max_tail is taken for their mean, so where all tails are as long as max_tail
+// the tails' SMs end later than the prefix's.  (Prefixes of 2048 / 8192 / 16384 tokens for 16 / 32 / 64 sequences: 27.7 / 34.1
+// / 53 us.  When this was built, with the prefix on all SMs and the tail behind it 38.6 / 47.9 / 67.1, side by side 30.9 /
+// 34.8 / 53.7.)
 static SharedShape shared_shape(int B, int Hq, int Hkv, int n_groups, int max_group, int max_shared, int max_tail)
 {
     SharedShape s;

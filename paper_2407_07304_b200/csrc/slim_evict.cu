@@ -19,8 +19,8 @@
 // of up to eight blocks, which read one another's histograms and lists through distributed shared memory;
 // beyond 131072 tokens one block walks the row again for each of four histograms of digits (rows of 131072 tokens cut to
 // 16384: 324 us that way, 33 us by the cluster).
-// Measured (512 rows of 2049 tokens / 256 of up to 4096 / 2 of 32768, selection alone): 15 / 15 / 19 us; forms before it:
-// four histograms of the keys' digits 34 / 36 / 29 us (weights share their leading bits, the additions to one counter
+// Measured (512 rows of 2049 tokens with their one move / 256 of up to 4096, selection alone / 2 of 32768 with their moves):
+// 10.6 / 15 / 19.8 us; forms before it, selection alone: four histograms of the keys' digits 34 / 36 / 29 us (weights share their leading bits, the additions to one counter
 // queue up), a search with three bounds a step 18 / 23 / 27 us.
 // Nothing depends on the order of atomic additions (counts, and a list that is only ranked), so equal inputs give equal
 // results.
