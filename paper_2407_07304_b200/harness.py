@@ -146,6 +146,8 @@ class RotatedRun:
 
     def _append(self, qkv, counts):
         """qkv bf16 [tokens, Hq + 2 Hkv, 128]: the next counts[b] tokens of every sequence, as the fused projection leaves them."""
+        if len(counts) != self.B or min(counts) < 0:
+            raise ValueError("one count of new tokens per sequence")
         if any(n + c > self.max_tokens for n, c in zip(self.lens, counts)):
             raise ValueError("the cache is full: evict first")
         q, k, v = qkv[:, :self.Hq], qkv[:, self.Hq:self.Hq + self.Hkv], qkv[:, self.Hq + self.Hkv:]
