@@ -278,8 +278,9 @@ int slim_attn_merge_partials(const float *partials, int32_t n_sets, void *out, i
  *   k_new, v_new  device bf16 [B][num_kv_heads][128], 16-byte aligned
  *   kv_len        device int32 [B]: cached tokens per sequence counting the new
  *                 one; a sequence with kv_len[b] <= 0 appends nothing and gets
- *                 zeros; a kv_len[b] beyond max_kv or the page table appends
- *                 nothing and attends over the tokens that fit
+ *                 zeros; a kv_len[b] beyond max_kv (rounded up to a multiple of
+ *                 256) or the page table appends nothing and attends over the
+ *                 tokens that fit
  *   others        as for slim_attn_decode
  */
 int slim_decode_step(const slim_cache_t *cache, const void *q, const void *k_new, const void *v_new, void *out,
