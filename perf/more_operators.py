@@ -1,8 +1,8 @@
 """Cases and plain forms of the operators around the 4-bit KV cache and of the page tables of a cache.
 
-  append4   quantising keys and values into the 4-bit cache, and reading the same rows back (slim4_kv_append, slim4_kv_read)
-  decode4   decode attention over the 4-bit cache, with "step" the new tokens going into it in the same call (slim4_attn_decode)
-  prefill4  causal attention of new rows over the 4-bit cache that holds them (slim4_attn_prefill)
+  append4   quantising keys and values into the 4-bit cache, and reading the same rows back (slim_kv4_append, slim_kv4_read)
+  decode4   decode attention over the 4-bit cache, with "step" the new tokens going into it in the same call (slim_attn4_decode)
+  prefill4  causal attention of new rows over the 4-bit cache that holds them (slim_attn4_prefill)
   fork      the page table's rows continue by parent, then every row gets room for its next tokens (slim_pages_fork, slim_pages_grow)
   compact   finished sequences leave the page table, then the pages in use move together (slim_pages_fork, slim_pages_compact)
 
@@ -299,18 +299,18 @@ def _run_own(s):
     slim, op, case = s["slim"], s["op"], s["case"]
     b = case["batch"]
     if op == "append4":
-        slim.slim4_kv_append(s["cache"], s["k"], s["v"], s["cu"], s["start"], b, s["longest"])
-        slim.slim4_kv_read(s["cache"], s["k_held"], s["v_held"], s["cu"], s["start"], b, s["longest"])
+        slim.slim_kv4_append(s["cache"], s["k"], s["v"], s["cu"], s["start"], b, s["longest"])
+        slim.slim_kv4_read(s["cache"], s["k_held"], s["v_held"], s["cu"], s["start"], b, s["longest"])
         return {"k": s["k_held"], "v": s["v_held"], "scales": s["scales"]}
     if op == "decode4":
-        slim.slim4_attn_decode(s["cache"], s["q"], s["out"], s["lens"], b, s["longest"], case["hq"], s["scale"], s["ws"],
+        slim.slim_attn4_decode(s["cache"], s["q"], s["out"], s["lens"], b, s["longest"], case["hq"], s["scale"], s["ws"],
                                k_new=s.get("k"), v_new=s.get("v"))
         if not case["step"]:
             return {"out": s["out"]}
-        slim.slim4_kv_read(s["cache"], s["k_held"], s["v_held"], s["cu"], s["start"], b, 1)
+        slim.slim_kv4_read(s["cache"], s["k_held"], s["v_held"], s["cu"], s["start"], b, 1)
         return {"out": s["out"], "k": s["k_held"], "v": s["v_held"], "scales": s["scales"]}
     if op == "prefill4":
-        slim.slim4_attn_prefill(s["cache"], s["q"], s["out"], s["cu"], s["lens"], b, s["longest"], case["before"] + s["longest"], case["hq"],
+        slim.slim_attn4_prefill(s["cache"], s["q"], s["out"], s["cu"], s["lens"], b, s["longest"], case["before"] + s["longest"], case["hq"],
                                 s["scale"], s["ws"])
         return {"out": s["out"]}
     if op == "fork":
@@ -332,7 +332,7 @@ def _pages_out(s, refs, table, held, kv_len, result, result2):
 def _quantised(x):
     """fp32 rows [..., 128] -> packed codes [..., 64], scale and offset (bf16)."""
     low, high = x.amin(-1), x.amax(-1)
-    scale = ((high - low) / 15.0).to(torch.bfloat16)
+    scale = ((high - low) / torch.full_like(low, 15.0)).to(torch.bfloat16)      # (by a number it would be a product with 1 / 15)
     step = scale.float().unsqueeze(-1)
     u = torch.where(step > 0, ((x - low.unsqueeze(-1)) / step).round().clamp(0, 15), torch.zeros_like(x)).to(torch.uint8)
     return u[..., :D // 2] | (u[..., D // 2:] << 4), scale, low.to(torch.bfloat16)
