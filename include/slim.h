@@ -502,6 +502,133 @@ int slim_kv_evict(const slim_cache_t *cache, const float *weight_in, float *weig
 size_t slim_evict_workspace_bytes(int32_t B, int32_t Hkv, int32_t max_kv, int32_t budget);
 
 /*
+ * The KV cache in 4 bits: half the bytes that a decode step has to read (Section 2.2, Eq. 1 with s_d = 1/2), for callers
+ * that accept its coarser values.  Pages, block table and slots are those of slim_cache_t; a row x (128 values of one
+ * token and kv head, K and V separately) is held as unsigned 4-bit codes u with a scale s and an offset z of its own:
+ *   z = min x (a bf16 value, exact);  s = (max x - min x) / 15, formed in fp32 and rounded to bf16;
+ *   u_d = clamp(round_half_even((x_d - z) / s), 0, 15), difference and quotient rounded to fp32 each; 0 where s == 0;
+ *   the value held is z + u_d * s.
+ *
+ *   codes   device uint8 [num_pages][num_kv_heads][2][128 slots][64]: byte i holds dim i (low four bits) and dim 64 + i
+ *   scales  device bf16  [num_pages][num_kv_heads][2][128 slots][2]: s, z
+ * Other fields and rules as for slim_cache_t.
+ */
+typedef struct slim_cache4 {
+    uint8_t       *codes;
+    uint16_t      *scales;
+    const int32_t *block_table;
+    int32_t        num_pages;
+    int32_t        page_tokens;        /* must be 128 */
+    int32_t        num_kv_heads;
+    int32_t        head_dim;           /* must be 128 */
+    int32_t        max_pages_per_seq;
+} slim_cache4_t;
+
+/* slim_kv_append into the 4-bit cache; codes, scales and offsets are reproducible bit for bit. */
+int slim_kv4_append(const slim_cache4_t *cache, const void *k_new, const void *v_new,
+                    const int32_t *cu_new, const int32_t *start_pos,
+                    int32_t B, int32_t max_new, void *stream);
+
+/*
+ * The way back: the values held for positions start_pos[b] .. of sequence b, rounded to bf16, as rows cu[b] .. cu[b+1]-1
+ * of k_out and v_out (bf16 [total][num_kv_heads][128], 16-byte aligned).  Rows of positions outside the page table or
+ * with a page id outside [0, num_pages) are left as they are.
+ */
+int slim_kv4_read(const slim_cache4_t *cache, void *k_out, void *v_out, const int32_t *cu, const int32_t *start_pos,
+                  int32_t B, int32_t max_rows, void *stream);
+
+/* slim_attn_prefill and slim_prefill_step over the 4-bit cache: arguments, workspace and errors are theirs. */
+int slim_attn4_prefill(const slim_cache4_t *cache, const void *q, void *out,
+                       const int32_t *cu_q, const int32_t *kv_len,
+                       int32_t B, int32_t max_q, int32_t max_kv, int32_t Hq, float sm_scale,
+                       void *workspace, size_t workspace_bytes, void *stream);
+int slim_prefill4_step(const slim_cache4_t *cache, const void *q, const void *k_new, const void *v_new, void *out,
+                       const int32_t *cu_q, const int32_t *kv_len,
+                       int32_t B, int32_t max_q, int32_t max_kv, int32_t Hq, float sm_scale,
+                       void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * slim_attn_decode over the 4-bit cache; with k_new and v_new (both or neither, bf16 [B][num_kv_heads][128], 16-byte
+ * aligned) slim_decode_step: every sequence's new token is quantised into position kv_len[b] - 1 by the kernel that
+ * attends over it, as slim_kv4_append does.
+ *
+ *   kv_len     device int32 [B]; kv_len[b] <= 0: zeros, nothing appended.  A kv_len[b] beyond max_kv or the page table
+ *              appends nothing and attends over the tokens that fit
+ *   workspace  device, 16-byte aligned, at least slim_attn4_workspace_bytes(Hq, Hkv) bytes, whatever the batch and lengths;
+ *              header as for slim_attn_decode.  Two calls that can overlap need one each
+ */
+int slim_attn4_decode(const slim_cache4_t *cache, const void *q, const void *k_new, const void *v_new, void *out,
+                      const int32_t *kv_len, int32_t B, int32_t max_kv, int32_t Hq, float sm_scale,
+                      void *workspace, size_t workspace_bytes, void *stream);
+size_t slim_attn4_workspace_bytes(int32_t Hq, int32_t Hkv);
+size_t slim_cache4_code_bytes(int32_t num_pages, int32_t num_kv_heads);
+size_t slim_cache4_scale_bytes(int32_t num_pages, int32_t num_kv_heads);
+
+/*
+ * Who holds which page.  The page tables of the caches (one table serves all layers of a model) are device arrays that
+ * these calls keep; a step decides nothing on the host.
+ *
+ *   refs   device int32 [num_pages]: rows (and other holders, counted by the caller) that hold a page; 0: free
+ *   table  device int32 [rows][stride]: a sequence's pages in order, -1 from held[row] on; a cache's block_table
+ *   held   device int32 [rows]: pages of a row, 0 to stride
+ * Only pages that are full may be held by more than one row.  Page ids outside [0, num_pages) are not followed.
+ * Pages are taken lowest id first; every result is the same from run to run.
+ */
+typedef struct slim_pages {
+    int32_t *refs;
+    int32_t *table;
+    int32_t *held;
+    int32_t  num_pages;
+    int32_t  rows;
+    int32_t  stride;
+} slim_pages_t;
+
+/* One layer's pool, whatever its cache: codes and scales of a slim_cache_t (row_bytes 128) or a slim_cache4_t (64). */
+typedef struct slim_layer {
+    void   *codes;
+    void   *scales;
+    int32_t num_kv_heads;
+    int32_t row_bytes;
+} slim_layer_t;
+
+/*
+ * Continues, forks and frees sequences: row i of `to` continues row parent[i] of `from`.  The first row that names a
+ * parent takes its row over, with all pages held; every other one shares the parent's full pages and gets a page of its
+ * own with a copy of the kv_len % 128 tokens behind them, in every layer.  Rows of `from` that no row names are freed,
+ * parent[i] < 0 (or >= from->rows) leaves row i empty: no pages, length -1.
+ *
+ *   from, to   to->table and to->held must not be from's; to->refs may be from->refs.  Same num_pages and stride
+ *   parent     device int32 [to->rows]
+ *   kv_len     device int32 [from->rows]: tokens of every row (held[b] * 128 at most);  len_out  device int32 [to->rows]
+ *   layers     host array of n_layers pools (0: tables only)
+ *   result     device int32 [2]: pages that are missing, pages free afterwards.  Where pages are missing nothing else is
+ *              written: free some and call again
+ *   workspace  device, 16-byte aligned, at least slim_pages_workspace_bytes(num_pages, most rows) bytes; no initialisation
+ */
+int slim_pages_fork(const slim_pages_t *from, const slim_pages_t *to, const int32_t *parent, const int32_t *kv_len,
+                    int32_t *len_out, const slim_layer_t *layers, int32_t n_layers, int32_t *result,
+                    void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Room for the next tokens: every row with kv_len[row] >= 0 gets pages until it holds kv_len[row] + room tokens, never more
+ * than stride pages.  Missing pages are taken by row, then by place.  result as above; where pages are missing nothing
+ * else is written.
+ */
+int slim_pages_grow(const slim_pages_t *pages, const int32_t *kv_len, int32_t room, int32_t *result,
+                    void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Moves the pages in use together: with n pages in use, those with ids from n on move to the free ids below n, both in
+ * ascending order, in every layer; table and refs follow.  Pages from n on are free afterwards (and keep what they held).
+ *
+ *   from, to  may be the same, array by array.  Same num_pages, rows and stride
+ *   result    device int32 [2]: pages in use, pages moved
+ */
+int slim_pages_compact(const slim_pages_t *from, const slim_pages_t *to, const slim_layer_t *layers, int32_t n_layers,
+                       int32_t *result, void *workspace, size_t workspace_bytes, void *stream);
+size_t slim_pages_workspace_bytes(int32_t num_pages, int32_t rows);
+
+/*
  * Device-side waits are bounded.  The attention kernels wait on hardware barriers (TMA copies, tensor-core
  * completion); every such wait gives up after a fixed number of tries, and a kernel whose wait ran out
  * stores SLIM_ERR_TIMEOUT in the first word of its workspace and finishes with undefined output instead of

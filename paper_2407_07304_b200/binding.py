@@ -31,6 +31,9 @@ EXPORTS = (
     "slim_version",
     "slim_norm_rope", "slim_norm_rope_append", "slim_attn_decode_shared", "slim_shared_workspace_bytes",
     "slim_attn_decode_weights", "slim_weights_workspace_bytes", "slim_kv_evict", "slim_evict_workspace_bytes",
+    "slim_kv4_append", "slim_kv4_read", "slim_attn4_prefill", "slim_prefill4_step", "slim_attn4_decode", "slim_attn4_workspace_bytes",
+    "slim_cache4_code_bytes", "slim_cache4_scale_bytes",
+    "slim_pages_fork", "slim_pages_grow", "slim_pages_compact", "slim_pages_workspace_bytes",
 )
 
 
@@ -59,6 +62,28 @@ class SlimNormRopeStruct(ctypes.Structure):
         ("rotary_dim", ctypes.c_int32),
         ("n_axes", ctypes.c_int32),
         ("interleaved", ctypes.c_int32),
+    ]
+
+
+class SlimPagesStruct(ctypes.Structure):
+    """Mirror of slim_pages_t."""
+    _fields_ = [
+        ("refs", ctypes.c_void_p),
+        ("table", ctypes.c_void_p),
+        ("held", ctypes.c_void_p),
+        ("num_pages", ctypes.c_int32),
+        ("rows", ctypes.c_int32),
+        ("stride", ctypes.c_int32),
+    ]
+
+
+class SlimLayerStruct(ctypes.Structure):
+    """Mirror of slim_layer_t."""
+    _fields_ = [
+        ("codes", ctypes.c_void_p),
+        ("scales", ctypes.c_void_p),
+        ("num_kv_heads", ctypes.c_int32),
+        ("row_bytes", ctypes.c_int32),
     ]
 
 
@@ -133,6 +158,22 @@ def lib():
         L.slim_kv_evict.restype = ctypes.c_int
         L.slim_evict_workspace_bytes.argtypes = [I, I, I, I]
         L.slim_evict_workspace_bytes.restype = Z
+        # (slim_cache4_t has the layout of slim_cache_t; its codes and scales are of other types)
+        L.slim_kv4_append.argtypes = [CP, P, P, P, P, I, I, P]
+        L.slim_kv4_read.argtypes = [CP, P, P, P, P, I, I, P]
+        L.slim_attn4_prefill.argtypes = [CP, P, P, P, P, I, I, I, I, F, P, Z, P]
+        L.slim_prefill4_step.argtypes = [CP, P, P, P, P, P, P, I, I, I, I, F, P, Z, P]
+        L.slim_attn4_decode.argtypes = [CP, P, P, P, P, P, I, I, I, F, P, Z, P]
+        GP, LP = ctypes.POINTER(SlimPagesStruct), ctypes.POINTER(SlimLayerStruct)
+        L.slim_pages_fork.argtypes = [GP, GP, P, P, P, LP, I, P, P, Z, P]
+        L.slim_pages_grow.argtypes = [GP, P, I, P, P, Z, P]
+        L.slim_pages_compact.argtypes = [GP, GP, LP, I, P, P, Z, P]
+        for name in ("slim_kv4_append", "slim_kv4_read", "slim_attn4_prefill", "slim_prefill4_step", "slim_attn4_decode", "slim_pages_fork",
+                     "slim_pages_grow", "slim_pages_compact"):
+            getattr(L, name).restype = ctypes.c_int
+        for name in ("slim_attn4_workspace_bytes", "slim_cache4_code_bytes", "slim_cache4_scale_bytes", "slim_pages_workspace_bytes"):
+            getattr(L, name).argtypes = [I, I]
+            getattr(L, name).restype = Z
         L.slim_read_status.argtypes = [P, P]
         L.slim_read_status.restype = ctypes.c_int
         L.slim_selftest_timeout.argtypes = [P, P]
@@ -172,7 +213,19 @@ def _check(rc, where):
         raise SlimError(rc, where)
 
 
-class SlimCache:
+class _BlockTable:
+    """What both caches do with their block table."""
+
+    def set_block_table(self, block_table):
+        """Uses another table (int32 [rows, pages], contiguous, on the cache's device) from the next call on: the rows of a SlimPages."""
+        if block_table.dtype is not torch.int32 or block_table.dim() != 2 or not block_table.is_contiguous() or block_table.device != self.codes.device:
+            raise TypeError("block tables must be contiguous int32 [rows, pages] on the cache's device")
+        self.B, self.max_pages_per_seq = block_table.shape
+        self.block_table = block_table
+        self.struct.block_table, self.struct.max_pages_per_seq = block_table.data_ptr(), self.max_pages_per_seq
+
+
+class SlimCache(_BlockTable):
     """Device memory of one layer's paged INT8 KV cache plus its slim_cache_t.
 
     Pages are handed to sequences in order: sequence b owns pages
@@ -448,6 +501,170 @@ def slim_kv_evict(cache, weight_in, weight_out, pos_in, pos_out, kv_len, placed,
                              _addr(kv_len), _addr(placed), _addr(seen), B, max_kv, budget, n_sink, n_recent, _addr(workspace),
                              _nbytes(workspace), _cuda_stream(stream))
     _check(rc, "slim_kv_evict")
+
+
+# ------------------------------------------------------------------ the cache in 4 bits
+class SlimCache4(_BlockTable):
+    """Device memory of one layer's paged 4-bit KV cache plus its slim_cache4_t; pages as for SlimCache."""
+
+    def __init__(self, B, num_kv_heads, max_pages_per_seq, device="cuda", block_table=None, num_pages=None):
+        self.B, self.Hkv, self.max_pages_per_seq = B, num_kv_heads, max_pages_per_seq
+        self.num_pages = num_pages if num_pages is not None else B * max_pages_per_seq
+        L = lib()
+        self.codes = torch.zeros(L.slim_cache4_code_bytes(self.num_pages, num_kv_heads), dtype=torch.uint8, device=device)
+        self.scales = torch.zeros(L.slim_cache4_scale_bytes(self.num_pages, num_kv_heads) // 2, dtype=torch.bfloat16, device=device)
+        if block_table is None:
+            block_table = torch.arange(B * max_pages_per_seq, dtype=torch.int32).view(B, max_pages_per_seq)
+        self.block_table = block_table.to(device=device, dtype=torch.int32).contiguous()
+        self.struct = SlimCacheStruct(self.codes.data_ptr(), self.scales.data_ptr(), self.block_table.data_ptr(),
+                                      self.num_pages, PAGE_TOKENS, num_kv_heads, HEAD_DIM, max_pages_per_seq)
+        self.ref = ctypes.byref(self.struct)
+
+    def codes_view(self):
+        """uint8 [num_pages, Hkv, 2, 128, 64]: byte i holds dim i (low four bits) and dim 64 + i"""
+        return self.codes.view(self.num_pages, self.Hkv, 2, PAGE_TOKENS, HEAD_DIM // 2)
+
+    def scales_view(self):
+        """bf16 [num_pages, Hkv, 2, 128, 2]: scale and offset"""
+        return self.scales.view(self.num_pages, self.Hkv, 2, PAGE_TOKENS, 2)
+
+
+def _cache4(cache, where):
+    if not isinstance(cache, SlimCache4):
+        raise SlimError(SLIM_ERR_INVALID_ARG, f"{where}: needs a SlimCache4")
+    return cache.ref
+
+
+def _rows4(where, Hkv, *rows):
+    for t in rows:
+        if t.dtype is not torch.bfloat16 or t.dim() != 3 or t.shape[1] != Hkv or t.shape[2] != HEAD_DIM or not t.is_contiguous():
+            raise SlimError(SLIM_ERR_INVALID_ARG, f"{where}: rows must be contiguous bfloat16 [tokens, kv heads, 128]")
+
+
+def slim_kv4_append(cache, k_new, v_new, cu_new, start_pos, B, max_new, stream=None):
+    """slim_kv_append into the 4-bit cache."""
+    where = "slim_kv4_append"
+    ref = _cache4(cache, where)
+    _rows4(where, cache.Hkv, k_new, v_new)
+    rc = lib().slim_kv4_append(ref, _addr(k_new), _addr(v_new), _addr(cu_new), _addr(start_pos), B, max_new, _cuda_stream(stream))
+    _check(rc, where)
+
+
+def slim_kv4_read(cache, k_out, v_out, cu, start_pos, B, max_rows, stream=None):
+    """The values held for positions start_pos[b] .. of every sequence, as bf16 rows cu[b] .. cu[b + 1] - 1 of k_out and v_out."""
+    where = "slim_kv4_read"
+    ref = _cache4(cache, where)
+    _rows4(where, cache.Hkv, k_out, v_out)
+    rc = lib().slim_kv4_read(ref, _addr(k_out), _addr(v_out), _addr(cu), _addr(start_pos), B, max_rows, _cuda_stream(stream))
+    _check(rc, where)
+
+
+def slim_attn4_prefill(cache, q, out, cu_q, kv_len, B, max_q, max_kv, Hq, sm_scale, workspace, stream=None):
+    rc = lib().slim_attn4_prefill(_cache4(cache, "slim_attn4_prefill"), _addr(q), _addr(out), _addr(cu_q), _addr(kv_len), B, max_q, max_kv, Hq,
+                                  sm_scale, _addr(workspace), _nbytes(workspace), _cuda_stream(stream))
+    _check(rc, "slim_attn4_prefill")
+
+
+def slim_prefill4_step(cache, q, k_new, v_new, out, cu_q, kv_len, B, max_q, max_kv, Hq, sm_scale, workspace, stream=None):
+    rc = lib().slim_prefill4_step(_cache4(cache, "slim_prefill4_step"), _addr(q), _addr(k_new), _addr(v_new), _addr(out), _addr(cu_q), _addr(kv_len),
+                                  B, max_q, max_kv, Hq, sm_scale, _addr(workspace), _nbytes(workspace), _cuda_stream(stream))
+    _check(rc, "slim_prefill4_step")
+
+
+def slim_attn4_decode(cache, q, out, kv_len, B, max_kv, Hq, sm_scale, workspace, stream=None, k_new=None, v_new=None):
+    """Decode attention over the 4-bit cache; with k_new and v_new the new tokens go into position kv_len - 1 in the same call."""
+    rc = lib().slim_attn4_decode(_cache4(cache, "slim_attn4_decode"), _addr(q), _addr(k_new), _addr(v_new), _addr(out), _addr(kv_len), B, max_kv, Hq,
+                                 sm_scale, _addr(workspace), _nbytes(workspace), _cuda_stream(stream))
+    if rc:
+        _check(rc, "slim_attn4_decode")
+
+
+def decode4_workspace(B, Hq, Hkv, max_kv, device="cuda"):
+    """A zeroed torch uint8 buffer for slim_attn4_decode (its size goes by Hq / Hkv alone)."""
+    return _scratch(lib().slim_attn4_workspace_bytes(Hq, Hkv), device)
+
+
+# ------------------------------------------------------------------ page tables
+class SlimPages:
+    """slim_pages_t over int32 tensors refs [num_pages], table [rows, stride] and held [rows] (see slim_pages_fork)."""
+
+    def __init__(self, refs, table, held):
+        for t in (refs, table, held):
+            if t.dtype is not torch.int32 or not t.is_contiguous():
+                raise TypeError("page tables, counters and counts must be contiguous int32")
+        if refs.dim() != 1 or table.dim() != 2 or held.shape != table.shape[:1]:
+            raise TypeError("refs [num_pages], table [rows, stride], held [rows]")
+        self.refs, self.table, self.held = refs, table, held   # kept here because the struct holds bare addresses
+        self.struct = SlimPagesStruct(refs.data_ptr(), table.data_ptr(), held.data_ptr(), refs.numel(), table.shape[0], table.shape[1])
+        self.ref = ctypes.byref(self.struct)
+
+    @classmethod
+    def empty(cls, num_pages, rows, stride, device="cuda"):
+        """A pool of free pages and rows without any."""
+        make = lambda value, *shape: torch.full(shape, value, dtype=torch.int32, device=device)  # noqa: E731
+        return cls(make(0, num_pages), make(-1, rows, stride), make(0, rows))
+
+
+class PageLayers:
+    """The pools (SlimCache or SlimCache4, one per layer) whose pages a SlimPages hands out."""
+
+    def __init__(self, caches):
+        self.caches = list(caches)
+        if len({c.num_pages for c in self.caches}) > 1:
+            raise ValueError("the layers' pools must have the same number of pages")
+        rows = [HEAD_DIM // 2 if isinstance(c, SlimCache4) else HEAD_DIM for c in self.caches]
+        self.array = (SlimLayerStruct * max(1, len(self.caches)))(
+            *[SlimLayerStruct(c.codes.data_ptr(), c.scales.data_ptr(), c.Hkv, n) for c, n in zip(self.caches, rows)])
+
+
+def _layers(where, layers, pages):
+    if layers is None:
+        return None, 0
+    if any(c.num_pages != pages.refs.numel() for c in layers.caches):
+        raise SlimError(SLIM_ERR_INVALID_ARG, f"{where}: a layer's pool and the page counters differ in size")
+    return layers.array, len(layers.caches)
+
+
+def _i32_vector(where, n, *vectors):
+    for t in vectors:
+        if t.dtype is not torch.int32 or t.numel() < n or not t.is_contiguous():
+            raise SlimError(SLIM_ERR_INVALID_ARG, f"{where}: lengths, parents and results must be contiguous int32, one per row (two results)")
+
+
+def slim_pages_fork(layers, src, dst, parent, kv_len, len_out, result, workspace, stream=None):
+    """Row i of dst continues row parent[i] of src (-1: an empty row): the first child takes the row over, others share its full
+    pages and get a copy of the last one, rows without children are freed.  layers: PageLayers, or None for the tables alone."""
+    where = "slim_pages_fork"
+    array, n = _layers(where, layers, src)
+    _i32_vector(where, len(dst.held), parent, len_out)
+    _i32_vector(where, len(src.held), kv_len)
+    _i32_vector(where, 2, result)
+    rc = lib().slim_pages_fork(src.ref, dst.ref, _addr(parent), _addr(kv_len), _addr(len_out), array, n, _addr(result), _addr(workspace),
+                               _nbytes(workspace), _cuda_stream(stream))
+    _check(rc, where)
+
+
+def slim_pages_grow(pages, kv_len, room, result, workspace, stream=None):
+    """Pages for kv_len + room tokens in every row of length 0 or more."""
+    where = "slim_pages_grow"
+    _i32_vector(where, len(pages.held), kv_len)
+    _i32_vector(where, 2, result)
+    rc = lib().slim_pages_grow(pages.ref, _addr(kv_len), room, _addr(result), _addr(workspace), _nbytes(workspace), _cuda_stream(stream))
+    _check(rc, where)
+
+
+def slim_pages_compact(layers, src, dst, result, workspace, stream=None):
+    """The pages in use move to the lowest ids, in every layer; dst (may be src) holds the tables afterwards."""
+    where = "slim_pages_compact"
+    array, n = _layers(where, layers, src)
+    _i32_vector(where, 2, result)
+    rc = lib().slim_pages_compact(src.ref, dst.ref, array, n, _addr(result), _addr(workspace), _nbytes(workspace), _cuda_stream(stream))
+    _check(rc, where)
+
+
+def pages_workspace(num_pages, rows, device="cuda"):
+    """A torch uint8 buffer for the slim_pages calls on up to `rows` rows."""
+    return _scratch(lib().slim_pages_workspace_bytes(num_pages, rows), device)
 
 
 def _scratch(n, device):

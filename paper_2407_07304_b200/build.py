@@ -7,7 +7,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libslim.so")
 SOURCES = ["slim_abi.cu", "slim_append.cu", "slim_norm_rope.cu", "slim_decode.cu", "slim_decode_stream.cu", "slim_decode_shared.cu",
-           "slim_decode_weights.cu", "slim_evict.cu", "slim_tmap.cu", "slim_prefill_tc.cu", "slim_prefill_row.cu"]
+           "slim_decode_weights.cu", "slim_evict.cu", "slim_tmap.cu", "slim_prefill_tc.cu", "slim_prefill_row.cu",
+           "slim4_abi.cu", "slim4_append.cu", "slim4_decode.cu", "slim_pages.cu"]
 
 
 def _nvcc():

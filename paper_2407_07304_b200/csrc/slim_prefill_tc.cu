@@ -31,6 +31,7 @@
 // landed (before its conversion), so the softmax of tile j never waits for it in practice.
 #include <cuda.h>
 
+#include "slim4_common.cuh"
 #include "slim_common.cuh"
 #include "slim_tcgen05.cuh"
 #include "slim_tmap.cuh"
@@ -64,7 +65,7 @@ static_assert(kBytes <= 232448, "shared memory budget of one block");
 }  // namespace pfl
 
 struct PrefillTcParams {
-    const float *scales;
+    const void *scales;   // fp32 per row; of the 4-bit cache a (scale, offset) pair of bf16, also four bytes
     const int32_t *block_table;
     const int32_t *cu_q;
     const int32_t *kv_len;
@@ -116,6 +117,12 @@ __device__ __forceinline__ uint32_t pf_hsub2(uint32_t a, uint32_t b)
     asm("sub.rn.f16x2 %0, %1, %2;\n" : "=r"(r) : "r"(a), "r"(b));
     return r;
 }
+__device__ __forceinline__ uint32_t pf_hfma2(uint32_t a, uint32_t b, uint32_t c)
+{
+    uint32_t r;
+    asm("fma.rn.f16x2 %0, %1, %2, %3;\n" : "=r"(r) : "r"(a), "r"(b), "r"(c));
+    return r;
+}
 __device__ __forceinline__ uint32_t pf_hmul2(uint32_t a, uint32_t b)
 {
     uint32_t r;
@@ -123,12 +130,24 @@ __device__ __forceinline__ uint32_t pf_hmul2(uint32_t a, uint32_t b)
     return r;
 }
 
+// What the power of two of a tile goes by: a row's scale, or its largest |value| where rows have offsets.
+template <int kBits>
+__device__ __forceinline__ float pf_row_size(uint32_t word)
+{
+    if (kBits == 8) return __uint_as_float(word);
+    const float z = pair_offset(word);
+    return fmaxf(fabsf(z), fabsf(fmaf(15.f, pair_scale(word), z)));
+}
+
 // kTwoPass: the literal order of Section 2.1 - every score of a row before its softmax.  The block walks its key
 // tiles twice: the first pass only takes the row maxima of the scores, the second computes P = 2^(s - max) against
 // that final maximum and accumulates P.V, so no accumulator is ever corrected.  Both passes run through the same
 // pipeline (a key tile is loaded and converted again in the second pass); the tile sequence of the block is
 // simply twice as long, and barrier phases count positions in that sequence.
-template <bool kTwoPass>
+//
+// kBits 4: the 4-bit cache.  Its raw rows are 64 bytes (64-byte swizzle), and a row's values scale * u + offset become
+// fp16 operands over the same kind of power of two, below the tile's largest |value| that its pairs allow.
+template <bool kTwoPass, int kBits = 8>
 __global__ void __launch_bounds__(kPfThreads, 1)
 slim_prefill_tc_kernel(const __grid_constant__ CUtensorMap codes_map, const PrefillTcParams p)
 {
@@ -176,9 +195,9 @@ slim_prefill_tc_kernel(const __grid_constant__ CUtensorMap codes_map, const Pref
         int page = page_next;
         page = (page >= 0 && page < p.num_pages) ? page : 0;
         const uint32_t full = bar(pfl::RAW_FULL, kv);
-        tc::mbar_arrive_expect_tx(full, 16384 + 512);
+        tc::mbar_arrive_expect_tx(full, kPageTokens * kHeadDim * kBits / 8 + 512);
         tc::tma_load_2d(sbase + pfl::kRaw + kv * 16384, &codes_map, 0, ((page * p.Hkv + head) * 2 + kv) * kPageTokens, full);
-        tc::bulk_load(sbase + pfl::kRawScales + kv * 512, p.scales + scale_block_offset(page, head, kv, p.Hkv), 512, full);
+        tc::bulk_load(sbase + pfl::kRawScales + kv * 512, static_cast<const uint32_t *>(p.scales) + scale_block_offset(page, head, kv, p.Hkv), 512, full);
         if (kv == 1 && j + 1 < NT) {
             // the next key tile's page id, and its two tiles on their way into the L2 a step before they are asked for
             page_next = __ldg(bt + ((kTwoPass && j + 1 >= T) ? j + 1 - T : j + 1));
@@ -461,16 +480,16 @@ slim_prefill_tc_kernel(const __grid_constant__ CUtensorMap codes_map, const Pref
             const int buf = j & 1;
             wait(bar(pfl::RAW_FULL, kv), (uint32_t)j & 1u);
             const unsigned char *raw = smem + pfl::kRaw + kv * 16384;
-            const float *scales = reinterpret_cast<const float *>(smem + pfl::kRawScales + kv * 512);
+            const uint32_t *scales = reinterpret_cast<const uint32_t *>(smem + pfl::kRawScales + kv * 512);
             const int n_valid = min(kPfBN, kvl - ((kTwoPass && j >= T) ? j - T : j) * kPfBN);   // rows past the cache length hold anything: zeroed
             // power of two below the tile's largest scale (every warp finds it for itself: four scales per lane)
             float wm = 0.f;
             {
-                const float4 s4 = *reinterpret_cast<const float4 *>(scales + 4 * lane);
-                const float sv[4] = {s4.x, s4.y, s4.z, s4.w};
+                const uint4 s4 = *reinterpret_cast<const uint4 *>(scales + 4 * lane);
+                const uint32_t sv[4] = {s4.x, s4.y, s4.z, s4.w};
 #pragma unroll
                 for (int k = 0; k < 4; ++k)
-                    if (4 * lane + k < n_valid) wm = fmaxf(wm, sv[k]);
+                    if (4 * lane + k < n_valid) wm = fmaxf(wm, pf_row_size<kBits>(sv[k]));
                 wm = warp_max(wm);
             }
             const float ex = (wm > 0.f) ? pow2_floor(wm) : 1.f;
@@ -492,9 +511,33 @@ slim_prefill_tc_kernel(const __grid_constant__ CUtensorMap codes_map, const Pref
             for (int q = 0; q < 2; ++q) {
                 if (q >= n_rows) break;
                 const int r = r0 + 64 * q;
-                const float f = ((r < n_valid) ? scales[r] : 0.f) * rex;   // scale / 2^e in [0, 2)
-                const uint32_t fac2 = pack_half2(f, f);
+                const uint32_t row_scale = (r < n_valid) ? scales[r] : 0u;
                 unsigned char *dstb = dst_tile + r * 128;
+                if constexpr (kBits == 4) {
+                    // scale and offset are bf16, over a power of two not far from the larger one: exact in fp16 down to 2^-14 of it
+                    const float f = pair_scale(row_scale) * rex, z = pair_offset(row_scale) * rex;
+                    const uint32_t fac2 = pack_half2(f, f), off2 = pack_half2(z, z);
+                    for (int c = c_first / 2; c < c_last / 2; ++c) {
+                        // piece c of a raw row: dims 16 c .. + 15 in the low halves of its bytes, 64 further in the high ones
+                        const uint4 w4 = *reinterpret_cast<const uint4 *>(raw + r * 64 + ((c ^ ((r >> 1) & 3)) << 4));
+                        const uint32_t w[4] = {w4.x, w4.y, w4.z, w4.w};
+#pragma unroll
+                        for (int hf = 0; hf < 2; ++hf) {
+                            uint32_t hh[8];
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) {
+                                const uint32_t x = (w[k] >> (4 * hf)) & 0x0F0F0F0Fu;   // under 0x64: the fp16 number 1024 + code
+                                hh[2 * k] = pf_hfma2(pf_hsub2(__byte_perm(x, 0x64646464u, 0x4140), 0x64006400u), fac2, off2);
+                                hh[2 * k + 1] = pf_hfma2(pf_hsub2(__byte_perm(x, 0x64646464u, 0x4342), 0x64006400u), fac2, off2);
+                            }
+                            *reinterpret_cast<uint4 *>(dstb + hf * 16384 + (((2 * c) ^ (r & 7)) << 4)) = make_uint4(hh[0], hh[1], hh[2], hh[3]);
+                            *reinterpret_cast<uint4 *>(dstb + hf * 16384 + (((2 * c + 1) ^ (r & 7)) << 4)) = make_uint4(hh[4], hh[5], hh[6], hh[7]);
+                        }
+                    }
+                    continue;
+                }
+                const float f = __uint_as_float(row_scale) * rex;   // scale / 2^e in [0, 2)
+                const uint32_t fac2 = pack_half2(f, f);
                 for (int c = c_first; c < c_last; ++c) {
                     const uint4 w4 = *reinterpret_cast<const uint4 *>(raw + r * 128 + ((c ^ (r & 7)) << 4));
                     const uint32_t w[4] = {w4.x, w4.y, w4.z, w4.w};
@@ -623,8 +666,9 @@ slim_prefill_tc_kernel(const __grid_constant__ CUtensorMap codes_map, const Pref
 // ---------------------------------------------------------------- host side
 size_t prefill_workspace_bytes() { return 16; }   // status word
 
-int launch_prefill_tc(const slim_cache_t *c, const void *q, void *out, const int32_t *cu_q, const int32_t *kv_len,
-                      int B, int max_q, int Hq, float sm_scale, void *workspace, cudaStream_t stream, bool two_pass, bool after_append)
+template <class Cache>
+static PrefillTcParams prefill_params(const Cache *c, const void *q, void *out, const int32_t *cu_q, const int32_t *kv_len, int max_q, int Hq,
+                                      float sm_scale, void *workspace)
 {
     PrefillTcParams p;
     p.scales = c->scales;
@@ -641,20 +685,42 @@ int launch_prefill_tc(const slim_cache_t *c, const void *q, void *out, const int
     p.num_pages = c->num_pages;
     p.n_qblocks = (max_q + kPfRows - 1) / kPfRows;
     p.scale_log2e = sm_scale * kLog2e;
-    if (p.n_qblocks == 0) return SLIM_OK;
-    CUtensorMap map;
-    int rc = codes_tensor_map(c, kPfBN, &map);
-    if (rc != SLIM_OK) return rc;
-    rc = allow_dynamic_smem(two_pass ? reinterpret_cast<const void *>(slim_prefill_tc_kernel<true>)
-                                     : reinterpret_cast<const void *>(slim_prefill_tc_kernel<false>), (int)pfl::kBytes);
+    return p;
+}
+
+template <bool kTwoPass, int kBits>
+static int launch_prefill(const CUtensorMap &map, const PrefillTcParams &p, int B, cudaStream_t stream, bool after_append)
+{
+    const int rc = allow_dynamic_smem(reinterpret_cast<const void *>(slim_prefill_tc_kernel<kTwoPass, kBits>), (int)pfl::kBytes);
     if (rc != SLIM_OK) return rc;
     if (p.n_qblocks > 65535 || B > 65535) return SLIM_ERR_UNSUPPORTED;
-    dim3 grid((unsigned)Hq, (unsigned)B, (unsigned)p.n_qblocks);
-    if (two_pass) slim_prefill_tc_kernel<true><<<grid, kPfThreads, pfl::kBytes, stream>>>(map, p);
-    else if (after_append) SLIM_CUDA_TRY(launch_pdl(slim_prefill_tc_kernel<false>, grid, dim3(kPfThreads), pfl::kBytes, stream, map, p));
-    else slim_prefill_tc_kernel<false><<<grid, kPfThreads, pfl::kBytes, stream>>>(map, p);
+    dim3 grid((unsigned)p.Hq, (unsigned)B, (unsigned)p.n_qblocks);
+    if (after_append) SLIM_CUDA_TRY(launch_pdl(slim_prefill_tc_kernel<kTwoPass, kBits>, grid, dim3(kPfThreads), pfl::kBytes, stream, map, p));
+    else slim_prefill_tc_kernel<kTwoPass, kBits><<<grid, kPfThreads, pfl::kBytes, stream>>>(map, p);
     SLIM_CUDA_TRY(cudaGetLastError());
     return SLIM_OK;
+}
+
+int launch_prefill_tc(const slim_cache_t *c, const void *q, void *out, const int32_t *cu_q, const int32_t *kv_len,
+                      int B, int max_q, int Hq, float sm_scale, void *workspace, cudaStream_t stream, bool two_pass, bool after_append)
+{
+    const PrefillTcParams p = prefill_params(c, q, out, cu_q, kv_len, max_q, Hq, sm_scale, workspace);
+    if (p.n_qblocks == 0) return SLIM_OK;
+    CUtensorMap map;
+    const int rc = codes_tensor_map(c, kPfBN, &map);
+    if (rc != SLIM_OK) return rc;
+    return two_pass ? launch_prefill<true, 8>(map, p, B, stream, false) : launch_prefill<false, 8>(map, p, B, stream, after_append);
+}
+
+int launch_prefill4_tc(const slim_cache4_t *c, const void *q, void *out, const int32_t *cu_q, const int32_t *kv_len,
+                       int B, int max_q, int Hq, float sm_scale, void *workspace, cudaStream_t stream, bool after_append)
+{
+    const PrefillTcParams p = prefill_params(c, q, out, cu_q, kv_len, max_q, Hq, sm_scale, workspace);
+    if (p.n_qblocks == 0) return SLIM_OK;
+    CUtensorMap map;
+    const int rc = codes4_tensor_map(c, kPfBN, &map);
+    if (rc != SLIM_OK) return rc;
+    return launch_prefill<false, 4>(map, p, B, stream, after_append);
 }
 
 }  // namespace slim

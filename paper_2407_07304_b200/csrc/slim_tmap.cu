@@ -21,13 +21,13 @@ typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t
 struct Entry {
     const void *ptr;
     long long rows;
-    int box_rows;
+    int row_bytes, box_rows;
     CUtensorMap map;
 };
 constexpr int kEntries = 32;
 }  // namespace
 
-int codes_tensor_map(const slim_cache_t *c, int box_rows, CUtensorMap *out)
+static int rows_tensor_map(void *codes, long long rows, int row_bytes, CUtensorMapSwizzle swizzle, int box_rows, CUtensorMap *out)
 {
     static std::mutex mu;
     static EncodeTiledFn encode = nullptr;
@@ -41,23 +41,23 @@ int codes_tensor_map(const slim_cache_t *c, int box_rows, CUtensorMap *out)
         if (fn == nullptr || qres != cudaDriverEntryPointSuccess) return SLIM_ERR_UNSUPPORTED;
         encode = reinterpret_cast<EncodeTiledFn>(fn);
     }
-    const long long rows = (long long)c->num_pages * c->num_kv_heads * 2 * kPageTokens;
     for (int i = 0; i < used; ++i) {
-        if (cache[i].ptr == c->codes && cache[i].rows == rows && cache[i].box_rows == box_rows) {
+        if (cache[i].ptr == codes && cache[i].rows == rows && cache[i].row_bytes == row_bytes && cache[i].box_rows == box_rows) {
             *out = cache[i].map;
             return SLIM_OK;
         }
     }
     Entry e;
-    e.ptr = c->codes;
+    e.ptr = codes;
     e.rows = rows;
+    e.row_bytes = row_bytes;
     e.box_rows = box_rows;
-    const cuuint64_t dims[2] = {(cuuint64_t)kHeadDim, (cuuint64_t)rows};
-    const cuuint64_t strides[1] = {(cuuint64_t)kHeadDim};
-    const cuuint32_t box[2] = {(cuuint32_t)kHeadDim, (cuuint32_t)box_rows};
+    const cuuint64_t dims[2] = {(cuuint64_t)row_bytes, (cuuint64_t)rows};
+    const cuuint64_t strides[1] = {(cuuint64_t)row_bytes};
+    const cuuint32_t box[2] = {(cuuint32_t)row_bytes, (cuuint32_t)box_rows};
     const cuuint32_t estr[2] = {1, 1};
-    const CUresult r = encode(&e.map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<int8_t *>(c->codes), dims, strides, box,
-                              estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+    const CUresult r = encode(&e.map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, codes, dims, strides, box,
+                              estr, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
                               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     if (r != CUDA_SUCCESS) return SLIM_ERR_CUDA;
     cache[next] = e;
@@ -65,6 +65,16 @@ int codes_tensor_map(const slim_cache_t *c, int box_rows, CUtensorMap *out)
     if (used < kEntries) ++used;
     *out = e.map;
     return SLIM_OK;
+}
+
+int codes_tensor_map(const slim_cache_t *c, int box_rows, CUtensorMap *out)
+{
+    return rows_tensor_map(c->codes, (long long)c->num_pages * c->num_kv_heads * 2 * kPageTokens, kHeadDim, CU_TENSOR_MAP_SWIZZLE_128B, box_rows, out);
+}
+
+int codes4_tensor_map(const slim_cache4_t *c, int box_rows, CUtensorMap *out)
+{
+    return rows_tensor_map(c->codes, (long long)c->num_pages * c->num_kv_heads * 2 * kPageTokens, kHeadDim / 2, CU_TENSOR_MAP_SWIZZLE_64B, box_rows, out);
 }
 
 int sm_count(int *out)

@@ -188,6 +188,92 @@ class RotatedRun:
         self.weighed, self.placed = list(self.lens), list(self.lens)
 
 
+class SampledRun:
+    """The attention layers of a batch whose sequences fork and end, on caches of 4 bits (or 8) that share one pool of pages.
+
+    A step is advance() (room for the new tokens), then prompt() or step() for every layer; fork() lets rows continue, share
+    or end by parent, compact() moves the pages in use together.  Lengths are kept on the device and, for the launches'
+    bounds, here.  A pool without enough pages is a MemoryError, and nothing has changed then."""
+
+    def __init__(self, n_layers, Hq, Hkv, num_pages, rows, max_tokens, bits=4, device="cuda"):
+        self.Hq, self.Hkv, self.rows, self.bits, self.device = Hq, Hkv, rows, bits, torch.device(device)
+        stride = (max_tokens + PAGE_TOKENS - 1) // PAGE_TOKENS
+        self.max_tokens, self.sm_scale = stride * PAGE_TOKENS, slim.HEAD_DIM ** -0.5
+        kind = slim.SlimCache4 if bits == 4 else slim.SlimCache
+        self.caches = [kind(rows, Hkv, stride, device=device, num_pages=num_pages) for _ in range(n_layers)]
+        self.layers = slim.PageLayers(self.caches)
+        self.pages = slim.SlimPages.empty(num_pages, rows, stride, device)
+        # the other tables: a fork goes from one set to the other (the page counters are kept in place)
+        self.other = slim.SlimPages(self.pages.refs, self.pages.table.clone(), self.pages.held.clone())
+        self.lens = [-1] * rows      # -1: the row is empty
+        self.kv_len, self.len_other = self._i32(self.lens), self._i32(self.lens)
+        self.result = self._i32([0, 0])
+        self.ws_pages = slim.pages_workspace(num_pages, rows, device)
+        self.ws_prefill = slim.workspace(slim.PHASE_PREFILL, rows, Hq, Hkv, self.max_tokens, self.max_tokens, device=device)
+        self.ws_decode = slim.decode4_workspace(rows, Hq, Hkv, self.max_tokens, device) if bits == 4 else \
+            slim.workspace(slim.PHASE_DECODE, rows, Hq, Hkv, 1, self.max_tokens, device=device)
+        self._use_tables()
+
+    def _i32(self, values):
+        return torch.tensor(values, dtype=torch.int32, device=self.device)
+
+    def _use_tables(self):
+        for cache in self.caches:
+            cache.set_block_table(self.pages.table)
+
+    def _enough(self):
+        missing = int(self.result[0])
+        if missing:
+            raise MemoryError(f"{missing} pages are missing")
+
+    def advance(self, counts):
+        """The next counts[row] tokens of every row; a row that gets its first ones starts a sequence."""
+        if len(counts) != self.rows or min(counts) < 0:
+            raise ValueError("one count of new tokens per row")
+        lens = [max(n, 0) + c if c else n for n, c in zip(self.lens, counts)]
+        if max(lens) > self.max_tokens:
+            raise ValueError("a row is full")
+        kv_len = self._i32(lens)
+        slim.slim_pages_grow(self.pages, kv_len, 0, self.result, self.ws_pages)
+        self._enough()
+        self.counts, self.lens, self.kv_len = list(counts), lens, kv_len
+
+    def prompt(self, layer, q, k, v):
+        """Layer `layer` of the tokens that advance() announced, all rows' one after the other (q bf16 [tokens, Hq, 128], k and v [tokens, Hkv, 128])."""
+        cu = [0]
+        for c in self.counts:
+            cu.append(cu[-1] + c)
+        out = torch.empty_like(q)
+        fn = slim.slim_prefill4_step if self.bits == 4 else slim.slim_prefill_step
+        fn(self.caches[layer], q, k, v, out, self._i32(cu), self.kv_len, self.rows, max(self.counts), max(self.lens), self.Hq, self.sm_scale, self.ws_prefill)
+        return out
+
+    def step(self, layer, q, k, v):
+        """Layer `layer` of one new token in every row that is not empty (q bf16 [rows, Hq, 128], k and v [rows, Hkv, 128]); empty rows give zeros."""
+        out = torch.empty_like(q)
+        if self.bits == 4:
+            slim.slim_attn4_decode(self.caches[layer], q, out, self.kv_len, self.rows, max(self.lens), self.Hq, self.sm_scale, self.ws_decode, k_new=k, v_new=v)
+        else:
+            slim.slim_decode_step(self.caches[layer], q, k, v, out, self.kv_len, self.rows, max(self.lens), self.Hq, self.sm_scale, self.ws_decode)
+        return out
+
+    def fork(self, parents):
+        """Row i continues row parents[i]; -1 leaves it empty.  Rows that nobody continues are freed."""
+        if len(parents) != self.rows or not all(-1 <= p < self.rows for p in parents):
+            raise ValueError("one parent per row, -1 for none")
+        slim.slim_pages_fork(self.layers, self.pages, self.other, self._i32(parents), self.kv_len, self.len_other, self.result, self.ws_pages)
+        self._enough()
+        self.pages, self.other = self.other, self.pages
+        self.kv_len, self.len_other = self.len_other, self.kv_len
+        self.lens = [self.lens[p] if p >= 0 else -1 for p in parents]
+        self._use_tables()
+
+    def compact(self):
+        """Moves the pages in use together; returns how many there are."""
+        slim.slim_pages_compact(self.layers, self.pages, self.pages, self.result, self.ws_pages)
+        return int(self.result[0])
+
+
 def run_workload(w: Workload, device="cuda", decode_steps=None, block_table=None, num_pages=None, one_call_step=False):
     """The workload's full call sequence.  Returns (LayerRun, prefill outputs per sequence or None,
     {decode step: output [B, Hq, 128]}); decode_steps limits which steps' outputs are kept.  With one_call_step
