@@ -31,14 +31,14 @@
 
 namespace slim {
 
-constexpr int kD4Unit = 64;                        // tokens of a ring stage
-constexpr int kD4Warps = 8;
-constexpr int kD4Stages = 2;
+constexpr int kD4Unit = 64;                        // tokens whose scores a warp holds at a time
 constexpr uint32_t kD4CodeBytes = kD4Unit * kRow4Bytes;
 constexpr uint32_t kD4PairBytes = kD4Unit * 4;
-constexpr uint32_t kD4StageBytes = 2 * (kD4CodeBytes + kD4PairBytes);
+constexpr uint32_t kD4SlotBytes = 2 * (kD4CodeBytes + kD4PairBytes);   // a ring slot: a unit's K codes, V codes, then their (scale, offset) words
 constexpr float kD4Grow = 4.f;                     // the running maximum moves when it is exceeded by 2^4
 constexpr float kD4Top = 512.f;                    // p s is scaled so that the largest s counts as 2^9 to 2^10 (with p <= 2^4 far below fp16's 2^16)
+constexpr int kD4MaxBlocks = 256;
+constexpr int kD4Group = 8;                        // blocks whose records are merged first where a pair spans many
 
 struct Decode4Params {
     const uint8_t *codes;
@@ -48,24 +48,27 @@ struct Decode4Params {
     const __nv_bfloat16 *q, *k_new, *v_new;
     __nv_bfloat16 *out;
     int *status;
-    int *counters;      // per block: arrivals for the pair that begins in it and ends in a later one
+    int *counters;      // arrivals: per record slot for the group that it begins, then per block for the pair that begins in it
     float *parts;       // two records per block
     int B, Hq, Hkv, G, max_pages_per_seq, num_pages, cap_tokens;
     float scale_log2e;
 };
 
-// A pair's records: O [heads][128], then m [heads] and l [heads].
+// A record: O [heads][128], then m [heads] and l [heads].
 template <int NT>
 struct D4 {
+    static constexpr int kWarps = 8;
+    static constexpr int kSlots = 2;                         // of a warp's ring
     static constexpr int kHeads = 8 * NT;
     static constexpr int kRecFloats = kHeads * (kHeadDim + 2);
-    static constexpr uint32_t kRing = 0;
-    static constexpr uint32_t kFirst = kD4Warps * kD4Stages * kD4StageBytes;     // a warp's record of its first pair
-    static constexpr uint32_t kMeta = kFirst + kD4Warps * kRecFloats * 4;        // D4Run [2 * warps], then the block's [2]
-    static constexpr uint32_t kBars = kMeta + (2 * kD4Warps + 2) * 16;
-    static constexpr uint32_t kFlags = kBars + kD4Warps * kD4Stages * 8;         // int[4]
+    static constexpr uint32_t kRingBytes = kSlots * kD4SlotBytes;
+    static constexpr uint32_t kFirst = kWarps * kRingBytes;                      // records of the warps' first pairs
+    static constexpr uint32_t kMeta = kFirst + kWarps * kRecFloats * 4;          // D4Run [2 * warps], then the block's [2]
+    static constexpr uint32_t kBars = kMeta + (2 * kWarps + 2) * 32;
+    static constexpr uint32_t kFlags = (kBars + kWarps * kSlots * 8 + 15) / 16 * 16;   // int[4]
     static constexpr uint32_t kBytes = kFlags + 16;
-    static_assert(kRecFloats * 4 <= kD4Stages * kD4StageBytes, "a warp's last record goes into its ring");
+    static_assert(kRecFloats * 4 <= kRingBytes, "a warp's last record goes into its ring");
+    static_assert(2 * kWarps <= 32, "a warp's lanes look at all records of the block");
     static_assert(kBytes <= 232448, "shared memory of one block");
 };
 
@@ -73,12 +76,12 @@ struct D4 {
 struct __align__(16) D4Run {
     int pair, units;    // pair -1: nothing
     long long first;    // the pair's first unit in the order of all units
+    int at;             // the record's place in shared memory
 };
 
 __device__ __forceinline__ void d4_mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
 {
-    asm volatile(
-        "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};\n"
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};\n"
         : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
@@ -93,6 +96,13 @@ __device__ __forceinline__ float d4_exp2(float x)
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;\n" : "=f"(y) : "f"(x));
     return y;
+}
+// a 16-byte load that stays where it is written
+__device__ __forceinline__ uint4 ld_now(const uint4 *ptr)
+{
+    uint4 v;
+    asm volatile("ld.global.nc.v4.u32 {%0, %1, %2, %3}, [%4];\n" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(ptr));
+    return v;
 }
 __device__ __forceinline__ float d4_max_rows(float v)   // over the lanes that hold other rows of the same columns
 {
@@ -194,49 +204,93 @@ __device__ __forceinline__ void d4_store(__nv_bfloat16 *dst, float4 o)
     *reinterpret_cast<uint2 *>(dst) = make_uint2(*reinterpret_cast<const uint32_t *>(&a), *reinterpret_cast<const uint32_t *>(&b));
 }
 
-// A record's share of a merge: O and l relative to the largest maximum so far (a lane owns four dims of one head).
-struct D4Merge {
-    float m = -INFINITY, l = 0.f;
-    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-    __device__ __forceinline__ void add(float m1, float l1, float4 o1)
-    {
-        const float M = fmaxf(m, m1);
-        const float f = (m == M) ? 1.f : exp2f(m - M), f1 = (m1 == M) ? 1.f : exp2f(m1 - M);
-        m = M;
-        l = l * f + l1 * f1;
-        o.x = o.x * f + o1.x * f1;
-        o.y = o.y * f + o1.y * f1;
-        o.z = o.z * f + o1.z * f1;
-        o.w = o.w * f + o1.w * f1;
-    }
+// Log-sum-exp merge of the records x = 0 .. n - 1 (those that `in` names) of head h by one warp; a lane owns four dims.
+// The largest maximum and the weights are found with a record per lane, the outputs are added up in record order.
+struct D4Merged {
+    float m, l;
+    float4 o;
     __device__ __forceinline__ void write(__nv_bfloat16 *dst) const
     {
         const float inv = (l > 0.f) ? 1.f / l : 0.f;
         d4_store(dst, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
     }
 };
+template <int kHeads, bool kGlobal, class In, class Rec>
+__device__ __forceinline__ D4Merged d4_merge(int n, int h, int lane, In in, Rec rec)
+{
+    constexpr int kBatch = kGlobal ? 8 : 4;
+    D4Merged r{-INFINITY, 0.f, make_float4(0.f, 0.f, 0.f, 0.f)};
+    for (int x0 = 0; x0 < n; x0 += 32) {
+        const int x = x0 + lane;
+        const bool mine = x < n && in(x);
+        const float *at = rec(mine ? x : 0) + kHeads * kHeadDim + h;
+        float m = -INFINITY, l = 0.f;
+        if (mine) m = kGlobal ? __ldcg(at) : at[0], l = kGlobal ? __ldcg(at + kHeads) : at[kHeads];
+        const float top = fmaxf(r.m, warp_max(m));
+        const float f = (r.m == -INFINITY) ? 0.f : exp2f(r.m - top), w = (m == -INFINITY) ? 0.f : exp2f(m - top);
+        r.m = top;
+        r.l = r.l * f + w * l;
+        r.o = make_float4(r.o.x * f, r.o.y * f, r.o.z * f, r.o.w * f);
+        unsigned todo = __ballot_sync(0xffffffffu, mine);
+        while (todo != 0u) {
+            float4 v[kBatch];
+            int who[kBatch];
+#pragma unroll
+            for (int u = 0; u < kBatch; ++u) {
+                who[u] = (todo != 0u) ? __ffs(todo) - 1 : -1;
+                todo &= todo - 1;
+                v[u] = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (who[u] >= 0) {
+                    const float4 *src = reinterpret_cast<const float4 *>(rec(x0 + who[u]) + h * kHeadDim) + lane;
+                    v[u] = kGlobal ? __ldcg(src) : *src;
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < kBatch; ++u) {
+                const float wu = __shfl_sync(0xffffffffu, w, max(who[u], 0));
+                if (who[u] < 0) continue;
+                r.o.x = fmaf(v[u].x, wu, r.o.x);
+                r.o.y = fmaf(v[u].y, wu, r.o.y);
+                r.o.z = fmaf(v[u].z, wu, r.o.z);
+                r.o.w = fmaf(v[u].w, wu, r.o.w);
+            }
+        }
+    }
+    r.l = warp_sum(r.l);
+    return r;
+}
+template <int kHeads>
+__device__ __forceinline__ void d4_put(float *part, int h, int lane, const D4Merged &r)
+{
+    __stcg(reinterpret_cast<float4 *>(part + h * kHeadDim) + lane, r.o);
+    if (lane == 0) {
+        __stcg(part + kHeads * kHeadDim + h, r.m);
+        __stcg(part + kHeads * (kHeadDim + 1) + h, r.l);
+    }
+}
 
 template <int NT, bool kStep>
-__global__ void __launch_bounds__(kD4Warps * 32, 1)
+__global__ void __launch_bounds__(D4<NT>::kWarps * 32, 1)
 slim4_decode_kernel(const Decode4Params p)
 {
     using L = D4<NT>;
+    constexpr int NW = L::kWarps, S = L::kSlots;
     extern __shared__ __align__(1024) unsigned char smem[];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
     const uint32_t sbase = smem_u32(smem);
     D4Run *runs = reinterpret_cast<D4Run *>(smem + L::kMeta);
-    volatile int *flags = reinterpret_cast<volatile int *>(smem + L::kFlags);   // [0]: a wait ran out; [1], [2]: this block merges its first, last pair
-    const uint32_t ring = sbase + L::kRing + warp * (kD4Stages * kD4StageBytes);
-    auto bar = [&](int s) { return sbase + L::kBars + 8u * (uint32_t)(warp * kD4Stages + s); };
+    volatile int *flags = reinterpret_cast<volatile int *>(smem + L::kFlags);   // [0]: a wait ran out; [1], [2]: what is left to merge of the block's first, last pair
+    const uint32_t ring = warp * L::kRingBytes;
+    auto bar = [&](int s) { return sbase + L::kBars + 8u * (uint32_t)(warp * S + s); };
 
     pdl_launch_dependents();
     if (lane == 0) {
-        for (int s = 0; s < kD4Stages; ++s) tc::mbar_init(bar(s), 1);
+        for (int s = 0; s < S; ++s) tc::mbar_init(bar(s), 1);
         tc::mbar_init_fence();
         runs[2 * warp].pair = runs[2 * warp + 1].pair = -1;
         if (warp == 0) {
             flags[0] = flags[1] = flags[2] = 0;
-            runs[2 * kD4Warps].pair = runs[2 * kD4Warps + 1].pair = -1;
+            runs[2 * NW].pair = runs[2 * NW + 1].pair = -1;
         }
     }
     __syncthreads();
@@ -244,60 +298,76 @@ slim4_decode_kernel(const Decode4Params p)
 
     // ---- this warp's range of units
     const long long U = d4_total(p, lane);
-    const long long W = (long long)gridDim.x * kD4Warps, gw = (long long)blockIdx.x * kD4Warps + warp;
+    const long long W = (long long)gridDim.x * NW, gw = (long long)blockIdx.x * NW + warp;
     const long long u0 = d4_div(U * gw, W), u1 = d4_div(U * (gw + 1), W);
     const int cnt = (int)(u1 - u0);
     bool ok = true;
-    int issued = 0;
     if (cnt > 0) {
         D4Walk w = d4_find(p, lane, u0), ahead = w;
-        int page_next = __ldg(p.block_table + (size_t)ahead.b * p.max_pages_per_seq + (ahead.unit >> 1));
-        // asks for the unit `ahead` stands on and steps ahead (the next page id is on its way while this unit's copies are)
-        auto issue = [&]() {
-            const int s = issued % kD4Stages;
-            const int n_tok = min(kD4Unit, ahead.len - ahead.unit * kD4Unit);
-            const int page = (page_next >= 0 && page_next < p.num_pages) ? page_next : 0;
-            const int head = ahead.head, slot = (ahead.unit & 1) * kD4Unit;
-            ++issued;
-            if (issued < cnt) {
-                ahead.next(p);
-                page_next = __ldg(p.block_table + (size_t)ahead.b * p.max_pages_per_seq + (ahead.unit >> 1));
-            }
-            if (lane == 0) {
-                const uint32_t dst = ring + s * kD4StageBytes;
-                const uint32_t code_bytes = (uint32_t)n_tok * kRow4Bytes, pair_bytes = (uint32_t)((n_tok + 3) & ~3) * 4u;
-                const uint8_t *c = p.codes + code4_block_offset(page, head, 0, p.Hkv) + (size_t)slot * kRow4Bytes;
-                const uint32_t *sc = p.pairs + scale_block_offset(page, head, 0, p.Hkv) + slot;
+        // ---- lane 0 asks for the units, one after the other, each into slot n mod kSlots
+        const bool asks = lane == 0;
+        int asked = 0, page_next = 0;
+        if (asks) page_next = __ldg(p.block_table + (size_t)ahead.b * p.max_pages_per_seq + (ahead.unit >> 1));
+        auto ask = [&]() {
+            const int s = asked % S;
+            if (asks) {
+                const int page = (page_next >= 0 && page_next < p.num_pages) ? page_next : 0;
+                const size_t row0 = ((size_t)((size_t)page * p.Hkv + ahead.head) * 2) * kPageTokens + (ahead.unit & 1) * kD4Unit;
+                const uint32_t n_tok = (uint32_t)min(kD4Unit, ahead.len - ahead.unit * kD4Unit);
+                const uint32_t dst = sbase + ring + s * kD4SlotBytes, code_bytes = n_tok * kRow4Bytes, pair_bytes = ((n_tok + 3) & ~3u) * 4u;
+                const uint8_t *codes = p.codes + row0 * kRow4Bytes;
+                const uint32_t *pairs = p.pairs + row0;
                 tc::mbar_arrive_expect_tx(bar(s), 2 * (code_bytes + pair_bytes));
-                tc::bulk_load(dst, c, code_bytes, bar(s));
-                tc::bulk_load(dst + 2 * kD4CodeBytes, sc, pair_bytes, bar(s));
-                tc::bulk_load(dst + kD4CodeBytes, c + kPageTokens * kRow4Bytes, code_bytes, bar(s));
-                tc::bulk_load(dst + 2 * kD4CodeBytes + kD4PairBytes, sc + kPageTokens, pair_bytes, bar(s));
+                tc::bulk_load(dst, codes, code_bytes, bar(s));
+                tc::bulk_load(dst + 2 * kD4CodeBytes, pairs, pair_bytes, bar(s));
+                tc::bulk_load(dst + kD4CodeBytes, codes + kPageTokens * kRow4Bytes, code_bytes, bar(s));
+                tc::bulk_load(dst + 2 * kD4CodeBytes + kD4PairBytes, pairs + kPageTokens, pair_bytes, bar(s));
+                if (asked + 1 < cnt) {   // (the next unit's page id is on its way while this unit's copies are)
+                    const int b_before = ahead.b;
+                    const bool same = (ahead.unit & 1) == 0;
+                    ahead.next(p);
+                    if (!same || ahead.unit == 0 || ahead.b != b_before)
+                        page_next = __ldg(p.block_table + (size_t)ahead.b * p.max_pages_per_seq + (ahead.unit >> 1));
+                }
+            }
+            ++asked;
+        };
+        // the query rows of the pair that starts with the next unit, as they are.  They are requested before the copies that
+        // fill the ring: a load behind those would wait until memory has delivered them
+        uint4 qraw[NT][4];
+        auto load_q = [&](int b, int head) {
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                const int h = nt * 8 + g;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) qraw[nt][i] = make_uint4(0, 0, 0, 0);
+                if (h < p.G) {
+                    const uint4 *src = reinterpret_cast<const uint4 *>(p.q + ((size_t)b * p.Hq + (size_t)head * p.G + h) * kHeadDim);
+                    qraw[nt][0] = ld_now(src + 2 * t), qraw[nt][1] = ld_now(src + 2 * t + 1);
+                    qraw[nt][2] = ld_now(src + 8 + 2 * t), qraw[nt][3] = ld_now(src + 9 + 2 * t);
+                }
             }
         };
-        for (int i = 0; i < min(kD4Stages, cnt); ++i) issue();
+        load_q(w.b, w.head);
+        for (int i = 0; i < min(S, cnt); ++i) ask();
 
         uint32_t qf[NT][8][2];                  // Q^T operands: dims 16 t + 4 j .. (even steps), 64 further (odd steps)
         float rs[NT][2], qz[NT][2];             // of the columns 2 t, 2 t + 1: what a product and a row's offset count for
         float o[NT][8][4];                      // O^T: dim 8 g + i (first two), 64 + 8 g + i, of the columns 2 t, 2 t + 1
         float m[NT][2], l[NT][2], z[NT][2];     // running maximum; this lane's share of sum p and sum p z
-        float r_cur = 0.f;                      // what the scales are multiplied with in P^T
+        float r_cur = 0.f;                      // what the scales are multiplied with in P^T (0: nothing of the pair seen yet)
         bool fresh = true;
         int run_index = 0, run_unit0 = w.unit;
+        const int row = g ^ ((g >> 1) & 1);     // token of this lane's row: neighbouring rows lie in opposite halves of the banks
+        const int k_off = row * kRow4Bytes + t * 16;
+        const int v_off0 = (2 * t ^ (t & 1)) * kRow4Bytes + 8 * g, v_off1 = ((2 * t + 1) ^ (t & 1)) * kRow4Bytes + 8 * g;
 
         for (int n = 0; n < cnt; ++n) {
             if (fresh) {
                 fresh = false;
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
-                    const int h = nt * 8 + g;
-                    uint4 v[4];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) v[i] = make_uint4(0, 0, 0, 0);
-                    if (h < p.G) {
-                        const uint4 *src = reinterpret_cast<const uint4 *>(p.q + ((size_t)w.b * p.Hq + (size_t)w.head * p.G + h) * kHeadDim);
-                        v[0] = __ldg(src + 2 * t), v[1] = __ldg(src + 2 * t + 1), v[2] = __ldg(src + 8 + 2 * t), v[3] = __ldg(src + 9 + 2 * t);
-                    }
+                    const uint4 (&v)[4] = qraw[nt];
                     float am = 0.f, sum = 0.f;
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
@@ -331,117 +401,148 @@ slim4_decode_kernel(const Decode4Params p)
                     for (int k = 0; k < 2; ++k) {
                         rs[nt][k] = __shfl_sync(0xffffffffu, mine, 8 * t + 4 * k);
                         qz[nt][k] = __shfl_sync(0xffffffffu, sz, 8 * t + 4 * k);
-                        m[nt][k] = -INFINITY;
-                        l[nt][k] = z[nt][k] = 0.f;
+                        m[nt][k] = l[nt][k] = z[nt][k] = 0.f;
                     }
 #pragma unroll
                     for (int i = 0; i < 8; ++i) o[nt][i][0] = o[nt][i][1] = o[nt][i][2] = o[nt][i][3] = 0.f;
                 }
                 r_cur = 0.f;
             }
-            const int s = n % kD4Stages;
             const int n_tok = min(kD4Unit, w.len - w.unit * kD4Unit);
-            if (!tc::mbar_wait(bar(s), (uint32_t)(n / kD4Stages) & 1u, ok ? (1u << 18) : 1u, flags)) {
+            const bool ends = w.unit == w.units - 1;                            // the pair's last unit
+            const bool complete = ends && run_unit0 == 0;
+            const bool leaves = (ends && !complete) || (n == cnt - 1 && !ends); // a record is left behind this unit
+            if (ends && n + 1 < cnt) {   // the next pair's query rows, a unit ahead
+                D4Walk next = w;
+                next.next(p);
+                load_q(next.b, next.head);
+            }
+            const int slot = n % S;
+            if (!tc::mbar_wait(bar(slot), (uint32_t)(n / S) & 1u, ok ? (1u << 18) : 1u, flags)) {
                 ok = false;
                 flags[0] = 1;
             }
             __syncwarp();
-            unsigned char *stage = smem + L::kRing + (warp * kD4Stages + s) * kD4StageBytes;
-            if (kStep && ok && w.unit == w.units - 1 && __ldg(p.kv_len + w.b) == w.len) {
+            unsigned char *kst = smem + ring + slot * kD4SlotBytes, *vst = kst + kD4CodeBytes;
+            uint32_t *kp = reinterpret_cast<uint32_t *>(kst + 2 * kD4CodeBytes), *vp = kp + kD4Unit;
+
+            if (kStep && ends && ok && __ldg(p.kv_len + w.b) == w.len) {
                 // ---- the new token: quantised here, stored in the cache and in the unit's copy of it
-                const int kv = lane >> 4, i = lane & 15, row = n_tok - 1, pos = w.len - 1;
+                const int kv = lane >> 4, i = lane & 15, at = n_tok - 1, pos = w.len - 1;
                 uint32_t codes, pair;
                 d4_quantise((kv ? p.v_new : p.k_new) + ((size_t)w.b * p.Hkv + w.head) * kHeadDim, i, codes, pair);
-                reinterpret_cast<uint32_t *>(stage + kv * kD4CodeBytes + row * kRow4Bytes)[i] = codes;
-                if (i == 0) reinterpret_cast<uint32_t *>(stage + 2 * kD4CodeBytes + kv * kD4PairBytes)[row] = pair;
+                reinterpret_cast<uint32_t *>(kst + kv * kD4CodeBytes + at * kRow4Bytes)[i] = codes;
+                if (i == 0) kp[kv * kD4Unit + at] = pair;
                 const int page = __ldg(p.block_table + (size_t)w.b * p.max_pages_per_seq + (pos >> 7));
                 if (page >= 0 && page < p.num_pages) {
-                    const int slot = pos & (kPageTokens - 1);
-                    uint8_t *dst = const_cast<uint8_t *>(p.codes) + code4_block_offset(page, w.head, kv, p.Hkv) + (size_t)slot * kRow4Bytes;
+                    const int in_page = pos & (kPageTokens - 1);
+                    uint8_t *dst = const_cast<uint8_t *>(p.codes) + code4_block_offset(page, w.head, kv, p.Hkv) + (size_t)in_page * kRow4Bytes;
                     reinterpret_cast<uint32_t *>(dst)[i] = codes;
-                    if (i == 0) const_cast<uint32_t *>(p.pairs)[scale_block_offset(page, w.head, kv, p.Hkv) + slot] = pair;
+                    if (i == 0) const_cast<uint32_t *>(p.pairs)[scale_block_offset(page, w.head, kv, p.Hkv) + in_page] = pair;
                 }
-                tc::fence_proxy_async();   // (the stage is filled by the copy engine again)
+                tc::fence_proxy_async();   // (the slot is filled by the copy engine again)
                 __syncwarp();
             }
-            const uint32_t *kp = reinterpret_cast<const uint32_t *>(stage + 2 * kD4CodeBytes), *vp = kp + kD4Unit;
-            const int row = g ^ ((g >> 1) & 1);           // token of this lane's row: neighbouring rows lie in opposite halves of the banks
-            const bool whole = n_tok == kD4Unit;
+            if (n_tok < kD4Unit) {   // what lies behind the last token may be anything: words of zero
+                if (lane + 32 >= n_tok) kp[lane + 32] = vp[lane + 32] = 0u;
+                if (lane >= n_tok) kp[lane] = vp[lane] = 0u;
+                tc::fence_proxy_async();
+                __syncwarp();
+            }
 
-            // ---- S^T = K Q^T: rows g and g + 8 of every 16 tokens
+            // ---- S^T = K Q^T: rows g and g + 8 of every 16 tokens; then the scores less the running maximum
+            //      (a tile's eight products form a chain: the four tiles' chains are issued in turn)
             float c[4][NT][4];
+            uint32_t ka[4][4], kb[4][4];
 #pragma unroll
             for (int mt = 0; mt < 4; ++mt) {
+                const uint4 a4 = *reinterpret_cast<const uint4 *>(kst + k_off + mt * 16 * kRow4Bytes);
+                const uint4 b4 = *reinterpret_cast<const uint4 *>(kst + k_off + (mt * 16 + 8) * kRow4Bytes);
+                ka[mt][0] = a4.x, ka[mt][1] = a4.y, ka[mt][2] = a4.z, ka[mt][3] = a4.w;
+                kb[mt][0] = b4.x, kb[mt][1] = b4.y, kb[mt][2] = b4.z, kb[mt][3] = b4.w;
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) c[mt][nt][0] = c[mt][nt][1] = c[mt][nt][2] = c[mt][nt][3] = 0.f;
-                if (mt * 16 < n_tok) {
-                    const uint4 a4 = *reinterpret_cast<const uint4 *>(stage + (mt * 16 + row) * kRow4Bytes + t * 16);
-                    const uint4 b4 = *reinterpret_cast<const uint4 *>(stage + (mt * 16 + 8 + row) * kRow4Bytes + t * 16);
-                    const uint32_t a[4] = {a4.x, a4.y, a4.z, a4.w}, b[4] = {b4.x, b4.y, b4.z, b4.w};
+            }
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const uint32_t a8 = a[j] >> 8, b8 = b[j] >> 8;
+            for (int j = 0; j < 4; ++j) {
+#pragma unroll
+                for (int mt = 0; mt < 4; ++mt) {
+                    const uint32_t a = ka[mt][j], b = kb[mt][j], a8 = a >> 8, b8 = b >> 8;
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+                        d4_mma(c[mt][nt], a & 0x000F000Fu, b & 0x000F000Fu, a8 & 0x000F000Fu, b8 & 0x000F000Fu, qf[nt][2 * j][0], qf[nt][2 * j][1]);
+                }
+#pragma unroll
+                for (int mt = 0; mt < 4; ++mt) {
+                    const uint32_t a = ka[mt][j], b = kb[mt][j], a8 = a >> 8, b8 = b >> 8;
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+                        d4_mma(c[mt][nt], a & 0x00F000F0u, b & 0x00F000F0u, a8 & 0x00F000F0u, b8 & 0x00F000F0u, qf[nt][2 * j + 1][0], qf[nt][2 * j + 1][1]);
+                }
+            }
+            float top[NT][2];
+            {
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) top[nt][0] = top[nt][1] = -INFINITY;
+#pragma unroll
+                for (int mt = 0; mt < 4; ++mt) {
+#pragma unroll
+                    for (int hf = 0; hf < 2; ++hf) {
+                        const uint32_t k2 = kp[mt * 16 + hf * 8 + row];
+                        const float sk = pair_scale(k2), zk = pair_offset(k2);
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt) {
-                            d4_mma(c[mt][nt], a[j] & 0x000F000Fu, b[j] & 0x000F000Fu, a8 & 0x000F000Fu, b8 & 0x000F000Fu, qf[nt][2 * j][0], qf[nt][2 * j][1]);
-                            d4_mma(c[mt][nt], a[j] & 0x00F000F0u, b[j] & 0x00F000F0u, a8 & 0x00F000F0u, b8 & 0x00F000F0u, qf[nt][2 * j + 1][0], qf[nt][2 * j + 1][1]);
+#pragma unroll
+                            for (int k = 0; k < 2; ++k) c[mt][nt][2 * hf + k] = fmaf(c[mt][nt][2 * hf + k], sk * rs[nt][k], fmaf(zk, qz[nt][k], -m[nt][k]));
                         }
                     }
                 }
-            }
-            // ---- scores, their maxima, the largest V scale
-            float mt_max[NT][2], sv_max = 0.f;
-            float sv[4][2], zv[4][2];
+                if (n_tok < kD4Unit) {
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) mt_max[nt][0] = mt_max[nt][1] = -INFINITY;
+                    for (int mt = 0; mt < 4; ++mt) {
 #pragma unroll
-            for (int mt = 0; mt < 4; ++mt) {
+                        for (int hf = 0; hf < 2; ++hf) {
+                            if (mt * 16 + hf * 8 + row < n_tok) continue;
 #pragma unroll
-                for (int hf = 0; hf < 2; ++hf) {
-                    const int tok = mt * 16 + hf * 8 + row;
-                    const bool seen = whole || tok < n_tok;   // (what lies behind the last token may be anything)
-                    const uint32_t k2 = seen ? kp[tok] : 0u, v2 = seen ? vp[tok] : 0u;
-                    const float sk = pair_scale(k2), zk = pair_offset(k2);
-                    sv[mt][hf] = pair_scale(v2), zv[mt][hf] = pair_offset(v2);
-                    sv_max = fmaxf(sv_max, sv[mt][hf]);
+                            for (int nt = 0; nt < NT; ++nt) c[mt][nt][2 * hf] = c[mt][nt][2 * hf + 1] = -INFINITY;
+                        }
+                    }
+                }
+#pragma unroll
+                for (int mt = 0; mt < 4; ++mt) {
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
-                        for (int k = 0; k < 2; ++k) {
-                            const float x = fmaf(c[mt][nt][2 * hf + k], sk * rs[nt][k], zk * qz[nt][k]);
-                            c[mt][nt][2 * hf + k] = seen ? x : -INFINITY;
-                            mt_max[nt][k] = fmaxf(mt_max[nt][k], c[mt][nt][2 * hf + k]);
-                        }
+                        for (int k = 0; k < 2; ++k) top[nt][k] = fmaxf(top[nt][k], fmaxf(c[mt][nt][k], c[mt][nt][2 + k]));
                     }
                 }
             }
-            bool grow = false;
+            // ---- a larger maximum, a much larger V scale (rarely, but for the pair's first unit)
+            bool grow = r_cur == 0.f;
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-#pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    mt_max[nt][k] = d4_max_rows(mt_max[nt][k]);
-                    grow |= mt_max[nt][k] > m[nt][k] + kD4Grow;
-                }
-            }
-            sv_max = d4_max_rows(sv_max);
-            grow |= sv_max * r_cur >= 4.f * kD4Top || r_cur == 0.f;
+            for (int nt = 0; nt < NT; ++nt) grow |= fmaxf(top[nt][0], top[nt][1]) > kD4Grow;
+            const uint2 v2 = *reinterpret_cast<const uint2 *>(vp + 2 * lane);
+            const float sv_max = fmaxf(pair_scale(v2.x), pair_scale(v2.y));
+            grow |= sv_max * r_cur >= 4.f * kD4Top;
             if (__any_sync(0xffffffffu, grow)) {
-                const float top = (r_cur == 0.f) ? sv_max : fmaxf(sv_max, 0.f);
-                const float r_new = (r_cur == 0.f || sv_max * r_cur >= 4.f * kD4Top) ? pow2_recip(pow2_floor(top)) * kD4Top : r_cur;
-                const float fr = (r_cur == 0.f) ? 0.f : r_new / r_cur;
+                const bool first = r_cur == 0.f;
+                const float sv_top = warp_max(sv_max);
+                const float r_new = (first || sv_top * r_cur >= 4.f * kD4Top) ? pow2_recip(pow2_floor(sv_top)) * kD4Top : r_cur;
+                const float fr = first ? 0.f : r_new / r_cur;
                 r_cur = r_new;
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
                     float al[2];
 #pragma unroll
                     for (int k = 0; k < 2; ++k) {
-                        const float m_new = fmaxf(m[nt][k], mt_max[nt][k]);
-                        al[k] = d4_exp2(m[nt][k] - m_new);
-                        m[nt][k] = m_new;
+                        const float up = first ? d4_max_rows(top[nt][k]) : fmaxf(d4_max_rows(top[nt][k]), 0.f);
+                        m[nt][k] += up;
+                        al[k] = first ? 0.f : d4_exp2(-up);
                         l[nt][k] *= al[k];
                         z[nt][k] *= al[k];
                         al[k] *= fr;
+#pragma unroll
+                        for (int mt = 0; mt < 4; ++mt) c[mt][nt][k] -= up, c[mt][nt][2 + k] -= up;
                     }
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
@@ -452,29 +553,31 @@ slim4_decode_kernel(const Decode4Params p)
                     }
                 }
             }
-            // ---- P^T, and O^T += V^T P^T
+            // ---- P^T of all four tiles, then O^T += V^T P^T
+            uint32_t pt[4][NT][2];
 #pragma unroll
             for (int mt = 0; mt < 4; ++mt) {
-                if (mt * 16 >= n_tok) continue;
-                uint32_t b[NT][2];
 #pragma unroll
                 for (int hf = 0; hf < 2; ++hf) {
-                    const float sr = sv[mt][hf] * r_cur;
+                    const uint32_t pair = vp[mt * 16 + hf * 8 + row];
+                    const float sr = pair_scale(pair) * r_cur, zv = pair_offset(pair);
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt) {
                         float e[2];
 #pragma unroll
                         for (int k = 0; k < 2; ++k) {
-                            e[k] = d4_exp2(c[mt][nt][2 * hf + k] - m[nt][k]);
+                            e[k] = d4_exp2(c[mt][nt][2 * hf + k]);
                             l[nt][k] += e[k];
-                            z[nt][k] = fmaf(e[k], zv[mt][hf], z[nt][k]);
+                            z[nt][k] = fmaf(e[k], zv, z[nt][k]);
                         }
-                        b[nt][hf] = d4_transpose(pack_half2(e[0] * sr, e[1] * sr));
+                        pt[mt][nt][hf] = d4_transpose(pack_half2(e[0] * sr, e[1] * sr));
                     }
                 }
+            }
+#pragma unroll
+            for (int mt = 0; mt < 4; ++mt) {
                 // token rows 2 t and 2 t + 1 (this lane's column pair of the operand) and the two eight further
-                const unsigned char *v0 = stage + kD4CodeBytes + (mt * 16 + (2 * t ^ (t & 1))) * kRow4Bytes + 8 * g;
-                const unsigned char *v1 = stage + kD4CodeBytes + (mt * 16 + ((2 * t + 1) ^ (t & 1))) * kRow4Bytes + 8 * g;
+                const unsigned char *v0 = vst + v_off0 + mt * 16 * kRow4Bytes, *v1 = vst + v_off1 + mt * 16 * kRow4Bytes;
                 const uint2 va = *reinterpret_cast<const uint2 *>(v0), vb = *reinterpret_cast<const uint2 *>(v1);
                 const uint2 vc = *reinterpret_cast<const uint2 *>(v0 + 8 * kRow4Bytes), vd = *reinterpret_cast<const uint2 *>(v1 + 8 * kRow4Bytes);
 #pragma unroll
@@ -487,22 +590,20 @@ slim4_decode_kernel(const Decode4Params p)
                         const int i = 4 * w2 + 2 * half;
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt) {
-                            d4_mma(o[nt][i], x & 0x000F000Fu, x & 0x00F000F0u, y & 0x000F000Fu, y & 0x00F000F0u, b[nt][0], b[nt][1]);
-                            d4_mma(o[nt][i + 1], x8 & 0x000F000Fu, x8 & 0x00F000F0u, y8 & 0x000F000Fu, y8 & 0x00F000F0u, b[nt][0], b[nt][1]);
+                            d4_mma(o[nt][i], x & 0x000F000Fu, x & 0x00F000F0u, y & 0x000F000Fu, y & 0x00F000F0u, pt[mt][nt][0], pt[mt][nt][1]);
+                            d4_mma(o[nt][i + 1], x8 & 0x000F000Fu, x8 & 0x00F000F0u, y8 & 0x000F000Fu, y8 & 0x00F000F0u, pt[mt][nt][0], pt[mt][nt][1]);
                         }
                     }
                 }
             }
-            __syncwarp();              // every lane has read the stage
-            if (issued < cnt) issue();
+            __syncwarp();              // every lane has read the slot
+            if (asked < cnt) ask();
 
             // ---- the end of the pair, or of the range
-            const bool ends = w.unit == w.units - 1;
-            if (ends || n == cnt - 1) {
-                const bool complete = ends && run_unit0 == 0;
+            if (complete || leaves) {
                 const float f1 = 16777216.f / r_cur, f2 = f1 * 0.0625f;    // the codes counted 2^-24 and 2^-20
-                float *rec = reinterpret_cast<float *>(run_index == 0 ? smem + L::kFirst + warp * L::kRecFloats * 4
-                                                                      : smem + L::kRing + warp * (kD4Stages * kD4StageBytes));
+                const uint32_t at = (run_index == 0) ? L::kFirst + warp * L::kRecFloats * 4 : ring;   // (the last record: nothing is in flight)
+                float *rec = reinterpret_cast<float *>(smem + at);
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
@@ -536,11 +637,12 @@ slim4_decode_kernel(const Decode4Params p)
                         }
                     }
                 }
-                if (!complete && lane == 0 && ok) {
+                if (leaves && lane == 0 && ok) {
                     D4Run &run = runs[2 * warp + (run_index == 0 ? 0 : 1)];
                     run.pair = w.b * p.Hkv + w.head;
                     run.units = w.units;
                     run.first = u0 + n - w.unit;
+                    run.at = (int)at;
                 }
                 ++run_index;
                 run_unit0 = 0;
@@ -549,14 +651,14 @@ slim4_decode_kernel(const Decode4Params p)
             if (n + 1 < cnt) w.next(p);
         }
         if (!ok) {   // copies still in flight get a bounded chance to land
-            for (int i = max(0, issued - kD4Stages); i < issued; ++i) tc::mbar_wait(bar(i % kD4Stages), (uint32_t)(i / kD4Stages) & 1u, 1u << 14);
+            for (int i = max(0, asked - S); i < asked; ++i) tc::mbar_wait(bar(i % S), (uint32_t)(i / S) & 1u, 1u << 14);
         }
     }
     // sequences without tokens: zeros
     for (int b = blockIdx.x; b < p.B; b += gridDim.x) {
         if (d4_len(p, b) != 0) continue;
         uint4 *dst = reinterpret_cast<uint4 *>(p.out + (size_t)b * p.Hq * kHeadDim);
-        for (int i = tid; i < p.Hq * (kHeadDim / 8); i += kD4Warps * 32) dst[i] = make_uint4(0, 0, 0, 0);
+        for (int i = tid; i < p.Hq * (kHeadDim / 8); i += NW * 32) dst[i] = make_uint4(0, 0, 0, 0);
     }
     __syncthreads();
     if (flags[0] != 0) {
@@ -564,78 +666,97 @@ slim4_decode_kernel(const Decode4Params p)
         return;
     }
 
-    // ---- records of the block's warps, in the order of the units: consecutive ones of one pair are merged
+    // ---- records of the block's warps, in the order of the units: those of one pair are merged
     const long long block0 = d4_div(U * blockIdx.x, gridDim.x), block1 = d4_div(U * (blockIdx.x + 1), gridDim.x);
-    auto record = [&](int e) {
-        return reinterpret_cast<const float *>((e & 1) ? smem + L::kRing + (e >> 1) * (kD4Stages * kD4StageBytes)
-                                                       : smem + L::kFirst + (e >> 1) * L::kRecFloats * 4);
+    auto out_row = [&](const D4Run &run, int h) {
+        return p.out + ((size_t)(run.pair / p.Hkv) * p.Hq + (size_t)(run.pair % p.Hkv) * p.G + h) * kHeadDim + 4 * lane;
     };
-    int task = 0, prev = -1;
-    for (int e = 0; e < 2 * kD4Warps; ++e) {
+    auto part_of = [&](int block, int slot) { return p.parts + ((size_t)block * 2 + slot) * L::kRecFloats; };
+    const int my_pair = (lane < 2 * NW) ? runs[lane].pair : -1;
+    unsigned left = __ballot_sync(0xffffffffu, my_pair >= 0);
+    int task = 0;
+    while (left != 0u) {
+        const int e = __ffs(left) - 1;
         const D4Run run = runs[e];
-        if (run.pair < 0 || run.pair == prev) continue;
-        prev = run.pair;
+        const unsigned same = __ballot_sync(0xffffffffu, my_pair == run.pair);
+        left &= ~same;
         const bool complete = run.first >= block0 && run.first + run.units <= block1;
         const int which = (run.first <= block0) ? 0 : 1;   // (of an incomplete one: the pair at the block's start, or at its end)
-        float *part = p.parts + ((size_t)blockIdx.x * 2 + which) * L::kRecFloats;
         for (int h = 0; h < p.G; ++h) {
-            if (task++ % kD4Warps != warp) continue;
-            D4Merge acc;
-            for (int x = e; x < 2 * kD4Warps; ++x) {
-                if (runs[x].pair != run.pair) {
-                    if (runs[x].pair >= 0) break;
-                    continue;
-                }
-                const float *rec = record(x);
-                acc.add(rec[L::kHeads * kHeadDim + h], rec[L::kHeads * (kHeadDim + 1) + h], reinterpret_cast<const float4 *>(rec + h * kHeadDim)[lane]);
-            }
-            if (complete) {
-                acc.write(p.out + ((size_t)(run.pair / p.Hkv) * p.Hq + (size_t)(run.pair % p.Hkv) * p.G + h) * kHeadDim + 4 * lane);
-            } else {
-                __stcg(reinterpret_cast<float4 *>(part + h * kHeadDim) + lane, acc.o);
-                if (lane == 0) {
-                    __stcg(part + L::kHeads * kHeadDim + h, acc.m);
-                    __stcg(part + L::kHeads * (kHeadDim + 1) + h, acc.l);
-                }
-            }
+            if (task++ % NW != warp) continue;
+            const D4Merged r = d4_merge<L::kHeads, false>(2 * NW, h, lane, [&](int x) { return ((same >> x) & 1u) != 0u; },
+                                                          [&](int x) { return reinterpret_cast<const float *>(smem + runs[x].at); });
+            if (complete) r.write(out_row(run, h));
+            else d4_put<L::kHeads>(part_of(blockIdx.x, which), h, lane, r);
         }
-        if (!complete && tid == 0) runs[2 * kD4Warps + which] = run;
+        if (!complete && tid == 0) runs[2 * NW + which] = run;
     }
     __threadfence();   // this thread's part of a record is visible before the block's arrival is counted
     __syncthreads();
-    // ---- pairs that span blocks: the block that arrives last merges them
+    // ---- pairs that span blocks: the block that arrives last merges their records; where there are many, first the
+    //      last one of every kD4Group blocks merges theirs into the group's first record
     auto holder = [&](long long x) { return (int)(d4_div((x + 1) * gridDim.x - 1, U)); };   // the block whose range holds unit x
-    if (tid < 2 && runs[2 * kD4Warps + tid].pair >= 0) {
-        const D4Run run = runs[2 * kD4Warps + tid];
-        const int i0 = holder(run.first), i1 = holder(run.first + run.units - 1);
-        const int expected = (U >= gridDim.x) ? i1 - i0 + 1 : run.units;   // (with fewer units than blocks every one has a block of its own)
-        if (atomicAdd(p.counters + i0, 1) + 1 == expected) {
-            p.counters[i0] = 0;   // ready for the next launch
-            __threadfence();
-            flags[1 + tid] = 1;
-        }
-    }
-    __syncthreads();
-    for (int which = 0; which < 2; ++which) {
-        if (flags[1 + which] == 0) continue;
-        const D4Run run = runs[2 * kD4Warps + which];
-        const int i0 = holder(run.first);
-        const int n_parts = (U >= gridDim.x) ? holder(run.first + run.units - 1) - i0 + 1 : run.units;
-        for (int h = warp; h < p.G; h += kD4Warps) {
-            D4Merge acc;
-            for (int x = 0; x < n_parts; ++x) {
-                const int i = (U >= gridDim.x) ? i0 + x : holder(run.first + x);
-                const int slot = (run.first <= d4_div(U * i, gridDim.x)) ? 0 : 1;
-                const float *part = p.parts + ((size_t)i * 2 + slot) * L::kRecFloats;
-                acc.add(__ldcg(part + L::kHeads * kHeadDim + h), __ldcg(part + L::kHeads * (kHeadDim + 1) + h),
-                        __ldcg(reinterpret_cast<const float4 *>(part + h * kHeadDim) + lane));
+    // (with fewer units than blocks every unit has a block of its own)
+    auto n_parts_of = [&](const D4Run &run) { return (U >= gridDim.x) ? holder(run.first + run.units - 1) - holder(run.first) + 1 : run.units; };
+    auto part_at = [&](const D4Run &run, int x) {
+        const int i = (U >= gridDim.x) ? holder(run.first) + x : holder(run.first + x);
+        return 2 * i + ((run.first <= d4_div(U * i, gridDim.x)) ? 0 : 1);
+    };
+    for (int level = 0; level < 2; ++level) {
+        if (tid < 2 && runs[2 * NW + tid].pair >= 0 && (level == 0 || flags[1 + tid] == 2)) {
+            const D4Run run = runs[2 * NW + tid];
+            const int n_parts = n_parts_of(run), n_groups = (n_parts + kD4Group - 1) / kD4Group;
+            const bool grouped = n_parts > 2 * kD4Group;
+            int *counter = p.counters + 2 * kD4MaxBlocks + holder(run.first);
+            int expected = grouped ? n_groups : n_parts;
+            if (level == 0 && grouped) {
+                // (which of the pair's records this block has left)
+                int x = blockIdx.x - holder(run.first);
+                if (U < gridDim.x) x = (int)(block0 - run.first);
+                const int first = x / kD4Group * kD4Group;
+                counter = p.counters + part_at(run, first);
+                expected = min(kD4Group, n_parts - first);
+                runs[2 * NW + tid].at = first;
             }
-            acc.write(p.out + ((size_t)(run.pair / p.Hkv) * p.Hq + (size_t)(run.pair % p.Hkv) * p.G + h) * kHeadDim + 4 * lane);
+            int state = 0;
+            if (atomicAdd(counter, 1) + 1 == expected) {
+                *counter = 0;   // ready for the next launch
+                __threadfence();
+                state = (level == 0 && grouped) ? 2 : 1;
+            }
+            flags[1 + tid] = state;
         }
+        __syncthreads();
+        for (int which = 0; which < 2; ++which) {
+            const int state = flags[1 + which];
+            if (state == 0) continue;
+            const D4Run run = runs[2 * NW + which];
+            const int n_parts = n_parts_of(run);
+            if (state == 2 && level == 0) {
+                const int first = run.at, n = min(kD4Group, n_parts - first);
+                for (int h = warp; h < p.G; h += NW) {
+                    const D4Merged r = d4_merge<L::kHeads, true>(n, h, lane, [](int) { return true; },
+                                                                 [&](int x) { return p.parts + (size_t)part_at(run, first + x) * L::kRecFloats; });
+                    __syncwarp();
+                    d4_put<L::kHeads>(p.parts + (size_t)part_at(run, first) * L::kRecFloats, h, lane, r);
+                }
+            } else if (state == 1) {
+                const bool grouped = n_parts > 2 * kD4Group;
+                const int step = grouped ? kD4Group : 1, n = (n_parts + step - 1) / step;
+                for (int h = warp; h < p.G; h += NW) {
+                    d4_merge<L::kHeads, true>(n, h, lane, [](int) { return true; },
+                                              [&](int x) { return p.parts + (size_t)part_at(run, x * step) * L::kRecFloats; })
+                        .write(out_row(run, h));
+                }
+            }
+        }
+        if (flags[1] != 2 && flags[2] != 2) break;   // (the same for every thread: the flags changed before the barrier above)
+        __threadfence();
+        __syncthreads();
+        if (tid < 2 && flags[1 + tid] == 1) flags[1 + tid] = 0;   // merged above
+        __syncthreads();
     }
 }
-
-constexpr int kD4MaxBlocks = 256;
 
 size_t decode4_workspace_bytes(int G)
 {
@@ -648,7 +769,7 @@ static int launch_d4(const Decode4Params &p, int blocks, cudaStream_t stream)
 {
     const int rc = allow_dynamic_smem(reinterpret_cast<const void *>(slim4_decode_kernel<NT, kStep>), (int)D4<NT>::kBytes);
     if (rc != SLIM_OK) return rc;
-    SLIM_CUDA_TRY(launch_pdl(slim4_decode_kernel<NT, kStep>, dim3((unsigned)blocks), dim3(kD4Warps * 32), D4<NT>::kBytes, stream, p));
+    SLIM_CUDA_TRY(launch_pdl(slim4_decode_kernel<NT, kStep>, dim3((unsigned)blocks), dim3(D4<NT>::kWarps * 32), D4<NT>::kBytes, stream, p));
     return SLIM_OK;
 }
 
