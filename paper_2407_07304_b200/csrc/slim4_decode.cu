@@ -24,6 +24,8 @@
 // Query rows are held as fp16 after division by a power of two near the row's largest value: exact down to 2^-24 of it.
 // The weights p_j s_j are rounded to fp16 (2^-11 of each), p_j itself, its sum and the offset's sum stay fp32.
 // Every wait is bounded; a wait that runs out raises the status word and the warp writes nothing more.
+#include <cuda.h>
+
 #include "slim4_common.cuh"
 #include "slim_decode_params.cuh"
 #include "slim_tcgen05.cuh"
@@ -37,46 +39,47 @@ constexpr uint32_t kD4PairBytes = kD4Unit * 4;
 constexpr uint32_t kD4SlotBytes = 2 * (kD4CodeBytes + kD4PairBytes);   // a ring slot: a unit's K codes, V codes, then their (scale, offset) words
 constexpr float kD4Grow = 4.f;                     // the running maximum moves when it is exceeded by 2^4
 constexpr float kD4Top = 512.f;                    // p s is scaled so that the largest s counts as 2^9 to 2^10 (with p <= 2^4 far below fp16's 2^16)
-constexpr int kD4MaxBlocks = 256;
+constexpr int kD4MaxBlocks = 160;
 constexpr int kD4Group = 8;                        // blocks whose records are merged first where a pair spans many
 
 struct Decode4Params {
-    const uint8_t *codes;
-    const uint32_t *pairs;
+    uint8_t *codes;
+    uint32_t *pairs;
     const int32_t *block_table;
     const int32_t *kv_len;
     const __nv_bfloat16 *q, *k_new, *v_new;
     __nv_bfloat16 *out;
     int *status;
     int *counters;      // arrivals: per record slot for the group that it begins, then per block for the pair that begins in it
-    float *parts;       // two records per block
+    float *parts;       // records: two per block for the other blocks, then one per warp (of the warp's first pair, where it is left unfinished)
     int B, Hq, Hkv, G, max_pages_per_seq, num_pages, cap_tokens;
     float scale_log2e;
 };
 
-// A record: O [heads][128], then m [heads] and l [heads].
-template <int NT>
-struct D4 {
-    static constexpr int kWarps = 8;
-    static constexpr int kSlots = 2;                         // of a warp's ring
-    static constexpr int kHeads = 8 * NT;
-    static constexpr int kRecFloats = kHeads * (kHeadDim + 2);
-    static constexpr uint32_t kRingBytes = kSlots * kD4SlotBytes;
-    static constexpr uint32_t kFirst = kWarps * kRingBytes;                      // records of the warps' first pairs
-    static constexpr uint32_t kMeta = kFirst + kWarps * kRecFloats * 4;          // D4Run [2 * warps], then the block's [2]
-    static constexpr uint32_t kBars = kMeta + (2 * kWarps + 2) * 32;
-    static constexpr uint32_t kFlags = (kBars + kWarps * kSlots * 8 + 15) / 16 * 16;   // int[4]
-    static constexpr uint32_t kBytes = kFlags + 16;
-    static_assert(kRecFloats * 4 <= kRingBytes, "a warp's last record goes into its ring");
-    static_assert(2 * kWarps <= 32, "a warp's lanes look at all records of the block");
-    static_assert(kBytes <= 232448, "shared memory of one block");
-};
+// A record: O [G][128], then m [G] and l [G].
+__host__ __device__ inline int d4_rec_floats(int G) { return (G * (kHeadDim + 2) + 3) / 4 * 4; }
 
 // Part of a pair that a warp (or block) has worked on.
 struct __align__(16) D4Run {
     int pair, units;    // pair -1: nothing
-    long long first;    // the pair's first unit in the order of all units
-    int at;             // the record's place in shared memory
+    int first;          // the pair's first unit in the order of all units
+    int block, parts;   // (a block's: the block in which the pair begins, the records that blocks leave of it,
+    int group;          //  the one that begins this block's group of them)
+    const float *at;    // the record
+};
+
+template <int NT>
+struct D4 {
+    static constexpr int kWarps = (NT == 1) ? 12 : 8;       // (registers: 168 and 255 per thread)
+    static constexpr int kSlots = 2;                         // of a warp's ring
+    static constexpr uint32_t kRingBytes = kSlots * kD4SlotBytes;
+    static constexpr uint32_t kMeta = kWarps * kRingBytes;                       // D4Run [2 * warps], then the block's [2]
+    static constexpr uint32_t kBars = kMeta + (2 * kWarps + 2) * sizeof(D4Run);
+    static constexpr uint32_t kFlags = (kBars + kWarps * kSlots * 8 + 15) / 16 * 16;   // int[4]
+    static constexpr uint32_t kBytes = kFlags + 16;
+    static_assert(8 * NT * (kHeadDim + 2) * 4 <= kRingBytes, "a warp's last record goes into its ring");
+    static_assert(2 * kWarps <= 32, "a warp's lanes look at all records of the block");
+    static_assert(kBytes <= 232448, "shared memory of one block");
 };
 
 __device__ __forceinline__ void d4_mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
@@ -116,10 +119,19 @@ __device__ __forceinline__ float d4_sum_rows(float v)
     for (int o = 4; o < 32; o <<= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
     return v;
 }
-__device__ __forceinline__ long long d4_div(long long a, long long b)
+// floor(n i / of) without leaving 32 bits (i <= of, of below 2^15): where part i of n things begins.
+__device__ __forceinline__ int d4_cut(int n, int i, int of)
 {
-    if ((((unsigned long long)a | (unsigned long long)b) >> 32) == 0ull) return (long long)((unsigned)a / (unsigned)b);
-    return a / b;
+    const int q = n / of, r = n - q * of;
+    return q * i + r * i / of;
+}
+// The block whose part of U units holds unit x: a first guess from the average part (off by few, in floating point), then steps.
+__device__ __forceinline__ int d4_holder(int x, int U, int blocks)
+{
+    int i = min(blocks - 1, (int)((float)x * ((float)blocks / (float)U)));
+    while (i > 0 && d4_cut(U, i, blocks) > x) --i;
+    while (i + 1 < blocks && d4_cut(U, i + 1, blocks) <= x) ++i;
+    return i;
 }
 
 __device__ __forceinline__ int d4_len(const Decode4Params &p, int b) { return min(max(__ldg(p.kv_len + b), 0), p.cap_tokens); }
@@ -141,23 +153,21 @@ struct D4Walk {
     }
 };
 
-// All units, and where unit x lies.  Executed by a whole warp.
-__device__ __forceinline__ long long d4_total(const Decode4Params &p, int lane)
+// All units, and where unit x lies.  Executed by a whole warp; first: the length of sequence `lane`, which both look at.
+__device__ __forceinline__ int d4_units(int len) { return (len + kD4Unit - 1) / kD4Unit; }
+__device__ __forceinline__ int d4_total(const Decode4Params &p, int lane, int first)
 {
-    long long sum = 0;
-    for (int base = 0; base < p.B; base += 32) {
-        const int n = (base + lane < p.B) ? (d4_len(p, base + lane) + kD4Unit - 1) / kD4Unit : 0;
-        sum += __reduce_add_sync(0xffffffffu, n);
-    }
+    int sum = __reduce_add_sync(0xffffffffu, d4_units(first));   // (the host has checked that all units fit 31 bits)
+    for (int base = 32; base < p.B; base += 32) sum += __reduce_add_sync(0xffffffffu, (base + lane < p.B) ? d4_units(d4_len(p, base + lane)) : 0);
     return sum * p.Hkv;
 }
-__device__ __forceinline__ D4Walk d4_find(const Decode4Params &p, int lane, long long x)
+__device__ __forceinline__ D4Walk d4_find(const Decode4Params &p, int lane, int first, int x)
 {
     D4Walk w{0, 0, 0, 1, 0};
-    long long before = 0;
+    int before = 0;
     for (int base = 0; base < p.B; base += 32) {
-        const int len = (base + lane < p.B) ? d4_len(p, base + lane) : 0;
-        const int n = (len + kD4Unit - 1) / kD4Unit;
+        const int len = (base == 0) ? first : ((base + lane < p.B) ? d4_len(p, base + lane) : 0);
+        const int n = d4_units(len);
         int upto = n;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -168,10 +178,10 @@ __device__ __forceinline__ D4Walk d4_find(const Decode4Params &p, int lane, long
         if (hit != 0u) {
             const int at = __ffs(hit) - 1;
             const int n_at = __shfl_sync(0xffffffffu, n, at);
-            const long long r = x - (before + __shfl_sync(0xffffffffu, upto, at) - n_at) * p.Hkv;   // < Hkv * n_at
+            const int r = x - (before + __shfl_sync(0xffffffffu, upto, at) - n_at) * p.Hkv;   // < Hkv * n_at
             w.b = base + at;
-            w.head = (int)d4_div(r, n_at);
-            w.unit = (int)(r - (long long)w.head * n_at);
+            w.head = r / n_at;
+            w.unit = r - w.head * n_at;
             w.units = n_at;
             w.len = __shfl_sync(0xffffffffu, len, at);
             return w;
@@ -204,74 +214,59 @@ __device__ __forceinline__ void d4_store(__nv_bfloat16 *dst, float4 o)
     *reinterpret_cast<uint2 *>(dst) = make_uint2(*reinterpret_cast<const uint32_t *>(&a), *reinterpret_cast<const uint32_t *>(&b));
 }
 
-// Log-sum-exp merge of the records x = 0 .. n - 1 (those that `in` names) of head h by one warp; a lane owns four dims.
-// The largest maximum and the weights are found with a record per lane, the outputs are added up in record order.
-struct D4Merged {
-    float m, l;
-    float4 o;
-    __device__ __forceinline__ void write(__nv_bfloat16 *dst) const
-    {
-        const float inv = (l > 0.f) ? 1.f / l : 0.f;
-        d4_store(dst, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
-    }
-};
-template <int kHeads, bool kGlobal, class In, class Rec>
-__device__ __forceinline__ D4Merged d4_merge(int n, int h, int lane, In in, Rec rec)
+// Log-sum-exp merge by one warp of head h of the records that its lanes name (null: none), in lane order, into a row of the
+// result or of another record.  A lane owns four dims.  Out of line: it is called from three places and each run through
+// cold instructions costs more than the call.  The loads go past the L1 (records of other blocks) and take shared memory too.
+__device__ __noinline__ void d4_merge(const float *mine, int G, int h, int lane, __nv_bfloat16 *out, float *part)
 {
-    constexpr int kBatch = kGlobal ? 8 : 4;
-    D4Merged r{-INFINITY, 0.f, make_float4(0.f, 0.f, 0.f, 0.f)};
-    for (int x0 = 0; x0 < n; x0 += 32) {
-        const int x = x0 + lane;
-        const bool mine = x < n && in(x);
-        const float *at = rec(mine ? x : 0) + kHeads * kHeadDim + h;
-        float m = -INFINITY, l = 0.f;
-        if (mine) m = kGlobal ? __ldcg(at) : at[0], l = kGlobal ? __ldcg(at + kHeads) : at[kHeads];
-        const float top = fmaxf(r.m, warp_max(m));
-        const float f = (r.m == -INFINITY) ? 0.f : exp2f(r.m - top), w = (m == -INFINITY) ? 0.f : exp2f(m - top);
-        r.m = top;
-        r.l = r.l * f + w * l;
-        r.o = make_float4(r.o.x * f, r.o.y * f, r.o.z * f, r.o.w * f);
-        unsigned todo = __ballot_sync(0xffffffffu, mine);
-        while (todo != 0u) {
-            float4 v[kBatch];
-            int who[kBatch];
+    constexpr int kBatch = 8;
+    float m = -INFINITY, l = 0.f;
+    if (mine != nullptr) {
+        const volatile float *at = mine + G * kHeadDim + h;
+        m = at[0], l = at[G];
+    }
+    unsigned todo = __ballot_sync(0xffffffffu, mine != nullptr);
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    const float top = warp_max(m), w = (m == -INFINITY) ? 0.f : exp2f(m - top);
+    l = warp_sum(l * w);
+    while (todo != 0u) {
+        float4 v[kBatch];
+        float wu[kBatch];
 #pragma unroll
-            for (int u = 0; u < kBatch; ++u) {
-                who[u] = (todo != 0u) ? __ffs(todo) - 1 : -1;
-                todo &= todo - 1;
-                v[u] = make_float4(0.f, 0.f, 0.f, 0.f);
-                if (who[u] >= 0) {
-                    const float4 *src = reinterpret_cast<const float4 *>(rec(x0 + who[u]) + h * kHeadDim) + lane;
-                    v[u] = kGlobal ? __ldcg(src) : *src;
-                }
-            }
+        for (int u = 0; u < kBatch; ++u) {
+            const int who = (todo != 0u) ? __ffs(todo) - 1 : 0;
+            wu[u] = __shfl_sync(0xffffffffu, w, who);
+            const float *rec = reinterpret_cast<const float *>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(mine), who));
+            v[u] = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (todo != 0u)
+                asm volatile("ld.volatile.v4.f32 {%0, %1, %2, %3}, [%4];\n"
+                             : "=f"(v[u].x), "=f"(v[u].y), "=f"(v[u].z), "=f"(v[u].w)
+                             : "l"(rec + h * kHeadDim + 4 * lane));
+            todo &= todo - 1;
+        }
 #pragma unroll
-            for (int u = 0; u < kBatch; ++u) {
-                const float wu = __shfl_sync(0xffffffffu, w, max(who[u], 0));
-                if (who[u] < 0) continue;
-                r.o.x = fmaf(v[u].x, wu, r.o.x);
-                r.o.y = fmaf(v[u].y, wu, r.o.y);
-                r.o.z = fmaf(v[u].z, wu, r.o.z);
-                r.o.w = fmaf(v[u].w, wu, r.o.w);
-            }
+        for (int u = 0; u < kBatch; ++u) {
+            o.x = fmaf(v[u].x, wu[u], o.x);
+            o.y = fmaf(v[u].y, wu[u], o.y);
+            o.z = fmaf(v[u].z, wu[u], o.z);
+            o.w = fmaf(v[u].w, wu[u], o.w);
         }
     }
-    r.l = warp_sum(r.l);
-    return r;
-}
-template <int kHeads>
-__device__ __forceinline__ void d4_put(float *part, int h, int lane, const D4Merged &r)
-{
-    __stcg(reinterpret_cast<float4 *>(part + h * kHeadDim) + lane, r.o);
-    if (lane == 0) {
-        __stcg(part + kHeads * kHeadDim + h, r.m);
-        __stcg(part + kHeads * (kHeadDim + 1) + h, r.l);
+    if (out != nullptr) {
+        const float inv = (l > 0.f) ? 1.f / l : 0.f;
+        d4_store(out + h * kHeadDim + 4 * lane, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
+    } else {
+        __stcg(reinterpret_cast<float4 *>(part + h * kHeadDim) + lane, o);
+        if (lane == 0) {
+            __stcg(part + G * kHeadDim + h, top);
+            __stcg(part + G * (kHeadDim + 1) + h, l);
+        }
     }
 }
 
 template <int NT, bool kStep>
 __global__ void __launch_bounds__(D4<NT>::kWarps * 32, 1)
-slim4_decode_kernel(const Decode4Params p)
+slim4_decode_kernel(const __grid_constant__ CUtensorMap map_codes, const __grid_constant__ CUtensorMap map_pairs, const Decode4Params p)
 {
     using L = D4<NT>;
     constexpr int NW = L::kWarps, S = L::kSlots;
@@ -279,12 +274,13 @@ slim4_decode_kernel(const Decode4Params p)
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
     const uint32_t sbase = smem_u32(smem);
     D4Run *runs = reinterpret_cast<D4Run *>(smem + L::kMeta);
-    volatile int *flags = reinterpret_cast<volatile int *>(smem + L::kFlags);   // [0]: a wait ran out; [1], [2]: what is left to merge of the block's first, last pair
+    volatile int *flags = reinterpret_cast<volatile int *>(smem + L::kFlags);   // [0]: a wait ran out; [1], [2]: what this block, arrived last, has to merge of its first, last pair
     const uint32_t ring = warp * L::kRingBytes;
     auto bar = [&](int s) { return sbase + L::kBars + 8u * (uint32_t)(warp * S + s); };
 
     pdl_launch_dependents();
     if (lane == 0) {
+        if (warp == 0) tc::prefetch_tensormap(&map_codes), tc::prefetch_tensormap(&map_pairs);
         for (int s = 0; s < S; ++s) tc::mbar_init(bar(s), 1);
         tc::mbar_init_fence();
         runs[2 * warp].pair = runs[2 * warp + 1].pair = -1;
@@ -297,40 +293,42 @@ slim4_decode_kernel(const Decode4Params p)
     pdl_wait();   // from here on what earlier kernels of the stream wrote is read
 
     // ---- this warp's range of units
-    const long long U = d4_total(p, lane);
-    const long long W = (long long)gridDim.x * NW, gw = (long long)blockIdx.x * NW + warp;
-    const long long u0 = d4_div(U * gw, W), u1 = d4_div(U * (gw + 1), W);
-    const int cnt = (int)(u1 - u0);
+    const int len_first = (lane < p.B) ? d4_len(p, lane) : 0;
+    const int U = d4_total(p, lane, len_first);
+    const int n_blocks = (int)gridDim.x, block = (int)blockIdx.x;
+    const int u0 = d4_cut(U, block * NW + warp, n_blocks * NW), cnt = d4_cut(U, block * NW + warp + 1, n_blocks * NW) - u0;
+    const int G = p.G, rec_floats = d4_rec_floats(G);
+    float *first_rec = p.parts + ((size_t)2 * n_blocks + block * NW + warp) * rec_floats;
+    const uint64_t policy = tc::policy_evict_first();   // cache rows are read once per launch
     bool ok = true;
     if (cnt > 0) {
-        D4Walk w = d4_find(p, lane, u0), ahead = w;
-        // ---- lane 0 asks for the units, one after the other, each into slot n mod kSlots
-        const bool asks = lane == 0;
-        int asked = 0, page_next = 0;
-        if (asks) page_next = __ldg(p.block_table + (size_t)ahead.b * p.max_pages_per_seq + (ahead.unit >> 1));
+        D4Walk w = d4_find(p, lane, len_first, u0), ahead = w;
+        // ---- asks for the next unit, into slot n mod kSlots: two copies, K and V together, whole units whatever the length
+        //      (the page's other slots exist, and what they hold is masked)
+        auto page_of = [&](const D4Walk &x) { return __ldg(p.block_table + (size_t)x.b * p.max_pages_per_seq + (x.unit >> 1)); };
+        int asked = 0, page_next = page_of(ahead), page_after = 0;
+        D4Walk after = ahead;
+        if (cnt > 1) {
+            after.next(p);
+            page_after = page_of(after);
+        }
         auto ask = [&]() {
             const int s = asked % S;
-            if (asks) {
-                const int page = (page_next >= 0 && page_next < p.num_pages) ? page_next : 0;
-                const size_t row0 = ((size_t)((size_t)page * p.Hkv + ahead.head) * 2) * kPageTokens + (ahead.unit & 1) * kD4Unit;
-                const uint32_t n_tok = (uint32_t)min(kD4Unit, ahead.len - ahead.unit * kD4Unit);
-                const uint32_t dst = sbase + ring + s * kD4SlotBytes, code_bytes = n_tok * kRow4Bytes, pair_bytes = ((n_tok + 3) & ~3u) * 4u;
-                const uint8_t *codes = p.codes + row0 * kRow4Bytes;
-                const uint32_t *pairs = p.pairs + row0;
-                tc::mbar_arrive_expect_tx(bar(s), 2 * (code_bytes + pair_bytes));
-                tc::bulk_load(dst, codes, code_bytes, bar(s));
-                tc::bulk_load(dst + 2 * kD4CodeBytes, pairs, pair_bytes, bar(s));
-                tc::bulk_load(dst + kD4CodeBytes, codes + kPageTokens * kRow4Bytes, code_bytes, bar(s));
-                tc::bulk_load(dst + 2 * kD4CodeBytes + kD4PairBytes, pairs + kPageTokens, pair_bytes, bar(s));
-                if (asked + 1 < cnt) {   // (the next unit's page id is on its way while this unit's copies are)
-                    const int b_before = ahead.b;
-                    const bool same = (ahead.unit & 1) == 0;
-                    ahead.next(p);
-                    if (!same || ahead.unit == 0 || ahead.b != b_before)
-                        page_next = __ldg(p.block_table + (size_t)ahead.b * p.max_pages_per_seq + (ahead.unit >> 1));
-                }
+            const int page = (page_next >= 0 && page_next < p.num_pages) ? page_next : 0;
+            const int z = (page * p.Hkv + ahead.head) * 2, slot = (ahead.unit & 1) * kD4Unit;
+            const uint32_t dst = sbase + ring + s * kD4SlotBytes;
+            if (lane == 0) {
+                tc::mbar_arrive_expect_tx(bar(s), kD4SlotBytes);
+                tc::tma_load_3d_hint(dst, &map_codes, 0, slot, z, bar(s), policy);
+                tc::tma_load_2d_hint(dst + 2 * kD4CodeBytes, &map_pairs, slot, z, bar(s), policy);
             }
             ++asked;
+            ahead = after;
+            page_next = page_after;
+            if (asked + 1 < cnt) {   // (page ids are asked for two units ahead)
+                after.next(p);
+                page_after = page_of(after);
+            }
         };
         // the query rows of the pair that starts with the next unit, as they are.  They are requested before the copies that
         // fill the ring: a load behind those would wait until memory has delivered them
@@ -436,9 +434,9 @@ slim4_decode_kernel(const Decode4Params p)
                 const int page = __ldg(p.block_table + (size_t)w.b * p.max_pages_per_seq + (pos >> 7));
                 if (page >= 0 && page < p.num_pages) {
                     const int in_page = pos & (kPageTokens - 1);
-                    uint8_t *dst = const_cast<uint8_t *>(p.codes) + code4_block_offset(page, w.head, kv, p.Hkv) + (size_t)in_page * kRow4Bytes;
+                    uint8_t *dst = p.codes + code4_block_offset(page, w.head, kv, p.Hkv) + (size_t)in_page * kRow4Bytes;
                     reinterpret_cast<uint32_t *>(dst)[i] = codes;
-                    if (i == 0) const_cast<uint32_t *>(p.pairs)[scale_block_offset(page, w.head, kv, p.Hkv) + in_page] = pair;
+                    if (i == 0) p.pairs[scale_block_offset(page, w.head, kv, p.Hkv) + in_page] = pair;
                 }
                 tc::fence_proxy_async();   // (the slot is filled by the copy engine again)
                 __syncwarp();
@@ -525,31 +523,43 @@ slim4_decode_kernel(const Decode4Params p)
             const float sv_max = fmaxf(pair_scale(v2.x), pair_scale(v2.y));
             grow |= sv_max * r_cur >= 4.f * kD4Top;
             if (__any_sync(0xffffffffu, grow)) {
-                const bool first = r_cur == 0.f;
                 const float sv_top = warp_max(sv_max);
-                const float r_new = (first || sv_top * r_cur >= 4.f * kD4Top) ? pow2_recip(pow2_floor(sv_top)) * kD4Top : r_cur;
-                const float fr = first ? 0.f : r_new / r_cur;
-                r_cur = r_new;
+                const float r_fit = pow2_recip(pow2_floor(sv_top)) * kD4Top;
+                if (r_cur == 0.f) {
+                    r_cur = r_fit;   // (nothing summed up yet)
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-                    float al[2];
+                    for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
-                    for (int k = 0; k < 2; ++k) {
-                        const float up = first ? d4_max_rows(top[nt][k]) : fmaxf(d4_max_rows(top[nt][k]), 0.f);
-                        m[nt][k] += up;
-                        al[k] = first ? 0.f : d4_exp2(-up);
-                        l[nt][k] *= al[k];
-                        z[nt][k] *= al[k];
-                        al[k] *= fr;
+                        for (int k = 0; k < 2; ++k) {
+                            m[nt][k] = d4_max_rows(top[nt][k]);
 #pragma unroll
-                        for (int mt = 0; mt < 4; ++mt) c[mt][nt][k] -= up, c[mt][nt][2 + k] -= up;
+                            for (int mt = 0; mt < 4; ++mt) c[mt][nt][k] -= m[nt][k], c[mt][nt][2 + k] -= m[nt][k];
+                        }
                     }
+                } else {
+                    const float r_new = (sv_top * r_cur >= 4.f * kD4Top) ? r_fit : r_cur, fr = r_new / r_cur;
+                    r_cur = r_new;
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        o[nt][i][0] *= al[0];
-                        o[nt][i][1] *= al[1];
-                        o[nt][i][2] *= al[0];
-                        o[nt][i][3] *= al[1];
+                    for (int nt = 0; nt < NT; ++nt) {
+                        float al[2];
+#pragma unroll
+                        for (int k = 0; k < 2; ++k) {
+                            const float up = fmaxf(d4_max_rows(top[nt][k]), 0.f);
+                            m[nt][k] += up;
+                            al[k] = d4_exp2(-up);
+                            l[nt][k] *= al[k];
+                            z[nt][k] *= al[k];
+                            al[k] *= fr;
+#pragma unroll
+                            for (int mt = 0; mt < 4; ++mt) c[mt][nt][k] -= up, c[mt][nt][2 + k] -= up;
+                        }
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            o[nt][i][0] *= al[0];
+                            o[nt][i][1] *= al[1];
+                            o[nt][i][2] *= al[0];
+                            o[nt][i][3] *= al[1];
+                        }
                     }
                 }
             }
@@ -602,8 +612,7 @@ slim4_decode_kernel(const Decode4Params p)
             // ---- the end of the pair, or of the range
             if (complete || leaves) {
                 const float f1 = 16777216.f / r_cur, f2 = f1 * 0.0625f;    // the codes counted 2^-24 and 2^-20
-                const uint32_t at = (run_index == 0) ? L::kFirst + warp * L::kRecFloats * 4 : ring;   // (the last record: nothing is in flight)
-                float *rec = reinterpret_cast<float *>(smem + at);
+                float *rec = (run_index == 0) ? first_rec : reinterpret_cast<float *>(smem + ring);   // (at the last one nothing is in flight)
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
@@ -631,8 +640,8 @@ slim4_decode_kernel(const Decode4Params p)
                             dst[16] = make_float4(hi[0], hi[1], hi[2], hi[3]);
                             dst[17] = make_float4(hi[4], hi[5], hi[6], hi[7]);
                             if (g == 0) {
-                                rec[L::kHeads * kHeadDim + h] = m[nt][k];
-                                rec[L::kHeads * (kHeadDim + 1) + h] = ls;
+                                rec[G * kHeadDim + h] = m[nt][k];
+                                rec[G * (kHeadDim + 1) + h] = ls;
                             }
                         }
                     }
@@ -642,7 +651,7 @@ slim4_decode_kernel(const Decode4Params p)
                     run.pair = w.b * p.Hkv + w.head;
                     run.units = w.units;
                     run.first = u0 + n - w.unit;
-                    run.at = (int)at;
+                    run.at = rec;
                 }
                 ++run_index;
                 run_unit0 = 0;
@@ -667,91 +676,70 @@ slim4_decode_kernel(const Decode4Params p)
     }
 
     // ---- records of the block's warps, in the order of the units: those of one pair are merged
-    const long long block0 = d4_div(U * blockIdx.x, gridDim.x), block1 = d4_div(U * (blockIdx.x + 1), gridDim.x);
-    auto out_row = [&](const D4Run &run, int h) {
-        return p.out + ((size_t)(run.pair / p.Hkv) * p.Hq + (size_t)(run.pair % p.Hkv) * p.G + h) * kHeadDim + 4 * lane;
-    };
-    auto part_of = [&](int block, int slot) { return p.parts + ((size_t)block * 2 + slot) * L::kRecFloats; };
-    const int my_pair = (lane < 2 * NW) ? runs[lane].pair : -1;
-    unsigned left = __ballot_sync(0xffffffffu, my_pair >= 0);
+    const int block0 = d4_cut(U, block, n_blocks), block1 = d4_cut(U, block + 1, n_blocks);
+    auto out_rows = [&](int pair) { return p.out + (size_t)pair * G * kHeadDim; };
+    auto part = [&](int i) { return p.parts + (size_t)i * rec_floats; };
+    D4Run mine;
+    mine.pair = -1;
+    if (lane < 2 * NW) mine = runs[lane];
+    unsigned left = __ballot_sync(0xffffffffu, mine.pair >= 0);
     int task = 0;
     while (left != 0u) {
-        const int e = __ffs(left) - 1;
-        const D4Run run = runs[e];
-        const unsigned same = __ballot_sync(0xffffffffu, my_pair == run.pair);
-        left &= ~same;
+        const D4Run run = runs[__ffs(left) - 1];
+        left &= ~__ballot_sync(0xffffffffu, mine.pair == run.pair);
         const bool complete = run.first >= block0 && run.first + run.units <= block1;
         const int which = (run.first <= block0) ? 0 : 1;   // (of an incomplete one: the pair at the block's start, or at its end)
-        for (int h = 0; h < p.G; ++h) {
-            if (task++ % NW != warp) continue;
-            const D4Merged r = d4_merge<L::kHeads, false>(2 * NW, h, lane, [&](int x) { return ((same >> x) & 1u) != 0u; },
-                                                          [&](int x) { return reinterpret_cast<const float *>(smem + runs[x].at); });
-            if (complete) r.write(out_row(run, h));
-            else d4_put<L::kHeads>(part_of(blockIdx.x, which), h, lane, r);
-        }
+        for (int h = 0; h < G; ++h)
+            if (task++ % NW == warp)
+                d4_merge(mine.pair == run.pair ? mine.at : nullptr, G, h, lane, complete ? out_rows(run.pair) : nullptr, part(2 * block + which));
         if (!complete && tid == 0) runs[2 * NW + which] = run;
     }
-    __threadfence();   // this thread's part of a record is visible before the block's arrival is counted
     __syncthreads();
     // ---- pairs that span blocks: the block that arrives last merges their records; where there are many, first the
-    //      last one of every kD4Group blocks merges theirs into the group's first record
-    auto holder = [&](long long x) { return (int)(d4_div((x + 1) * gridDim.x - 1, U)); };   // the block whose range holds unit x
-    // (with fewer units than blocks every unit has a block of its own)
-    auto n_parts_of = [&](const D4Run &run) { return (U >= gridDim.x) ? holder(run.first + run.units - 1) - holder(run.first) + 1 : run.units; };
-    auto part_at = [&](const D4Run &run, int x) {
-        const int i = (U >= gridDim.x) ? holder(run.first) + x : holder(run.first + x);
-        return 2 * i + ((run.first <= d4_div(U * i, gridDim.x)) ? 0 : 1);
+    //      last one of every kD4Group blocks merges theirs into the group's first record.  (With fewer units than blocks
+    //      every unit has a block of its own.)
+    static_assert((kD4MaxBlocks + kD4Group - 1) / kD4Group <= 32 && 2 * kD4Group <= 32, "a warp's lanes name all records of a merge");
+    const bool sparse = U < n_blocks;
+    auto part_at = [&](const D4Run &run, int x) {   // a pair's record x, of the two per block
+        const int i = sparse ? d4_holder(run.first + x, U, n_blocks) : run.block + x;
+        return 2 * i + ((run.first <= d4_cut(U, i, n_blocks)) ? 0 : 1);
     };
     for (int level = 0; level < 2; ++level) {
-        if (tid < 2 && runs[2 * NW + tid].pair >= 0 && (level == 0 || flags[1 + tid] == 2)) {
-            const D4Run run = runs[2 * NW + tid];
-            const int n_parts = n_parts_of(run), n_groups = (n_parts + kD4Group - 1) / kD4Group;
-            const bool grouped = n_parts > 2 * kD4Group;
-            int *counter = p.counters + 2 * kD4MaxBlocks + holder(run.first);
-            int expected = grouped ? n_groups : n_parts;
-            if (level == 0 && grouped) {
-                // (which of the pair's records this block has left)
-                int x = blockIdx.x - holder(run.first);
-                if (U < gridDim.x) x = (int)(block0 - run.first);
-                const int first = x / kD4Group * kD4Group;
-                counter = p.counters + part_at(run, first);
-                expected = min(kD4Group, n_parts - first);
-                runs[2 * NW + tid].at = first;
+        if (warp < 2 && lane == 0 && runs[2 * NW + warp].pair >= 0 && (level == 0 || flags[1 + warp] == 2)) {
+            D4Run &run = runs[2 * NW + warp];
+            if (level == 0) {
+                run.block = d4_holder(run.first, U, n_blocks);
+                run.parts = sparse ? run.units : d4_holder(run.first + run.units - 1, U, n_blocks) - run.block + 1;
             }
+            const bool grouped = run.parts > 2 * kD4Group;
+            int *counter = p.counters + 2 * kD4MaxBlocks + run.block;
+            int expected = grouped ? (run.parts + kD4Group - 1) / kD4Group : run.parts;
+            if (level == 0 && grouped) {
+                run.group = (sparse ? block0 - run.first : block - run.block) / kD4Group * kD4Group;
+                counter = p.counters + part_at(run, run.group);
+                expected = min(kD4Group, run.parts - run.group);
+            }
+            __threadfence();   // the block's records (written before the barrier) are visible before its arrival is counted
             int state = 0;
             if (atomicAdd(counter, 1) + 1 == expected) {
                 *counter = 0;   // ready for the next launch
                 __threadfence();
                 state = (level == 0 && grouped) ? 2 : 1;
             }
-            flags[1 + tid] = state;
+            flags[1 + warp] = state;
         }
         __syncthreads();
         for (int which = 0; which < 2; ++which) {
             const int state = flags[1 + which];
             if (state == 0) continue;
             const D4Run run = runs[2 * NW + which];
-            const int n_parts = n_parts_of(run);
-            if (state == 2 && level == 0) {
-                const int first = run.at, n = min(kD4Group, n_parts - first);
-                for (int h = warp; h < p.G; h += NW) {
-                    const D4Merged r = d4_merge<L::kHeads, true>(n, h, lane, [](int) { return true; },
-                                                                 [&](int x) { return p.parts + (size_t)part_at(run, first + x) * L::kRecFloats; });
-                    __syncwarp();
-                    d4_put<L::kHeads>(p.parts + (size_t)part_at(run, first) * L::kRecFloats, h, lane, r);
-                }
-            } else if (state == 1) {
-                const bool grouped = n_parts > 2 * kD4Group;
-                const int step = grouped ? kD4Group : 1, n = (n_parts + step - 1) / step;
-                for (int h = warp; h < p.G; h += NW) {
-                    d4_merge<L::kHeads, true>(n, h, lane, [](int) { return true; },
-                                              [&](int x) { return p.parts + (size_t)part_at(run, x * step) * L::kRecFloats; })
-                        .write(out_row(run, h));
-                }
-            }
+            const int step = (state == 1 && run.parts > 2 * kD4Group) ? kD4Group : 1;
+            const int x = (state == 2) ? run.group + lane : lane * step;
+            const float *rec = (x < run.parts && (state == 1 || lane < kD4Group)) ? part(part_at(run, x)) : nullptr;
+            float *to = (state == 2) ? part(part_at(run, run.group)) : nullptr;
+            for (int h = (warp + NW - which * NW / 2) % NW; h < G; h += NW) d4_merge(rec, G, h, lane, state == 1 ? out_rows(run.pair) : nullptr, to);
         }
         if (flags[1] != 2 && flags[2] != 2) break;   // (the same for every thread: the flags changed before the barrier above)
-        __threadfence();
         __syncthreads();
         if (tid < 2 && flags[1 + tid] == 1) flags[1 + tid] = 0;   // merged above
         __syncthreads();
@@ -760,16 +748,30 @@ slim4_decode_kernel(const Decode4Params p)
 
 size_t decode4_workspace_bytes(int G)
 {
-    const size_t heads = (G <= 8) ? 8 : 16;
-    return kDecodeHeaderBytes + (size_t)kD4MaxBlocks * 2 * heads * (kHeadDim + 2) * sizeof(float);
+    const size_t warps = (G <= 8) ? D4<1>::kWarps : D4<2>::kWarps;
+    return kDecodeHeaderBytes + (size_t)kD4MaxBlocks * (2 + warps) * d4_rec_floats(G) * sizeof(float);
 }
 
 template <int NT, bool kStep>
-static int launch_d4(const Decode4Params &p, int blocks, cudaStream_t stream)
+static int launch_d4(const slim_cache4_t *c, const Decode4Params &p, int max_kv, cudaStream_t stream)
 {
-    const int rc = allow_dynamic_smem(reinterpret_cast<const void *>(slim4_decode_kernel<NT, kStep>), (int)D4<NT>::kBytes);
+    int sms = 0;
+    int rc = sm_count(&sms);
     if (rc != SLIM_OK) return rc;
-    SLIM_CUDA_TRY(launch_pdl(slim4_decode_kernel<NT, kStep>, dim3((unsigned)blocks), dim3(D4<NT>::kWarps * 32), D4<NT>::kBytes, stream, p));
+    if (sms > kD4MaxBlocks) sms = kD4MaxBlocks;
+    const long long pairs = (long long)p.B * p.Hkv, per_pair = (max_kv + kD4Unit - 1) / kD4Unit, units = pairs * per_pair;
+    if (units > 0x7FFFFFFFLL) return SLIM_ERR_UNSUPPORTED;   // (units are counted in 32 bits)
+    // One block per SM; where a pair is at most a unit for every warp and there is an SM for every pair, one block per pair:
+    // nothing is merged between blocks then (32 pairs of 272 tokens: see below)
+    long long blocks = units < sms ? units : sms;
+    if (per_pair <= D4<NT>::kWarps && pairs < blocks) blocks = pairs;
+    if (blocks < 1) blocks = 1;
+    CUtensorMap codes, scales;
+    rc = unit4_tensor_maps(c, &codes, &scales);
+    if (rc != SLIM_OK) return rc;
+    rc = allow_dynamic_smem(reinterpret_cast<const void *>(slim4_decode_kernel<NT, kStep>), (int)D4<NT>::kBytes);
+    if (rc != SLIM_OK) return rc;
+    SLIM_CUDA_TRY(launch_pdl(slim4_decode_kernel<NT, kStep>, dim3((unsigned)blocks), dim3(D4<NT>::kWarps * 32), D4<NT>::kBytes, stream, codes, scales, p));
     return SLIM_OK;
 }
 
@@ -778,7 +780,7 @@ int launch_decode4(const slim_cache4_t *c, const void *q, const void *k_new, con
 {
     Decode4Params p;
     p.codes = c->codes;
-    p.pairs = reinterpret_cast<const uint32_t *>(c->scales);
+    p.pairs = reinterpret_cast<uint32_t *>(c->scales);
     p.block_table = c->block_table;
     p.kv_len = kv_len;
     p.q = static_cast<const __nv_bfloat16 *>(q);
@@ -796,16 +798,8 @@ int launch_decode4(const slim_cache4_t *c, const void *q, const void *k_new, con
     p.num_pages = c->num_pages;
     p.cap_tokens = max_kv;   // (the caller has checked it against the page table)
     p.scale_log2e = sm_scale * kLog2e;
-    int sms = 0;
-    int rc = sm_count(&sms);
-    if (rc != SLIM_OK) return rc;
-    const long long units = (long long)B * p.Hkv * ((max_kv + kD4Unit - 1) / kD4Unit);
-    long long blocks = units < sms ? units : sms;
-    if (blocks > kD4MaxBlocks) blocks = kD4MaxBlocks;
-    if (blocks < 1) blocks = 1;
-    if (p.G <= 8)
-        return k_new != nullptr ? launch_d4<1, true>(p, (int)blocks, stream) : launch_d4<1, false>(p, (int)blocks, stream);
-    return k_new != nullptr ? launch_d4<2, true>(p, (int)blocks, stream) : launch_d4<2, false>(p, (int)blocks, stream);
+    if (p.G <= 8) return k_new != nullptr ? launch_d4<1, true>(c, p, max_kv, stream) : launch_d4<1, false>(c, p, max_kv, stream);
+    return k_new != nullptr ? launch_d4<2, true>(c, p, max_kv, stream) : launch_d4<2, false>(c, p, max_kv, stream);
 }
 
 }  // namespace slim

@@ -177,6 +177,15 @@ __device__ __forceinline__ void tma_load_2d(uint32_t dst_smem, const void *tmap,
         "l"(tmap), "r"(x), "r"(y), "r"(mbar_smem)
         : "memory");
 }
+// The same in three dimensions, with a cache policy.
+__device__ __forceinline__ void tma_load_3d_hint(uint32_t dst_smem, const void *tmap, int x, int y, int z, uint32_t mbar_smem, uint64_t policy)
+{
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1, {%2, %3, %4}], [%5], %6;\n" ::"r"(
+            dst_smem),
+        "l"(tmap), "r"(x), "r"(y), "r"(z), "r"(mbar_smem), "l"(policy)
+        : "memory");
+}
 // Brings the box at (x, y) of a tiled tensor into the L2 without copying it anywhere (same alignment rule for x).
 __device__ __forceinline__ void tma_prefetch_2d(const void *tmap, int x, int y)
 {

@@ -18,16 +18,31 @@ typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t
                                   const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
                                   CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
-struct Entry {
+// What a map is made of: a pool seen as rows (2-D) or as blocks of rows (3-D).
+struct Shape {
     const void *ptr;
-    long long rows;
-    int row_bytes, box_rows;
+    CUtensorMapDataType type;
+    int dims;
+    cuuint64_t size[3], stride[2];   // elements; bytes
+    cuuint32_t box[3];
+    CUtensorMapSwizzle swizzle;
+};
+struct Entry {
+    Shape shape;
     CUtensorMap map;
 };
-constexpr int kEntries = 32;
-}  // namespace
+constexpr int kEntries = 64;
 
-static int rows_tensor_map(void *codes, long long rows, int row_bytes, CUtensorMapSwizzle swizzle, int box_rows, CUtensorMap *out)
+bool same_shape(const Shape &a, const Shape &b)
+{
+    if (a.ptr != b.ptr || a.type != b.type || a.dims != b.dims || a.swizzle != b.swizzle) return false;
+    for (int i = 0; i < a.dims; ++i)
+        if (a.size[i] != b.size[i] || a.box[i] != b.box[i] || (i > 0 && a.stride[i - 1] != b.stride[i - 1])) return false;
+    return true;
+}
+
+// Maps are cached by their shape; thread-safe.
+int tensor_map(const Shape &want, CUtensorMap *out)
 {
     static std::mutex mu;
     static EncodeTiledFn encode = nullptr;
@@ -42,23 +57,16 @@ static int rows_tensor_map(void *codes, long long rows, int row_bytes, CUtensorM
         encode = reinterpret_cast<EncodeTiledFn>(fn);
     }
     for (int i = 0; i < used; ++i) {
-        if (cache[i].ptr == codes && cache[i].rows == rows && cache[i].row_bytes == row_bytes && cache[i].box_rows == box_rows) {
+        if (same_shape(cache[i].shape, want)) {
             *out = cache[i].map;
             return SLIM_OK;
         }
     }
     Entry e;
-    e.ptr = codes;
-    e.rows = rows;
-    e.row_bytes = row_bytes;
-    e.box_rows = box_rows;
-    const cuuint64_t dims[2] = {(cuuint64_t)row_bytes, (cuuint64_t)rows};
-    const cuuint64_t strides[1] = {(cuuint64_t)row_bytes};
-    const cuuint32_t box[2] = {(cuuint32_t)row_bytes, (cuuint32_t)box_rows};
-    const cuuint32_t estr[2] = {1, 1};
-    const CUresult r = encode(&e.map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, codes, dims, strides, box,
-                              estr, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
-                              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    e.shape = want;
+    const cuuint32_t estr[3] = {1, 1, 1};
+    const CUresult r = encode(&e.map, want.type, (cuuint32_t)want.dims, const_cast<void *>(want.ptr), want.size, want.stride, want.box, estr,
+                              CU_TENSOR_MAP_INTERLEAVE_NONE, want.swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     if (r != CUDA_SUCCESS) return SLIM_ERR_CUDA;
     cache[next] = e;
     next = (next + 1) % kEntries;
@@ -67,14 +75,59 @@ static int rows_tensor_map(void *codes, long long rows, int row_bytes, CUtensorM
     return SLIM_OK;
 }
 
+Shape rows_shape(const void *ptr, long long rows, int row_bytes, CUtensorMapSwizzle swizzle, int box_rows)
+{
+    Shape s = {};
+    s.ptr = ptr;
+    s.type = CU_TENSOR_MAP_DATA_TYPE_UINT8;
+    s.dims = 2;
+    s.size[0] = s.stride[0] = s.box[0] = (cuuint32_t)row_bytes;
+    s.size[1] = (cuuint64_t)rows;
+    s.box[1] = (cuuint32_t)box_rows;
+    s.swizzle = swizzle;
+    return s;
+}
+template <class Cache>
+long long pool_blocks(const Cache *c)   // (page, head, K|V)
+{
+    return (long long)c->num_pages * c->num_kv_heads * 2;
+}
+}  // namespace
+
 int codes_tensor_map(const slim_cache_t *c, int box_rows, CUtensorMap *out)
 {
-    return rows_tensor_map(c->codes, (long long)c->num_pages * c->num_kv_heads * 2 * kPageTokens, kHeadDim, CU_TENSOR_MAP_SWIZZLE_128B, box_rows, out);
+    return tensor_map(rows_shape(c->codes, pool_blocks(c) * kPageTokens, kHeadDim, CU_TENSOR_MAP_SWIZZLE_128B, box_rows), out);
 }
 
 int codes4_tensor_map(const slim_cache4_t *c, int box_rows, CUtensorMap *out)
 {
-    return rows_tensor_map(c->codes, (long long)c->num_pages * c->num_kv_heads * 2 * kPageTokens, kHeadDim / 2, CU_TENSOR_MAP_SWIZZLE_64B, box_rows, out);
+    return tensor_map(rows_shape(c->codes, pool_blocks(c) * kPageTokens, kHeadDim / 2, CU_TENSOR_MAP_SWIZZLE_64B, box_rows), out);
+}
+
+int unit4_tensor_maps(const slim_cache4_t *c, CUtensorMap *codes, CUtensorMap *pairs)
+{
+    Shape s = {};
+    s.ptr = c->codes;
+    s.type = CU_TENSOR_MAP_DATA_TYPE_UINT8;
+    s.dims = 3;
+    s.size[0] = s.stride[0] = s.box[0] = kHeadDim / 2;
+    s.size[1] = kPageTokens;
+    s.stride[1] = kPageTokens * kHeadDim / 2;
+    s.size[2] = (cuuint64_t)pool_blocks(c);
+    s.box[1] = kPageTokens / 2;
+    s.box[2] = 2;
+    s.swizzle = CU_TENSOR_MAP_SWIZZLE_NONE;
+    const int rc = tensor_map(s, codes);
+    if (rc != SLIM_OK) return rc;
+    s.ptr = c->scales;
+    s.type = CU_TENSOR_MAP_DATA_TYPE_UINT32;
+    s.dims = 2;
+    s.size[0] = kPageTokens;
+    s.stride[0] = kPageTokens * 4;
+    s.size[1] = (cuuint64_t)pool_blocks(c);
+    s.box[0] = kPageTokens / 2;
+    s.box[1] = 2;
+    return tensor_map(s, pairs);
 }
 
 int sm_count(int *out)
