@@ -35,8 +35,8 @@ namespace slim {
 
 constexpr int kD4Unit = 64;                        // tokens whose scores a warp holds at a time
 constexpr uint32_t kD4CodeBytes = kD4Unit * kRow4Bytes;
-constexpr uint32_t kD4PairBytes = kD4Unit * 4;
-constexpr uint32_t kD4SlotBytes = 2 * (kD4CodeBytes + kD4PairBytes);   // a ring slot: a unit's K codes, V codes, then their (scale, offset) words
+constexpr uint32_t kD4PairBytes = 2 * kD4Unit * 4;   // its (scale, offset) words, K's and then V's
+constexpr int kD4Slots = 3;                          // of a warp's ring: the K or the V codes of a unit each.  K(n) goes behind V(n - 2), V(n) behind K(n - 1)
 constexpr float kD4Grow = 4.f;                     // the running maximum moves when it is exceeded by 2^4
 constexpr float kD4Top = 512.f;                    // p s is scaled so that the largest s counts as 2^9 to 2^10 (with p <= 2^4 far below fp16's 2^16)
 constexpr int kD4MaxBlocks = 160;
@@ -51,7 +51,7 @@ struct Decode4Params {
     __nv_bfloat16 *out;
     int *status;
     int *counters;      // arrivals: per record slot for the group that it begins, then per block for the pair that begins in it
-    float *parts;       // records: two per block for the other blocks, then one per warp (of the warp's first pair, where it is left unfinished)
+    float *parts;       // two records per block: of the pair at its start and of the one at its end, where they go on in others
     int B, Hq, Hkv, G, max_pages_per_seq, num_pages, cap_tokens;
     float scale_log2e;
 };
@@ -71,13 +71,15 @@ struct __align__(16) D4Run {
 template <int NT>
 struct D4 {
     static constexpr int kWarps = (NT == 1) ? 12 : 8;       // (registers: 168 and 255 per thread)
-    static constexpr int kSlots = 2;                         // of a warp's ring
-    static constexpr uint32_t kRingBytes = kSlots * kD4SlotBytes;
-    static constexpr uint32_t kMeta = kWarps * kRingBytes;                       // D4Run [2 * warps], then the block's [2]
+    static constexpr uint32_t kWarpCodes = kD4Slots * kD4CodeBytes;              // a warp's ring of codes ...
+    static constexpr uint32_t kPairs = kWarps * kWarpCodes;                      // ... and of two units' words
+    static constexpr uint32_t kRecBytes = 8 * NT * (kHeadDim + 2) * 4;
+    static constexpr uint32_t kFirst = kPairs + kWarps * 2 * kD4PairBytes;       // records of the warps' first pairs
+    static constexpr uint32_t kMeta = kFirst + kWarps * kRecBytes;                // D4Run [2 * warps], then the block's [2]
     static constexpr uint32_t kBars = kMeta + (2 * kWarps + 2) * sizeof(D4Run);
-    static constexpr uint32_t kFlags = (kBars + kWarps * kSlots * 8 + 15) / 16 * 16;   // int[4]
+    static constexpr uint32_t kFlags = (kBars + kWarps * kD4Slots * 8 + 15) / 16 * 16;   // int[4]
     static constexpr uint32_t kBytes = kFlags + 16;
-    static_assert(8 * NT * (kHeadDim + 2) * 4 <= kRingBytes, "a warp's last record goes into its ring");
+    static_assert(kRecBytes <= kWarpCodes, "a warp's last record goes into its ring");
     static_assert(2 * kWarps <= 32, "a warp's lanes look at all records of the block");
     static_assert(kBytes <= 232448, "shared memory of one block");
 };
@@ -269,13 +271,13 @@ __global__ void __launch_bounds__(D4<NT>::kWarps * 32, 1)
 slim4_decode_kernel(const __grid_constant__ CUtensorMap map_codes, const __grid_constant__ CUtensorMap map_pairs, const Decode4Params p)
 {
     using L = D4<NT>;
-    constexpr int NW = L::kWarps, S = L::kSlots;
+    constexpr int NW = L::kWarps, S = kD4Slots;
     extern __shared__ __align__(1024) unsigned char smem[];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
     const uint32_t sbase = smem_u32(smem);
     D4Run *runs = reinterpret_cast<D4Run *>(smem + L::kMeta);
     volatile int *flags = reinterpret_cast<volatile int *>(smem + L::kFlags);   // [0]: a wait ran out; [1], [2]: what this block, arrived last, has to merge of its first, last pair
-    const uint32_t ring = warp * L::kRingBytes;
+    const uint32_t ring = warp * L::kWarpCodes, pair_ring = L::kPairs + warp * 2 * kD4PairBytes;
     auto bar = [&](int s) { return sbase + L::kBars + 8u * (uint32_t)(warp * S + s); };
 
     pdl_launch_dependents();
@@ -298,30 +300,28 @@ slim4_decode_kernel(const __grid_constant__ CUtensorMap map_codes, const __grid_
     const int n_blocks = (int)gridDim.x, block = (int)blockIdx.x;
     const int u0 = d4_cut(U, block * NW + warp, n_blocks * NW), cnt = d4_cut(U, block * NW + warp + 1, n_blocks * NW) - u0;
     const int G = p.G, rec_floats = d4_rec_floats(G);
-    float *first_rec = p.parts + ((size_t)2 * n_blocks + block * NW + warp) * rec_floats;
     const uint64_t policy = tc::policy_evict_first();   // cache rows are read once per launch
     bool ok = true;
     if (cnt > 0) {
         D4Walk w = d4_find(p, lane, len_first, u0), ahead = w;
-        // ---- asks for the next unit, into slot n mod kSlots: two copies, K and V together, whole units whatever the length
-        //      (the page's other slots exist, and what they hold is masked)
+        // ---- asks for the codes of the next K or V half (whole units whatever the length: the page's other slots exist, and
+        //      what they hold is masked), with K's for the words of both
         auto page_of = [&](const D4Walk &x) { return __ldg(p.block_table + (size_t)x.b * p.max_pages_per_seq + (x.unit >> 1)); };
-        int asked = 0, page_next = page_of(ahead), page_after = 0;
+        int asked = 0, ask_slot = 0, blk = 0, row0 = 0, page_next = page_of(ahead), page_after = 0;
         D4Walk after = ahead;
         if (cnt > 1) {
             after.next(p);
             page_after = page_of(after);
         }
-        auto ask = [&]() {
-            const int s = asked % S;
+        auto ask_k = [&]() {
             const int page = (page_next >= 0 && page_next < p.num_pages) ? page_next : 0;
-            const int z = (page * p.Hkv + ahead.head) * 2, slot = (ahead.unit & 1) * kD4Unit;
-            const uint32_t dst = sbase + ring + s * kD4SlotBytes;
+            blk = (page * p.Hkv + ahead.head) * 2, row0 = (ahead.unit & 1) * kD4Unit;
             if (lane == 0) {
-                tc::mbar_arrive_expect_tx(bar(s), kD4SlotBytes);
-                tc::tma_load_3d_hint(dst, &map_codes, 0, slot, z, bar(s), policy);
-                tc::tma_load_2d_hint(dst + 2 * kD4CodeBytes, &map_pairs, slot, z, bar(s), policy);
+                tc::mbar_arrive_expect_tx(bar(ask_slot), kD4CodeBytes + kD4PairBytes);
+                tc::tma_load_3d_hint(sbase + ring + ask_slot * kD4CodeBytes, &map_codes, 0, row0, blk, bar(ask_slot), policy);
+                tc::tma_load_2d_hint(sbase + pair_ring + (asked & 1) * kD4PairBytes, &map_pairs, row0, blk, bar(ask_slot), policy);
             }
+            ask_slot = (ask_slot == S - 1) ? 0 : ask_slot + 1;
             ++asked;
             ahead = after;
             page_next = page_after;
@@ -329,6 +329,25 @@ slim4_decode_kernel(const __grid_constant__ CUtensorMap map_codes, const __grid_
                 after.next(p);
                 page_after = page_of(after);
             }
+        };
+        auto ask_v = [&]() {
+            if (lane == 0) {
+                tc::mbar_arrive_expect_tx(bar(ask_slot), kD4CodeBytes);
+                tc::tma_load_3d_hint(sbase + ring + ask_slot * kD4CodeBytes, &map_codes, 0, row0, blk + 1, bar(ask_slot), policy);
+            }
+            ask_slot = (ask_slot == S - 1) ? 0 : ask_slot + 1;
+        };
+        int take_slot = 0;
+        uint32_t parity = 0;
+        auto landed = [&]() {   // waits for the next half and returns its place
+            if (!tc::mbar_wait(bar(take_slot), parity, ok ? (1u << 18) : 1u, flags)) {
+                ok = false;
+                flags[0] = 1;
+            }
+            __syncwarp();
+            unsigned char *at = smem + ring + take_slot * kD4CodeBytes;
+            if (++take_slot == S) take_slot = 0, parity ^= 1u;
+            return at;
         };
         // the query rows of the pair that starts with the next unit, as they are.  They are requested before the copies that
         // fill the ring: a load behind those would wait until memory has delivered them
@@ -347,7 +366,9 @@ slim4_decode_kernel(const __grid_constant__ CUtensorMap map_codes, const __grid_
             }
         };
         load_q(w.b, w.head);
-        for (int i = 0; i < min(S, cnt); ++i) ask();
+        ask_k();
+        ask_v();
+        if (cnt > 1) ask_k();
 
         uint32_t qf[NT][8][2];                  // Q^T operands: dims 16 t + 4 j .. (even steps), 64 further (odd steps)
         float rs[NT][2], qz[NT][2];             // of the columns 2 t, 2 t + 1: what a product and a row's offset count for
@@ -415,27 +436,22 @@ slim4_decode_kernel(const __grid_constant__ CUtensorMap map_codes, const __grid_
                 next.next(p);
                 load_q(next.b, next.head);
             }
-            const int slot = n % S;
-            if (!tc::mbar_wait(bar(slot), (uint32_t)(n / S) & 1u, ok ? (1u << 18) : 1u, flags)) {
-                ok = false;
-                flags[0] = 1;
-            }
-            __syncwarp();
-            unsigned char *kst = smem + ring + slot * kD4SlotBytes, *vst = kst + kD4CodeBytes;
-            uint32_t *kp = reinterpret_cast<uint32_t *>(kst + 2 * kD4CodeBytes), *vp = kp + kD4Unit;
-
-            if (kStep && ends && ok && __ldg(p.kv_len + w.b) == w.len) {
+            unsigned char *kst = landed(), *vst = smem + ring + take_slot * kD4CodeBytes;
+            uint32_t *kp = reinterpret_cast<uint32_t *>(smem + pair_ring + (n & 1) * kD4PairBytes), *vp = kp + kD4Unit;
+            const bool appends = kStep && ends && ok && __ldg(p.kv_len + w.b) == w.len;
+            uint32_t new_codes = 0;
+            if (kStep && appends) {
                 // ---- the new token: quantised here, stored in the cache and in the unit's copy of it
                 const int kv = lane >> 4, i = lane & 15, at = n_tok - 1, pos = w.len - 1;
-                uint32_t codes, pair;
-                d4_quantise((kv ? p.v_new : p.k_new) + ((size_t)w.b * p.Hkv + w.head) * kHeadDim, i, codes, pair);
-                reinterpret_cast<uint32_t *>(kst + kv * kD4CodeBytes + at * kRow4Bytes)[i] = codes;
+                uint32_t pair;
+                d4_quantise((kv ? p.v_new : p.k_new) + ((size_t)w.b * p.Hkv + w.head) * kHeadDim, i, new_codes, pair);
+                if (kv == 0) reinterpret_cast<uint32_t *>(kst + at * kRow4Bytes)[i] = new_codes;
                 if (i == 0) kp[kv * kD4Unit + at] = pair;
                 const int page = __ldg(p.block_table + (size_t)w.b * p.max_pages_per_seq + (pos >> 7));
                 if (page >= 0 && page < p.num_pages) {
                     const int in_page = pos & (kPageTokens - 1);
                     uint8_t *dst = p.codes + code4_block_offset(page, w.head, kv, p.Hkv) + (size_t)in_page * kRow4Bytes;
-                    reinterpret_cast<uint32_t *>(dst)[i] = codes;
+                    reinterpret_cast<uint32_t *>(dst)[i] = new_codes;
                     if (i == 0) p.pairs[scale_block_offset(page, w.head, kv, p.Hkv) + in_page] = pair;
                 }
                 tc::fence_proxy_async();   // (the slot is filled by the copy engine again)
@@ -514,6 +530,14 @@ slim4_decode_kernel(const __grid_constant__ CUtensorMap map_codes, const __grid_
                         for (int k = 0; k < 2; ++k) top[nt][k] = fmaxf(top[nt][k], fmaxf(c[mt][nt][k], c[mt][nt][2 + k]));
                     }
                 }
+            }
+            __syncwarp();              // every lane has read the K half
+            if (n + 1 < cnt) ask_v();
+            landed();
+            if (kStep && appends) {
+                if (lane >= 16) reinterpret_cast<uint32_t *>(vst + (n_tok - 1) * kRow4Bytes)[lane & 15] = new_codes;
+                tc::fence_proxy_async();
+                __syncwarp();
             }
             // ---- a larger maximum, a much larger V scale (rarely, but for the pair's first unit)
             bool grow = r_cur == 0.f;
@@ -606,13 +630,13 @@ slim4_decode_kernel(const __grid_constant__ CUtensorMap map_codes, const __grid_
                     }
                 }
             }
-            __syncwarp();              // every lane has read the slot
-            if (asked < cnt) ask();
+            __syncwarp();              // every lane has read the V half
+            if (n + 2 < cnt) ask_k();
 
             // ---- the end of the pair, or of the range
             if (complete || leaves) {
                 const float f1 = 16777216.f / r_cur, f2 = f1 * 0.0625f;    // the codes counted 2^-24 and 2^-20
-                float *rec = (run_index == 0) ? first_rec : reinterpret_cast<float *>(smem + ring);   // (at the last one nothing is in flight)
+                float *rec = reinterpret_cast<float *>(smem + (run_index == 0 ? L::kFirst + warp * L::kRecBytes : ring));   // (at the last one nothing is in flight)
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
@@ -660,7 +684,10 @@ slim4_decode_kernel(const __grid_constant__ CUtensorMap map_codes, const __grid_
             if (n + 1 < cnt) w.next(p);
         }
         if (!ok) {   // copies still in flight get a bounded chance to land
-            for (int i = max(0, asked - S); i < asked; ++i) tc::mbar_wait(bar(i % S), (uint32_t)(i / S) & 1u, 1u << 14);
+            for (int s = 0; s < S; ++s) {
+                tc::mbar_wait(bar(s), 0, 1u << 14);
+                tc::mbar_wait(bar(s), 1, 1u << 14);
+            }
         }
     }
     // sequences without tokens: zeros
@@ -748,8 +775,7 @@ slim4_decode_kernel(const __grid_constant__ CUtensorMap map_codes, const __grid_
 
 size_t decode4_workspace_bytes(int G)
 {
-    const size_t warps = (G <= 8) ? D4<1>::kWarps : D4<2>::kWarps;
-    return kDecodeHeaderBytes + (size_t)kD4MaxBlocks * (2 + warps) * d4_rec_floats(G) * sizeof(float);
+    return kDecodeHeaderBytes + (size_t)kD4MaxBlocks * 2 * d4_rec_floats(G) * sizeof(float);
 }
 
 template <int NT, bool kStep>

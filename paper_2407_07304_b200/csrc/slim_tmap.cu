@@ -115,7 +115,7 @@ int unit4_tensor_maps(const slim_cache4_t *c, CUtensorMap *codes, CUtensorMap *p
     s.stride[1] = kPageTokens * kHeadDim / 2;
     s.size[2] = (cuuint64_t)pool_blocks(c);
     s.box[1] = kPageTokens / 2;
-    s.box[2] = 2;
+    s.box[2] = 1;
     s.swizzle = CU_TENSOR_MAP_SWIZZLE_NONE;
     const int rc = tensor_map(s, codes);
     if (rc != SLIM_OK) return rc;
