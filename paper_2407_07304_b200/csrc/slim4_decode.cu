@@ -36,7 +36,6 @@ namespace slim {
 constexpr int kD4Unit = 64;                        // tokens whose scores a warp holds at a time
 constexpr uint32_t kD4CodeBytes = kD4Unit * kRow4Bytes;
 constexpr uint32_t kD4PairBytes = 2 * kD4Unit * 4;   // its (scale, offset) words, K's and then V's
-constexpr int kD4Slots = 3;                          // of a warp's ring: the K or the V codes of a unit each.  K(n) goes behind V(n - 2), V(n) behind K(n - 1)
 constexpr float kD4Grow = 4.f;                     // the running maximum moves when it is exceeded by 2^4
 constexpr float kD4Top = 512.f;                    // p s is scaled so that the largest s counts as 2^9 to 2^10 (with p <= 2^4 far below fp16's 2^16)
 constexpr int kD4MaxBlocks = 160;
@@ -68,16 +67,21 @@ struct __align__(16) D4Run {
     const float *at;    // the record
 };
 
-template <int NT>
+// What a block is made of, by the query heads that a kv head serves at most: NT groups of eight columns of the products.
+// A warp's ring of S slots (the K or the V codes of a unit each): with four, units n and n + 1; with three, K(n) goes behind
+// V(n - 2) and V(n) behind K(n - 1).
+template <int kHeads>
 struct D4 {
-    static constexpr int kWarps = (NT == 1) ? 12 : 8;       // (registers: 168 and 255 per thread)
-    static constexpr uint32_t kWarpCodes = kD4Slots * kD4CodeBytes;              // a warp's ring of codes ...
-    static constexpr uint32_t kPairs = kWarps * kWarpCodes;                      // ... and of two units' words
-    static constexpr uint32_t kRecBytes = 8 * NT * (kHeadDim + 2) * 4;
+    static constexpr int NT = (kHeads + 7) / 8;
+    static constexpr int kWarps = (kHeads <= 8) ? 12 : 8;
+    static constexpr int S = (kHeads > 2 && kHeads <= 8) ? 3 : 4;   // (what shared memory holds beside the records)
+    static constexpr uint32_t kWarpCodes = S * kD4CodeBytes;
+    static constexpr uint32_t kPairs = kWarps * kWarpCodes;                      // two units' words per warp
+    static constexpr uint32_t kRecBytes = kHeads * (kHeadDim + 2) * 4;
     static constexpr uint32_t kFirst = kPairs + kWarps * 2 * kD4PairBytes;       // records of the warps' first pairs
     static constexpr uint32_t kMeta = kFirst + kWarps * kRecBytes;                // D4Run [2 * warps], then the block's [2]
     static constexpr uint32_t kBars = kMeta + (2 * kWarps + 2) * sizeof(D4Run);
-    static constexpr uint32_t kFlags = (kBars + kWarps * kD4Slots * 8 + 15) / 16 * 16;   // int[4]
+    static constexpr uint32_t kFlags = (kBars + kWarps * S * 8 + 15) / 16 * 16;   // int[4]
     static constexpr uint32_t kBytes = kFlags + 16;
     static_assert(kRecBytes <= kWarpCodes, "a warp's last record goes into its ring");
     static_assert(2 * kWarps <= 32, "a warp's lanes look at all records of the block");
@@ -89,6 +93,18 @@ __device__ __forceinline__ void d4_mma(float (&c)[4], uint32_t a0, uint32_t a1, 
     asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};\n"
         : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// the same from zero
+__device__ __forceinline__ void d4_mma0(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
+{
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};\n"
+        : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
+}
+// A wait that did not succeed at once; false where it ran out.
+__device__ __noinline__ bool d4_wait(uint32_t bar, uint32_t parity, const volatile int *failed)
+{
+    return tc::mbar_wait(bar, parity, *failed != 0 ? 1u : (1u << 18), failed);
 }
 __device__ __forceinline__ uint32_t d4_transpose(uint32_t x)
 {
@@ -109,6 +125,13 @@ __device__ __forceinline__ uint4 ld_now(const uint4 *ptr)
     asm volatile("ld.global.nc.v4.u32 {%0, %1, %2, %3}, [%4];\n" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(ptr));
     return v;
 }
+// order-preserving map between floats and signed integers (its own inverse)
+__device__ __forceinline__ int d4_ordered_int(float x)
+{
+    const int i = __float_as_int(x);
+    return i ^ ((i >> 31) & 0x7FFFFFFF);
+}
+__device__ __forceinline__ float d4_ordered_float(int i) { return __int_as_float(i ^ ((i >> 31) & 0x7FFFFFFF)); }
 __device__ __forceinline__ float d4_max_rows(float v)   // over the lanes that hold other rows of the same columns
 {
 #pragma unroll
@@ -229,7 +252,8 @@ __device__ __noinline__ void d4_merge(const float *mine, int G, int h, int lane,
     }
     unsigned todo = __ballot_sync(0xffffffffu, mine != nullptr);
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-    const float top = warp_max(m), w = (m == -INFINITY) ? 0.f : exp2f(m - top);
+    const float top = d4_ordered_float(__reduce_max_sync(0xffffffffu, d4_ordered_int(m)));
+    const float w = (m == -INFINITY) ? 0.f : d4_exp2(m - top);
     l = warp_sum(l * w);
     while (todo != 0u) {
         float4 v[kBatch];
@@ -266,12 +290,12 @@ __device__ __noinline__ void d4_merge(const float *mine, int G, int h, int lane,
     }
 }
 
-template <int NT, bool kStep>
-__global__ void __launch_bounds__(D4<NT>::kWarps * 32, 1)
+template <int kHeads, bool kStep>
+__global__ void __launch_bounds__(D4<kHeads>::kWarps * 32, 1)
 slim4_decode_kernel(const __grid_constant__ CUtensorMap map_codes, const __grid_constant__ CUtensorMap map_pairs, const Decode4Params p)
 {
-    using L = D4<NT>;
-    constexpr int NW = L::kWarps, S = kD4Slots;
+    using L = D4<kHeads>;
+    constexpr int NT = L::NT, NW = L::kWarps, S = L::S;
     extern __shared__ __align__(1024) unsigned char smem[];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
     const uint32_t sbase = smem_u32(smem);
@@ -303,34 +327,33 @@ slim4_decode_kernel(const __grid_constant__ CUtensorMap map_codes, const __grid_
     const uint64_t policy = tc::policy_evict_first();   // cache rows are read once per launch
     bool ok = true;
     if (cnt > 0) {
-        D4Walk w = d4_find(p, lane, len_first, u0), ahead = w;
-        // ---- asks for the codes of the next K or V half (whole units whatever the length: the page's other slots exist, and
-        //      what they hold is masked), with K's for the words of both
+        // ---- units n, n + 1 and n + 2 of the range; their page ids are asked for as far ahead
         auto page_of = [&](const D4Walk &x) { return __ldg(p.block_table + (size_t)x.b * p.max_pages_per_seq + (x.unit >> 1)); };
-        int asked = 0, ask_slot = 0, blk = 0, row0 = 0, page_next = page_of(ahead), page_after = 0;
-        D4Walk after = ahead;
+        D4Walk w = d4_find(p, lane, len_first, u0), w1 = w, w2;
+        int page0 = page_of(w), page1 = 0, page2 = 0;
         if (cnt > 1) {
-            after.next(p);
-            page_after = page_of(after);
+            w1.next(p);
+            page1 = page_of(w1);
         }
-        auto ask_k = [&]() {
-            const int page = (page_next >= 0 && page_next < p.num_pages) ? page_next : 0;
-            blk = (page * p.Hkv + ahead.head) * 2, row0 = (ahead.unit & 1) * kD4Unit;
+        w2 = w1;
+        if (cnt > 2) {
+            w2.next(p);
+            page2 = page_of(w2);
+        }
+        // ---- asks for the codes of a K or V half (whole units whatever the length: the page's other slots exist, and what they
+        //      hold is masked), with K's for the words of both
+        int ask_slot = 0, blk = 0, row0 = 0;
+        auto ask_k = [&](const D4Walk &x, int page, int n) {
+            page = (page >= 0 && page < p.num_pages) ? page : 0;
+            blk = (page * p.Hkv + x.head) * 2, row0 = (x.unit & 1) * kD4Unit;
             if (lane == 0) {
                 tc::mbar_arrive_expect_tx(bar(ask_slot), kD4CodeBytes + kD4PairBytes);
                 tc::tma_load_3d_hint(sbase + ring + ask_slot * kD4CodeBytes, &map_codes, 0, row0, blk, bar(ask_slot), policy);
-                tc::tma_load_2d_hint(sbase + pair_ring + (asked & 1) * kD4PairBytes, &map_pairs, row0, blk, bar(ask_slot), policy);
+                tc::tma_load_2d_hint(sbase + pair_ring + (n & 1) * kD4PairBytes, &map_pairs, row0, blk, bar(ask_slot), policy);
             }
             ask_slot = (ask_slot == S - 1) ? 0 : ask_slot + 1;
-            ++asked;
-            ahead = after;
-            page_next = page_after;
-            if (asked + 1 < cnt) {   // (page ids are asked for two units ahead)
-                after.next(p);
-                page_after = page_of(after);
-            }
         };
-        auto ask_v = [&]() {
+        auto ask_v = [&]() {   // (of the unit whose K was asked for last)
             if (lane == 0) {
                 tc::mbar_arrive_expect_tx(bar(ask_slot), kD4CodeBytes);
                 tc::tma_load_3d_hint(sbase + ring + ask_slot * kD4CodeBytes, &map_codes, 0, row0, blk + 1, bar(ask_slot), policy);
@@ -339,15 +362,13 @@ slim4_decode_kernel(const __grid_constant__ CUtensorMap map_codes, const __grid_
         };
         int take_slot = 0;
         uint32_t parity = 0;
-        auto landed = [&]() {   // waits for the next half and returns its place
-            if (!tc::mbar_wait(bar(take_slot), parity, ok ? (1u << 18) : 1u, flags)) {
+        auto landed = [&]() {   // waits for the next half
+            if (!tc::mbar_try(bar(take_slot), parity) && !d4_wait(bar(take_slot), parity, flags)) {
                 ok = false;
                 flags[0] = 1;
             }
             __syncwarp();
-            unsigned char *at = smem + ring + take_slot * kD4CodeBytes;
             if (++take_slot == S) take_slot = 0, parity ^= 1u;
-            return at;
         };
         // the query rows of the pair that starts with the next unit, as they are.  They are requested before the copies that
         // fill the ring: a load behind those would wait until memory has delivered them
@@ -366,9 +387,7 @@ slim4_decode_kernel(const __grid_constant__ CUtensorMap map_codes, const __grid_
             }
         };
         load_q(w.b, w.head);
-        ask_k();
-        ask_v();
-        if (cnt > 1) ask_k();
+        ask_k(w, page0, 0);
 
         uint32_t qf[NT][8][2];                  // Q^T operands: dims 16 t + 4 j .. (even steps), 64 further (odd steps)
         float rs[NT][2], qz[NT][2];             // of the columns 2 t, 2 t + 1: what a product and a row's offset count for
@@ -426,17 +445,24 @@ slim4_decode_kernel(const __grid_constant__ CUtensorMap map_codes, const __grid_
                     for (int i = 0; i < 8; ++i) o[nt][i][0] = o[nt][i][1] = o[nt][i][2] = o[nt][i][3] = 0.f;
                 }
                 r_cur = 0.f;
+                if (n == 0) {   // (the rest of the ring is filled once the query rows are there: they do not queue behind it)
+                    ask_v();
+                    if (cnt > 1) {
+                        ask_k(w1, page1, 1);
+                        if (S == 4) ask_v();
+                    }
+                }
             }
             const int n_tok = min(kD4Unit, w.len - w.unit * kD4Unit);
             const bool ends = w.unit == w.units - 1;                            // the pair's last unit
             const bool complete = ends && run_unit0 == 0;
             const bool leaves = (ends && !complete) || (n == cnt - 1 && !ends); // a record is left behind this unit
             if (ends && n + 1 < cnt) {   // the next pair's query rows, a unit ahead
-                D4Walk next = w;
-                next.next(p);
-                load_q(next.b, next.head);
+                load_q(w1.b, w1.head);
             }
-            unsigned char *kst = landed(), *vst = smem + ring + take_slot * kD4CodeBytes;
+            unsigned char *kst = smem + ring + take_slot * kD4CodeBytes;
+            landed();
+            unsigned char *vst = smem + ring + take_slot * kD4CodeBytes;
             uint32_t *kp = reinterpret_cast<uint32_t *>(smem + pair_ring + (n & 1) * kD4PairBytes), *vp = kp + kD4Unit;
             const bool appends = kStep && ends && ok && __ldg(p.kv_len + w.b) == w.len;
             uint32_t new_codes = 0;
@@ -474,8 +500,6 @@ slim4_decode_kernel(const __grid_constant__ CUtensorMap map_codes, const __grid_
                 const uint4 b4 = *reinterpret_cast<const uint4 *>(kst + k_off + (mt * 16 + 8) * kRow4Bytes);
                 ka[mt][0] = a4.x, ka[mt][1] = a4.y, ka[mt][2] = a4.z, ka[mt][3] = a4.w;
                 kb[mt][0] = b4.x, kb[mt][1] = b4.y, kb[mt][2] = b4.z, kb[mt][3] = b4.w;
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) c[mt][nt][0] = c[mt][nt][1] = c[mt][nt][2] = c[mt][nt][3] = 0.f;
             }
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
@@ -483,8 +507,10 @@ slim4_decode_kernel(const __grid_constant__ CUtensorMap map_codes, const __grid_
                 for (int mt = 0; mt < 4; ++mt) {
                     const uint32_t a = ka[mt][j], b = kb[mt][j], a8 = a >> 8, b8 = b >> 8;
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt)
-                        d4_mma(c[mt][nt], a & 0x000F000Fu, b & 0x000F000Fu, a8 & 0x000F000Fu, b8 & 0x000F000Fu, qf[nt][2 * j][0], qf[nt][2 * j][1]);
+                    for (int nt = 0; nt < NT; ++nt) {
+                        if (j == 0) d4_mma0(c[mt][nt], a & 0x000F000Fu, b & 0x000F000Fu, a8 & 0x000F000Fu, b8 & 0x000F000Fu, qf[nt][2 * j][0], qf[nt][2 * j][1]);
+                        else d4_mma(c[mt][nt], a & 0x000F000Fu, b & 0x000F000Fu, a8 & 0x000F000Fu, b8 & 0x000F000Fu, qf[nt][2 * j][0], qf[nt][2 * j][1]);
+                    }
                 }
 #pragma unroll
                 for (int mt = 0; mt < 4; ++mt) {
@@ -532,7 +558,7 @@ slim4_decode_kernel(const __grid_constant__ CUtensorMap map_codes, const __grid_
                 }
             }
             __syncwarp();              // every lane has read the K half
-            if (n + 1 < cnt) ask_v();
+            if (S == 3 && n + 1 < cnt) ask_v();
             landed();
             if (kStep && appends) {
                 if (lane >= 16) reinterpret_cast<uint32_t *>(vst + (n_tok - 1) * kRow4Bytes)[lane & 15] = new_codes;
@@ -631,7 +657,10 @@ slim4_decode_kernel(const __grid_constant__ CUtensorMap map_codes, const __grid_
                 }
             }
             __syncwarp();              // every lane has read the V half
-            if (n + 2 < cnt) ask_k();
+            if (n + 2 < cnt) {
+                ask_k(w2, page2, n);
+                if (S == 4) ask_v();
+            }
 
             // ---- the end of the pair, or of the range
             if (complete || leaves) {
@@ -681,7 +710,12 @@ slim4_decode_kernel(const __grid_constant__ CUtensorMap map_codes, const __grid_
                 run_unit0 = 0;
                 fresh = true;
             }
-            if (n + 1 < cnt) w.next(p);
+            w = w1;
+            w1 = w2;
+            if (n + 3 < cnt) {
+                w2.next(p);
+                page2 = page_of(w2);
+            }
         }
         if (!ok) {   // copies still in flight get a bounded chance to land
             for (int s = 0; s < S; ++s) {
@@ -706,20 +740,29 @@ slim4_decode_kernel(const __grid_constant__ CUtensorMap map_codes, const __grid_
     const int block0 = d4_cut(U, block, n_blocks), block1 = d4_cut(U, block + 1, n_blocks);
     auto out_rows = [&](int pair) { return p.out + (size_t)pair * G * kHeadDim; };
     auto part = [&](int i) { return p.parts + (size_t)i * rec_floats; };
-    D4Run mine;
-    mine.pair = -1;
-    if (lane < 2 * NW) mine = runs[lane];
-    unsigned left = __ballot_sync(0xffffffffu, mine.pair >= 0);
-    int task = 0;
-    while (left != 0u) {
-        const D4Run run = runs[__ffs(left) - 1];
-        left &= ~__ballot_sync(0xffffffffu, mine.pair == run.pair);
-        const bool complete = run.first >= block0 && run.first + run.units <= block1;
-        const int which = (run.first <= block0) ? 0 : 1;   // (of an incomplete one: the pair at the block's start, or at its end)
-        for (int h = 0; h < G; ++h)
-            if (task++ % NW == warp)
-                d4_merge(mine.pair == run.pair ? mine.at : nullptr, G, h, lane, complete ? out_rows(run.pair) : nullptr, part(2 * block + which));
-        if (!complete && tid == 0) runs[2 * NW + which] = run;
+    {
+        // lane e looks at record e; the first one of every pair stands for the pair
+        const D4Run &mine = runs[min(lane, 2 * NW - 1)];
+        const int pair = (lane < 2 * NW) ? mine.pair : -1;
+        const float *rec = mine.at;
+        const unsigned valid = __ballot_sync(0xffffffffu, pair >= 0), below = valid & ((1u << lane) - 1u);
+        const int before = __shfl_sync(0xffffffffu, pair, below != 0u ? 31 - __clz(below) : 0);
+        unsigned heads_left = __ballot_sync(0xffffffffu, pair >= 0 && (below == 0u || before != pair));
+        int h = warp;   // tasks (pair, head) are dealt to the warps in turn
+        while (heads_left != 0u) {
+            const int e = __ffs(heads_left) - 1;
+            const int pair_e = __shfl_sync(0xffffffffu, pair, e), first = runs[e].first, units = runs[e].units;
+            heads_left &= heads_left - 1;
+            const bool complete = first >= block0 && first + units <= block1;
+            const int which = (first <= block0) ? 0 : 1;   // (of an incomplete one: the pair at the block's start, or at its end)
+            for (; h < G; h += NW) d4_merge(pair == pair_e ? rec : nullptr, G, h, lane, complete ? out_rows(pair_e) : nullptr, part(2 * block + which));
+            h -= G;
+            if (!complete && tid == 0) {
+                runs[2 * NW + which].pair = pair_e;
+                runs[2 * NW + which].units = units;
+                runs[2 * NW + which].first = first;
+            }
+        }
     }
     __syncthreads();
     // ---- pairs that span blocks: the block that arrives last merges their records; where there are many, first the
@@ -778,7 +821,7 @@ size_t decode4_workspace_bytes(int G)
     return kDecodeHeaderBytes + (size_t)kD4MaxBlocks * 2 * d4_rec_floats(G) * sizeof(float);
 }
 
-template <int NT, bool kStep>
+template <int kHeads, bool kStep>
 static int launch_d4(const slim_cache4_t *c, const Decode4Params &p, int max_kv, cudaStream_t stream)
 {
     int sms = 0;
@@ -790,14 +833,14 @@ static int launch_d4(const slim_cache4_t *c, const Decode4Params &p, int max_kv,
     // One block per SM; where a pair is at most a unit for every warp and there is an SM for every pair, one block per pair:
     // nothing is merged between blocks then (32 pairs of 272 tokens: see below)
     long long blocks = units < sms ? units : sms;
-    if (per_pair <= D4<NT>::kWarps && pairs < blocks) blocks = pairs;
+    if (per_pair <= D4<kHeads>::kWarps && pairs < blocks) blocks = pairs;
     if (blocks < 1) blocks = 1;
     CUtensorMap codes, scales;
     rc = unit4_tensor_maps(c, &codes, &scales);
     if (rc != SLIM_OK) return rc;
-    rc = allow_dynamic_smem(reinterpret_cast<const void *>(slim4_decode_kernel<NT, kStep>), (int)D4<NT>::kBytes);
+    rc = allow_dynamic_smem(reinterpret_cast<const void *>(slim4_decode_kernel<kHeads, kStep>), (int)D4<kHeads>::kBytes);
     if (rc != SLIM_OK) return rc;
-    SLIM_CUDA_TRY(launch_pdl(slim4_decode_kernel<NT, kStep>, dim3((unsigned)blocks), dim3(D4<NT>::kWarps * 32), D4<NT>::kBytes, stream, codes, scales, p));
+    SLIM_CUDA_TRY(launch_pdl(slim4_decode_kernel<kHeads, kStep>, dim3((unsigned)blocks), dim3(D4<kHeads>::kWarps * 32), D4<kHeads>::kBytes, stream, codes, scales, p));
     return SLIM_OK;
 }
 
@@ -824,8 +867,10 @@ int launch_decode4(const slim_cache4_t *c, const void *q, const void *k_new, con
     p.num_pages = c->num_pages;
     p.cap_tokens = max_kv;   // (the caller has checked it against the page table)
     p.scale_log2e = sm_scale * kLog2e;
-    if (p.G <= 8) return k_new != nullptr ? launch_d4<1, true>(c, p, max_kv, stream) : launch_d4<1, false>(c, p, max_kv, stream);
-    return k_new != nullptr ? launch_d4<2, true>(c, p, max_kv, stream) : launch_d4<2, false>(c, p, max_kv, stream);
+    const bool step = k_new != nullptr;
+    if (p.G <= 2) return step ? launch_d4<2, true>(c, p, max_kv, stream) : launch_d4<2, false>(c, p, max_kv, stream);
+    if (p.G <= 8) return step ? launch_d4<8, true>(c, p, max_kv, stream) : launch_d4<8, false>(c, p, max_kv, stream);
+    return step ? launch_d4<16, true>(c, p, max_kv, stream) : launch_d4<16, false>(c, p, max_kv, stream);
 }
 
 }  // namespace slim

@@ -167,6 +167,18 @@ __device__ __forceinline__ bool mbar_wait(uint32_t mbar_smem, uint32_t parity, u
     return false;
 }
 
+// One try of such a wait (the hardware may suspend the thread for up to kWaitHintNs).
+__device__ __forceinline__ bool mbar_try(uint32_t mbar_smem, uint32_t parity)
+{
+    uint32_t done;
+    asm volatile(
+        "{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\nselp.b32 %0, 1, 0, p;\n}\n"
+        : "=r"(done)
+        : "r"(mbar_smem), "r"(parity), "r"(kWaitHintNs)
+        : "memory");
+    return done != 0;
+}
+
 // ---------------------------------------------------------------- TMA: every copy is addressed to this block alone
 // 2-D tiled tensor copy global -> shared; x (the innermost coordinate, in elements) must keep
 // x * element size a multiple of 16 bytes.  Completion is counted in bytes on the mbarrier.
