@@ -342,23 +342,29 @@ slim4_decode_kernel(const __grid_constant__ CUtensorMap map_codes, const __grid_
         }
         // ---- asks for the codes of a K or V half (whole units whatever the length: the page's other slots exist, and what they
         //      hold is masked), with K's for the words of both
+        constexpr bool kWhole = S == 4;   // K and V by one copy, one wait
         int ask_slot = 0, blk = 0, row0 = 0;
+        auto step_slot = [](int &slot) {
+            slot += kWhole ? 2 : 1;
+            if (slot == S) slot = 0;
+        };
         auto ask_k = [&](const D4Walk &x, int page, int n) {
             page = (page >= 0 && page < p.num_pages) ? page : 0;
             blk = (page * p.Hkv + x.head) * 2, row0 = (x.unit & 1) * kD4Unit;
             if (lane == 0) {
-                tc::mbar_arrive_expect_tx(bar(ask_slot), kD4CodeBytes + kD4PairBytes);
+                tc::mbar_arrive_expect_tx(bar(ask_slot), (kWhole ? 2 : 1) * kD4CodeBytes + kD4PairBytes);
                 tc::tma_load_3d_hint(sbase + ring + ask_slot * kD4CodeBytes, &map_codes, 0, row0, blk, bar(ask_slot), policy);
                 tc::tma_load_2d_hint(sbase + pair_ring + (n & 1) * kD4PairBytes, &map_pairs, row0, blk, bar(ask_slot), policy);
             }
-            ask_slot = (ask_slot == S - 1) ? 0 : ask_slot + 1;
+            step_slot(ask_slot);
         };
         auto ask_v = [&]() {   // (of the unit whose K was asked for last)
+            if (kWhole) return;
             if (lane == 0) {
                 tc::mbar_arrive_expect_tx(bar(ask_slot), kD4CodeBytes);
                 tc::tma_load_3d_hint(sbase + ring + ask_slot * kD4CodeBytes, &map_codes, 0, row0, blk + 1, bar(ask_slot), policy);
             }
-            ask_slot = (ask_slot == S - 1) ? 0 : ask_slot + 1;
+            step_slot(ask_slot);
         };
         int take_slot = 0;
         uint32_t parity = 0;
@@ -368,7 +374,8 @@ slim4_decode_kernel(const __grid_constant__ CUtensorMap map_codes, const __grid_
                 flags[0] = 1;
             }
             __syncwarp();
-            if (++take_slot == S) take_slot = 0, parity ^= 1u;
+            step_slot(take_slot);
+            if (take_slot == 0) parity ^= 1u;
         };
         // the query rows of the pair that starts with the next unit, as they are.  They are requested before the copies that
         // fill the ring: a load behind those would wait until memory has delivered them
@@ -391,7 +398,7 @@ slim4_decode_kernel(const __grid_constant__ CUtensorMap map_codes, const __grid_
 
         uint32_t qf[NT][8][2];                  // Q^T operands: dims 16 t + 4 j .. (even steps), 64 further (odd steps)
         float rs[NT][2], qz[NT][2];             // of the columns 2 t, 2 t + 1: what a product and a row's offset count for
-        float o[NT][8][4];                      // O^T: dim 8 g + i (first two), 64 + 8 g + i, of the columns 2 t, 2 t + 1
+        float o[NT][8][4];                      // O^T: dim 8 g + i (first two) and that plus 16 times dim 64 + 8 g + i, of the columns 2 t, 2 t + 1
         float m[NT][2], l[NT][2], z[NT][2];     // running maximum; this lane's share of sum p and sum p z
         float r_cur = 0.f;                      // what the scales are multiplied with in P^T (0: nothing of the pair seen yet)
         bool fresh = true;
@@ -447,10 +454,7 @@ slim4_decode_kernel(const __grid_constant__ CUtensorMap map_codes, const __grid_
                 r_cur = 0.f;
                 if (n == 0) {   // (the rest of the ring is filled once the query rows are there: they do not queue behind it)
                     ask_v();
-                    if (cnt > 1) {
-                        ask_k(w1, page1, 1);
-                        if (S == 4) ask_v();
-                    }
+                    if (cnt > 1) ask_k(w1, page1, 1);
                 }
             }
             const int n_tok = min(kD4Unit, w.len - w.unit * kD4Unit);
@@ -462,7 +466,7 @@ slim4_decode_kernel(const __grid_constant__ CUtensorMap map_codes, const __grid_
             }
             unsigned char *kst = smem + ring + take_slot * kD4CodeBytes;
             landed();
-            unsigned char *vst = smem + ring + take_slot * kD4CodeBytes;
+            unsigned char *vst = kWhole ? kst + kD4CodeBytes : smem + ring + take_slot * kD4CodeBytes;
             uint32_t *kp = reinterpret_cast<uint32_t *>(smem + pair_ring + (n & 1) * kD4PairBytes), *vp = kp + kD4Unit;
             const bool appends = kStep && ends && ok && __ldg(p.kv_len + w.b) == w.len;
             uint32_t new_codes = 0;
@@ -557,9 +561,11 @@ slim4_decode_kernel(const __grid_constant__ CUtensorMap map_codes, const __grid_
                     }
                 }
             }
-            __syncwarp();              // every lane has read the K half
-            if (S == 3 && n + 1 < cnt) ask_v();
-            landed();
+            if (!kWhole) {
+                __syncwarp();          // every lane has read the K half
+                if (n + 1 < cnt) ask_v();
+                landed();
+            }
             if (kStep && appends) {
                 if (lane >= 16) reinterpret_cast<uint32_t *>(vst + (n_tok - 1) * kRow4Bytes)[lane & 15] = new_codes;
                 tc::fence_proxy_async();
@@ -646,21 +652,18 @@ slim4_decode_kernel(const __grid_constant__ CUtensorMap map_codes, const __grid_
 #pragma unroll
                     for (int half = 0; half < 2; ++half) {
                         const uint32_t x = __byte_perm(wa, wb, half ? 0x7632 : 0x5410), y = __byte_perm(wc, wd, half ? 0x7632 : 0x5410);
-                        const uint32_t x8 = x >> 8, y8 = y >> 8;
+                        const uint32_t x8 = __byte_perm(x, 0u, 0x4341), y8 = __byte_perm(y, 0u, 0x4341);   // the odd bytes, whole
                         const int i = 4 * w2 + 2 * half;
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt) {
-                            d4_mma(o[nt][i], x & 0x000F000Fu, x & 0x00F000F0u, y & 0x000F000Fu, y & 0x00F000F0u, pt[mt][nt][0], pt[mt][nt][1]);
-                            d4_mma(o[nt][i + 1], x8 & 0x000F000Fu, x8 & 0x00F000F0u, y8 & 0x000F000Fu, y8 & 0x00F000F0u, pt[mt][nt][0], pt[mt][nt][1]);
+                            d4_mma(o[nt][i], x & 0x000F000Fu, x & 0x00FF00FFu, y & 0x000F000Fu, y & 0x00FF00FFu, pt[mt][nt][0], pt[mt][nt][1]);
+                            d4_mma(o[nt][i + 1], x8 & 0x000F000Fu, x8, y8 & 0x000F000Fu, y8, pt[mt][nt][0], pt[mt][nt][1]);
                         }
                     }
                 }
             }
             __syncwarp();              // every lane has read the V half
-            if (n + 2 < cnt) {
-                ask_k(w2, page2, n);
-                if (S == 4) ask_v();
-            }
+            if (n + 2 < cnt) ask_k(w2, page2, n);
 
             // ---- the end of the pair, or of the range
             if (complete || leaves) {
@@ -676,7 +679,7 @@ slim4_decode_kernel(const __grid_constant__ CUtensorMap map_codes, const __grid_
 #pragma unroll
                         for (int i = 0; i < 8; ++i) {
                             lo[i] = fmaf(o[nt][i][k], f1, zs);
-                            hi[i] = fmaf(o[nt][i][2 + k], f2, zs);
+                            hi[i] = fmaf(o[nt][i][2 + k] - o[nt][i][k], f2, zs);   // (whole bytes less their low halves)
                         }
                         if (h >= p.G || !ok) continue;
                         if (complete) {
@@ -836,7 +839,7 @@ static int launch_d4(const slim_cache4_t *c, const Decode4Params &p, int max_kv,
     if (per_pair <= D4<kHeads>::kWarps && pairs < blocks) blocks = pairs;
     if (blocks < 1) blocks = 1;
     CUtensorMap codes, scales;
-    rc = unit4_tensor_maps(c, &codes, &scales);
+    rc = unit4_tensor_maps(c, D4<kHeads>::S == 4 ? 2 : 1, &codes, &scales);
     if (rc != SLIM_OK) return rc;
     rc = allow_dynamic_smem(reinterpret_cast<const void *>(slim4_decode_kernel<kHeads, kStep>), (int)D4<kHeads>::kBytes);
     if (rc != SLIM_OK) return rc;

@@ -104,7 +104,7 @@ int codes4_tensor_map(const slim_cache4_t *c, int box_rows, CUtensorMap *out)
     return tensor_map(rows_shape(c->codes, pool_blocks(c) * kPageTokens, kHeadDim / 2, CU_TENSOR_MAP_SWIZZLE_64B, box_rows), out);
 }
 
-int unit4_tensor_maps(const slim_cache4_t *c, CUtensorMap *codes, CUtensorMap *pairs)
+int unit4_tensor_maps(const slim_cache4_t *c, int blocks, CUtensorMap *codes, CUtensorMap *pairs)
 {
     Shape s = {};
     s.ptr = c->codes;
@@ -115,7 +115,7 @@ int unit4_tensor_maps(const slim_cache4_t *c, CUtensorMap *codes, CUtensorMap *p
     s.stride[1] = kPageTokens * kHeadDim / 2;
     s.size[2] = (cuuint64_t)pool_blocks(c);
     s.box[1] = kPageTokens / 2;
-    s.box[2] = 1;
+    s.box[2] = (cuuint32_t)blocks;
     s.swizzle = CU_TENSOR_MAP_SWIZZLE_NONE;
     const int rc = tensor_map(s, codes);
     if (rc != SLIM_OK) return rc;
