@@ -353,7 +353,7 @@ slim4_decode_kernel(const __grid_constant__ CUtensorMap map_codes, const __grid_
             blk = (page * p.Hkv + x.head) * 2, row0 = (x.unit & 1) * kD4Unit;
             if (lane == 0) {
                 tc::mbar_arrive_expect_tx(bar(ask_slot), (kWhole ? 2 : 1) * kD4CodeBytes + kD4PairBytes);
-                tc::tma_load_3d_hint(sbase + ring + ask_slot * kD4CodeBytes, &map_codes, 0, row0, blk, bar(ask_slot), policy);
+                tc::tma_load_3d_hint(sbase + ring + ask_slot * kD4CodeBytes, &map_codes, 0, row0 / 16, blk, bar(ask_slot), policy);
                 tc::tma_load_2d_hint(sbase + pair_ring + (n & 1) * kD4PairBytes, &map_pairs, row0, blk, bar(ask_slot), policy);
             }
             step_slot(ask_slot);
@@ -362,7 +362,7 @@ slim4_decode_kernel(const __grid_constant__ CUtensorMap map_codes, const __grid_
             if (kWhole) return;
             if (lane == 0) {
                 tc::mbar_arrive_expect_tx(bar(ask_slot), kD4CodeBytes);
-                tc::tma_load_3d_hint(sbase + ring + ask_slot * kD4CodeBytes, &map_codes, 0, row0, blk + 1, bar(ask_slot), policy);
+                tc::tma_load_3d_hint(sbase + ring + ask_slot * kD4CodeBytes, &map_codes, 0, row0 / 16, blk + 1, bar(ask_slot), policy);
             }
             step_slot(ask_slot);
         };

@@ -106,21 +106,23 @@ int codes4_tensor_map(const slim_cache4_t *c, int box_rows, CUtensorMap *out)
 
 int unit4_tensor_maps(const slim_cache4_t *c, int blocks, CUtensorMap *codes, CUtensorMap *pairs)
 {
+    // (rows of 1 KB, sixteen slots each: the copy engine takes a box row by row)
+    constexpr int kBlock = kPageTokens * kHeadDim / 2, kRow = 1024;
     Shape s = {};
     s.ptr = c->codes;
-    s.type = CU_TENSOR_MAP_DATA_TYPE_UINT8;
+    s.type = CU_TENSOR_MAP_DATA_TYPE_UINT32;
     s.dims = 3;
-    s.size[0] = s.stride[0] = s.box[0] = kHeadDim / 2;
-    s.size[1] = kPageTokens;
-    s.stride[1] = kPageTokens * kHeadDim / 2;
+    s.size[0] = s.box[0] = kRow / 4;
+    s.stride[0] = kRow;
+    s.size[1] = kBlock / kRow;
+    s.stride[1] = kBlock;
     s.size[2] = (cuuint64_t)pool_blocks(c);
-    s.box[1] = kPageTokens / 2;
+    s.box[1] = kBlock / kRow / 2;
     s.box[2] = (cuuint32_t)blocks;
     s.swizzle = CU_TENSOR_MAP_SWIZZLE_NONE;
     const int rc = tensor_map(s, codes);
     if (rc != SLIM_OK) return rc;
     s.ptr = c->scales;
-    s.type = CU_TENSOR_MAP_DATA_TYPE_UINT32;
     s.dims = 2;
     s.size[0] = kPageTokens;
     s.stride[0] = kPageTokens * 4;
