@@ -58,13 +58,13 @@ struct Decode4Params {
 // A record: O [G][128], then m [G] and l [G].
 __host__ __device__ inline int d4_rec_floats(int G) { return (G * (kHeadDim + 2) + 3) / 4 * 4; }
 
-// Part of a pair that a warp (or block) has worked on.
-struct __align__(16) D4Run {
-    int pair, units;    // pair -1: nothing
-    int first;          // the pair's first unit in the order of all units
-    int block, parts;   // (a block's: the block in which the pair begins, the records that blocks leave of it,
-    int group;          //  the one that begins this block's group of them)
-    const float *at;    // the record
+// A pair that a block shares with others: where it lies and what the blocks leave of it.
+struct D4Span {
+    int pair, first, units;   // -1: none; its units in the order of all units
+    int block, parts;         // the block in which it begins, the records that blocks leave of it
+    int slot0;                // which of the two records of that first block it is (always the first one of the later blocks)
+    int group;                // where there are many: the record that begins this block's group of them
+    int pad;
 };
 
 // What a block is made of, by the query heads that a kv head serves at most: NT groups of eight columns of the products.
@@ -79,8 +79,11 @@ struct D4 {
     static constexpr uint32_t kPairs = kWarps * kWarpCodes;                      // two units' words per warp
     static constexpr uint32_t kRecBytes = kHeads * (kHeadDim + 2) * 4;
     static constexpr uint32_t kFirst = kPairs + kWarps * 2 * kD4PairBytes;       // records of the warps' first pairs
-    static constexpr uint32_t kMeta = kFirst + kWarps * kRecBytes;                // D4Run [2 * warps], then the block's [2]
-    static constexpr uint32_t kBars = kMeta + (2 * kWarps + 2) * sizeof(D4Run);
+    static constexpr uint32_t kSpans = kFirst + kWarps * kRecBytes;               // D4Span [2]: of the block's first and last unit
+    static constexpr uint32_t kLeft = kSpans + 2 * sizeof(D4Span);                // int [2 * warps]: the pair of a warp's first, last record
+    // (record e: of warp e / 2, its first or its last one)
+    static __host__ __device__ __forceinline__ constexpr uint32_t record(int e) { return (e & 1) ? (e >> 1) * kWarpCodes : kFirst + (e >> 1) * kRecBytes; }
+    static constexpr uint32_t kBars = (kLeft + 2 * kWarps * 4 + 7) / 8 * 8;
     static constexpr uint32_t kFlags = (kBars + kWarps * S * 8 + 15) / 16 * 16;   // int[4]
     static constexpr uint32_t kBytes = kFlags + 16;
     static_assert(kRecBytes <= kWarpCodes, "a warp's last record goes into its ring");
@@ -239,67 +242,87 @@ __device__ __forceinline__ void d4_store(__nv_bfloat16 *dst, float4 o)
     *reinterpret_cast<uint2 *>(dst) = make_uint2(*reinterpret_cast<const uint32_t *>(&a), *reinterpret_cast<const uint32_t *>(&b));
 }
 
-// Log-sum-exp merge by one warp of head h of the records that its lanes name (null: none), in lane order, into a row of the
-// result or of another record.  A lane owns four dims.  Out of line: it is called from three places and each run through
-// cold instructions costs more than the call.  The loads go past the L1 (records of other blocks) and take shared memory too.
-__device__ __noinline__ void d4_merge(const float *mine, int G, int h, int lane, __nv_bfloat16 *out, float *part)
+// Log-sum-exp merge by one warp of head h of the records that its lanes name (rec: a lane's record, null: none), in lane
+// order.  A lane owns four dims.  kGlobal: records of other blocks, read past the L1; at(x): record x's address (x a lane that
+// names one).  The first outputs are on their way before the maxima are known.
+struct D4Merged {
+    float m, l;
+    float4 o;
+};
+template <bool kGlobal, class At>
+__device__ __forceinline__ D4Merged d4_merge(const float *rec, int G, int h, int lane, At at)
 {
-    constexpr int kBatch = 8;
+    constexpr int kBatch = 4;
+    D4Merged r;
+    unsigned todo = __ballot_sync(0xffffffffu, rec != nullptr);
     float m = -INFINITY, l = 0.f;
-    if (mine != nullptr) {
-        const volatile float *at = mine + G * kHeadDim + h;
-        m = at[0], l = at[G];
+    if (rec != nullptr) {
+        const float *ml = rec + G * kHeadDim + h;
+        m = kGlobal ? __ldcg(ml) : ml[0], l = kGlobal ? __ldcg(ml + G) : ml[G];
     }
-    unsigned todo = __ballot_sync(0xffffffffu, mine != nullptr);
-    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-    const float top = d4_ordered_float(__reduce_max_sync(0xffffffffu, d4_ordered_int(m)));
-    const float w = (m == -INFINITY) ? 0.f : d4_exp2(m - top);
-    l = warp_sum(l * w);
-    while (todo != 0u) {
-        float4 v[kBatch];
-        float wu[kBatch];
+    float4 v[2][kBatch];
+    int who[2][kBatch];
+    auto load = [&](int k) {
 #pragma unroll
         for (int u = 0; u < kBatch; ++u) {
-            const int who = (todo != 0u) ? __ffs(todo) - 1 : 0;
-            wu[u] = __shfl_sync(0xffffffffu, w, who);
-            const float *rec = reinterpret_cast<const float *>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(mine), who));
-            v[u] = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (todo != 0u)
-                asm volatile("ld.volatile.v4.f32 {%0, %1, %2, %3}, [%4];\n"
-                             : "=f"(v[u].x), "=f"(v[u].y), "=f"(v[u].z), "=f"(v[u].w)
-                             : "l"(rec + h * kHeadDim + 4 * lane));
+            who[k][u] = (todo != 0u) ? __ffs(todo) - 1 : -1;
+            v[k][u] = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (todo != 0u) {
+                const float4 *src = reinterpret_cast<const float4 *>(at(who[k][u]) + h * kHeadDim) + lane;
+                v[k][u] = kGlobal ? __ldcg(src) : *src;
+            }
             todo &= todo - 1;
         }
+    };
+    load(0);
+    load(1);
+    r.m = d4_ordered_float(__reduce_max_sync(0xffffffffu, d4_ordered_int(m)));
+    const float w = (m == -INFINITY) ? 0.f : d4_exp2(m - r.m);
+    r.l = warp_sum(l * w);
+    r.o = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (;;) {
 #pragma unroll
-        for (int u = 0; u < kBatch; ++u) {
-            o.x = fmaf(v[u].x, wu[u], o.x);
-            o.y = fmaf(v[u].y, wu[u], o.y);
-            o.z = fmaf(v[u].z, wu[u], o.z);
-            o.w = fmaf(v[u].w, wu[u], o.w);
+        for (int k = 0; k < 2; ++k) {
+#pragma unroll
+            for (int u = 0; u < kBatch; ++u) {
+                const float wu = (who[k][u] >= 0) ? __shfl_sync(0xffffffffu, w, max(who[k][u], 0)) : 0.f;
+                r.o.x = fmaf(v[k][u].x, wu, r.o.x);
+                r.o.y = fmaf(v[k][u].y, wu, r.o.y);
+                r.o.z = fmaf(v[k][u].z, wu, r.o.z);
+                r.o.w = fmaf(v[k][u].w, wu, r.o.w);
+            }
         }
+        if (todo == 0u) return r;
+        load(0);
+        load(1);
     }
+}
+// Where a merge goes: a row of the result, or another record.
+__device__ __forceinline__ void d4_put(const D4Merged &r, int G, int h, int lane, __nv_bfloat16 *out, float *part)
+{
     if (out != nullptr) {
-        const float inv = (l > 0.f) ? 1.f / l : 0.f;
-        d4_store(out + h * kHeadDim + 4 * lane, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
+        const float inv = (r.l > 0.f) ? 1.f / r.l : 0.f;
+        d4_store(out + h * kHeadDim + 4 * lane, make_float4(r.o.x * inv, r.o.y * inv, r.o.z * inv, r.o.w * inv));
     } else {
-        __stcg(reinterpret_cast<float4 *>(part + h * kHeadDim) + lane, o);
+        __stcg(reinterpret_cast<float4 *>(part + h * kHeadDim) + lane, r.o);
         if (lane == 0) {
-            __stcg(part + G * kHeadDim + h, top);
-            __stcg(part + G * (kHeadDim + 1) + h, l);
+            __stcg(part + G * kHeadDim + h, r.m);
+            __stcg(part + G * (kHeadDim + 1) + h, r.l);
         }
     }
 }
 
 template <int kHeads, bool kStep>
 __global__ void __launch_bounds__(D4<kHeads>::kWarps * 32, 1)
-slim4_decode_kernel(const __grid_constant__ CUtensorMap map_codes, const __grid_constant__ CUtensorMap map_pairs, const Decode4Params p)
+slim4_decode_kernel(const __grid_constant__ CUtensorMap map_codes, const __grid_constant__ CUtensorMap map_pairs, const __grid_constant__ Decode4Params p)
 {
     using L = D4<kHeads>;
     constexpr int NT = L::NT, NW = L::kWarps, S = L::S;
     extern __shared__ __align__(1024) unsigned char smem[];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
     const uint32_t sbase = smem_u32(smem);
-    D4Run *runs = reinterpret_cast<D4Run *>(smem + L::kMeta);
+    D4Span *spans = reinterpret_cast<D4Span *>(smem + L::kSpans);
+    int *left_of = reinterpret_cast<int *>(smem + L::kLeft);
     volatile int *flags = reinterpret_cast<volatile int *>(smem + L::kFlags);   // [0]: a wait ran out; [1], [2]: what this block, arrived last, has to merge of its first, last pair
     const uint32_t ring = warp * L::kWarpCodes, pair_ring = L::kPairs + warp * 2 * kD4PairBytes;
     auto bar = [&](int s) { return sbase + L::kBars + 8u * (uint32_t)(warp * S + s); };
@@ -309,10 +332,9 @@ slim4_decode_kernel(const __grid_constant__ CUtensorMap map_codes, const __grid_
         if (warp == 0) tc::prefetch_tensormap(&map_codes), tc::prefetch_tensormap(&map_pairs);
         for (int s = 0; s < S; ++s) tc::mbar_init(bar(s), 1);
         tc::mbar_init_fence();
-        runs[2 * warp].pair = runs[2 * warp + 1].pair = -1;
+        left_of[2 * warp] = left_of[2 * warp + 1] = -1;
         if (warp == 0) {
             flags[0] = flags[1] = flags[2] = 0;
-            runs[2 * NW].pair = runs[2 * NW + 1].pair = -1;
         }
     }
     __syncthreads();
@@ -326,6 +348,36 @@ slim4_decode_kernel(const __grid_constant__ CUtensorMap map_codes, const __grid_
     const int G = p.G, rec_floats = d4_rec_floats(G);
     const uint64_t policy = tc::policy_evict_first();   // cache rows are read once per launch
     bool ok = true;
+    const int block0 = d4_cut(U, block, n_blocks), block1 = d4_cut(U, block + 1, n_blocks);
+    const bool sparse = U < n_blocks;   // (every unit has a block of its own)
+    // ---- the pairs at the block's start and end, if they go on in other blocks (found here, where there is time: the first
+    //      copies will be on their way)
+    auto find_spans = [&]() {
+        if (warp < NW - 2) return;
+        const int which = warp - (NW - 2);
+        D4Span span;
+        span.pair = -1;
+        if (block1 > block0) {
+            const D4Walk x = d4_find(p, lane, len_first, which ? block1 - 1 : block0);
+            span.first = (which ? block1 - 1 : block0) - x.unit;
+            span.units = x.units;
+            if ((which == 0 || span.first > block0) && (span.first < block0 || span.first + span.units > block1)) {
+                span.pair = x.b * p.Hkv + x.head;
+                span.block = d4_holder(span.first, U, n_blocks);
+                span.parts = sparse ? span.units : d4_holder(span.first + span.units - 1, U, n_blocks) - span.block + 1;
+                span.slot0 = (span.first <= d4_cut(U, span.block, n_blocks)) ? 0 : 1;
+                span.group = (sparse ? block0 - span.first : block - span.block) / kD4Group * kD4Group;
+            }
+        }
+        if (lane == 0) spans[which] = span;
+    };
+    // ---- sequences without tokens: zeros
+    for (int b = block; b < p.B; b += n_blocks) {
+        if (d4_len(p, b) != 0) continue;
+        uint4 *dst = reinterpret_cast<uint4 *>(p.out + (size_t)b * p.Hq * kHeadDim);
+        for (int i = tid; i < p.Hq * (kHeadDim / 8); i += NW * 32) dst[i] = make_uint4(0, 0, 0, 0);
+    }
+    if (cnt == 0) find_spans();
     if (cnt > 0) {
         // ---- units n, n + 1 and n + 2 of the range; their page ids are asked for as far ahead
         auto page_of = [&](const D4Walk &x) { return __ldg(p.block_table + (size_t)x.b * p.max_pages_per_seq + (x.unit >> 1)); };
@@ -452,7 +504,8 @@ slim4_decode_kernel(const __grid_constant__ CUtensorMap map_codes, const __grid_
                     for (int i = 0; i < 8; ++i) o[nt][i][0] = o[nt][i][1] = o[nt][i][2] = o[nt][i][3] = 0.f;
                 }
                 r_cur = 0.f;
-                if (n == 0) {   // (the rest of the ring is filled once the query rows are there: they do not queue behind it)
+                if (n == 0) {
+                    find_spans();   // (the rest of the ring is filled once the query rows are there: they do not queue behind it)
                     ask_v();
                     if (cnt > 1) ask_k(w1, page1, 1);
                 }
@@ -668,7 +721,7 @@ slim4_decode_kernel(const __grid_constant__ CUtensorMap map_codes, const __grid_
             // ---- the end of the pair, or of the range
             if (complete || leaves) {
                 const float f1 = 16777216.f / r_cur, f2 = f1 * 0.0625f;    // the codes counted 2^-24 and 2^-20
-                float *rec = reinterpret_cast<float *>(smem + (run_index == 0 ? L::kFirst + warp * L::kRecBytes : ring));   // (at the last one nothing is in flight)
+                float *rec = reinterpret_cast<float *>(smem + L::record(2 * warp + (run_index == 0 ? 0 : 1)));   // (a last one lies in the ring: nothing is in flight)
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
@@ -703,11 +756,7 @@ slim4_decode_kernel(const __grid_constant__ CUtensorMap map_codes, const __grid_
                     }
                 }
                 if (leaves && lane == 0 && ok) {
-                    D4Run &run = runs[2 * warp + (run_index == 0 ? 0 : 1)];
-                    run.pair = w.b * p.Hkv + w.head;
-                    run.units = w.units;
-                    run.first = u0 + n - w.unit;
-                    run.at = rec;
+                    left_of[2 * warp + (run_index == 0 ? 0 : 1)] = w.b * p.Hkv + w.head;
                 }
                 ++run_index;
                 run_unit0 = 0;
@@ -727,12 +776,6 @@ slim4_decode_kernel(const __grid_constant__ CUtensorMap map_codes, const __grid_
             }
         }
     }
-    // sequences without tokens: zeros
-    for (int b = blockIdx.x; b < p.B; b += gridDim.x) {
-        if (d4_len(p, b) != 0) continue;
-        uint4 *dst = reinterpret_cast<uint4 *>(p.out + (size_t)b * p.Hq * kHeadDim);
-        for (int i = tid; i < p.Hq * (kHeadDim / 8); i += NW * 32) dst[i] = make_uint4(0, 0, 0, 0);
-    }
     __syncthreads();
     if (flags[0] != 0) {
         if (tid == 0) atomicExch(p.status, SLIM_ERR_TIMEOUT);
@@ -740,77 +783,61 @@ slim4_decode_kernel(const __grid_constant__ CUtensorMap map_codes, const __grid_
     }
 
     // ---- records of the block's warps, in the order of the units: those of one pair are merged
-    const int block0 = d4_cut(U, block, n_blocks), block1 = d4_cut(U, block + 1, n_blocks);
     auto out_rows = [&](int pair) { return p.out + (size_t)pair * G * kHeadDim; };
     auto part = [&](int i) { return p.parts + (size_t)i * rec_floats; };
     {
         // lane e looks at record e; the first one of every pair stands for the pair
-        const D4Run &mine = runs[min(lane, 2 * NW - 1)];
-        const int pair = (lane < 2 * NW) ? mine.pair : -1;
-        const float *rec = mine.at;
+        const int pair = (lane < 2 * NW) ? left_of[lane] : -1;
         const unsigned valid = __ballot_sync(0xffffffffu, pair >= 0), below = valid & ((1u << lane) - 1u);
         const int before = __shfl_sync(0xffffffffu, pair, below != 0u ? 31 - __clz(below) : 0);
-        unsigned heads_left = __ballot_sync(0xffffffffu, pair >= 0 && (below == 0u || before != pair));
+        unsigned firsts = __ballot_sync(0xffffffffu, pair >= 0 && (below == 0u || before != pair));
+        auto at = [&](int e) { return reinterpret_cast<const float *>(smem + L::record(e)); };
+        const int span0 = spans[0].pair, span1 = spans[1].pair;
         int h = warp;   // tasks (pair, head) are dealt to the warps in turn
-        while (heads_left != 0u) {
-            const int e = __ffs(heads_left) - 1;
-            const int pair_e = __shfl_sync(0xffffffffu, pair, e), first = runs[e].first, units = runs[e].units;
-            heads_left &= heads_left - 1;
-            const bool complete = first >= block0 && first + units <= block1;
-            const int which = (first <= block0) ? 0 : 1;   // (of an incomplete one: the pair at the block's start, or at its end)
-            for (; h < G; h += NW) d4_merge(pair == pair_e ? rec : nullptr, G, h, lane, complete ? out_rows(pair_e) : nullptr, part(2 * block + which));
-            h -= G;
-            if (!complete && tid == 0) {
-                runs[2 * NW + which].pair = pair_e;
-                runs[2 * NW + which].units = units;
-                runs[2 * NW + which].first = first;
+        while (firsts != 0u) {
+            const int of = __shfl_sync(0xffffffffu, pair, __ffs(firsts) - 1);
+            firsts &= firsts - 1;
+            for (; h < G; h += NW) {
+                const D4Merged r = d4_merge<false>(pair == of ? at(lane) : nullptr, G, h, lane, at);
+                d4_put(r, G, h, lane, (of != span0 && of != span1) ? out_rows(of) : nullptr, part(2 * block + (of == span0 ? 0 : 1)));
             }
+            h -= G;
         }
     }
     __syncthreads();
     // ---- pairs that span blocks: the block that arrives last merges their records; where there are many, first the
-    //      last one of every kD4Group blocks merges theirs into the group's first record.  (With fewer units than blocks
-    //      every unit has a block of its own.)
+    //      last one of every kD4Group blocks merges theirs into the group's first record
     static_assert((kD4MaxBlocks + kD4Group - 1) / kD4Group <= 32 && 2 * kD4Group <= 32, "a warp's lanes name all records of a merge");
-    const bool sparse = U < n_blocks;
-    auto part_at = [&](const D4Run &run, int x) {   // a pair's record x, of the two per block
-        const int i = sparse ? d4_holder(run.first + x, U, n_blocks) : run.block + x;
-        return 2 * i + ((run.first <= d4_cut(U, i, n_blocks)) ? 0 : 1);
+    auto part_at = [&](const D4Span &span, int x) {   // a pair's record x, of the two per block
+        if (sparse) return 2 * d4_holder(span.first + x, U, n_blocks);
+        return 2 * (span.block + x) + (x == 0 ? span.slot0 : 0);
     };
     for (int level = 0; level < 2; ++level) {
-        if (warp < 2 && lane == 0 && runs[2 * NW + warp].pair >= 0 && (level == 0 || flags[1 + warp] == 2)) {
-            D4Run &run = runs[2 * NW + warp];
-            if (level == 0) {
-                run.block = d4_holder(run.first, U, n_blocks);
-                run.parts = sparse ? run.units : d4_holder(run.first + run.units - 1, U, n_blocks) - run.block + 1;
-            }
-            const bool grouped = run.parts > 2 * kD4Group;
-            int *counter = p.counters + 2 * kD4MaxBlocks + run.block;
-            int expected = grouped ? (run.parts + kD4Group - 1) / kD4Group : run.parts;
-            if (level == 0 && grouped) {
-                run.group = (sparse ? block0 - run.first : block - run.block) / kD4Group * kD4Group;
-                counter = p.counters + part_at(run, run.group);
-                expected = min(kD4Group, run.parts - run.group);
-            }
-            __threadfence();   // the block's records (written before the barrier) are visible before its arrival is counted
-            int state = 0;
-            if (atomicAdd(counter, 1) + 1 == expected) {
-                *counter = 0;   // ready for the next launch
-                __threadfence();
-                state = (level == 0 && grouped) ? 2 : 1;
-            }
-            flags[1 + warp] = state;
+        if (warp < 2 && lane == 0 && spans[warp].pair >= 0 && (level == 0 || flags[1 + warp] == 2)) {
+            const D4Span &span = spans[warp];
+            const bool grouped = span.parts > 2 * kD4Group, first = level == 0 && grouped;
+            int *counter = p.counters + (first ? part_at(span, span.group) : 2 * kD4MaxBlocks + span.block);
+            const int expected = first ? min(kD4Group, span.parts - span.group) : (grouped ? (span.parts + kD4Group - 1) / kD4Group : span.parts);
+            // (releases the block's records, which were written before the barrier, and acquires those of the others)
+            int before;
+            asm volatile("atom.acq_rel.gpu.global.add.s32 %0, [%1], 1;\n" : "=r"(before) : "l"(counter) : "memory");
+            const bool last = before + 1 == expected;
+            if (last) *counter = 0;   // ready for the next launch
+            flags[1 + warp] = last ? (first ? 2 : 1) : 0;
         }
         __syncthreads();
         for (int which = 0; which < 2; ++which) {
             const int state = flags[1 + which];
             if (state == 0) continue;
-            const D4Run run = runs[2 * NW + which];
-            const int step = (state == 1 && run.parts > 2 * kD4Group) ? kD4Group : 1;
-            const int x = (state == 2) ? run.group + lane : lane * step;
-            const float *rec = (x < run.parts && (state == 1 || lane < kD4Group)) ? part(part_at(run, x)) : nullptr;
-            float *to = (state == 2) ? part(part_at(run, run.group)) : nullptr;
-            for (int h = (warp + NW - which * NW / 2) % NW; h < G; h += NW) d4_merge(rec, G, h, lane, state == 1 ? out_rows(run.pair) : nullptr, to);
+            const D4Span span = spans[which];
+            const int step = (state == 1 && span.parts > 2 * kD4Group) ? kD4Group : 1;
+            const int x = (state == 2) ? span.group + lane : lane * step;
+            const int index = (x < span.parts && (state == 1 || lane < kD4Group)) ? part_at(span, x) : -1;
+            const float *rec = (index >= 0) ? part(index) : nullptr;
+            for (int h = (warp + NW - which * NW / 2) % NW; h < G; h += NW) {
+                const D4Merged r = d4_merge<true>(rec, G, h, lane, [&](int e) { return part(__shfl_sync(0xffffffffu, index, e)); });
+                d4_put(r, G, h, lane, state == 1 ? out_rows(span.pair) : nullptr, part(__shfl_sync(0xffffffffu, index, 0)));
+            }
         }
         if (flags[1] != 2 && flags[2] != 2) break;   // (the same for every thread: the flags changed before the barrier above)
         __syncthreads();
