@@ -530,15 +530,16 @@ class SlimCache4(_BlockTable):
 
 
 def _cache4(cache, where):
-    if not isinstance(cache, SlimCache4):
+    if type(cache) is not SlimCache4 and not isinstance(cache, SlimCache4):
         raise SlimError(SLIM_ERR_INVALID_ARG, f"{where}: needs a SlimCache4")
     return cache.ref
 
 
-def _rows4(where, Hkv, *rows):
-    for t in rows:
-        if t.dtype is not torch.bfloat16 or t.dim() != 3 or t.shape[1] != Hkv or t.shape[2] != HEAD_DIM or not t.is_contiguous():
-            raise SlimError(SLIM_ERR_INVALID_ARG, f"{where}: rows must be contiguous bfloat16 [tokens, kv heads, 128]")
+def _rows4(where, Hkv, k, v):
+    shape = k.shape
+    if k.dtype is not torch.bfloat16 or v.dtype is not torch.bfloat16 or v.shape != shape or len(shape) != 3 or shape[1] != Hkv or \
+            shape[2] != HEAD_DIM or not k.is_contiguous() or not v.is_contiguous():
+        raise SlimError(SLIM_ERR_INVALID_ARG, f"{where}: rows must be contiguous bfloat16 [tokens, kv heads, 128], K's and V's alike")
 
 
 def slim_kv4_append(cache, k_new, v_new, cu_new, start_pos, B, max_new, stream=None):
@@ -546,8 +547,9 @@ def slim_kv4_append(cache, k_new, v_new, cu_new, start_pos, B, max_new, stream=N
     where = "slim_kv4_append"
     ref = _cache4(cache, where)
     _rows4(where, cache.Hkv, k_new, v_new)
-    rc = lib().slim_kv4_append(ref, _addr(k_new), _addr(v_new), _addr(cu_new), _addr(start_pos), B, max_new, _cuda_stream(stream))
-    _check(rc, where)
+    rc = (_lib or lib()).slim_kv4_append(ref, k_new.data_ptr(), v_new.data_ptr(), cu_new.data_ptr(), start_pos.data_ptr(), B, max_new, _cuda_stream(stream))
+    if rc:
+        _check(rc, where)
 
 
 def slim_kv4_read(cache, k_out, v_out, cu, start_pos, B, max_rows, stream=None):
@@ -555,8 +557,9 @@ def slim_kv4_read(cache, k_out, v_out, cu, start_pos, B, max_rows, stream=None):
     where = "slim_kv4_read"
     ref = _cache4(cache, where)
     _rows4(where, cache.Hkv, k_out, v_out)
-    rc = lib().slim_kv4_read(ref, _addr(k_out), _addr(v_out), _addr(cu), _addr(start_pos), B, max_rows, _cuda_stream(stream))
-    _check(rc, where)
+    rc = (_lib or lib()).slim_kv4_read(ref, k_out.data_ptr(), v_out.data_ptr(), cu.data_ptr(), start_pos.data_ptr(), B, max_rows, _cuda_stream(stream))
+    if rc:
+        _check(rc, where)
 
 
 def slim_attn4_prefill(cache, q, out, cu_q, kv_len, B, max_q, max_kv, Hq, sm_scale, workspace, stream=None):
@@ -573,7 +576,7 @@ def slim_prefill4_step(cache, q, k_new, v_new, out, cu_q, kv_len, B, max_q, max_
 
 def slim_attn4_decode(cache, q, out, kv_len, B, max_kv, Hq, sm_scale, workspace, stream=None, k_new=None, v_new=None):
     """Decode attention over the 4-bit cache; with k_new and v_new the new tokens go into position kv_len - 1 in the same call."""
-    rc = lib().slim_attn4_decode(_cache4(cache, "slim_attn4_decode"), _addr(q), _addr(k_new), _addr(v_new), _addr(out), _addr(kv_len), B, max_kv, Hq,
+    rc = (_lib or lib()).slim_attn4_decode(_cache4(cache, "slim_attn4_decode"), _addr(q), _addr(k_new), _addr(v_new), _addr(out), _addr(kv_len), B, max_kv, Hq,
                                  sm_scale, _addr(workspace), _nbytes(workspace), _cuda_stream(stream))
     if rc:
         _check(rc, "slim_attn4_decode")
@@ -639,7 +642,7 @@ def slim_pages_fork(layers, src, dst, parent, kv_len, len_out, result, workspace
     _i32_vector(where, len(dst.held), parent, len_out)
     _i32_vector(where, len(src.held), kv_len)
     _i32_vector(where, 2, result)
-    rc = lib().slim_pages_fork(src.ref, dst.ref, _addr(parent), _addr(kv_len), _addr(len_out), array, n, _addr(result), _addr(workspace),
+    rc = (_lib or lib()).slim_pages_fork(src.ref, dst.ref, _addr(parent), _addr(kv_len), _addr(len_out), array, n, _addr(result), _addr(workspace),
                                _nbytes(workspace), _cuda_stream(stream))
     _check(rc, where)
 
@@ -649,7 +652,7 @@ def slim_pages_grow(pages, kv_len, room, result, workspace, stream=None):
     where = "slim_pages_grow"
     _i32_vector(where, len(pages.held), kv_len)
     _i32_vector(where, 2, result)
-    rc = lib().slim_pages_grow(pages.ref, _addr(kv_len), room, _addr(result), _addr(workspace), _nbytes(workspace), _cuda_stream(stream))
+    rc = (_lib or lib()).slim_pages_grow(pages.ref, _addr(kv_len), room, _addr(result), _addr(workspace), _nbytes(workspace), _cuda_stream(stream))
     _check(rc, where)
 
 
@@ -658,7 +661,7 @@ def slim_pages_compact(layers, src, dst, result, workspace, stream=None):
     where = "slim_pages_compact"
     array, n = _layers(where, layers, src)
     _i32_vector(where, 2, result)
-    rc = lib().slim_pages_compact(src.ref, dst.ref, array, n, _addr(result), _addr(workspace), _nbytes(workspace), _cuda_stream(stream))
+    rc = (_lib or lib()).slim_pages_compact(src.ref, dst.ref, array, n, _addr(result), _addr(workspace), _nbytes(workspace), _cuda_stream(stream))
     _check(rc, where)
 
 

@@ -147,7 +147,7 @@ __device__ __forceinline__ float pf_row_size(uint32_t word)
 //
 // kBits 4: the 4-bit cache.  Its raw rows are 64 bytes (64-byte swizzle), and a row's values scale * u + offset become
 // fp16 operands over the same kind of power of two, below the tile's largest |value| that its pairs allow.
-template <bool kTwoPass, int kBits = 8>
+template <bool kTwoPass, int kBits = 8, bool kPack = false>
 __global__ void __launch_bounds__(kPfThreads, 1)
 slim_prefill_tc_kernel(const __grid_constant__ CUtensorMap codes_map, const PrefillTcParams p)
 {
@@ -161,7 +161,16 @@ slim_prefill_tc_kernel(const __grid_constant__ CUtensorMap codes_map, const Pref
     const int q0 = p.cu_q[b];
     const int q_len = p.cu_q[b + 1] - q0;
     const int m0 = qblock * kPfRows;
-    if (m0 >= q_len) return;
+    // A block's rows: those of one query head, or (kPack, h is then the kv head) those of the G heads of its kv head token by
+    // token, so that a few query tokens of many heads fill the tiles and no more than 256 / G tokens share a causal border.
+    const int n_rows_all = kPack ? q_len * p.G : q_len;
+    auto token_of = [&](int row) { return kPack ? row / p.G : row; };
+    auto row_at = [&](int row) {   // index of a block's row among the rows of q and out
+        if (!kPack) return ((size_t)(q0 + row) * p.Hq + h);
+        const int token = row / p.G;
+        return (size_t)(q0 + token) * p.Hq + (size_t)h * p.G + (row - token * p.G);
+    };
+    if (m0 >= n_rows_all) return;
     const int kvl = min(p.kv_len[b], p.max_pages_per_seq * kPageTokens);
     const int offset = kvl - q_len;                                   // row r sees keys j <= offset + r
     // key tiles of the two query tiles: tile t covers rows [m0 + 128 t, m0 + 128 t + 128)
@@ -169,13 +178,13 @@ slim_prefill_tc_kernel(const __grid_constant__ CUtensorMap codes_map, const Pref
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
         const int first = m0 + t * kPfBM;
-        const int n_keys = (first < q_len) ? min(kvl, offset + min(first + kPfBM, q_len)) : 0;
+        const int n_keys = (first < n_rows_all) ? min(kvl, offset + token_of(min(first + kPfBM, n_rows_all) - 1) + 1) : 0;
         Tt[t] = n_keys > 0 ? (n_keys + kPfBN - 1) / kPfBN : 0;
     }
     const int T0 = Tt[0], T1 = Tt[1];
     const int T = max(T0, T1);
     const int NT = kTwoPass ? 2 * T : T;   // positions in the block's tile sequence
-    const int head = h / p.G;
+    const int head = kPack ? h : h / p.G;
 
     const uint32_t sbase = smem_u32(smem);
     float *misc_f = reinterpret_cast<float *>(smem + pfl::kMisc);
@@ -231,8 +240,8 @@ slim_prefill_tc_kernel(const __grid_constant__ CUtensorMap codes_map, const Pref
             const int rr = (warp & 3) * 32 + 2 * i + (lane >> 4);
             const int row = m0 + t * kPfBM + rr;
             qv[i] = make_uint4(0, 0, 0, 0);
-            if (Tt[t] > 0 && row < q_len)
-                qv[i] = __ldg(reinterpret_cast<const uint4 *>(p.q + ((size_t)(q0 + row) * p.Hq + h) * kHeadDim) + (lane & 15));
+            if (Tt[t] > 0 && row < n_rows_all)
+                qv[i] = __ldg(reinterpret_cast<const uint4 *>(p.q + row_at(row) * kHeadDim) + (lane & 15));
         }
     }
 
@@ -309,8 +318,8 @@ slim_prefill_tc_kernel(const __grid_constant__ CUtensorMap codes_map, const Pref
         const int t = warp >> 2;
         const int r = tid & 127;
         const int row = m0 + t * kPfBM + r;
-        const bool row_valid = row < q_len;
-        const int last_key = offset + row;
+        const bool row_valid = row < n_rows_all;
+        const int last_key = offset + token_of(row);
         const int Tmine = t ? T1 : T0;
         const uint32_t lane_base = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t tS = tmem + lane_base + kPfTmemS + (uint32_t)t * 128u;
@@ -456,12 +465,11 @@ slim_prefill_tc_kernel(const __grid_constant__ CUtensorMap codes_map, const Pref
                 const int rr = (warp & 3) * 32 + 2 * i + (lane >> 4);
                 const int orow = m0 + t * kPfBM + rr;
                 const uint4 o = *reinterpret_cast<const uint4 *>(stage + rr * 256 + (((piece + rr) & 15) << 4));
-                if (orow < q_len)
-                    reinterpret_cast<uint4 *>(p.out + ((size_t)(q0 + orow) * p.Hq + h) * kHeadDim)[piece] = o;
+                if (orow < n_rows_all) reinterpret_cast<uint4 *>(p.out + row_at(orow) * kHeadDim)[piece] = o;
             }
         } else if (row_valid) {
             // a row that sees no key
-            uint4 *dst = reinterpret_cast<uint4 *>(p.out + ((size_t)(q0 + row) * p.Hq + h) * kHeadDim);
+            uint4 *dst = reinterpret_cast<uint4 *>(p.out + row_at(row) * kHeadDim);
 #pragma unroll
             for (int i = 0; i < 16; ++i) dst[i] = make_uint4(0, 0, 0, 0);
         }
@@ -688,15 +696,15 @@ static PrefillTcParams prefill_params(const Cache *c, const void *q, void *out, 
     return p;
 }
 
-template <bool kTwoPass, int kBits>
+template <bool kTwoPass, int kBits, bool kPack = false>
 static int launch_prefill(const CUtensorMap &map, const PrefillTcParams &p, int B, cudaStream_t stream, bool after_append)
 {
-    const int rc = allow_dynamic_smem(reinterpret_cast<const void *>(slim_prefill_tc_kernel<kTwoPass, kBits>), (int)pfl::kBytes);
+    const int rc = allow_dynamic_smem(reinterpret_cast<const void *>(slim_prefill_tc_kernel<kTwoPass, kBits, kPack>), (int)pfl::kBytes);
     if (rc != SLIM_OK) return rc;
     if (p.n_qblocks > 65535 || B > 65535) return SLIM_ERR_UNSUPPORTED;
-    dim3 grid((unsigned)p.Hq, (unsigned)B, (unsigned)p.n_qblocks);
-    if (after_append) SLIM_CUDA_TRY(launch_pdl(slim_prefill_tc_kernel<kTwoPass, kBits>, grid, dim3(kPfThreads), pfl::kBytes, stream, map, p));
-    else slim_prefill_tc_kernel<kTwoPass, kBits><<<grid, kPfThreads, pfl::kBytes, stream>>>(map, p);
+    dim3 grid((unsigned)(kPack ? p.Hkv : p.Hq), (unsigned)B, (unsigned)p.n_qblocks);
+    if (after_append) SLIM_CUDA_TRY(launch_pdl(slim_prefill_tc_kernel<kTwoPass, kBits, kPack>, grid, dim3(kPfThreads), pfl::kBytes, stream, map, p));
+    else slim_prefill_tc_kernel<kTwoPass, kBits, kPack><<<grid, kPfThreads, pfl::kBytes, stream>>>(map, p);
     SLIM_CUDA_TRY(cudaGetLastError());
     return SLIM_OK;
 }
@@ -715,12 +723,14 @@ int launch_prefill_tc(const slim_cache_t *c, const void *q, void *out, const int
 int launch_prefill4_tc(const slim_cache4_t *c, const void *q, void *out, const int32_t *cu_q, const int32_t *kv_len,
                        int B, int max_q, int Hq, float sm_scale, void *workspace, cudaStream_t stream, bool after_append)
 {
-    const PrefillTcParams p = prefill_params(c, q, out, cu_q, kv_len, max_q, Hq, sm_scale, workspace);
+    PrefillTcParams p = prefill_params(c, q, out, cu_q, kv_len, max_q, Hq, sm_scale, workspace);
     if (p.n_qblocks == 0) return SLIM_OK;
+    if ((long long)max_q * p.G > (long long)kPfRows * 65535) return SLIM_ERR_UNSUPPORTED;
+    p.n_qblocks = (int)(((long long)max_q * p.G + kPfRows - 1) / kPfRows);
     CUtensorMap map;
     const int rc = codes4_tensor_map(c, kPfBN, &map);
     if (rc != SLIM_OK) return rc;
-    return launch_prefill<false, 4>(map, p, B, stream, after_append);
+    return p.G > 1 ? launch_prefill<false, 4, true>(map, p, B, stream, after_append) : launch_prefill<false, 4>(map, p, B, stream, after_append);
 }
 
 }  // namespace slim
