@@ -1,53 +1,45 @@
 // Page tables of the caches: fork (continue, share, copy, free), grow, compact.
 //
 // Each call is a plan and, where pages have to be copied, the copies.  The plan is integer work on a few thousand words
-// and all of it is latency: one cluster of eight blocks runs it in a handful of phases with the cluster's barrier between
-// them (one block alone took as many round trips to memory per phase as it has entries per thread).  Nothing depends on
-// the order in which atomics arrive: they only add to counters and take minima, and free pages are found by rank - every
-// warp counts those of its slice of the pool, the counts are summed over the warps before it, and a second look at the
-// slice names the page of each rank.
+// and all of it is latency, so one block runs it, with the page counters and what it notes per row in shared memory where
+// they fit (below 50,000 words: phases then cost a barrier each.  A cluster of eight blocks with its counters in global memory,
+// a cluster barrier and a trip to the L2 per phase took 10.9 us where this form takes KFORK on 16 rows of 59 pages in all).
+// Nothing depends on the order in which atomics arrive: they only add to counters and take minima, and free pages are found
+// by rank - every warp counts those of its slice of the pool, the counts of the warps before it are summed, and a second
+// look at the slice names the page of each rank.
 //
 // The copies (a job is a source page, a target page and a number of tokens) are bound by HBM: a warp copies the codes of
 // one (job, kv head, K or V), eight 16-byte words per lane in flight.
-#include <cooperative_groups.h>
-
 #include "slim_common.cuh"
 #include "slim_tmap.cuh"
 
 namespace slim {
 
-namespace cg = cooperative_groups;
+constexpr int kPgThreads = 1024;
+constexpr int kPgWarps = kPgThreads / 32;
+constexpr int kPgMaxLayers = 64;           // of one launch (they are passed by value)
+constexpr int kPgSharedInts = 50000;       // counters and rows' notes that go into shared memory
 
-constexpr int kPgCluster = 8;
-constexpr int kPgThreads = 512;
-constexpr int kPgWarps = kPgCluster * kPgThreads / 32;
-constexpr int kPgMaxLayers = 64;   // of one launch (they are passed by value)
-
-constexpr int kAll = kPgCluster * kPgThreads;
-
-// Workspace, in ints: how many jobs there are; the warps' totals; then by page: counters, job sources, job targets; then
-// by row: the first child, the rank of the first page that a row needs, and by job the tokens to copy.
+// Workspace, in ints: how many jobs there are; by page: job sources and targets, counters; by row: tokens of the job, the
+// row's notes.  The copies read the jobs; counters and notes are used only where shared memory does not hold them.
 struct PagesWork {
-    int *n_jobs, *totals, *count, *source, *target, *first, *rank, *part;
+    int *n_jobs, *source, *target, *part, *notes;
 };
-constexpr int kPgHead = 4 + 3 * kPgWarps;
+constexpr int kPgHead = 4;
+constexpr int kPgNotes = 4;   // notes per row
 static PagesWork pages_work(void *workspace, int num_pages, int rows)
 {
-    int *w = static_cast<int *>(workspace);
     PagesWork p;
-    p.n_jobs = w;
-    p.totals = w + 4;
-    p.count = w + kPgHead;
-    p.source = p.count + num_pages;
+    p.n_jobs = static_cast<int *>(workspace);
+    p.source = p.n_jobs + kPgHead;
     p.target = p.source + num_pages;
-    p.first = p.target + num_pages;
-    p.rank = p.first + rows;
-    p.part = p.rank + rows;
+    p.part = p.target + num_pages;
+    p.notes = p.part + rows;
     return p;
 }
 size_t pages_workspace_bytes(int num_pages, int rows)
 {
-    return ((size_t)kPgHead + 3 * (size_t)num_pages + 3 * (size_t)rows) * sizeof(int);
+    return (kPgHead + 3 * (size_t)num_pages + (1 + kPgNotes) * (size_t)rows) * sizeof(int);
 }
 
 struct PagesParams {
@@ -55,13 +47,22 @@ struct PagesParams {
     PagesWork w;
     const int32_t *parent, *kv_len;
     int32_t *len_out, *result;
-    int room;
+    int room, rows;   // rows: the larger of the two tables'
 };
 
-// What the cluster's threads have written becomes visible to all of them.  Words that another block has written are read
-// with pg_ld, past the L1.
-__device__ __forceinline__ void pg_sync() { cg::this_cluster().sync(); }
-__device__ __forceinline__ int pg_ld(const int *ptr) { return __ldcg(ptr); }
+// The block's arrays: counters by page, then four notes by row.  Where they lie in global memory the atomics on them bypass
+// the L1, and so do these loads.
+template <bool kShared>
+struct PgArrays {
+    int *count, *a, *b, *c, *d;
+    __device__ __forceinline__ PgArrays(const PagesParams &p, int *smem)
+    {
+        count = kShared ? smem : p.w.notes;
+        a = count + p.from.num_pages;
+        b = a + p.rows, c = b + p.rows, d = c + p.rows;
+    }
+    __device__ __forceinline__ static int ld(const int *ptr) { return kShared ? *ptr : __ldcg(ptr); }
+};
 
 // The warp's contiguous slice of n things, in whole groups of 32.
 __device__ __forceinline__ void pg_slice(int n, int warp, int &lo, int &hi)
@@ -73,14 +74,9 @@ __device__ __forceinline__ void pg_slice(int n, int warp, int &lo, int &hi)
 // Sum of the totals of the warps before this one, and of all.
 __device__ __forceinline__ int pg_before(const int *totals, int warp, int lane, int &all)
 {
-    int mine = 0, sum = 0;
-    for (int i = lane; i < kPgWarps; i += 32) {
-        const int v = pg_ld(totals + i);
-        sum += v;
-        if (i < warp) mine += v;
-    }
-    all = __reduce_add_sync(0xffffffffu, sum);
-    return __reduce_add_sync(0xffffffffu, mine);
+    const int v = totals[lane];
+    all = __reduce_add_sync(0xffffffffu, v);
+    return __reduce_add_sync(0xffffffffu, lane < warp ? v : 0);
 }
 // How many i of the warp's slice of n satisfy `is`.
 template <class Is>
@@ -104,245 +100,240 @@ __device__ __forceinline__ void pg_rank(int n, int warp, int lane, int base, Is 
         base += __popc(all);
     }
 }
-
-__device__ __forceinline__ int pg_held(const slim_pages_t &p, int row) { return min(max(__ldg(p.held + row), 0), p.stride); }
-
-// What row i of the new table takes over from its parent: all pages held as the heir, else the full ones; a row that is
-// no heir and whose parent's last page is filled in part gets a copy of it.
-struct PgRow {
-    int parent, shared, part;   // part: tokens of the page to copy (0: none)
-    bool heir;
-};
-__device__ __forceinline__ PgRow pg_row(const PagesParams &p, int i)
+// Calls body(row, j) for every entry of a table, several of a thread's entries in flight.
+template <class Body>
+__device__ __forceinline__ void pg_entries(int rows, int stride, Body body)
 {
-    PgRow r;
-    r.parent = __ldg(p.parent + i);
-    r.shared = r.part = 0;
-    r.heir = false;
-    if (r.parent < 0 || r.parent >= p.from.rows) {
-        r.parent = -1;
-        return r;
+    const long long n = (long long)rows * stride;
+    if (n <= 0x7FFFFFFF - 4 * kPgThreads) {
+#pragma unroll 4
+        for (int i = threadIdx.x; i < (int)n; i += kPgThreads) body((int)((unsigned)i / (unsigned)stride), (int)((unsigned)i % (unsigned)stride));
+    } else {
+        for (long long i = threadIdx.x; i < n; i += kPgThreads) body((int)(i / stride), (int)(i % stride));
     }
-    const int held = pg_held(p.from, r.parent), len = max(__ldg(p.kv_len + r.parent), 0), whole = len / kPageTokens;
-    r.heir = pg_ld(p.w.first + r.parent) == i;
-    r.shared = r.heir ? held : min(whole, held);
-    r.part = (!r.heir && whole < held) ? len % kPageTokens : 0;
-    return r;
 }
+__device__ __forceinline__ int pg_held(const slim_pages_t &p, int row) { return min(max(p.held[row], 0), p.stride); }
 
-__global__ void __cluster_dims__(kPgCluster, 1, 1) __launch_bounds__(kPgThreads)
+template <bool kShared>
+__global__ void __launch_bounds__(kPgThreads, 1)
 slim_pages_fork_kernel(const PagesParams p)
 {
-    const int lane = threadIdx.x & 31, warp = blockIdx.x * (kPgThreads / 32) + (threadIdx.x >> 5);
-    const int thread = blockIdx.x * kPgThreads + threadIdx.x, n_pages = p.from.num_pages;
-    int *count = p.w.count;
+    extern __shared__ int smem_ints[];
+    __shared__ int totals[2][kPgWarps];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, n_pages = p.from.num_pages, n_in = p.from.rows, n_out = p.to.rows;
+    const PgArrays<kShared> ar(p, smem_ints);
+    auto ld = [](const int *ptr) { return PgArrays<kShared>::ld(ptr); };
+    int *count = ar.count, *first = ar.a, *kids = ar.b;      // by old row: its first child, how many it has
     pdl_launch_dependents();   // the copies queued behind this launch wait for its end
     pdl_wait();
-    for (int i = thread; i < n_pages; i += kAll) count[i] = p.from.refs[i];
-    for (int i = thread; i < p.from.rows; i += kAll) p.w.first[i] = 0x7FFFFFFF;
-    pg_sync();
-    // ---- the old rows let go of their pages; the first child of every row
-    for (int b = warp; b < p.from.rows; b += kPgWarps) {
-        const int held = pg_held(p.from, b);
-        for (int j = lane; j < held; j += 32) {
-            const int page = __ldg(p.from.table + (size_t)b * p.from.stride + j);
-            if (page >= 0 && page < n_pages) atomicSub(count + page, 1);
-        }
-    }
-    for (int i = thread; i < p.to.rows; i += kAll) {
+    for (int i = tid; i < n_pages; i += kPgThreads) count[i] = p.from.refs[i];
+    for (int b = tid; b < n_in; b += kPgThreads) first[b] = 0x7FFFFFFF, kids[b] = 0;
+    __syncthreads();
+    for (int i = tid; i < n_out; i += kPgThreads) {
         const int parent = __ldg(p.parent + i);
-        if (parent >= 0 && parent < p.from.rows) atomicMin(p.w.first + parent, i);
-    }
-    pg_sync();
-    // ---- the new rows take theirs
-    for (int i = warp; i < p.to.rows; i += kPgWarps) {
-        const PgRow r = pg_row(p, i);
-        for (int j = lane; j < r.shared; j += 32) {
-            const int page = __ldg(p.from.table + (size_t)r.parent * p.from.stride + j);
-            if (page >= 0 && page < n_pages) atomicAdd(count + page, 1);
+        if (parent >= 0 && parent < n_in) {
+            atomicMin(first + parent, i);
+            atomicAdd(kids + parent, 1);
         }
     }
-    auto copies = [&](int i) { return pg_row(p, i).part > 0; };
-    auto is_free = [&](int page) { return pg_ld(count + page) == 0; };
-    {
-        const int n = pg_count(p.to.rows, warp, lane, copies);
-        if (lane == 0) p.w.totals[warp] = n;
+    __syncthreads();
+    // ---- a full page is held by all children from now on, the pages behind those by the first child
+    pg_entries(n_in, p.from.stride, [&](int b, int j) {
+        const int n = ld(kids + b);
+        if (n == 1 || j >= pg_held(p.from, b)) return;
+        const int change = (n == 0) ? -1 : (j < max(__ldg(p.kv_len + b), 0) / kPageTokens ? n - 1 : 0);
+        if (change == 0) return;
+        const int page = __ldg(p.from.table + (size_t)b * p.from.stride + j);
+        if (page >= 0 && page < n_pages) atomicAdd(count + page, change);
+    });
+    // ---- what a new row takes over: all pages held as its parent's first child, else the full ones and a copy of the tokens
+    //      behind them
+    int *shared = ar.c, *rank = ar.d;   // by new row: pages taken over; tokens to copy, later the copy's rank
+    for (int i = tid; i < n_out; i += kPgThreads) {
+        const int parent = __ldg(p.parent + i);
+        int take = 0, part = 0;
+        if (parent >= 0 && parent < n_in) {
+            const int held = pg_held(p.from, parent), len = max(__ldg(p.kv_len + parent), 0), whole = len / kPageTokens;
+            const bool heir = ld(first + parent) == i;
+            take = heir ? held : min(whole, held);
+            part = (!heir && whole < held) ? len % kPageTokens : 0;
+        }
+        shared[i] = take, rank[i] = part;
     }
-    pg_sync();
+    __syncthreads();
+    auto copies = [&](int i) { return ld(rank + i) > 0; };
+    auto is_free = [&](int page) { return ld(count + page) == 0; };
     {
-        const int n = pg_count(n_pages, warp, lane, is_free);
-        if (lane == 0) p.w.totals[kPgWarps + warp] = n;
+        const int a = pg_count(n_out, warp, lane, copies), b = pg_count(n_pages, warp, lane, is_free);
+        if (lane == 0) totals[0][warp] = a, totals[1][warp] = b;
     }
-    pg_sync();
+    __syncthreads();
     int need, free_pages;
-    const int row_base = pg_before(p.w.totals, warp, lane, need), page_base = pg_before(p.w.totals + kPgWarps, warp, lane, free_pages);
-    if (thread == 0) {
+    const int row_base = pg_before(totals[0], warp, lane, need), page_base = pg_before(totals[1], warp, lane, free_pages);
+    if (tid == 0) {
         p.result[0] = max(0, need - free_pages);
         p.result[1] = max(0, free_pages - need);
         *p.w.n_jobs = (need <= free_pages) ? need : 0;
     }
-    if (need > free_pages) return;   // (every thread of the cluster)
-    pg_rank(n_pages, warp, lane, page_base, is_free, [&](int page, int rank) {
-        if (rank < need) p.w.target[rank] = page;
+    if (need > free_pages) return;   // (every thread)
+    // ---- free pages by rank, jobs by rank; a page taken has one holder
+    pg_rank(n_pages, warp, lane, page_base, is_free, [&](int page, int r) {
+        if (r < need) p.w.target[r] = page;
+        p.to.refs[page] = (r < need) ? 1 : 0;
     });
-    pg_rank(p.to.rows, warp, lane, row_base, copies, [&](int i, int rank) { p.w.rank[i] = rank; });
-    pg_sync();
-    // ---- rows, jobs and counters
-    for (int i = warp; i < p.to.rows; i += kPgWarps) {
-        const PgRow r = pg_row(p, i);
-        const int32_t *old = p.from.table + (size_t)max(r.parent, 0) * p.from.stride;
-        int32_t *row = p.to.table + (size_t)i * p.to.stride;
-        int fresh = -1;
-        if (r.part > 0) {
-            const int rank = pg_ld(p.w.rank + i);
-            fresh = pg_ld(p.w.target + rank);
-            if (lane == 0) {
-                const int page = __ldg(old + r.shared);
-                const bool real = page >= 0 && page < n_pages;
-                p.w.source[rank] = real ? page : fresh;
-                p.w.part[rank] = real ? r.part : 0;
-            }
-        }
-        for (int j = lane; j < p.to.stride; j += 32) row[j] = (j < r.shared) ? __ldg(old + j) : (j == r.shared ? fresh : -1);
-        if (lane == 0) {
-            p.to.held[i] = r.shared + (r.part > 0 ? 1 : 0);
-            p.len_out[i] = (r.parent < 0) ? -1 : __ldg(p.kv_len + r.parent);
-        }
-    }
-    // (a fresh page's counter is 0 in `count` and 1 in the result)
-    pg_rank(n_pages, warp, lane, page_base, is_free, [&](int page, int rank) { p.to.refs[page] = (rank < need) ? 1 : 0; });
-    for (int i = thread; i < n_pages; i += kAll) {
-        const int v = pg_ld(count + i);
+    pg_rank(n_out, warp, lane, row_base, copies, [&](int i, int r) {
+        const int page = __ldg(p.from.table + (size_t)__ldg(p.parent + i) * p.from.stride + ld(shared + i));
+        const bool real = page >= 0 && page < n_pages;
+        p.w.source[r] = real ? page : 0;
+        p.w.part[r] = real ? ld(rank + i) : 0;
+        rank[i] = -1 - r;
+    });
+    for (int i = tid; i < n_pages; i += kPgThreads) {
+        const int v = ld(count + i);
         if (v != 0) p.to.refs[i] = v;
     }
+    __syncthreads();
+    pg_entries(n_out, p.to.stride, [&](int i, int j) {
+        const int take = ld(shared + i), r = ld(rank + i);
+        int page = -1;
+        if (j < take) page = __ldg(p.from.table + (size_t)__ldg(p.parent + i) * p.from.stride + j);
+        else if (j == take && r < 0) page = __ldcg(p.w.target - 1 - r);
+        p.to.table[(size_t)i * p.to.stride + j] = page;
+    });
+    for (int i = tid; i < n_out; i += kPgThreads) {
+        const int parent = __ldg(p.parent + i);
+        p.to.held[i] = ld(shared + i) + (ld(rank + i) < 0 ? 1 : 0);
+        p.len_out[i] = (parent >= 0 && parent < n_in) ? __ldg(p.kv_len + parent) : -1;
+    }
 }
 
-// Pages that row i lacks for its tokens.
-__device__ __forceinline__ int pg_lacks(const PagesParams &p, int i)
-{
-    const int len = __ldg(p.kv_len + i);
-    if (len < 0) return 0;
-    const long long want = ((long long)len + p.room + kPageTokens - 1) / kPageTokens;
-    return max(0, (int)min(want, (long long)p.from.stride) - min(max(p.from.held[i], 0), p.from.stride));
-}
-
-__global__ void __cluster_dims__(kPgCluster, 1, 1) __launch_bounds__(kPgThreads)
+template <bool kShared>
+__global__ void __launch_bounds__(kPgThreads, 1)
 slim_pages_grow_kernel(const PagesParams p)
 {
-    const int lane = threadIdx.x & 31, warp = blockIdx.x * (kPgThreads / 32) + (threadIdx.x >> 5);
-    const int n_pages = p.from.num_pages;
+    extern __shared__ int smem_ints[];
+    __shared__ int totals[2][kPgWarps];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, n_pages = p.from.num_pages, n = p.from.rows, stride = p.from.stride;
+    const PgArrays<kShared> ar(p, smem_ints);
+    auto ld = [](const int *ptr) { return PgArrays<kShared>::ld(ptr); };
+    int *count = ar.count, *lacks = ar.a, *base = ar.b, *held = ar.c;   // by row: pages that it lacks, the rank of the first of them
     pdl_launch_dependents();
     pdl_wait();
-    auto is_free = [&](int page) { return pg_ld(p.from.refs + page) == 0; };
-    int lo, hi, lacking = 0;
-    pg_slice(p.from.rows, warp, lo, hi);
+    for (int i = tid; i < n_pages; i += kPgThreads) count[i] = p.from.refs[i];
+    for (int i = tid; i < n; i += kPgThreads) {
+        const int len = __ldg(p.kv_len + i), has = pg_held(p.from, i);
+        const long long want = ((long long)max(len, 0) + p.room + kPageTokens - 1) / kPageTokens;
+        lacks[i] = (len < 0) ? 0 : max(0, (int)min(want, (long long)stride) - has);
+        held[i] = has;
+    }
+    __syncthreads();
+    auto is_free = [&](int page) { return ld(count + page) == 0; };
+    int lo, hi, mine = 0;
+    pg_slice(n, warp, lo, hi);
     // (bounded so that no sum passes 32 bits: more than the largest pool has, and the call ends below)
     constexpr int kMost = (1 << 24) - 1;
-    for (int i = lo + lane; i < hi; i += 32) lacking = min(lacking + min(pg_lacks(p, i), kMost), kMost);
-    lacking = __reduce_add_sync(0xffffffffu, lacking);
+    for (int i = lo + lane; i < hi; i += 32) mine = min(mine + min(ld(lacks + i), kMost), kMost);
+    mine = min(__reduce_add_sync(0xffffffffu, mine), kMost);
     const int n_free = pg_count(n_pages, warp, lane, is_free);
-    if (lane == 0) {
-        p.w.totals[warp] = min(lacking, kMost);
-        p.w.totals[kPgWarps + warp] = n_free;
-    }
-    pg_sync();
+    if (lane == 0) totals[0][warp] = mine, totals[1][warp] = n_free;
+    __syncthreads();
     int need, free_pages;
-    const int row_base = pg_before(p.w.totals, warp, lane, need), page_base = pg_before(p.w.totals + kPgWarps, warp, lane, free_pages);
-    if (blockIdx.x == 0 && threadIdx.x == 0) {
+    int at = pg_before(totals[0], warp, lane, need);
+    const int page_base = pg_before(totals[1], warp, lane, free_pages);
+    if (tid == 0) {
         p.result[0] = max(0, need - free_pages);
         p.result[1] = max(0, free_pages - need);
     }
-    if (need > free_pages || need == 0) return;   // (every thread of the cluster)
-    pg_rank(n_pages, warp, lane, page_base, is_free, [&](int page, int rank) {
-        if (rank < need) p.w.target[rank] = page;
+    if (need > free_pages || need == 0) return;   // (every thread)
+    pg_rank(n_pages, warp, lane, page_base, is_free, [&](int page, int r) {
+        if (r < need) p.w.target[r] = page, p.from.refs[page] = 1;
     });
-    pg_sync();   // (the counters of the pages taken change from here on)
-    int base = row_base;
     for (int i0 = lo; i0 < hi; i0 += 32) {
-        const int i = i0 + lane, n = (i < hi) ? pg_lacks(p, i) : 0;
-        int upto = n;
+        const int v = (i0 + lane < hi) ? ld(lacks + i0 + lane) : 0;
+        int upto = v;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
-            const int v = __shfl_up_sync(0xffffffffu, upto, o);
-            if (lane >= o) upto += v;
+            const int x = __shfl_up_sync(0xffffffffu, upto, o);
+            if (lane >= o) upto += x;
         }
-        const int held = (i < hi) ? min(max(p.from.held[i], 0), p.from.stride) : 0;
-        for (int r = 0; r < min(32, hi - i0); ++r) {
-            const int n_r = __shfl_sync(0xffffffffu, n, r), at = base + __shfl_sync(0xffffffffu, upto, r) - n_r, held_r = __shfl_sync(0xffffffffu, held, r);
-            for (int j = lane; j < n_r; j += 32) {
-                const int page = pg_ld(p.w.target + at + j);
-                p.from.table[(size_t)(i0 + r) * p.from.stride + held_r + j] = page;
-                p.from.refs[page] = 1;
-            }
-        }
-        if (n > 0) p.from.held[i] = held + n;
-        base += __shfl_sync(0xffffffffu, upto, 31);
+        if (i0 + lane < hi) base[i0 + lane] = at + upto - v;
+        at += __shfl_sync(0xffffffffu, upto, 31);
+    }
+    __syncthreads();
+    // (a row lacks few pages as a rule: a warp takes a row at a time, several in flight)
+#pragma unroll 4
+    for (int i = warp; i < n; i += kPgWarps) {
+        const int v = ld(lacks + i), b = ld(base + i), has = ld(held + i);
+        for (int j = lane; j < v; j += 32) p.from.table[(size_t)i * stride + has + j] = __ldcg(p.w.target + b + j);
+        if (lane == 0 && v > 0) p.from.held[i] = has + v;
     }
 }
 
-__global__ void __cluster_dims__(kPgCluster, 1, 1) __launch_bounds__(kPgThreads)
+template <bool kShared>
+__global__ void __launch_bounds__(kPgThreads, 1)
 slim_pages_compact_kernel(const PagesParams p)
 {
-    const int lane = threadIdx.x & 31, warp = blockIdx.x * (kPgThreads / 32) + (threadIdx.x >> 5);
-    const int thread = blockIdx.x * kPgThreads + threadIdx.x, n_pages = p.from.num_pages;
-    int *count = p.w.count;
+    extern __shared__ int smem_ints[];
+    __shared__ int totals[3][kPgWarps];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, n_pages = p.from.num_pages, n = p.from.rows, stride = p.from.stride;
+    const PgArrays<kShared> ar(p, smem_ints);
+    auto ld = [](const int *ptr) { return PgArrays<kShared>::ld(ptr); };
+    int *count = ar.count, *held = ar.a;
     pdl_launch_dependents();
     pdl_wait();
-    for (int i = thread; i < n_pages; i += kAll) count[i] = p.from.refs[i];   // (`to` may be `from`)
-    pg_sync();
-    auto is_used = [&](int page) { return pg_ld(count + page) != 0; };
-    const int mine = pg_count(n_pages, warp, lane, is_used);
-    if (lane == 0) p.w.totals[warp] = mine;
-    pg_sync();
+    for (int i = tid; i < n_pages; i += kPgThreads) count[i] = p.from.refs[i];   // (`to` may be `from`)
+    for (int b = tid; b < n; b += kPgThreads) held[b] = pg_held(p.from, b);
+    __syncthreads();
+    auto is_used = [&](int page) { return ld(count + page) != 0; };
+    {
+        const int a = pg_count(n_pages, warp, lane, is_used);
+        if (lane == 0) totals[0][warp] = a;
+    }
+    __syncthreads();
     int n_used;
-    const int before = pg_before(p.w.totals, warp, lane, n_used);
-    (void)before;
+    (void)pg_before(totals[0], warp, lane, n_used);
     auto moves = [&](int page) { return page >= n_used && is_used(page); };
     auto hole = [&](int page) { return page < n_used && !is_used(page); };
-    const int n_moves = pg_count(n_pages, warp, lane, moves), n_holes = pg_count(n_pages, warp, lane, hole);
-    if (lane == 0) {
-        p.w.totals[kPgWarps + warp] = n_moves;
-        p.w.totals[2 * kPgWarps + warp] = n_holes;
+    {
+        const int a = pg_count(n_pages, warp, lane, moves), b = pg_count(n_pages, warp, lane, hole);
+        if (lane == 0) totals[1][warp] = a, totals[2][warp] = b;
     }
-    pg_sync();
+    __syncthreads();
     int all, all_holes;   // (as many holes as movers)
-    const int base = pg_before(p.w.totals + kPgWarps, warp, lane, all), hole_base = pg_before(p.w.totals + 2 * kPgWarps, warp, lane, all_holes);
-    if (thread == 0) {
+    const int base = pg_before(totals[1], warp, lane, all), hole_base = pg_before(totals[2], warp, lane, all_holes);
+    if (tid == 0) {
         p.result[0] = n_used;
         p.result[1] = all;
         *p.w.n_jobs = all;
     }
-    pg_rank(n_pages, warp, lane, hole_base, hole, [&](int page, int rank) { p.w.target[rank] = page; });
-    pg_sync();
+    pg_rank(n_pages, warp, lane, hole_base, hole, [&](int page, int r) { p.w.target[r] = page; });
+    __syncthreads();
     // ---- a mover's page takes its counter along and leaves its new id in `count` (as a negative number)
-    pg_rank(n_pages, warp, lane, base, moves, [&](int page, int rank) {
-        const int to = pg_ld(p.w.target + rank);
-        p.w.source[rank] = page;
-        p.to.refs[to] = pg_ld(count + page);
+    pg_rank(n_pages, warp, lane, base, moves, [&](int page, int r) {
+        const int to = __ldcg(p.w.target + r);
+        p.w.source[r] = page;
+        p.to.refs[to] = ld(count + page);
         p.to.refs[page] = 0;
         count[page] = -1 - to;
     });
-    pg_sync();
-    for (int i = thread; i < n_pages; i += kAll) {
-        const int v = pg_ld(count + i);
+    __syncthreads();
+    for (int i = tid; i < n_pages; i += kPgThreads) {
+        const int v = ld(count + i);
         if (i < n_used && v != 0) p.to.refs[i] = v;
         if (i >= n_used && v == 0) p.to.refs[i] = 0;
     }
-    for (int b = warp; b < p.from.rows; b += kPgWarps) {
-        const int held = min(max(p.from.held[b], 0), p.from.stride);
-        for (int j = lane; j < p.from.stride; j += 32) {
-            int page = -1;
-            if (j < held) {
-                page = p.from.table[(size_t)b * p.from.stride + j];
-                if (page >= n_used && page < n_pages) {
-                    const int v = pg_ld(count + page);
-                    if (v < 0) page = -1 - v;
-                }
+    pg_entries(n, stride, [&](int b, int j) {
+        int page = -1;
+        if (j < ld(held + b)) {
+            page = p.from.table[(size_t)b * stride + j];
+            if (page >= n_used && page < n_pages) {
+                const int v = ld(count + page);
+                if (v < 0) page = -1 - v;
             }
-            p.to.table[(size_t)b * p.to.stride + j] = page;
         }
-        if (lane == 0) p.to.held[b] = held;
-    }
+        p.to.table[(size_t)b * stride + j] = page;
+    });
+    for (int b = tid; b < n; b += kPgThreads) p.to.held[b] = ld(held + b);
 }
 
 // ---------------------------------------------------------------- copies
@@ -378,11 +369,11 @@ slim_pages_copy_kernel(const __grid_constant__ PageLayersArg layers, const Pages
     const slim_layer_t &layer = layers.at[blockIdx.y];
     pdl_wait();
     const int blocks = 2 * layer.num_kv_heads;
-    const long long items = (long long)pg_ld(w.n_jobs) * blocks;
+    const long long items = (long long)__ldcg(w.n_jobs) * blocks;
     for (long long it = (long long)blockIdx.x * (kCopyThreads / 32) + (threadIdx.x >> 5); it < items; it += (long long)gridDim.x * (kCopyThreads / 32)) {
         const int job = (int)(it / blocks), part = (int)(it - (long long)job * blocks);
-        const int tokens = whole ? kPageTokens : pg_ld(w.part + job);
-        const size_t from = (size_t)pg_ld(w.source + job) * blocks + part, to = (size_t)pg_ld(w.target + job) * blocks + part;
+        const int tokens = whole ? kPageTokens : __ldcg(w.part + job);
+        const size_t from = (size_t)__ldcg(w.source + job) * blocks + part, to = (size_t)__ldcg(w.target + job) * blocks + part;
         const size_t code_block = (size_t)kPageTokens * layer.row_bytes, scale_block = (size_t)kPageTokens * 4;
         unsigned char *codes = static_cast<unsigned char *>(layer.codes), *scales = static_cast<unsigned char *>(layer.scales);
         pg_copy(codes + to * code_block, codes + from * code_block, tokens * layer.row_bytes, lane);
@@ -413,49 +404,56 @@ static int launch_copies(const PagesWork &w, const slim_layer_t *layers, int n_l
     return SLIM_OK;
 }
 
-int launch_pages_fork(const slim_pages_t *from, const slim_pages_t *to, const int32_t *parent, const int32_t *kv_len, int32_t *len_out,
-                      const slim_layer_t *layers, int n_layers, int32_t *result, void *workspace, cudaStream_t stream)
+// One block; its arrays in shared memory where they fit.
+static int launch_plan(void (*in_shared)(PagesParams), void (*in_global)(PagesParams), const PagesParams &p, cudaStream_t stream)
+{
+    const long long ints = (long long)p.from.num_pages + (long long)kPgNotes * p.rows;
+    const bool fits = ints <= kPgSharedInts;
+    if (fits) {
+        const int rc = allow_dynamic_smem(reinterpret_cast<const void *>(in_shared), kPgSharedInts * (int)sizeof(int));
+        if (rc != SLIM_OK) return rc;
+    }
+    SLIM_CUDA_TRY(launch_pdl(fits ? in_shared : in_global, dim3(1), dim3(kPgThreads), fits ? (size_t)ints * sizeof(int) : 0, stream, p));
+    return SLIM_OK;
+}
+static PagesParams pages_params(const slim_pages_t *from, const slim_pages_t *to, const int32_t *kv_len, int32_t *result, void *workspace)
 {
     PagesParams p;
     p.from = *from;
     p.to = *to;
-    p.w = pages_work(workspace, from->num_pages, from->rows > to->rows ? from->rows : to->rows);
-    p.parent = parent;
-    p.kv_len = kv_len;
-    p.len_out = len_out;
-    p.result = result;
-    p.room = 0;
-    SLIM_CUDA_TRY(launch_pdl(slim_pages_fork_kernel, dim3(kPgCluster), dim3(kPgThreads), 0, stream, p));
-    return launch_copies(p.w, layers, n_layers, to->rows, false, stream);
-}
-
-int launch_pages_grow(const slim_pages_t *pages, const int32_t *kv_len, int room, int32_t *result, void *workspace, cudaStream_t stream)
-{
-    PagesParams p;
-    p.from = p.to = *pages;
-    p.w = pages_work(workspace, pages->num_pages, pages->rows);
+    p.rows = from->rows > to->rows ? from->rows : to->rows;
+    p.w = pages_work(workspace, from->num_pages, p.rows);
     p.parent = nullptr;
     p.kv_len = kv_len;
     p.len_out = nullptr;
     p.result = result;
+    p.room = 0;
+    return p;
+}
+
+int launch_pages_fork(const slim_pages_t *from, const slim_pages_t *to, const int32_t *parent, const int32_t *kv_len, int32_t *len_out,
+                      const slim_layer_t *layers, int n_layers, int32_t *result, void *workspace, cudaStream_t stream)
+{
+    PagesParams p = pages_params(from, to, kv_len, result, workspace);
+    p.parent = parent;
+    p.len_out = len_out;
+    const int rc = launch_plan(slim_pages_fork_kernel<true>, slim_pages_fork_kernel<false>, p, stream);
+    return rc != SLIM_OK ? rc : launch_copies(p.w, layers, n_layers, to->rows, false, stream);
+}
+
+int launch_pages_grow(const slim_pages_t *pages, const int32_t *kv_len, int room, int32_t *result, void *workspace, cudaStream_t stream)
+{
+    PagesParams p = pages_params(pages, pages, kv_len, result, workspace);
     p.room = room;
-    SLIM_CUDA_TRY(launch_pdl(slim_pages_grow_kernel, dim3(kPgCluster), dim3(kPgThreads), 0, stream, p));
-    return SLIM_OK;
+    return launch_plan(slim_pages_grow_kernel<true>, slim_pages_grow_kernel<false>, p, stream);
 }
 
 int launch_pages_compact(const slim_pages_t *from, const slim_pages_t *to, const slim_layer_t *layers, int n_layers, int32_t *result,
                          void *workspace, cudaStream_t stream)
 {
-    PagesParams p;
-    p.from = *from;
-    p.to = *to;
-    p.w = pages_work(workspace, from->num_pages, from->rows);
-    p.parent = p.kv_len = nullptr;
-    p.len_out = nullptr;
-    p.result = result;
-    p.room = 0;
-    SLIM_CUDA_TRY(launch_pdl(slim_pages_compact_kernel, dim3(kPgCluster), dim3(kPgThreads), 0, stream, p));
-    return launch_copies(p.w, layers, n_layers, from->num_pages, true, stream);
+    const PagesParams p = pages_params(from, to, nullptr, result, workspace);
+    const int rc = launch_plan(slim_pages_compact_kernel<true>, slim_pages_compact_kernel<false>, p, stream);
+    return rc != SLIM_OK ? rc : launch_copies(p.w, layers, n_layers, from->num_pages, true, stream);
 }
 
 }  // namespace slim

@@ -65,6 +65,7 @@ static_assert(kBytes <= 232448, "shared memory budget of one block");
 }  // namespace pfl
 
 struct PrefillTcParams {
+    const uint8_t *codes4;   // of the 4-bit cache, whose tiles are copied as they lie (INT8 tiles go by a tensor map)
     const void *scales;   // fp32 per row; of the 4-bit cache a (scale, offset) pair of bf16, also four bytes
     const int32_t *block_table;
     const int32_t *cu_q;
@@ -145,8 +146,11 @@ __device__ __forceinline__ float pf_row_size(uint32_t word)
 // pipeline (a key tile is loaded and converted again in the second pass); the tile sequence of the block is
 // simply twice as long, and barrier phases count positions in that sequence.
 //
-// kBits 4: the 4-bit cache.  Its raw rows are 64 bytes (64-byte swizzle), and a row's values scale * u + offset become
-// fp16 operands over the same kind of power of two, below the tile's largest |value| that its pairs allow.
+// kBits 4: the 4-bit cache.  A raw tile is 8 KB in one piece, converted by warps that take eight rows at a time (four lanes
+// per row, 16 bytes each: neither the loads nor the swizzled stores collide on banks); a row's values scale * u + offset become
+// fp16 operands over the same kind of power of two, below the tile's largest |value| that its pairs allow.  (Rows of 64
+// bytes in a swizzled tensor map, a row per thread, took the same time on 8192 tokens and 300 us in place of 295 on pieces
+// of 256 to 512 rows behind 4000 tokens.)
 template <bool kTwoPass, int kBits = 8, bool kPack = false>
 __global__ void __launch_bounds__(kPfThreads, 1)
 slim_prefill_tc_kernel(const __grid_constant__ CUtensorMap codes_map, const PrefillTcParams p)
@@ -205,14 +209,19 @@ slim_prefill_tc_kernel(const __grid_constant__ CUtensorMap codes_map, const Pref
         page = (page >= 0 && page < p.num_pages) ? page : 0;
         const uint32_t full = bar(pfl::RAW_FULL, kv);
         tc::mbar_arrive_expect_tx(full, kPageTokens * kHeadDim * kBits / 8 + 512);
-        tc::tma_load_2d(sbase + pfl::kRaw + kv * 16384, &codes_map, 0, ((page * p.Hkv + head) * 2 + kv) * kPageTokens, full);
+        if constexpr (kBits == 4) tc::bulk_load(sbase + pfl::kRaw + kv * 16384, p.codes4 + code4_block_offset(page, head, kv, p.Hkv), 8192, full);
+        else tc::tma_load_2d(sbase + pfl::kRaw + kv * 16384, &codes_map, 0, ((page * p.Hkv + head) * 2 + kv) * kPageTokens, full);
         tc::bulk_load(sbase + pfl::kRawScales + kv * 512, static_cast<const uint32_t *>(p.scales) + scale_block_offset(page, head, kv, p.Hkv), 512, full);
         if (kv == 1 && j + 1 < NT) {
             // the next key tile's page id, and its two tiles on their way into the L2 a step before they are asked for
             page_next = __ldg(bt + ((kTwoPass && j + 1 >= T) ? j + 1 - T : j + 1));
             const int pn = (page_next >= 0 && page_next < p.num_pages) ? page_next : 0;
-            tc::tma_prefetch_2d(&codes_map, 0, ((pn * p.Hkv + head) * 2) * kPageTokens);
-            tc::tma_prefetch_2d(&codes_map, 0, ((pn * p.Hkv + head) * 2 + 1) * kPageTokens);
+            if constexpr (kBits == 4) {
+                tc::bulk_prefetch(p.codes4 + code4_block_offset(pn, head, 0, p.Hkv), 16384);   // (V's tile follows K's)
+            } else {
+                tc::tma_prefetch_2d(&codes_map, 0, ((pn * p.Hkv + head) * 2) * kPageTokens);
+                tc::tma_prefetch_2d(&codes_map, 0, ((pn * p.Hkv + head) * 2 + 1) * kPageTokens);
+            }
         }
         ++raw_issued;
     };
@@ -515,35 +524,40 @@ slim_prefill_tc_kernel(const __grid_constant__ CUtensorMap codes_map, const Pref
                 wait(bar(pfl::VF_EMPTY, buf), ((uint32_t)(j >> 1) & 1u) ^ 1u);
             }
             unsigned char *dst_tile = smem + (is_k ? pfl::kKf : pfl::kVf) + buf * 32768;
+            if constexpr (kBits == 4) {
+                // warps 8-11 take three of the sixteen groups of eight rows each, the two spare warps two
+                const int g0 = main_cv ? (warp - 8) * 3 : 12 + (warp - 14) * 2, n_groups = main_cv ? 3 : 2;
+                const int c = lane & 3;
+                for (int gr = g0; gr < g0 + n_groups; ++gr) {
+                    const int r = gr * 8 + (lane >> 2);
+                    const uint4 w4 = *reinterpret_cast<const uint4 *>(raw + gr * 512 + lane * 16);
+                    const uint32_t row_scale = (r < n_valid) ? scales[r] : 0u;
+                    // scale and offset are bf16, over a power of two not far from the larger one: exact in fp16 down to 2^-14 of it
+                    const float f = pair_scale(row_scale) * rex, z = pair_offset(row_scale) * rex;
+                    const uint32_t fac2 = pack_half2(f, f), off2 = pack_half2(z, z);
+                    unsigned char *dstb = dst_tile + r * 128;
+                    const uint32_t w[4] = {w4.x, w4.y, w4.z, w4.w};
 #pragma unroll
-            for (int q = 0; q < 2; ++q) {
+                    for (int hf = 0; hf < 2; ++hf) {
+                        // dims 16 c .. + 15 in the low halves of the bytes, 64 further in the high ones
+                        uint32_t hh[8];
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            const uint32_t x = (w[k] >> (4 * hf)) & 0x0F0F0F0Fu;   // under 0x64: the fp16 number 1024 + code
+                            hh[2 * k] = pf_hfma2(pf_hsub2(__byte_perm(x, 0x64646464u, 0x4140), 0x64006400u), fac2, off2);
+                            hh[2 * k + 1] = pf_hfma2(pf_hsub2(__byte_perm(x, 0x64646464u, 0x4342), 0x64006400u), fac2, off2);
+                        }
+                        *reinterpret_cast<uint4 *>(dstb + hf * 16384 + (((2 * c) ^ (r & 7)) << 4)) = make_uint4(hh[0], hh[1], hh[2], hh[3]);
+                        *reinterpret_cast<uint4 *>(dstb + hf * 16384 + (((2 * c + 1) ^ (r & 7)) << 4)) = make_uint4(hh[4], hh[5], hh[6], hh[7]);
+                    }
+                }
+            }
+#pragma unroll
+            for (int q = 0; q < (kBits == 4 ? 0 : 2); ++q) {
                 if (q >= n_rows) break;
                 const int r = r0 + 64 * q;
                 const uint32_t row_scale = (r < n_valid) ? scales[r] : 0u;
                 unsigned char *dstb = dst_tile + r * 128;
-                if constexpr (kBits == 4) {
-                    // scale and offset are bf16, over a power of two not far from the larger one: exact in fp16 down to 2^-14 of it
-                    const float f = pair_scale(row_scale) * rex, z = pair_offset(row_scale) * rex;
-                    const uint32_t fac2 = pack_half2(f, f), off2 = pack_half2(z, z);
-                    for (int c = c_first / 2; c < c_last / 2; ++c) {
-                        // piece c of a raw row: dims 16 c .. + 15 in the low halves of its bytes, 64 further in the high ones
-                        const uint4 w4 = *reinterpret_cast<const uint4 *>(raw + r * 64 + ((c ^ ((r >> 1) & 3)) << 4));
-                        const uint32_t w[4] = {w4.x, w4.y, w4.z, w4.w};
-#pragma unroll
-                        for (int hf = 0; hf < 2; ++hf) {
-                            uint32_t hh[8];
-#pragma unroll
-                            for (int k = 0; k < 4; ++k) {
-                                const uint32_t x = (w[k] >> (4 * hf)) & 0x0F0F0F0Fu;   // under 0x64: the fp16 number 1024 + code
-                                hh[2 * k] = pf_hfma2(pf_hsub2(__byte_perm(x, 0x64646464u, 0x4140), 0x64006400u), fac2, off2);
-                                hh[2 * k + 1] = pf_hfma2(pf_hsub2(__byte_perm(x, 0x64646464u, 0x4342), 0x64006400u), fac2, off2);
-                            }
-                            *reinterpret_cast<uint4 *>(dstb + hf * 16384 + (((2 * c) ^ (r & 7)) << 4)) = make_uint4(hh[0], hh[1], hh[2], hh[3]);
-                            *reinterpret_cast<uint4 *>(dstb + hf * 16384 + (((2 * c + 1) ^ (r & 7)) << 4)) = make_uint4(hh[4], hh[5], hh[6], hh[7]);
-                        }
-                    }
-                    continue;
-                }
                 const float f = __uint_as_float(row_scale) * rex;   // scale / 2^e in [0, 2)
                 const uint32_t fac2 = pack_half2(f, f);
                 for (int c = c_first; c < c_last; ++c) {
@@ -679,6 +693,7 @@ static PrefillTcParams prefill_params(const Cache *c, const void *q, void *out, 
                                       float sm_scale, void *workspace)
 {
     PrefillTcParams p;
+    p.codes4 = nullptr;
     p.scales = c->scales;
     p.block_table = c->block_table;
     p.cu_q = cu_q;
@@ -727,9 +742,8 @@ int launch_prefill4_tc(const slim_cache4_t *c, const void *q, void *out, const i
     if (p.n_qblocks == 0) return SLIM_OK;
     if ((long long)max_q * p.G > (long long)kPfRows * 65535) return SLIM_ERR_UNSUPPORTED;
     p.n_qblocks = (int)(((long long)max_q * p.G + kPfRows - 1) / kPfRows);
-    CUtensorMap map;
-    const int rc = codes4_tensor_map(c, kPfBN, &map);
-    if (rc != SLIM_OK) return rc;
+    p.codes4 = c->codes;
+    const CUtensorMap map = {};   // (not read)
     return p.G > 1 ? launch_prefill<false, 4, true>(map, p, B, stream, after_append) : launch_prefill<false, 4>(map, p, B, stream, after_append);
 }
 

@@ -234,6 +234,11 @@ __device__ __forceinline__ void bulk_load(uint32_t dst_smem, const void *src, ui
         "l"(src), "r"(bytes), "r"(mbar_smem)
         : "memory");
 }
+// Brings a run of memory into the L2 without copying it anywhere (same alignment rules).
+__device__ __forceinline__ void bulk_prefetch(const void *src, uint32_t bytes)
+{
+    asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;\n" ::"l"(src), "r"(bytes) : "memory");
+}
 // Barrier among `count` threads (a multiple of 32) of the block, id 1..15.
 __device__ __forceinline__ void named_barrier(int id, int count)
 {

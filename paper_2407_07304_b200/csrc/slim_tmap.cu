@@ -75,16 +75,16 @@ int tensor_map(const Shape &want, CUtensorMap *out)
     return SLIM_OK;
 }
 
-Shape rows_shape(const void *ptr, long long rows, int row_bytes, CUtensorMapSwizzle swizzle, int box_rows)
+Shape rows_shape(const void *ptr, long long rows, int box_rows)
 {
     Shape s = {};
     s.ptr = ptr;
     s.type = CU_TENSOR_MAP_DATA_TYPE_UINT8;
     s.dims = 2;
-    s.size[0] = s.stride[0] = s.box[0] = (cuuint32_t)row_bytes;
+    s.size[0] = s.stride[0] = s.box[0] = kHeadDim;
     s.size[1] = (cuuint64_t)rows;
     s.box[1] = (cuuint32_t)box_rows;
-    s.swizzle = swizzle;
+    s.swizzle = CU_TENSOR_MAP_SWIZZLE_128B;
     return s;
 }
 template <class Cache>
@@ -96,12 +96,7 @@ long long pool_blocks(const Cache *c)   // (page, head, K|V)
 
 int codes_tensor_map(const slim_cache_t *c, int box_rows, CUtensorMap *out)
 {
-    return tensor_map(rows_shape(c->codes, pool_blocks(c) * kPageTokens, kHeadDim, CU_TENSOR_MAP_SWIZZLE_128B, box_rows), out);
-}
-
-int codes4_tensor_map(const slim_cache4_t *c, int box_rows, CUtensorMap *out)
-{
-    return tensor_map(rows_shape(c->codes, pool_blocks(c) * kPageTokens, kHeadDim / 2, CU_TENSOR_MAP_SWIZZLE_64B, box_rows), out);
+    return tensor_map(rows_shape(c->codes, pool_blocks(c) * kPageTokens, box_rows), out);
 }
 
 int unit4_tensor_maps(const slim_cache4_t *c, int blocks, CUtensorMap *codes, CUtensorMap *pairs)

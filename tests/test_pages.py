@@ -126,7 +126,7 @@ def check_tokens(model, caches):
             assert (scales == (1000 * i + want)[:, None, None].to(torch.int32)).all()
 
 
-@pytest.mark.parametrize("seed,num_pages,rows,stride", [(1, 40, 5, 4), (2, 150, 17, 6), (3, 700, 70, 5), (4, 5000, 3, 40)])
+@pytest.mark.parametrize("seed,num_pages,rows,stride", [(1, 40, 5, 4), (2, 150, 17, 6), (3, 700, 70, 5), (4, 5000, 3, 40), (5, 60000, 9, 6)])
 def test_a_random_run(seed, num_pages, rows, stride):
     """Twenty random steps of grow, fork (other numbers of rows too) and compact, every table after every step."""
     rng = random.Random(seed)
