@@ -598,6 +598,7 @@ class SlimPages:
         if refs.dim() != 1 or table.dim() != 2 or held.shape != table.shape[:1]:
             raise TypeError("refs [num_pages], table [rows, stride], held [rows]")
         self.refs, self.table, self.held = refs, table, held   # kept here because the struct holds bare addresses
+        self.num_pages, self.rows = refs.numel(), table.shape[0]
         self.struct = SlimPagesStruct(refs.data_ptr(), table.data_ptr(), held.data_ptr(), refs.numel(), table.shape[0], table.shape[1])
         self.ref = ctypes.byref(self.struct)
 
@@ -615,6 +616,7 @@ class PageLayers:
         self.caches = list(caches)
         if len({c.num_pages for c in self.caches}) > 1:
             raise ValueError("the layers' pools must have the same number of pages")
+        self.num_pages = self.caches[0].num_pages if self.caches else None
         rows = [HEAD_DIM // 2 if isinstance(c, SlimCache4) else HEAD_DIM for c in self.caches]
         self.array = (SlimLayerStruct * max(1, len(self.caches)))(
             *[SlimLayerStruct(c.codes.data_ptr(), c.scales.data_ptr(), c.Hkv, n) for c, n in zip(self.caches, rows)])
@@ -623,15 +625,16 @@ class PageLayers:
 def _layers(where, layers, pages):
     if layers is None:
         return None, 0
-    if any(c.num_pages != pages.refs.numel() for c in layers.caches):
+    if layers.num_pages != pages.num_pages and layers.caches:
         raise SlimError(SLIM_ERR_INVALID_ARG, f"{where}: a layer's pool and the page counters differ in size")
     return layers.array, len(layers.caches)
 
 
-def _i32_vector(where, n, *vectors):
-    for t in vectors:
-        if t.dtype is not torch.int32 or t.numel() < n or not t.is_contiguous():
-            raise SlimError(SLIM_ERR_INVALID_ARG, f"{where}: lengths, parents and results must be contiguous int32, one per row (two results)")
+def _i32(where, t, n):
+    """The address of n numbers at least."""
+    if t.dtype is not torch.int32 or t.numel() < n or not t.is_contiguous():
+        raise SlimError(SLIM_ERR_INVALID_ARG, f"{where}: lengths, parents and results must be contiguous int32, one per row (two results)")
+    return t.data_ptr()
 
 
 def slim_pages_fork(layers, src, dst, parent, kv_len, len_out, result, workspace, stream=None):
@@ -639,30 +642,29 @@ def slim_pages_fork(layers, src, dst, parent, kv_len, len_out, result, workspace
     pages and get a copy of the last one, rows without children are freed.  layers: PageLayers, or None for the tables alone."""
     where = "slim_pages_fork"
     array, n = _layers(where, layers, src)
-    _i32_vector(where, len(dst.held), parent, len_out)
-    _i32_vector(where, len(src.held), kv_len)
-    _i32_vector(where, 2, result)
-    rc = (_lib or lib()).slim_pages_fork(src.ref, dst.ref, _addr(parent), _addr(kv_len), _addr(len_out), array, n, _addr(result), _addr(workspace),
-                               _nbytes(workspace), _cuda_stream(stream))
-    _check(rc, where)
+    rc = (_lib or lib()).slim_pages_fork(src.ref, dst.ref, _i32(where, parent, dst.rows), _i32(where, kv_len, src.rows), _i32(where, len_out, dst.rows),
+                                         array, n, _i32(where, result, 2), workspace.data_ptr(), _nbytes(workspace), _cuda_stream(stream))
+    if rc:
+        _check(rc, where)
 
 
 def slim_pages_grow(pages, kv_len, room, result, workspace, stream=None):
     """Pages for kv_len + room tokens in every row of length 0 or more."""
     where = "slim_pages_grow"
-    _i32_vector(where, len(pages.held), kv_len)
-    _i32_vector(where, 2, result)
-    rc = (_lib or lib()).slim_pages_grow(pages.ref, _addr(kv_len), room, _addr(result), _addr(workspace), _nbytes(workspace), _cuda_stream(stream))
-    _check(rc, where)
+    rc = (_lib or lib()).slim_pages_grow(pages.ref, _i32(where, kv_len, pages.rows), room, _i32(where, result, 2), workspace.data_ptr(),
+                                         _nbytes(workspace), _cuda_stream(stream))
+    if rc:
+        _check(rc, where)
 
 
 def slim_pages_compact(layers, src, dst, result, workspace, stream=None):
     """The pages in use move to the lowest ids, in every layer; dst (may be src) holds the tables afterwards."""
     where = "slim_pages_compact"
     array, n = _layers(where, layers, src)
-    _i32_vector(where, 2, result)
-    rc = (_lib or lib()).slim_pages_compact(src.ref, dst.ref, array, n, _addr(result), _addr(workspace), _nbytes(workspace), _cuda_stream(stream))
-    _check(rc, where)
+    rc = (_lib or lib()).slim_pages_compact(src.ref, dst.ref, array, n, _i32(where, result, 2), workspace.data_ptr(), _nbytes(workspace),
+                                            _cuda_stream(stream))
+    if rc:
+        _check(rc, where)
 
 
 def pages_workspace(num_pages, rows, device="cuda"):

@@ -343,25 +343,8 @@ struct PageLayersArg {
 constexpr int kCopyThreads = 256;
 constexpr int kCopyUnroll = 8;
 
-// `bytes` (a multiple of 4) from one 16-byte aligned place to another by a warp.
-__device__ __forceinline__ void pg_copy(unsigned char *dst, const unsigned char *src, int bytes, int lane)
-{
-    const uint4 *s = reinterpret_cast<const uint4 *>(src);
-    uint4 *d = reinterpret_cast<uint4 *>(dst);
-    const int words = bytes / 16;
-    int i = lane;
-    for (; i + 32 * (kCopyUnroll - 1) < words; i += 32 * kCopyUnroll) {
-        uint4 v[kCopyUnroll];
-#pragma unroll
-        for (int k = 0; k < kCopyUnroll; ++k) v[k] = __ldcs(s + i + 32 * k);
-#pragma unroll
-        for (int k = 0; k < kCopyUnroll; ++k) __stcs(d + i + 32 * k, v[k]);
-    }
-    for (; i < words; i += 32) d[i] = __ldcs(s + i);
-    for (int k = words * 4 + lane; k < bytes / 4; k += 32) reinterpret_cast<uint32_t *>(dst)[k] = reinterpret_cast<const uint32_t *>(src)[k];
-}
-
-// blockIdx.y: the layer.  An item is one (job, kv head, K or V): the codes of its tokens and their scales.
+// blockIdx.y: the layer.  An item is one (job, kv head, K or V): the codes of its tokens and their scales.  A lane takes four
+// tokens' scales (its 16 bytes are on their way with the first codes).
 __global__ void __launch_bounds__(kCopyThreads)
 slim_pages_copy_kernel(const __grid_constant__ PageLayersArg layers, const PagesWork w, const int whole)
 {
@@ -374,10 +357,29 @@ slim_pages_copy_kernel(const __grid_constant__ PageLayersArg layers, const Pages
         const int job = (int)(it / blocks), part = (int)(it - (long long)job * blocks);
         const int tokens = whole ? kPageTokens : __ldcg(w.part + job);
         const size_t from = (size_t)__ldcg(w.source + job) * blocks + part, to = (size_t)__ldcg(w.target + job) * blocks + part;
-        const size_t code_block = (size_t)kPageTokens * layer.row_bytes, scale_block = (size_t)kPageTokens * 4;
-        unsigned char *codes = static_cast<unsigned char *>(layer.codes), *scales = static_cast<unsigned char *>(layer.scales);
-        pg_copy(codes + to * code_block, codes + from * code_block, tokens * layer.row_bytes, lane);
-        pg_copy(scales + to * scale_block, scales + from * scale_block, tokens * 4, lane);
+        const int code_words = kPageTokens * layer.row_bytes / 16, words = tokens * layer.row_bytes / 16;
+        const uint4 *src = static_cast<const uint4 *>(layer.codes) + from * code_words;
+        uint4 *dst = static_cast<uint4 *>(layer.codes) + to * code_words;
+        const uint4 *scale_src = static_cast<const uint4 *>(layer.scales) + from * (kPageTokens / 4) + lane;
+        uint4 *scale_dst = static_cast<uint4 *>(layer.scales) + to * (kPageTokens / 4) + lane;
+        const bool scales = 4 * lane < tokens;
+        uint4 sc = make_uint4(0, 0, 0, 0);
+        if (scales) sc = __ldcs(scale_src);
+        int i = lane;
+        for (; i + 32 * (kCopyUnroll - 1) < words; i += 32 * kCopyUnroll) {
+            uint4 v[kCopyUnroll];
+#pragma unroll
+            for (int k = 0; k < kCopyUnroll; ++k) v[k] = __ldcs(src + i + 32 * k);
+#pragma unroll
+            for (int k = 0; k < kCopyUnroll; ++k) __stcs(dst + i + 32 * k, v[k]);
+        }
+        for (; i < words; i += 32) __stcs(dst + i, __ldcs(src + i));
+        if (4 * lane + 4 <= tokens) {
+            __stcs(scale_dst, sc);
+        } else if (scales) {   // (the tokens behind the last one keep theirs)
+            const uint32_t v[3] = {sc.x, sc.y, sc.z};
+            for (int k = 0; k < tokens - 4 * lane; ++k) reinterpret_cast<uint32_t *>(scale_dst)[k] = v[k];
+        }
     }
 }
 
