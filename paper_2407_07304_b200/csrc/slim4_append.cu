@@ -72,14 +72,13 @@ slim4_append_kernel(uint8_t *__restrict__ codes, uint32_t *__restrict__ pairs, c
     const uint32_t pair = q4_pair(lo, hi);
     const Q4Row q(pair);
     if (!stored) return;
-#pragma unroll
-    for (int v = 0; v < 2; ++v) {
-        // dims 8 (4 v + l) .. + 7 low, 64 further high
-        uint2 w;
-        w.x = q.codes4(raw[v].x, raw[v].y) | (q.codes4(raw[v + 2].x, raw[v + 2].y) << 4);
-        w.y = q.codes4(raw[v].z, raw[v].w) | (q.codes4(raw[v + 2].z, raw[v + 2].w) << 4);
-        reinterpret_cast<uint2 *>(codes + at.code)[v * 4 + l] = w;
-    }
+    // dims 8 (4 v + l) .. + 7 low, 64 further high, v = 0, 1
+    const uint32_t low[8] = {raw[0].x, raw[0].y, raw[0].z, raw[0].w, raw[1].x, raw[1].y, raw[1].z, raw[1].w};
+    const uint32_t high[8] = {raw[2].x, raw[2].y, raw[2].z, raw[2].w, raw[3].x, raw[3].y, raw[3].z, raw[3].w};
+    uint32_t w[4];
+    q.words<4>(low, high, w);
+    reinterpret_cast<uint2 *>(codes + at.code)[l] = make_uint2(w[0], w[1]);
+    reinterpret_cast<uint2 *>(codes + at.code)[4 + l] = make_uint2(w[2], w[3]);
     if (l == 0) pairs[at.pair] = pair;
 }
 

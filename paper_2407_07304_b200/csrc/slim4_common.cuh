@@ -36,38 +36,60 @@ __device__ __forceinline__ uint32_t q4_pair(float lo, float hi)
 }
 
 // What the codes of a row are formed with.  The quotient (x - z) / s is the correctly rounded one: p = d * rc with
-// rc = RN(1 / s), its exact residual r = d - s p by a fused multiply-add, q = p + r rc (Markstein's correction).  A scale
-// outside [2^-60, 2^60] is brought to the middle of the range together with the differences, by an exact power of two.
+// rc = RN(1 / s), its exact residual r = d - s p by a fused multiply-add, q = p + r rc (Markstein's correction).  Rows whose
+// scale lies outside [2^-60, 2^60] (constant rows among them) divide instead: intermediates could leave the normal range there,
+// and only a scale that is a subnormal of few bits can be so much too small that a quotient passes 15.5 (the others are
+// within 2^-9: 15.06 at most).
 struct Q4Row {
-    float z, f, ns, rc;
-    __device__ __forceinline__ explicit Q4Row(uint32_t pair)
+    uint64_t nz2, ns2, rc2;   // -z, -s and 1 / s, twice each
+    uint32_t pair;
+    bool far;
+    __device__ __forceinline__ explicit Q4Row(uint32_t of) : pair(of)
     {
-        const float s = pair_scale(pair);
-        z = pair_offset(pair);
-        f = 1.f;
-        if (s < 0x1p-60f) f = 0x1p100f;
-        else if (s > 0x1p60f) f = 0x1p-100f;
-        const float ss = s * f;
-        ns = -ss;
-        rc = (s > 0.f) ? __frcp_rn(ss) : 0.f;
+        const float s = pair_scale(pair), z = pair_offset(pair);
+        far = !(s >= 0x1p-60f && s <= 0x1p60f);
+        const float rc = far ? 0.f : __frcp_rn(s);
+        nz2 = ap_pack(-z, -z), ns2 = ap_pack(-s, -s), rc2 = ap_pack(rc, rc);
     }
-    // 0x4B400000 + round((x - z) / s) of two values, not yet clamped to 15
-    __device__ __forceinline__ void codes(float x0, float x1, uint32_t &u0, uint32_t &u1) const
+    // 0x4B400000 + the code of two values
+    __device__ __forceinline__ void codes(uint32_t xx, uint32_t &u0, uint32_t &u1) const
     {
-        const uint64_t d2 = ap_mul2(ap_add2(ap_pack(x0, x1), ap_pack(-z, -z)), ap_pack(f, f));
-        const uint64_t rc2 = ap_pack(rc, rc), p2 = ap_mul2(d2, rc2);
-        const uint64_t q2 = ap_fma2(ap_fma2(ap_pack(ns, ns), p2, d2), rc2, p2);
-        const uint64_t t2 = ap_add2(q2, ap_pack(kRoundMagic, kRoundMagic));
-        u0 = min((uint32_t)t2, 0x4B40000Fu);
-        u1 = min((uint32_t)(t2 >> 32), 0x4B40000Fu);
+        const uint64_t d2 = ap_add2(ap_pack(__uint_as_float(xx << 16), __uint_as_float(xx & 0xFFFF0000u)), nz2);
+        const uint64_t p2 = ap_mul2(d2, rc2);
+        const uint64_t t2 = ap_add2(ap_fma2(ap_fma2(ns2, p2, d2), rc2, p2), ap_pack(kRoundMagic, kRoundMagic));
+        u0 = (uint32_t)t2, u1 = (uint32_t)(t2 >> 32);
+    }
+    __device__ __noinline__ static uint32_t far_codes4(uint32_t pair, uint32_t a, uint32_t b)
+    {
+        const float s = pair_scale(pair), z = pair_offset(pair);
+        uint32_t w = 0;
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t xx = (i < 2) ? a : b;
+            const float x = __uint_as_float((i & 1) ? (xx & 0xFFFF0000u) : (xx << 16));
+            const float u = (s > 0.f) ? fminf(rintf(__fdiv_rn(x - z, s)), 15.f) : 0.f;
+            w |= (uint32_t)u << (8 * i);
+        }
+        return w;
     }
     // four values (two words of bf16 pairs): a code in every byte
     __device__ __forceinline__ uint32_t codes4(uint32_t a, uint32_t b) const
     {
         uint32_t u0, u1, u2, u3;
-        codes(__uint_as_float(a << 16), __uint_as_float(a & 0xFFFF0000u), u0, u1);
-        codes(__uint_as_float(b << 16), __uint_as_float(b & 0xFFFF0000u), u2, u3);
+        codes(a, u0, u1);
+        codes(b, u2, u3);
         return __byte_perm(__byte_perm(u0, u1, 0x0040), __byte_perm(u2, u3, 0x0040), 0x5410);
+    }
+    // N words of codes: of the dims in lo[2 i], lo[2 i + 1] (low halves of the bytes) and those 64 further
+    template <int N>
+    __device__ __forceinline__ void words(const uint32_t (&lo)[2 * N], const uint32_t (&hi)[2 * N], uint32_t (&w)[N]) const
+    {
+        if (far) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) w[i] = far_codes4(pair, lo[2 * i], lo[2 * i + 1]) | (far_codes4(pair, hi[2 * i], hi[2 * i + 1]) << 4);
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i) w[i] = codes4(lo[2 * i], lo[2 * i + 1]) | (codes4(hi[2 * i], hi[2 * i + 1]) << 4);
+        }
     }
 };
 

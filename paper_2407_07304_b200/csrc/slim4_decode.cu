@@ -233,7 +233,10 @@ __device__ __forceinline__ void d4_quantise(const __nv_bfloat16 *row, int i, uin
     pair = q4_pair(fminf(__uint_as_float(lo2 << 16), __uint_as_float(lo2 & 0xFFFF0000u)),
                    fmaxf(__uint_as_float(hi2 << 16), __uint_as_float(hi2 & 0xFFFF0000u)));
     const Q4Row q(pair);
-    codes = q.codes4(a.x, a.y) | (q.codes4(c.x, c.y) << 4);
+    const uint32_t lo[2] = {a.x, a.y}, hi[2] = {c.x, c.y};
+    uint32_t w[1];
+    q.words<1>(lo, hi, w);
+    codes = w[0];
 }
 
 __device__ __forceinline__ void d4_store(__nv_bfloat16 *dst, float4 o)
