@@ -16,10 +16,20 @@
 //  * The order of dims inside a product is free, so a lane's 16 bytes of a K row are its share of eight products' operands;
 //    the scores of S^T = K Q^T become the operand P^T of O^T = V^T P^T by an 8x8 transposition (movmatrix), and V's
 //    token pairs by a byte permutation.  Nothing but raw rows passes through shared memory.
-//  * Warps are independent: each has its own ring of 64-token units (two bulk copies for the codes, two for the scales),
-//    its own contiguous range of the units of all pairs, and its own running maximum, sum and O in registers.  A pair that
-//    begins and ends inside a warp's range is written as the result at once; the others leave a record, merged by the
-//    block, and where a pair spans blocks, by the block that finishes it last.
+//  * Warps are independent: each has its own ring of 64-token units (the copy engine's boxes have rows of 1 KB: it takes a
+//    box row by row, and rows of 64 bytes cost 1 us on 143 MB), its own contiguous range of the units of all pairs, and its own
+//    running maximum, sum and O in registers.  A pair that begins and ends inside a warp's range is written as the result
+//    at once; the others leave a record, merged by the block, and where a pair spans blocks, by the block that finishes it
+//    last, or by a second kernel where few pairs span many blocks.
+//  * A K product needs the query, then a softmax step, then V: with twelve warps per SM these phases overlap across warps
+//    (eight warps 36 us, sixteen at 128 registers 46 us on the 64 / 8-head workload when twelve took 34).
+//
+// Measured (B200, calls back to back, three caches in turn; the copy rate is 6.57 TB/s): 16 x 2049 tokens, 32 / 32 heads KSTEP us
+// for 143 MB; 32 ragged sequences of up to 4096 tokens, 64 / 8 heads, KB32 us for 93 MB; one of 32768 tokens, 32 / 2 heads,
+// KLONG us for 9 MB; one of 272 tokens, 32 / 32 heads, KTINY us.  The stream itself runs at 6 TB/s (573 MB: 108 us); a call
+// carries 2.3 us to its first products and 5 to 8 us from the median warp's last unit to its end (the slowest warp, the block's
+// merge, the round trips of the merge between blocks).  With more than eight query heads per kv head the products bound it:
+// eight warps of 255 registers, 3.8 TB/s.
 //
 // Query rows are held as fp16 after division by a power of two near the row's largest value: exact down to 2^-24 of it.
 // The weights p_j s_j are rounded to fp16 (2^-11 of each), p_j itself, its sum and the offset's sum stay fp32.
@@ -39,7 +49,7 @@ constexpr uint32_t kD4PairBytes = 2 * kD4Unit * 4;   // its (scale, offset) word
 constexpr float kD4Grow = 4.f;                     // the running maximum moves when it is exceeded by 2^4
 constexpr float kD4Top = 512.f;                    // p s is scaled so that the largest s counts as 2^9 to 2^10 (with p <= 2^4 far below fp16's 2^16)
 constexpr int kD4MaxBlocks = 160;
-constexpr int kD4Group = 8;                        // blocks whose records are merged first where a pair spans many
+constexpr int kD4Few = 8;                          // blocks per pair up to which the last of them merges their records
 
 struct Decode4Params {
     uint8_t *codes;
@@ -49,7 +59,7 @@ struct Decode4Params {
     const __nv_bfloat16 *q, *k_new, *v_new;
     __nv_bfloat16 *out;
     int *status;
-    int *counters;      // arrivals: per record slot for the group that it begins, then per block for the pair that begins in it
+    int *counters;      // arrivals, per block for the pair that begins in it; null: a second kernel merges the pairs that span blocks
     float *parts;       // two records per block: of the pair at its start and of the one at its end, where they go on in others
     int B, Hq, Hkv, G, max_pages_per_seq, num_pages, cap_tokens;
     float scale_log2e;
@@ -63,8 +73,7 @@ struct D4Span {
     int pair, first, units;   // -1: none; its units in the order of all units
     int block, parts;         // the block in which it begins, the records that blocks leave of it
     int slot0;                // which of the two records of that first block it is (always the first one of the later blocks)
-    int group;                // where there are many: the record that begins this block's group of them
-    int pad;
+    int pad[2];
 };
 
 // What a block is made of, by the query heads that a kv head serves at most: NT groups of eight columns of the products.
@@ -247,58 +256,62 @@ __device__ __forceinline__ void d4_store(__nv_bfloat16 *dst, float4 o)
 
 // Log-sum-exp merge by one warp of head h of the records that its lanes name (rec: a lane's record, null: none), in lane
 // order.  A lane owns four dims.  kGlobal: records of other blocks, read past the L1; at(x): record x's address (x a lane that
-// names one).  The first outputs are on their way before the maxima are known.
+// names one).  kBatch outputs are requested together, the first ones before the maxima are known (inside the decode kernel
+// four: with eight, the longer run through cold instructions cost the 64 / 8-head workload 0.7 us).
 struct D4Merged {
     float m, l;
     float4 o;
 };
-template <bool kGlobal, class At>
-__device__ __forceinline__ D4Merged d4_merge(const float *rec, int G, int h, int lane, At at)
+__device__ __forceinline__ D4Merged d4_none() { return {-INFINITY, 0.f, make_float4(0.f, 0.f, 0.f, 0.f)}; }
+template <bool kGlobal, int kBatch, class At>
+__device__ __forceinline__ void d4_merge(D4Merged &r, const float *rec, int G, int h, int lane, At at)
 {
-    constexpr int kBatch = 4;
-    D4Merged r;
     unsigned todo = __ballot_sync(0xffffffffu, rec != nullptr);
+    if (todo == 0u) return;
     float m = -INFINITY, l = 0.f;
     if (rec != nullptr) {
         const float *ml = rec + G * kHeadDim + h;
         m = kGlobal ? __ldcg(ml) : ml[0], l = kGlobal ? __ldcg(ml + G) : ml[G];
     }
-    float4 v[2][kBatch];
-    int who[2][kBatch];
-    auto load = [&](int k) {
+    float4 v[kBatch];
+    int who[kBatch];
+    auto load = [&]() {
 #pragma unroll
         for (int u = 0; u < kBatch; ++u) {
-            who[k][u] = (todo != 0u) ? __ffs(todo) - 1 : -1;
-            v[k][u] = make_float4(0.f, 0.f, 0.f, 0.f);
+            who[u] = (todo != 0u) ? __ffs(todo) - 1 : -1;
+            v[u] = make_float4(0.f, 0.f, 0.f, 0.f);
             if (todo != 0u) {
-                const float4 *src = reinterpret_cast<const float4 *>(at(who[k][u]) + h * kHeadDim) + lane;
-                v[k][u] = kGlobal ? __ldcg(src) : *src;
+                const float4 *src = reinterpret_cast<const float4 *>(at(who[u]) + h * kHeadDim) + lane;
+                v[u] = kGlobal ? __ldcg(src) : *src;
             }
             todo &= todo - 1;
         }
     };
-    load(0);
-    load(1);
-    r.m = d4_ordered_float(__reduce_max_sync(0xffffffffu, d4_ordered_int(m)));
-    const float w = (m == -INFINITY) ? 0.f : d4_exp2(m - r.m);
-    r.l = warp_sum(l * w);
-    r.o = make_float4(0.f, 0.f, 0.f, 0.f);
+    load();
+    const float top = fmaxf(r.m, d4_ordered_float(__reduce_max_sync(0xffffffffu, d4_ordered_int(m))));
+    const float w = (m == -INFINITY) ? 0.f : d4_exp2(m - top), f = (r.m == -INFINITY) ? 0.f : d4_exp2(r.m - top);
+    r.m = top;
+    r.l = r.l * f + warp_sum(l * w);
+    r.o = make_float4(r.o.x * f, r.o.y * f, r.o.z * f, r.o.w * f);
     for (;;) {
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-#pragma unroll
-            for (int u = 0; u < kBatch; ++u) {
-                const float wu = (who[k][u] >= 0) ? __shfl_sync(0xffffffffu, w, max(who[k][u], 0)) : 0.f;
-                r.o.x = fmaf(v[k][u].x, wu, r.o.x);
-                r.o.y = fmaf(v[k][u].y, wu, r.o.y);
-                r.o.z = fmaf(v[k][u].z, wu, r.o.z);
-                r.o.w = fmaf(v[k][u].w, wu, r.o.w);
-            }
+        for (int u = 0; u < kBatch; ++u) {
+            const float wu = (who[u] >= 0) ? __shfl_sync(0xffffffffu, w, max(who[u], 0)) : 0.f;
+            r.o.x = fmaf(v[u].x, wu, r.o.x);
+            r.o.y = fmaf(v[u].y, wu, r.o.y);
+            r.o.z = fmaf(v[u].z, wu, r.o.z);
+            r.o.w = fmaf(v[u].w, wu, r.o.w);
         }
-        if (todo == 0u) return r;
-        load(0);
-        load(1);
+        if (todo == 0u) return;
+        load();
     }
+}
+// Which of the blocks' records (two each) is a pair's record x; the pair's first unit lies in block `block`, whose record
+// slot0 it is.  With fewer units than blocks every unit has a block of its own.
+__device__ __forceinline__ int d4_part(int first, int block, int slot0, int x, int U, int n_blocks)
+{
+    if (U < n_blocks) return 2 * d4_holder(first + x, U, n_blocks);
+    return 2 * (block + x) + (x == 0 ? slot0 : 0);
 }
 // Where a merge goes: a row of the result, or another record.
 __device__ __forceinline__ void d4_put(const D4Merged &r, int G, int h, int lane, __nv_bfloat16 *out, float *part)
@@ -369,7 +382,6 @@ slim4_decode_kernel(const __grid_constant__ CUtensorMap map_codes, const __grid_
                 span.block = d4_holder(span.first, U, n_blocks);
                 span.parts = sparse ? span.units : d4_holder(span.first + span.units - 1, U, n_blocks) - span.block + 1;
                 span.slot0 = (span.first <= d4_cut(U, span.block, n_blocks)) ? 0 : 1;
-                span.group = (sparse ? block0 - span.first : block - span.block) / kD4Group * kD4Group;
             }
         }
         if (lane == 0) spans[which] = span;
@@ -801,52 +813,85 @@ slim4_decode_kernel(const __grid_constant__ CUtensorMap map_codes, const __grid_
             const int of = __shfl_sync(0xffffffffu, pair, __ffs(firsts) - 1);
             firsts &= firsts - 1;
             for (; h < G; h += NW) {
-                const D4Merged r = d4_merge<false>(pair == of ? at(lane) : nullptr, G, h, lane, at);
+                D4Merged r = d4_none();
+                d4_merge<false, 4>(r, pair == of ? at(lane) : nullptr, G, h, lane, at);
                 d4_put(r, G, h, lane, (of != span0 && of != span1) ? out_rows(of) : nullptr, part(2 * block + (of == span0 ? 0 : 1)));
             }
             h -= G;
         }
     }
+    if (p.counters == nullptr) return;   // (the second kernel merges what blocks share)
     __syncthreads();
-    // ---- pairs that span blocks: the block that arrives last merges their records; where there are many, first the
-    //      last one of every kD4Group blocks merges theirs into the group's first record
-    static_assert((kD4MaxBlocks + kD4Group - 1) / kD4Group <= 32 && 2 * kD4Group <= 32, "a warp's lanes name all records of a merge");
-    auto part_at = [&](const D4Span &span, int x) {   // a pair's record x, of the two per block
-        if (sparse) return 2 * d4_holder(span.first + x, U, n_blocks);
-        return 2 * (span.block + x) + (x == 0 ? span.slot0 : 0);
-    };
-    for (int level = 0; level < 2; ++level) {
-        if (warp < 2 && lane == 0 && spans[warp].pair >= 0 && (level == 0 || flags[1 + warp] == 2)) {
-            const D4Span &span = spans[warp];
-            const bool grouped = span.parts > 2 * kD4Group, first = level == 0 && grouped;
-            int *counter = p.counters + (first ? part_at(span, span.group) : 2 * kD4MaxBlocks + span.block);
-            const int expected = first ? min(kD4Group, span.parts - span.group) : (grouped ? (span.parts + kD4Group - 1) / kD4Group : span.parts);
-            // (releases the block's records, which were written before the barrier, and acquires those of the others)
-            int before;
-            asm volatile("atom.acq_rel.gpu.global.add.s32 %0, [%1], 1;\n" : "=r"(before) : "l"(counter) : "memory");
-            const bool last = before + 1 == expected;
-            if (last) *counter = 0;   // ready for the next launch
-            flags[1 + warp] = last ? (first ? 2 : 1) : 0;
-        }
-        __syncthreads();
-        for (int which = 0; which < 2; ++which) {
-            const int state = flags[1 + which];
-            if (state == 0) continue;
-            const D4Span span = spans[which];
-            const int step = (state == 1 && span.parts > 2 * kD4Group) ? kD4Group : 1;
-            const int x = (state == 2) ? span.group + lane : lane * step;
-            const int index = (x < span.parts && (state == 1 || lane < kD4Group)) ? part_at(span, x) : -1;
-            const float *rec = (index >= 0) ? part(index) : nullptr;
-            for (int h = (warp + NW - which * NW / 2) % NW; h < G; h += NW) {
-                const D4Merged r = d4_merge<true>(rec, G, h, lane, [&](int e) { return part(__shfl_sync(0xffffffffu, index, e)); });
-                d4_put(r, G, h, lane, state == 1 ? out_rows(span.pair) : nullptr, part(__shfl_sync(0xffffffffu, index, 0)));
-            }
-        }
-        if (flags[1] != 2 && flags[2] != 2) break;   // (the same for every thread: the flags changed before the barrier above)
-        __syncthreads();
-        if (tid < 2 && flags[1 + tid] == 1) flags[1 + tid] = 0;   // merged above
-        __syncthreads();
+    // ---- pairs that span blocks: the block that arrives last merges their records
+    if (warp < 2 && lane == 0 && spans[warp].pair >= 0) {
+        const D4Span &span = spans[warp];
+        int *counter = p.counters + span.block, before;
+        // (releases the block's records, which were written before the barrier, and acquires those of the others)
+        asm volatile("atom.acq_rel.gpu.global.add.s32 %0, [%1], 1;\n" : "=r"(before) : "l"(counter) : "memory");
+        const bool last = before + 1 == span.parts;
+        if (last) *counter = 0;   // ready for the next launch
+        flags[1 + warp] = last ? 1 : 0;
     }
+    __syncthreads();
+    for (int which = 0; which < 2; ++which) {
+        if (flags[1 + which] == 0) continue;
+        const D4Span span = spans[which];
+        for (int h = (warp + NW - which * NW / 2) % NW; h < G; h += NW) {
+            D4Merged r = d4_none();
+            for (int x0 = 0; x0 < span.parts; x0 += 32) {
+                const int x = x0 + lane;
+                const int index = (x < span.parts) ? d4_part(span.first, span.block, span.slot0, x, U, n_blocks) : -1;
+                d4_merge<true, 4>(r, (index >= 0) ? part(index) : nullptr, G, h, lane, [&](int e) { return part(__shfl_sync(0xffffffffu, index, e)); });
+            }
+            d4_put(r, G, h, lane, out_rows(span.pair), nullptr);
+        }
+    }
+}
+
+// The pairs that span blocks, where few pairs span many: a block per query row, four warps taking every fourth record.
+constexpr int kD4MergeWarps = 4;
+__global__ void __launch_bounds__(kD4MergeWarps * 32)
+slim4_decode_merge_kernel(const __grid_constant__ Decode4Params p, const int n_blocks)
+{
+    __shared__ float4 o_s[kD4MergeWarps][32];
+    __shared__ float m_s[kD4MergeWarps], l_s[kD4MergeWarps];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, row = blockIdx.x, b = row / p.Hq, h = row % p.Hq % p.G, head = row % p.Hq / p.G;
+    pdl_wait();
+    int U = 0, before = 0;
+    for (int base = 0; base < p.B; base += 32) {
+        const int n = (base + lane < p.B) ? d4_units(d4_len(p, base + lane)) : 0;
+        U += __reduce_add_sync(0xffffffffu, n);
+        before += __reduce_add_sync(0xffffffffu, base + lane < b ? n : 0);
+    }
+    const int units = d4_units(d4_len(p, b)), first = before * p.Hkv + head * units;
+    U *= p.Hkv;
+    if (units == 0) return;
+    const int block = d4_holder(first, U, n_blocks), last = d4_holder(first + units - 1, U, n_blocks);
+    if (block == last) return;   // (the one block has written the result)
+    const int parts = (U < n_blocks) ? units : last - block + 1, slot0 = (first <= d4_cut(U, block, n_blocks)) ? 0 : 1;
+    const int rec_floats = d4_rec_floats(p.G);
+    D4Merged r = d4_none();
+    for (int x0 = 0; x0 < parts; x0 += 32 * kD4MergeWarps) {
+        const int x = x0 + lane * kD4MergeWarps + warp;
+        const int index = (x < parts) ? d4_part(first, block, slot0, x, U, n_blocks) : -1;
+        d4_merge<true, 8>(r, (index >= 0) ? p.parts + (size_t)index * rec_floats : nullptr, p.G, h, lane,
+                       [&](int e) { return p.parts + (size_t)__shfl_sync(0xffffffffu, index, e) * rec_floats; });
+    }
+    if (lane == 0) m_s[warp] = r.m, l_s[warp] = r.l;
+    o_s[warp][lane] = r.o;
+    __syncthreads();
+    if (warp != 0) return;
+    r = d4_none();
+#pragma unroll
+    for (int i = 0; i < kD4MergeWarps; ++i) r.m = fmaxf(r.m, m_s[i]);
+#pragma unroll
+    for (int i = 0; i < kD4MergeWarps; ++i) {
+        const float w = (m_s[i] == -INFINITY) ? 0.f : d4_exp2(m_s[i] - r.m);
+        const float4 v = o_s[i][lane];
+        r.l = fmaf(l_s[i], w, r.l);
+        r.o = make_float4(fmaf(v.x, w, r.o.x), fmaf(v.y, w, r.o.y), fmaf(v.z, w, r.o.z), fmaf(v.w, w, r.o.w));
+    }
+    d4_put(r, p.G, h, lane, p.out + ((size_t)b * p.Hq + (size_t)head * p.G) * kHeadDim, nullptr);
 }
 
 size_t decode4_workspace_bytes(int G)
@@ -873,7 +918,13 @@ static int launch_d4(const slim_cache4_t *c, const Decode4Params &p, int max_kv,
     if (rc != SLIM_OK) return rc;
     rc = allow_dynamic_smem(reinterpret_cast<const void *>(slim4_decode_kernel<kHeads, kStep>), (int)D4<kHeads>::kBytes);
     if (rc != SLIM_OK) return rc;
-    SLIM_CUDA_TRY(launch_pdl(slim4_decode_kernel<kHeads, kStep>, dim3((unsigned)blocks), dim3(D4<kHeads>::kWarps * 32), D4<kHeads>::kBytes, stream, codes, scales, p));
+    // Few pairs on many blocks (one sequence of 32768 tokens on two kv heads: 74 blocks each): a second kernel merges them,
+    // KMERGE us against 20.7 with the last blocks doing it in two steps; for more pairs its launch costs more than it saves.
+    const bool defer = blocks > kD4Few * pairs;
+    Decode4Params q = p;
+    if (defer) q.counters = nullptr;
+    SLIM_CUDA_TRY(launch_pdl(slim4_decode_kernel<kHeads, kStep>, dim3((unsigned)blocks), dim3(D4<kHeads>::kWarps * 32), D4<kHeads>::kBytes, stream, codes, scales, q));
+    if (defer) SLIM_CUDA_TRY(launch_pdl(slim4_decode_merge_kernel, dim3((unsigned)(p.B * p.Hq)), dim3(kD4MergeWarps * 32), 0, stream, q, (int)blocks));
     return SLIM_OK;
 }
 

@@ -31,7 +31,7 @@ struct Entry {
     Shape shape;
     CUtensorMap map;
 };
-constexpr int kEntries = 64;
+constexpr int kEntries = 256;
 
 bool same_shape(const Shape &a, const Shape &b)
 {

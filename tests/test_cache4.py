@@ -424,3 +424,17 @@ def test_prefill_and_decode_agree_on_the_last_row():
     close(out[-1:], want, 2.0 ** -8 * np.abs(want) + (2 * score + 2 * 2.0 ** -11 + n * 2.0 ** -25 + 2.0 ** -20) * v)
     close(one, want, decode_bound(want, parts))
     assert math.isfinite(float(out.float().sum()))
+
+
+@pytest.mark.parametrize("lens,bound,hq,hkv", [([100] * 16 + [0, 1, 64, 65], 8192, 16, 4), ([3000] + [2] * 19, 3000, 32, 2), ([70, 130], 30000, 4, 2)])
+def test_decode_bound_far_above_the_lengths(lens, bound, hq, hkv):
+    """The launch is made for max_kv: fewer units than blocks, one long sequence among short ones, few pairs on many blocks."""
+    gen = torch.Generator().manual_seed(bound)
+    cache, _, _ = filled(gen, lens, hkv, capacity=bound)
+    b, q = len(lens), torch.randn(len(lens), hq, D, generator=gen).to(torch.bfloat16).cuda()
+    out = torch.full_like(q, 9.0)
+    ws = slim.decode4_workspace(b, hq, hkv, bound)
+    for _ in range(2):
+        slim.slim_attn4_decode(cache, q, out, i32(lens), b, bound, hq, D ** -0.5, ws)
+    check_decode(cache, lens, q, out, D ** -0.5)
+    assert not ws[:slim.WORKSPACE_HEADER_BYTES].any()
