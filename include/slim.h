@@ -556,6 +556,9 @@ int slim_prefill4_step(const slim_cache4_t *cache, const void *q, const void *k_
  *              appends nothing and attends over the tokens that fit
  *   workspace  device, 16-byte aligned, at least slim_attn4_workspace_bytes(Hq, Hkv) bytes, whatever the batch and lengths;
  *              header as for slim_attn_decode.  Two calls that can overlap need one each
+ * Scores are exact to fp32; the products of a token's weight and its scale are rounded to fp16 (2^-11 of each of a result's
+ * terms).  The copies read whole halves of a page (64 slots), whatever the length; what lies behind it is ignored.  B *
+ * num_kv_heads * max_kv / 64 beyond 31 bits is SLIM_ERR_UNSUPPORTED.
  */
 int slim_attn4_decode(const slim_cache4_t *cache, const void *q, const void *k_new, const void *v_new, void *out,
                       const int32_t *kv_len, int32_t B, int32_t max_kv, int32_t Hq, float sm_scale,
@@ -571,7 +574,8 @@ size_t slim_cache4_scale_bytes(int32_t num_pages, int32_t num_kv_heads);
  *   refs   device int32 [num_pages]: rows (and other holders, counted by the caller) that hold a page; 0: free
  *   table  device int32 [rows][stride]: a sequence's pages in order, -1 from held[row] on; a cache's block_table
  *   held   device int32 [rows]: pages of a row, 0 to stride
- * Only pages that are full may be held by more than one row.  Page ids outside [0, num_pages) are not followed.
+ * Only pages that are full may be held by more than one row.  Page ids outside [0, num_pages) are not followed.  Up to 2^23
+ * pages and rows.
  * Pages are taken lowest id first; every result is the same from run to run.
  */
 typedef struct slim_pages {
@@ -599,7 +603,7 @@ typedef struct slim_layer {
  *
  *   from, to   to->table and to->held must not be from's; to->refs may be from->refs.  Same num_pages and stride
  *   parent     device int32 [to->rows]
- *   kv_len     device int32 [from->rows]: tokens of every row (held[b] * 128 at most);  len_out  device int32 [to->rows]
+ *   kv_len     device int32 [from->rows]: tokens of every row (held[b] * 128 at most);  len_out  device int32 [to->rows], another array
  *   layers     host array of n_layers pools (0: tables only)
  *   result     device int32 [2]: pages that are missing, pages free afterwards.  Where pages are missing nothing else is
  *              written: free some and call again

@@ -222,7 +222,8 @@ class _BlockTable:
             raise TypeError("block tables must be contiguous int32 [rows, pages] on the cache's device")
         self.B, self.max_pages_per_seq = block_table.shape
         self.block_table = block_table
-        self.struct.block_table, self.struct.max_pages_per_seq = block_table.data_ptr(), self.max_pages_per_seq
+        held = self.held_struct
+        held.block_table, held.max_pages_per_seq = block_table.data_ptr(), self.max_pages_per_seq
 
 
 class SlimCache(_BlockTable):
@@ -244,6 +245,7 @@ class SlimCache(_BlockTable):
         self.block_table = block_table.to(device=device, dtype=torch.int32).contiguous()
         self.struct = SlimCacheStruct(self.codes.data_ptr(), self.scales.data_ptr(), self.block_table.data_ptr(),
                                       self.num_pages, PAGE_TOKENS, num_kv_heads, HEAD_DIM, max_pages_per_seq)
+        self.held_struct = self.struct
 
     def codes_view(self):
         """int8 [num_pages, Hkv, 2, 128, 128]"""
@@ -516,9 +518,14 @@ class SlimCache4(_BlockTable):
         if block_table is None:
             block_table = torch.arange(B * max_pages_per_seq, dtype=torch.int32).view(B, max_pages_per_seq)
         self.block_table = block_table.to(device=device, dtype=torch.int32).contiguous()
-        self.struct = SlimCacheStruct(self.codes.data_ptr(), self.scales.data_ptr(), self.block_table.data_ptr(),
-                                      self.num_pages, PAGE_TOKENS, num_kv_heads, HEAD_DIM, max_pages_per_seq)
-        self.ref = ctypes.byref(self.struct)
+        self.held_struct = SlimCacheStruct(self.codes.data_ptr(), self.scales.data_ptr(), self.block_table.data_ptr(),
+                                           self.num_pages, PAGE_TOKENS, num_kv_heads, HEAD_DIM, max_pages_per_seq)
+        self.ref = ctypes.byref(self.held_struct)
+
+    @property
+    def struct(self):
+        """What the calls on the INT8 cache ask for: they would read and write this pool as one of twice its size."""
+        raise SlimError(SLIM_ERR_INVALID_ARG, "this call takes a SlimCache (INT8), not a SlimCache4")
 
     def codes_view(self):
         """uint8 [num_pages, Hkv, 2, 128, 64]: byte i holds dim i (low four bits) and dim 64 + i"""
@@ -542,6 +549,12 @@ def _rows4(where, Hkv, k, v):
         raise SlimError(SLIM_ERR_INVALID_ARG, f"{where}: rows must be contiguous bfloat16 [tokens, kv heads, 128], K's and V's alike")
 
 
+def _queries4(where, rows, q, out):
+    for t in (q, out):
+        if t.dtype is not torch.bfloat16 or not t.is_contiguous() or t.numel() < rows * HEAD_DIM:
+            raise SlimError(SLIM_ERR_INVALID_ARG, f"{where}: q and out must be contiguous bfloat16 [rows, heads, 128]")
+
+
 def slim_kv4_append(cache, k_new, v_new, cu_new, start_pos, B, max_new, stream=None):
     """slim_kv_append into the 4-bit cache."""
     where = "slim_kv4_append"
@@ -563,12 +576,15 @@ def slim_kv4_read(cache, k_out, v_out, cu, start_pos, B, max_rows, stream=None):
 
 
 def slim_attn4_prefill(cache, q, out, cu_q, kv_len, B, max_q, max_kv, Hq, sm_scale, workspace, stream=None):
+    _queries4("slim_attn4_prefill", 0, q, out)
     rc = lib().slim_attn4_prefill(_cache4(cache, "slim_attn4_prefill"), _addr(q), _addr(out), _addr(cu_q), _addr(kv_len), B, max_q, max_kv, Hq,
                                   sm_scale, _addr(workspace), _nbytes(workspace), _cuda_stream(stream))
     _check(rc, "slim_attn4_prefill")
 
 
 def slim_prefill4_step(cache, q, k_new, v_new, out, cu_q, kv_len, B, max_q, max_kv, Hq, sm_scale, workspace, stream=None):
+    _queries4("slim_prefill4_step", 0, q, out)
+    _rows4("slim_prefill4_step", cache.Hkv, k_new, v_new)
     rc = lib().slim_prefill4_step(_cache4(cache, "slim_prefill4_step"), _addr(q), _addr(k_new), _addr(v_new), _addr(out), _addr(cu_q), _addr(kv_len),
                                   B, max_q, max_kv, Hq, sm_scale, _addr(workspace), _nbytes(workspace), _cuda_stream(stream))
     _check(rc, "slim_prefill4_step")
@@ -576,6 +592,9 @@ def slim_prefill4_step(cache, q, k_new, v_new, out, cu_q, kv_len, B, max_q, max_
 
 def slim_attn4_decode(cache, q, out, kv_len, B, max_kv, Hq, sm_scale, workspace, stream=None, k_new=None, v_new=None):
     """Decode attention over the 4-bit cache; with k_new and v_new the new tokens go into position kv_len - 1 in the same call."""
+    _queries4("slim_attn4_decode", B * Hq, q, out)
+    if k_new is not None and v_new is not None:
+        _rows4("slim_attn4_decode", cache.Hkv, k_new, v_new)
     rc = (_lib or lib()).slim_attn4_decode(_cache4(cache, "slim_attn4_decode"), _addr(q), _addr(k_new), _addr(v_new), _addr(out), _addr(kv_len), B, max_kv, Hq,
                                  sm_scale, _addr(workspace), _nbytes(workspace), _cuda_stream(stream))
     if rc:

@@ -168,6 +168,14 @@ def test_binding_refuses():
     with pytest.raises(slim.SlimError):      # the other cache's codes would be read as this one's
         slim.slim_kv4_append(int8, rows, rows, make(2), make(1), 1, 1)
     with pytest.raises(slim.SlimError):
+        slim.slim_kv_append(int4, rows, rows, make(2), make(1), 1, 1)
+    with pytest.raises(slim.SlimError):
+        slim.slim_attn_decode(int4, rows, rows, make(1), 1, 1, 2, 0.1, ws)
+    with pytest.raises(slim.SlimError):      # rows that do not lie one behind the other
+        slim.slim_attn4_decode(int4, torch.zeros((1, 4, 128), dtype=torch.bfloat16)[:, ::2], rows, make(1), 1, 1, 2, 0.1, ws)
+    with pytest.raises(slim.SlimError):
+        slim.slim_attn4_decode(int4, rows.float(), rows, make(1), 1, 1, 2, 0.1, ws)
+    with pytest.raises(slim.SlimError):
         slim.slim_kv4_append(int4, rows[:, :1], rows, make(2), make(1), 1, 1)
     with pytest.raises(slim.SlimError):
         slim.slim_kv4_read(int4, rows.float(), rows, make(2), make(1), 1, 1)
