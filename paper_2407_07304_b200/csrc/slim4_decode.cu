@@ -477,6 +477,7 @@ slim4_decode_kernel(const __grid_constant__ CUtensorMap map_codes, const __grid_
         for (int n = 0; n < cnt; ++n) {
             if (fresh) {
                 fresh = false;
+                if (NT > 1 && n > 0) load_q(w.b, w.head);
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
                     const uint4 (&v)[4] = qraw[nt];
@@ -529,7 +530,7 @@ slim4_decode_kernel(const __grid_constant__ CUtensorMap map_codes, const __grid_
             const bool ends = w.unit == w.units - 1;                            // the pair's last unit
             const bool complete = ends && run_unit0 == 0;
             const bool leaves = (ends && !complete) || (n == cnt - 1 && !ends); // a record is left behind this unit
-            if (ends && n + 1 < cnt) {   // the next pair's query rows, a unit ahead
+            if (NT == 1 && ends && n + 1 < cnt) {   // the next pair's query rows, a unit ahead (with NT = 2 their 32 registers cost more)
                 load_q(w1.b, w1.head);
             }
             unsigned char *kst = smem + ring + take_slot * kD4CodeBytes;
