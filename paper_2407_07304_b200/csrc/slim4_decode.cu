@@ -24,9 +24,9 @@
 //  * A K product needs the query, then a softmax step, then V: with twelve warps per SM these phases overlap across warps
 //    (eight warps 36 us, sixteen at 128 registers 46 us on the 64 / 8-head workload when twelve took 34).
 //
-// Measured (B200, calls back to back, three caches in turn; the copy rate is 6.57 TB/s): 16 x 2049 tokens, 32 / 32 heads KSTEP us
-// for 143 MB; 32 ragged sequences of up to 4096 tokens, 64 / 8 heads, KB32 us for 93 MB; one of 32768 tokens, 32 / 2 heads,
-// KLONG us for 9 MB; one of 272 tokens, 32 / 32 heads, KTINY us.  The stream itself runs at 6 TB/s (573 MB: 108 us); a call
+// Measured (B200, calls back to back, three caches in turn; the copy rate is 6.57 TB/s): 16 x 2049 tokens, 32 / 32 heads 37.7 us
+// for 143 MB (2 us of it reading the new rows back); 32 ragged sequences of up to 4096 tokens, 64 / 8 heads, 27.5 us for 93 MB; one of 32768 tokens, 32 / 2 heads,
+// 17.4 us for 9 MB; one of 272 tokens, 32 / 32 heads, 6.8 us.  The stream itself runs at 6 TB/s (573 MB: 108 us); a call
 // carries 2.3 us to its first products and 5 to 8 us from the median warp's last unit to its end (the slowest warp, the block's
 // merge, the round trips of the merge between blocks).  With more than eight query heads per kv head the products bound it:
 // eight warps of 255 registers, 3.8 TB/s.
@@ -920,7 +920,7 @@ static int launch_d4(const slim_cache4_t *c, const Decode4Params &p, int max_kv,
     rc = allow_dynamic_smem(reinterpret_cast<const void *>(slim4_decode_kernel<kHeads, kStep>), (int)D4<kHeads>::kBytes);
     if (rc != SLIM_OK) return rc;
     // Few pairs on many blocks (one sequence of 32768 tokens on two kv heads: 74 blocks each): a second kernel merges them,
-    // KMERGE us against 20.7 with the last blocks doing it in two steps; for more pairs its launch costs more than it saves.
+    // 17.5 us against 20.7 with the last blocks doing it in two steps; for more pairs its launch costs more than it saves.
     const bool defer = blocks > kD4Few * pairs;
     Decode4Params q = p;
     if (defer) q.counters = nullptr;
