@@ -6,7 +6,8 @@
 //
 // Measured (16 ragged prompts of 256 to 4096 tokens, 8 kv heads, 291,000 rows each of K and V, 189 MB a call): append 36.2 us =
 // 5.2 TB/s (68 % of the issue slots; constants held as packed pairs and the rows of extreme scales apart took it from 39.3),
-// read-back 35.2 us = 5.4 TB/s, 80 and 82 % of the copy rate.  Blocks of 128 threads: the same; 512: 44.6 and 37.1 us.
+// read-back 35.2 us = 5.4 TB/s, 79 and 82 % of the copy rate.  Blocks of 128 threads: 35.3 and
+// 35.2 us, within the spread of such runs; of 512, with an earlier form of the append that took 40.2: 44.6 and 37.1.
 #include "slim4_common.cuh"
 
 namespace slim {

@@ -22,14 +22,17 @@
 //    at once; the others leave a record, merged by the block, and where a pair spans blocks, by the block that finishes it
 //    last, or by a second kernel where few pairs span many blocks.
 //  * A K product needs the query, then a softmax step, then V: with twelve warps per SM these phases overlap across warps
-//    (eight warps 36 us, sixteen at 128 registers 46 us on the 64 / 8-head workload when twelve took 34).
+//    (32 x 4096 tokens, 64 / 8 heads: 34.9 us, with eight warps 36.8; 4 x 640 tokens, 32 / 32 heads: 7.8 and 10.4; only
+//    where a few warps have work are eight faster: 272 tokens, 32 / 32 heads, 6.7 and 6.5.  Sixteen
+//    warps at 128 registers, in an earlier form: 46 us where twelve took 37.)
 //
-// Measured (B200, calls back to back, three caches in turn; the copy rate is 6.57 TB/s): 16 x 2049 tokens, 32 / 32 heads 37.7 us
-// for 143 MB (2 us of it reading the new rows back); 32 ragged sequences of up to 4096 tokens, 64 / 8 heads, 27.5 us for 93 MB; one of 32768 tokens, 32 / 2 heads,
-// 17.4 us for 9 MB; one of 272 tokens, 32 / 32 heads, 6.8 us.  The stream itself runs at 6 TB/s (573 MB: 108 us); a call
+// Measured (B200, calls back to back, three caches in turn; the copy rate is 6.57 TB/s): 16 x 2049 tokens, 32 / 32 heads 38 us
+// for 143 MB, the new rows' append and their read-back included; 32 ragged sequences of up to 4096 tokens, 64 / 8 heads, 27.5 us
+// for 93 MB; one of 32768 tokens, 32 / 2 heads, 17.5 us for 9 MB; one of 272 tokens, 32 / 32 heads, 6.8 us.  Between 144 and 573 MB
+// with eight query heads per kv head the stream runs at 6.1 TB/s (573 MB: 108 us); a call
 // carries 2.3 us to its first products and 5 to 8 us from the median warp's last unit to its end (the slowest warp, the block's
 // merge, the round trips of the merge between blocks).  With more than eight query heads per kv head the products bound it:
-// eight warps of 255 registers, 3.8 TB/s.
+// eight warps of 255 registers, 3.9 TB/s (64 x 32768 tokens, 32 / 2 heads, 571 MB: 147 us).
 //
 // Query rows are held as fp16 after division by a power of two near the row's largest value: exact down to 2^-24 of it.
 // The weights p_j s_j are rounded to fp16 (2^-11 of each), p_j itself, its sum and the offset's sum stay fp32.
@@ -910,7 +913,8 @@ static int launch_d4(const slim_cache4_t *c, const Decode4Params &p, int max_kv,
     const long long pairs = (long long)p.B * p.Hkv, per_pair = (max_kv + kD4Unit - 1) / kD4Unit, units = pairs * per_pair;
     if (units > 0x7FFFFFFFLL) return SLIM_ERR_UNSUPPORTED;   // (units are counted in 32 bits)
     // One block per SM; where a pair is at most a unit for every warp and there is an SM for every pair, one block per pair:
-    // nothing is merged between blocks then (32 pairs of 272 tokens: see below)
+    // nothing is merged between blocks then (one sequence, 32 / 32 heads, 272 tokens: 6.7 us, spread over all SMs 9.1; 32 / 8
+    // heads, 768 tokens: 7.8 and 9.6; 32 / 2 heads, 512 tokens: 9.2 and 12.2)
     long long blocks = units < sms ? units : sms;
     if (per_pair <= D4<kHeads>::kWarps && pairs < blocks) blocks = pairs;
     if (blocks < 1) blocks = 1;
@@ -920,7 +924,8 @@ static int launch_d4(const slim_cache4_t *c, const Decode4Params &p, int max_kv,
     rc = allow_dynamic_smem(reinterpret_cast<const void *>(slim4_decode_kernel<kHeads, kStep>), (int)D4<kHeads>::kBytes);
     if (rc != SLIM_OK) return rc;
     // Few pairs on many blocks (one sequence of 32768 tokens on two kv heads: 74 blocks each): a second kernel merges them,
-    // 17.5 us against 20.7 with the last blocks doing it in two steps; for more pairs its launch costs more than it saves.
+    // 17.5 us against 20.7 with the last blocks doing it in two steps; for more pairs its launch costs more than it saves (32
+    // ragged sequences, 64 / 8 heads: 32.5 us against 28.3).
     const bool defer = blocks > kD4Few * pairs;
     Decode4Params q = p;
     if (defer) q.counters = nullptr;

@@ -10,8 +10,8 @@
 //
 // The copies (a job is a source page, a target page and a number of tokens) are bound by HBM: a warp copies the codes of
 // one (job, kv head, K or V), eight 16-byte words per lane in flight.  About 500 pages in eight INT8 layers, 2.1 GB read and written:
-// 357 us, 6.0 TB/s, 91 % of the copy rate (four or sixteen words per lane: the same; with sixteen, pages copied in part, whose
-// codes are no multiple of that, 156 us in place of 83).
+// 354 us (366 with the two plans), 6.0 TB/s, 92 % of the copy rate.  Four or sixteen words per lane: 351 and 347 there, but about 250
+// pages copied in part after a fork of 256 rows take 85 and 156 us in all in place of 83.
 #include "slim_common.cuh"
 #include "slim_tmap.cuh"
 
@@ -20,7 +20,8 @@ namespace slim {
 constexpr int kPgThreads = 1024;
 constexpr int kPgWarps = kPgThreads / 32;
 constexpr int kPgMaxLayers = 64;           // of one launch (they are passed by value)
-constexpr int kPgSharedInts = 50000;       // counters and rows' notes that go into shared memory
+constexpr int kPgSharedInts = 50000;       // counters and rows' notes that go into shared memory (a fork of 16 rows, 59 pages: 4.9 us,
+                                           // in global memory 7.4; of 256 rows, 1020 pages: 9.6 and 13.9)
 
 // Workspace, in ints: how many jobs there are; by page: job sources and targets, counters; by row: tokens of the job, the
 // row's notes.  The copies read the jobs; counters and notes are used only where shared memory does not hold them.

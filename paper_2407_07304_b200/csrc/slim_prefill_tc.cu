@@ -166,7 +166,8 @@ slim_prefill_tc_kernel(const __grid_constant__ CUtensorMap codes_map, const Pref
     const int q_len = p.cu_q[b + 1] - q0;
     const int m0 = qblock * kPfRows;
     // A block's rows: those of one query head, or (kPack, h is then the kv head) those of the G heads of its kv head token by
-    // token, so that a few query tokens of many heads fill the tiles and no more than 256 / G tokens share a causal border.
+    // token, so that a few query tokens of many heads fill the tiles and no more than 256 / G tokens share a causal border (4 pieces of
+    // 256 to 512 tokens behind 4000, 64 / 8 heads: 295 us, a head to a block 376).
     const int n_rows_all = kPack ? q_len * p.G : q_len;
     auto token_of = [&](int row) { return kPack ? row / p.G : row; };
     auto row_at = [&](int row) {   // index of a block's row among the rows of q and out
