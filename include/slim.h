@@ -601,9 +601,10 @@ typedef struct slim_layer {
  * own with a copy of the kv_len % 128 tokens behind them, in every layer.  Rows of `from` that no row names are freed,
  * parent[i] < 0 (or >= from->rows) leaves row i empty: no pages, length -1.
  *
- *   from, to   to->table and to->held must not be from's; to->refs may be from->refs.  Same num_pages and stride
+ *   from, to   to->table and to->held must not overlap from's; to->refs may be from->refs.  Same num_pages and stride
  *   parent     device int32 [to->rows]
- *   kv_len     device int32 [from->rows]: tokens of every row (held[b] * 128 at most);  len_out  device int32 [to->rows], another array
+ *   kv_len     device int32 [from->rows]: tokens of every row (held[b] * 128 at most);  len_out  device int32 [to->rows],
+ *              overlapping neither kv_len nor parent
  *   layers     host array of n_layers pools (0: tables only)
  *   result     device int32 [2]: pages that are missing, pages free afterwards.  Where pages are missing nothing else is
  *              written: free some and call again
@@ -625,7 +626,7 @@ int slim_pages_grow(const slim_pages_t *pages, const int32_t *kv_len, int32_t ro
  * Moves the pages in use together: with n pages in use, those with ids from n on move to the free ids below n, both in
  * ascending order, in every layer; table and refs follow.  Pages from n on are free afterwards (and keep what they held).
  *
- *   from, to  may be the same, array by array.  Same num_pages, rows and stride
+ *   from, to  may be the same, array by array, and must not overlap otherwise.  Same num_pages, rows and stride
  *   result    device int32 [2]: pages in use, pages moved
  */
 int slim_pages_compact(const slim_pages_t *from, const slim_pages_t *to, const slim_layer_t *layers, int32_t n_layers,

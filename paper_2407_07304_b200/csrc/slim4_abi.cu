@@ -166,6 +166,13 @@ static int check_pages(const slim_pages_t *p)
     if (p->num_pages > (1 << 23) || p->rows > (1 << 23)) return SLIM_ERR_UNSUPPORTED;   // (sums over either stay inside 32 bits)
     return SLIM_OK;
 }
+// Whether two arrays of 32-bit numbers share one.
+static bool overlap(const int32_t *a, size_t n_a, const int32_t *b, size_t n_b)
+{
+    return n_a > 0 && n_b > 0 && (uintptr_t)a < (uintptr_t)(b + n_b) && (uintptr_t)b < (uintptr_t)(a + n_a);
+}
+static bool overlap_in_part(const int32_t *a, const int32_t *b, size_t n) { return a != b && overlap(a, n, b, n); }
+static size_t entries(const slim_pages_t *p) { return (size_t)p->rows * p->stride; }
 static int check_layers(const slim_layer_t *layers, int32_t n_layers)
 {
     if (n_layers < 0 || (n_layers > 0 && layers == nullptr)) return SLIM_ERR_INVALID_ARG;
@@ -188,7 +195,10 @@ SLIM_EXPORT int slim_pages_fork(const slim_pages_t *from, const slim_pages_t *to
     if (rc != SLIM_OK) return rc;
     if (from->num_pages != to->num_pages || from->stride != to->stride) return SLIM_ERR_INVALID_ARG;
     if (result == nullptr || (to->rows > 0 && (parent == nullptr || len_out == nullptr)) || (from->rows > 0 && kv_len == nullptr)) return SLIM_ERR_INVALID_ARG;
-    if (from->rows > 0 && to->rows > 0 && (from->table == to->table || from->held == to->held || kv_len == len_out)) return SLIM_ERR_INVALID_ARG;
+    // (rows of `from`, lengths and parents are read while those of `to` are written)
+    if (overlap(from->table, entries(from), to->table, entries(to)) || overlap(from->held, from->rows, to->held, to->rows)) return SLIM_ERR_INVALID_ARG;
+    if (overlap(kv_len, from->rows, len_out, to->rows) || overlap(parent, to->rows, len_out, to->rows)) return SLIM_ERR_INVALID_ARG;
+    if (overlap_in_part(from->refs, to->refs, from->num_pages)) return SLIM_ERR_INVALID_ARG;
     rc = check_scratch(workspace, workspace_bytes, slim_pages_workspace_bytes(from->num_pages, from->rows > to->rows ? from->rows : to->rows));
     if (rc != SLIM_OK) return rc;
     return launch_pages_fork(from, to, parent, kv_len, len_out, layers, n_layers, result, workspace, (cudaStream_t)stream);
@@ -213,6 +223,8 @@ SLIM_EXPORT int slim_pages_compact(const slim_pages_t *from, const slim_pages_t 
     if (rc == SLIM_OK) rc = check_layers(layers, n_layers);
     if (rc != SLIM_OK) return rc;
     if (from->num_pages != to->num_pages || from->stride != to->stride || from->rows != to->rows || result == nullptr) return SLIM_ERR_INVALID_ARG;
+    if (overlap_in_part(from->table, to->table, entries(from)) || overlap_in_part(from->held, to->held, from->rows) ||
+        overlap_in_part(from->refs, to->refs, from->num_pages)) return SLIM_ERR_INVALID_ARG;
     rc = check_scratch(workspace, workspace_bytes, slim_pages_workspace_bytes(from->num_pages, from->rows));
     if (rc != SLIM_OK) return rc;
     return launch_pages_compact(from, to, layers, n_layers, result, workspace, (cudaStream_t)stream);

@@ -144,6 +144,25 @@ def test_page_calls_refuse(call, kw, want):
     assert call(**kw) == want
 
 
+@pytest.mark.parametrize("call,kw", [
+    # a table of 48 bytes, counts of 12: the second one begins inside the first, or the first inside the second
+    (call_fork, dict(dst=pages(table=A + 16, held=C))), (call_fork, dict(src=pages(table=A + 44), dst=pages(table=A, held=C))),
+    (call_fork, dict(dst=pages(table=C, held=A + 8))), (call_fork, dict(src=pages(refs=A + 28), dst=pages(table=C, held=C))),
+    (call_fork, dict(len=A + 8)), (call_fork, dict(parent=C)), (call_fork, dict(parent=C + 8)),
+    (call_fork, dict(src=pages(rows=1), dst=pages(table=A - 32, held=C))),
+    (call_compact, dict(dst=pages(table=A + 16))), (call_compact, dict(dst=pages(table=A - 16))), (call_compact, dict(dst=pages(held=A + 4))),
+    (call_compact, dict(dst=pages(refs=A + 4))),
+])
+def test_tables_that_overlap_in_part_are_refused(call, kw):
+    # (too small a workspace: a call that passes this check never launches)
+    assert call(n=0, **kw) == INVALID
+
+
+def test_tables_side_by_side_are_not():
+    assert call_fork(n=0, dst=pages(table=A + 48, held=A + 12), len=A + 12) == WORKSPACE
+    assert call_compact(n=0) == call_compact(n=0, dst=pages(table=A - 48, held=A + 12, refs=A + 32)) == WORKSPACE
+
+
 def test_binding_refuses():
     make = lambda *shape, dtype=torch.int32: torch.zeros(shape, dtype=dtype)  # noqa: E731
     with pytest.raises(TypeError):
