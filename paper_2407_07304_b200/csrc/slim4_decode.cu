@@ -439,7 +439,9 @@ slim4_decode_kernel(const __grid_constant__ CUtensorMap map_codes, const __grid_
         int take_slot = 0;
         uint32_t parity = 0;
         auto landed = [&]() {   // waits for the next half
-            if (!tc::mbar_try(bar(take_slot), parity) && !d4_wait(bar(take_slot), parity, flags)) {
+            // (by vote: `ok` decides which way the whole warp goes, also where a wait runs out for some of its lanes only)
+            if (!__all_sync(0xffffffffu, tc::mbar_try(bar(take_slot), parity)) &&
+                !__all_sync(0xffffffffu, d4_wait(bar(take_slot), parity, flags))) {
                 ok = false;
                 flags[0] = 1;
             }
