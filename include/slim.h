@@ -118,7 +118,7 @@ int slim_kv_append(const slim_cache_t *cache, const void *k_new, const void *v_n
  * head h reads kv head h / (Hq / Hkv).  For each (row, head):
  *   s_j = sm_scale * sum_d q_d * (k_code[j][d] * k_scale[j]);  p = softmax_j(s);
  *   o_d = sum_j p_j * (v_code[j][d] * v_scale[j]).
- * A row that sees no key gets zeros.
+ * A row that sees no key gets zeros.  sm_scale may be negative or zero.
  *
  *   q      device bf16 [total_q][Hq][128], 16-byte aligned
  *   out    device bf16 [total_q][Hq][128], 16-byte aligned
