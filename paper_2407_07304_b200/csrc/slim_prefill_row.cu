@@ -132,14 +132,14 @@ slim_prefill_row_kernel(const __grid_constant__ CUtensorMap codes_map, const Pre
 #pragma unroll
             for (int o = 8; o > 0; o >>= 1) am = fmaxf(am, __shfl_xor_sync(0xffffffffu, am, o));
             const float p2 = pow2_floor(am);
-            const float inv = pow2_recip(p2);
+            const float inv = copysignf(pow2_recip(p2), p.scale_log2e);   // (the factor c below is positive: a negative scale turns the row)
             uint32_t hw[4];
 #pragma unroll
             for (int k = 0; k < 4; ++k)
                 hw[k] = pack_half2(bf16_bits_to_float(w[k] & 0xFFFFu) * inv, bf16_bits_to_float(w[k] >> 16) * inv);
             const uint32_t off = rwl::kQ + (uint32_t)(piece >> 3) * 16384u + (uint32_t)rr * 128u + (uint32_t)(((piece & 7) ^ (rr & 7)) << 4);
             *reinterpret_cast<uint4 *>(smem + off) = make_uint4(hw[0], hw[1], hw[2], hw[3]);
-            if (piece == 0) row_scale[rr] = p2 * p.scale_log2e;
+            if (piece == 0) row_scale[rr] = p2 * fabsf(p.scale_log2e);
         }
         tc::fence_proxy_async();
     }

@@ -63,3 +63,26 @@ def check_int8(form, scale, n):
     held = codes * scales[..., None]
     err = np.abs(out.double().cpu().numpy() - dense_attention(q.double().cpu().numpy(), held[0], held[1], n, scale))
     assert err.max() <= MAX_ABS and err.mean() <= MEAN_ABS, f"max {err.max():.3e}, mean {err.mean():.3e}"
+
+
+@pytest.mark.parametrize("scale", SCALES)
+def test_int8_full_row(scale):
+    check_int8("slim_attn_prefill_full_row", scale, 250)
+
+
+@pytest.mark.parametrize("scale", SCALES)
+@pytest.mark.parametrize("hq,hkv", [(2, 2), (16, 2)])
+def test_int8_decode(hq, hkv, scale):
+    """Decode takes the same scales."""
+    gen = torch.Generator().manual_seed(6)
+    n = 700
+    cache = slim.SlimCache(1, hkv, 6)
+    k, v = (torch.randn(n, hkv, D, generator=gen).to(torch.bfloat16).cuda() for _ in range(2))
+    slim.slim_kv_append(cache, k, v, i32([0, n]), i32([0]), 1, n)
+    q = torch.randn(1, hq, D, generator=gen).to(torch.bfloat16).cuda()
+    out = torch.empty_like(q)
+    slim.slim_attn_decode(cache, q, out, i32([n]), 1, n, hq, scale, slim.workspace(slim.PHASE_DECODE, 1, hq, hkv, 1, n))
+    codes = cache.codes_view().permute(2, 0, 3, 1, 4).reshape(2, -1, hkv, D)[:, :n].double().cpu().numpy()
+    held = codes * cache.scales_view().permute(2, 0, 3, 1).reshape(2, -1, hkv)[:, :n].double().cpu().numpy()[..., None]
+    err = np.abs(out.double().cpu().numpy() - dense_attention(q.double().cpu().numpy(), held[0], held[1], n, scale))
+    assert err.max() <= MAX_ABS and err.mean() <= MEAN_ABS, f"max {err.max():.3e}, mean {err.mean():.3e}"
