@@ -508,6 +508,9 @@ size_t slim_evict_workspace_bytes(int32_t B, int32_t Hkv, int32_t max_kv, int32_
  *   z = min x (a bf16 value, exact);  s = (max x - min x) / 15, formed in fp32 and rounded to bf16;
  *   u_d = clamp(round_half_even((x_d - z) / s), 0, 15), difference and quotient rounded to fp32 each; 0 where s == 0;
  *   the value held is z + u_d * s.
+ * A row with a NaN or an infinity (outside the contract, as everywhere), or whose max x - min x is beyond fp32, holds no finite
+ * value, and other rows are as they would be without it.  Sequences that see the row get NaN from that kv head; in a prefill so may
+ * rows of the same kv head up to 254 tokens before it.
  *
  *   codes   device uint8 [num_pages][num_kv_heads][2][128 slots][64]: byte i holds dim i (low four bits) and dim 64 + i
  *   scales  device bf16  [num_pages][num_kv_heads][2][128 slots][2]: s, z

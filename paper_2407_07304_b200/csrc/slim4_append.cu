@@ -65,16 +65,14 @@ slim4_append_kernel(uint8_t *__restrict__ codes, uint32_t *__restrict__ pairs, c
 #pragma unroll
     for (int v = 0; v < 4; ++v) {
         lo2 = q4_min_bf16x2(lo2, q4_min_bf16x2(q4_min_bf16x2(raw[v].x, raw[v].y), q4_min_bf16x2(raw[v].z, raw[v].w)));
-        hi2 = ap_max_bf16x2(hi2, ap_max_bf16x2(ap_max_bf16x2(raw[v].x, raw[v].y), ap_max_bf16x2(raw[v].z, raw[v].w)));
+        hi2 = q4_max_bf16x2(hi2, q4_max_bf16x2(q4_max_bf16x2(raw[v].x, raw[v].y), q4_max_bf16x2(raw[v].z, raw[v].w)));
     }
 #pragma unroll
     for (int o = 1; o <= 2; o <<= 1) {
         lo2 = q4_min_bf16x2(lo2, __shfl_xor_sync(0xffffffffu, lo2, o));
-        hi2 = ap_max_bf16x2(hi2, __shfl_xor_sync(0xffffffffu, hi2, o));
+        hi2 = q4_max_bf16x2(hi2, __shfl_xor_sync(0xffffffffu, hi2, o));
     }
-    const float lo = fminf(__uint_as_float(lo2 << 16), __uint_as_float(lo2 & 0xFFFF0000u));
-    const float hi = fmaxf(__uint_as_float(hi2 << 16), __uint_as_float(hi2 & 0xFFFF0000u));
-    const uint32_t pair = q4_pair(lo, hi);
+    const uint32_t pair = q4_pair(q4_min_of(lo2), q4_max_of(hi2));
     const Q4Row q(pair);
     if (!stored) return;
     // dims 8 (4 v + l) .. + 7 low, 64 further high, v = 0, 1

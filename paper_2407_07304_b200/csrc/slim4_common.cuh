@@ -20,10 +20,30 @@ __host__ __device__ inline size_t code4_block_offset(int page, int head, int kv,
 __device__ __forceinline__ float pair_scale(uint32_t pair) { return __uint_as_float(pair << 16); }
 __device__ __forceinline__ float pair_offset(uint32_t pair) { return __uint_as_float(pair & 0xFFFF0000u); }
 
+// (A NaN stays one: a row that holds a NaN gets it as scale and offset, and so as its values.)
 __device__ __forceinline__ uint32_t q4_min_bf16x2(uint32_t a, uint32_t b)
 {
     uint32_t r;
-    asm("min.bf16x2 %0, %1, %2;\n" : "=r"(r) : "r"(a), "r"(b));
+    asm("min.NaN.bf16x2 %0, %1, %2;\n" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+__device__ __forceinline__ uint32_t q4_max_bf16x2(uint32_t a, uint32_t b)
+{
+    uint32_t r;
+    asm("max.NaN.bf16x2 %0, %1, %2;\n" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+// the smaller (the larger) value of a pair
+__device__ __forceinline__ float q4_min_of(uint32_t a)
+{
+    float r;
+    asm("min.NaN.f32 %0, %1, %2;\n" : "=f"(r) : "f"(__uint_as_float(a << 16)), "f"(__uint_as_float(a & 0xFFFF0000u)));
+    return r;
+}
+__device__ __forceinline__ float q4_max_of(uint32_t a)
+{
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;\n" : "=f"(r) : "f"(__uint_as_float(a << 16)), "f"(__uint_as_float(a & 0xFFFF0000u)));
     return r;
 }
 
@@ -37,9 +57,9 @@ __device__ __forceinline__ uint32_t q4_pair(float lo, float hi)
 
 // What the codes of a row are formed with.  The quotient (x - z) / s is the correctly rounded one: p = d * rc with
 // rc = RN(1 / s), its exact residual r = d - s p by a fused multiply-add, q = p + r rc (Markstein's correction).  Rows whose
-// scale lies outside [2^-60, 2^60] (constant rows among them) divide instead: intermediates could leave the normal range there,
-// and only a scale that is a subnormal of few bits can be so much too small that a quotient passes 15.5 (the others are
-// within 2^-9: 15.06 at most).
+// scale lies outside [2^-60, 2^60] (constant rows among them, and rows with a NaN or an infinity, whose scale is one) divide
+// instead: intermediates could leave the normal range there, and only a scale that is a subnormal of few bits can be so much too
+// small that a quotient passes 15.5 (the others are within 2^-9: 15.06 at most).  So a code never has more than four bits.
 struct Q4Row {
     uint64_t nz2, ns2, rc2;   // -z, -s and 1 / s, twice each
     uint32_t pair;

@@ -236,14 +236,13 @@ __device__ __forceinline__ void d4_quantise(const __nv_bfloat16 *row, int i, uin
 {
     const uint2 a = __ldg(reinterpret_cast<const uint2 *>(row) + i), c = __ldg(reinterpret_cast<const uint2 *>(row) + 16 + i);
     uint32_t lo2 = q4_min_bf16x2(q4_min_bf16x2(a.x, a.y), q4_min_bf16x2(c.x, c.y));
-    uint32_t hi2 = ap_max_bf16x2(ap_max_bf16x2(a.x, a.y), ap_max_bf16x2(c.x, c.y));
+    uint32_t hi2 = q4_max_bf16x2(q4_max_bf16x2(a.x, a.y), q4_max_bf16x2(c.x, c.y));
 #pragma unroll
     for (int o = 1; o < 16; o <<= 1) {
         lo2 = q4_min_bf16x2(lo2, __shfl_xor_sync(0xffffffffu, lo2, o));
-        hi2 = ap_max_bf16x2(hi2, __shfl_xor_sync(0xffffffffu, hi2, o));
+        hi2 = q4_max_bf16x2(hi2, __shfl_xor_sync(0xffffffffu, hi2, o));
     }
-    pair = q4_pair(fminf(__uint_as_float(lo2 << 16), __uint_as_float(lo2 & 0xFFFF0000u)),
-                   fmaxf(__uint_as_float(hi2 << 16), __uint_as_float(hi2 & 0xFFFF0000u)));
+    pair = q4_pair(q4_min_of(lo2), q4_max_of(hi2));
     const Q4Row q(pair);
     const uint32_t lo[2] = {a.x, a.y}, hi[2] = {c.x, c.y};
     uint32_t w[1];
