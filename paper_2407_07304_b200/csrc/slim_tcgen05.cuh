@@ -29,6 +29,7 @@ __host__ __device__ constexpr uint32_t instr_desc(uint32_t c_fmt, uint32_t a_fmt
     return (c_fmt << 4) | (a_fmt << 7) | (b_fmt << 10) | ((a_mn ? 1u : 0u) << 15) | ((b_mn ? 1u : 0u) << 16) |
            ((N >> 3) << 17) | ((M >> 4) << 24);
 }
+constexpr uint32_t kNegateA = 1u << 13;   // of a floating-point kind: -A instead of A
 
 // ---------------------------------------------------------------- MMA issue (one thread), commit
 __device__ __forceinline__ void mma_i8(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, bool accumulate)
