@@ -577,7 +577,8 @@ size_t slim_cache4_scale_bytes(int32_t num_pages, int32_t num_kv_heads);
  *   refs   device int32 [num_pages]: rows (and other holders, counted by the caller) that hold a page; 0: free
  *   table  device int32 [rows][stride]: a sequence's pages in order, -1 from held[row] on; a cache's block_table
  *   held   device int32 [rows]: pages of a row, 0 to stride
- * Only pages that are full may be held by more than one row.  Page ids outside [0, num_pages) are not followed.  Up to 2^23
+ * Only pages that are full may be held by more than one row, and nothing may be appended to those.  (After a fork at a length
+ * that is a multiple of 128 this is so of the last token's page: the next token needs room, a longer kv_len, first.)  Page ids outside [0, num_pages) are not followed.  Up to 2^23
  * pages and rows.
  * Pages are taken lowest id first; every result is the same from run to run.
  */

@@ -193,7 +193,8 @@ class SampledRun:
 
     A step is advance() (room for the new tokens), then prompt() or step() for every layer; fork() lets rows continue, share
     or end by parent, compact() moves the pages in use together.  Lengths are kept on the device and, for the launches'
-    bounds, here.  A pool without enough pages is a MemoryError, and nothing has changed then."""
+    bounds, here.  A pool without enough pages is a MemoryError, and nothing has changed then.  step() writes one token
+    into every row that is not empty: a finished row has to end (a fork in which nobody continues it) before."""
 
     def __init__(self, n_layers, Hq, Hkv, num_pages, rows, max_tokens, bits=4, device="cuda"):
         self.Hq, self.Hkv, self.rows, self.bits, self.device = Hq, Hkv, rows, bits, torch.device(device)
@@ -206,6 +207,7 @@ class SampledRun:
         # the other tables: a fork goes from one set to the other (the page counters are kept in place)
         self.other = slim.SlimPages(self.pages.refs, self.pages.table.clone(), self.pages.held.clone())
         self.lens = [-1] * rows      # -1: the row is empty
+        self.counts = [0] * rows     # new tokens of every row, as the last advance() announced them
         self.kv_len, self.len_other = self._i32(self.lens), self._i32(self.lens)
         self.result = self._i32([0, 0])
         self.ws_pages = slim.pages_workspace(num_pages, rows, device)
@@ -250,6 +252,10 @@ class SampledRun:
 
     def step(self, layer, q, k, v):
         """Layer `layer` of one new token in every row that is not empty (q bf16 [rows, Hq, 128], k and v [rows, Hkv, 128]); empty rows give zeros."""
+        # (the token goes to a row's last position: without room of its own it would take the place of one that is there,
+        # which at the end of a page is one that forked rows share)
+        if any(c != (1 if n >= 0 else 0) for n, c in zip(self.lens, self.counts)):
+            raise ValueError("advance() has to announce one token for every row that is not empty")
         out = torch.empty_like(q)
         if self.bits == 4:
             slim.slim_attn4_decode(self.caches[layer], q, out, self.kv_len, self.rows, max(self.lens), self.Hq, self.sm_scale, self.ws_decode, k_new=k, v_new=v)
@@ -258,15 +264,19 @@ class SampledRun:
         return out
 
     def fork(self, parents):
-        """Row i continues row parents[i]; -1 leaves it empty.  Rows that nobody continues are freed."""
+        """Row i continues row parents[i]; -1 leaves it empty.  Rows that nobody continues are freed.  Ends the step: advance() comes next."""
         if len(parents) != self.rows or not all(-1 <= p < self.rows for p in parents):
             raise ValueError("one parent per row, -1 for none")
         slim.slim_pages_fork(self.layers, self.pages, self.other, self._i32(parents), self.kv_len, self.len_other, self.result, self.ws_pages)
         self._enough()
         self.pages, self.other = self.other, self.pages
         self.kv_len, self.len_other = self.len_other, self.kv_len
-        self.lens = [self.lens[p] if p >= 0 else -1 for p in parents]
+        self._forked(parents)
         self._use_tables()
+
+    def _forked(self, parents):
+        self.lens = [self.lens[p] if p >= 0 else -1 for p in parents]
+        self.counts = [0] * self.rows
 
     def compact(self):
         """Moves the pages in use together; returns how many there are."""
