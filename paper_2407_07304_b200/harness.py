@@ -246,6 +246,8 @@ class SampledRun:
         for c in self.counts:
             cu.append(cu[-1] + c)
         out = torch.empty_like(q)
+        if cu[-1] == 0:
+            return out
         fn = slim.slim_prefill4_step if self.bits == 4 else slim.slim_prefill_step
         fn(self.caches[layer], q, k, v, out, self._i32(cu), self.kv_len, self.rows, max(self.counts), max(self.lens), self.Hq, self.sm_scale, self.ws_prefill)
         return out
@@ -256,6 +258,8 @@ class SampledRun:
         # which at the end of a page is one that forked rows share)
         if any(c != (1 if n >= 0 else 0) for n, c in zip(self.lens, self.counts)):
             raise ValueError("advance() has to announce one token for every row that is not empty")
+        if max(self.lens) < 0:
+            return torch.zeros_like(q)
         out = torch.empty_like(q)
         if self.bits == 4:
             slim.slim_attn4_decode(self.caches[layer], q, out, self.kv_len, self.rows, max(self.lens), self.Hq, self.sm_scale, self.ws_decode, k_new=k, v_new=v)

@@ -27,6 +27,15 @@ def test_a_fork_ends_the_step():
         run.step(0, bf16(2, 4, 128), bf16(2, 2, 128), bf16(2, 2, 128))
 
 
+@pytest.mark.parametrize("bits", [4, 8])
+def test_empty_rows_give_zeros(bits):
+    run = harness.SampledRun(2, 4, 2, num_pages=4, rows=3, max_tokens=256, bits=bits, device="cpu")
+    out = run.step(1, bf16(3, 4, 128), bf16(3, 2, 128), bf16(3, 2, 128))
+    assert out.shape == (3, 4, 128) and not out.any()
+    out = run.prompt(0, bf16(0, 4, 128), bf16(0, 2, 128), bf16(0, 2, 128))
+    assert out.shape == (0, 4, 128)
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("bits", [4, 8])
 @pytest.mark.parametrize("length", [255, 256, 257])
@@ -57,3 +66,17 @@ def test_siblings_keep_their_tokens(bits, length):
     run.advance([1, 1, 1])
     run.step(0, q, draw(3, hkv), draw(3, hkv))
     assert all(torch.equal(a, held(row)) for row, a in enumerate(before))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("bits", [4, 8])
+def test_every_row_ends(bits):
+    gen = torch.Generator().manual_seed(3)
+    run = harness.SampledRun(1, 4, 2, num_pages=4, rows=2, max_tokens=256, bits=bits)
+    run.advance([3, 1])
+    run.prompt(0, *(bf16(4, h, 128, gen=gen, device="cuda") for h in (4, 2, 2)))
+    run.fork([-1, -1])
+    run.advance([0, 0])
+    assert not run.step(0, *(bf16(2, h, 128, gen=gen, device="cuda") for h in (4, 2, 2))).any()
+    run.advance([1, 0])
+    assert run.step(0, *(bf16(2, h, 128, gen=gen, device="cuda") for h in (4, 2, 2)))[0].isfinite().all()
