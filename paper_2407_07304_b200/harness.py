@@ -197,6 +197,8 @@ class SampledRun:
     into every row that is not empty: a finished row has to end (a fork in which nobody continues it) before."""
 
     def __init__(self, n_layers, Hq, Hkv, num_pages, rows, max_tokens, bits=4, device="cuda"):
+        if bits not in (4, 8):
+            raise ValueError("caches hold 4 or 8 bits")
         self.Hq, self.Hkv, self.rows, self.bits, self.device = Hq, Hkv, rows, bits, torch.device(device)
         stride = (max_tokens + PAGE_TOKENS - 1) // PAGE_TOKENS
         self.max_tokens, self.sm_scale = stride * PAGE_TOKENS, slim.HEAD_DIM ** -0.5

@@ -36,6 +36,12 @@ def test_empty_rows_give_zeros(bits):
     assert out.shape == (0, 4, 128)
 
 
+@pytest.mark.parametrize("bits", [2, 16, 5])
+def test_other_widths_are_refused(bits):
+    with pytest.raises(ValueError):
+        harness.SampledRun(1, 4, 2, num_pages=4, rows=3, max_tokens=256, bits=bits, device="cpu")
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("bits", [4, 8])
 @pytest.mark.parametrize("length", [255, 256, 257])
