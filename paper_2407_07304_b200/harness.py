@@ -242,11 +242,17 @@ class SampledRun:
         self._enough()
         self.counts, self.lens, self.kv_len = list(counts), lens, kv_len
 
+    @staticmethod
+    def _rows_are(n, *tensors):
+        if any(len(t) != n for t in tensors):
+            raise ValueError(f"{n} rows of queries, keys and values are needed")
+
     def prompt(self, layer, q, k, v):
         """Layer `layer` of the tokens that advance() announced, all rows' one after the other (q bf16 [tokens, Hq, 128], k and v [tokens, Hkv, 128])."""
         cu = [0]
         for c in self.counts:
             cu.append(cu[-1] + c)
+        self._rows_are(cu[-1], q, k, v)
         out = torch.empty_like(q)
         if cu[-1] == 0:
             return out
@@ -256,6 +262,7 @@ class SampledRun:
 
     def step(self, layer, q, k, v):
         """Layer `layer` of one new token in every row that is not empty (q bf16 [rows, Hq, 128], k and v [rows, Hkv, 128]); empty rows give zeros."""
+        self._rows_are(self.rows, q, k, v)
         # (the token goes to a row's last position: without room of its own it would take the place of one that is there,
         # which at the end of a page is one that forked rows share)
         if any(c != (1 if n >= 0 else 0) for n, c in zip(self.lens, self.counts)):

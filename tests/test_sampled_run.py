@@ -20,11 +20,26 @@ def test_step_refuses_rows_without_one_new_token(lens, counts):
 
 def test_a_fork_ends_the_step():
     run = harness.SampledRun(1, 4, 2, num_pages=8, rows=2, max_tokens=512, device="cpu")
+    with pytest.raises(ValueError):      # nothing announced yet
+        run.prompt(0, bf16(3, 4, 128), bf16(3, 2, 128), bf16(3, 2, 128))
     run.lens, run.counts = [3, 3], [1, 1]
     run._forked([1, -1])
     assert run.lens == [3, -1] and run.counts == [0, 0]
+    for call in (run.step, run.prompt):
+        with pytest.raises(ValueError):
+            call(0, bf16(2, 4, 128), bf16(2, 2, 128), bf16(2, 2, 128))
+
+
+@pytest.mark.parametrize("q,k,v", [(4, 5, 5), (6, 5, 5), (5, 4, 5), (5, 5, 4)])
+def test_rows_as_announced(q, k, v):
+    run = harness.SampledRun(1, 4, 2, num_pages=8, rows=3, max_tokens=512, device="cpu")
+    run.lens, run.counts = [2, 3, -1], [2, 3, 0]
     with pytest.raises(ValueError):
-        run.step(0, bf16(2, 4, 128), bf16(2, 2, 128), bf16(2, 2, 128))
+        run.prompt(0, bf16(q, 4, 128), bf16(k, 2, 128), bf16(v, 2, 128))
+    run.lens, run.counts = [2, 3, -1, 1, 1], [1, 1, 0, 1, 1]
+    run.rows = 5
+    with pytest.raises(ValueError):
+        run.step(0, bf16(q, 4, 128), bf16(k, 2, 128), bf16(v, 2, 128))
 
 
 @pytest.mark.parametrize("bits", [4, 8])
