@@ -578,8 +578,8 @@ size_t slim_cache4_scale_bytes(int32_t num_pages, int32_t num_kv_heads);
  *   table  device int32 [rows][stride]: a sequence's pages in order, -1 from held[row] on; a cache's block_table
  *   held   device int32 [rows]: pages of a row, 0 to stride
  * Only pages that are full may be held by more than one row, and nothing may be appended to those.  (After a fork at a length
- * that is a multiple of 128 this is so of the last token's page: the next token needs room, a longer kv_len, first.)  Page ids outside [0, num_pages) are not followed.  Up to 2^23
- * pages and rows.
+ * that is a multiple of 128 this is so of the last token's page: the next token needs room, a longer kv_len, first.)  Page ids
+ * outside [0, num_pages) are not followed.  Up to 2^23 pages and rows.
  * Pages are taken lowest id first; every result is the same from run to run.
  */
 typedef struct slim_pages {
@@ -630,9 +630,15 @@ int slim_pages_grow(const slim_pages_t *pages, const int32_t *kv_len, int32_t ro
  * Moves the pages in use together: with n pages in use, those with ids from n on move to the free ids below n, both in
  * ascending order, in every layer; table and refs follow.  Pages from n on are free afterwards (and keep what they held).
  *
+ * Other holders of pages (what refs counts beyond this table) have to follow: their pages move too, the old ids are free
+ * afterwards, and the moves stand in the workspace until its next use.
+ *
  *   from, to  may be the same, array by array, and must not overlap otherwise.  Same num_pages, rows and stride
  *   result    device int32 [2]: pages in use, pages moved
+ *   workspace as for slim_pages_fork.  Afterwards, from byte SLIM_PAGES_MOVED_OFFSET on, int32 [2][num_pages]: the old ids of
+ *             the pages moved, ascending, then their new ids; of both the first result[1] are written
  */
+#define SLIM_PAGES_MOVED_OFFSET 16
 int slim_pages_compact(const slim_pages_t *from, const slim_pages_t *to, const slim_layer_t *layers, int32_t n_layers,
                        int32_t *result, void *workspace, size_t workspace_bytes, void *stream);
 size_t slim_pages_workspace_bytes(int32_t num_pages, int32_t rows);

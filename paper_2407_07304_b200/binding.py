@@ -677,13 +677,25 @@ def slim_pages_grow(pages, kv_len, room, result, workspace, stream=None):
 
 
 def slim_pages_compact(layers, src, dst, result, workspace, stream=None):
-    """The pages in use move to the lowest ids, in every layer; dst (may be src) holds the tables afterwards."""
+    """The pages in use move to the lowest ids, in every layer; dst (may be src) holds the tables afterwards.  Pages that others
+    hold too move with them: see pages_moved."""
     where = "slim_pages_compact"
     array, n = _layers(where, layers, src)
     rc = (_lib or lib()).slim_pages_compact(src.ref, dst.ref, array, n, _i32(where, result, 2), workspace.data_ptr(), _nbytes(workspace),
                                             _cuda_stream(stream))
     if rc:
         _check(rc, where)
+
+
+PAGES_MOVED_OFFSET = 16   # SLIM_PAGES_MOVED_OFFSET
+
+
+def pages_moved(workspace, num_pages):
+    """Old and new ids of the pages that the last slim_pages_compact on this workspace moved: int32 [num_pages] each, ascending, of
+    which the first result[1] count.  Whoever holds pages beside the table (a counter one higher) looks them up here, before the
+    workspace is used again."""
+    ids = workspace[PAGES_MOVED_OFFSET:PAGES_MOVED_OFFSET + 8 * num_pages].view(torch.int32)
+    return ids[:num_pages], ids[num_pages:]
 
 
 def pages_workspace(num_pages, rows, device="cuda"):

@@ -24,11 +24,12 @@ constexpr int kPgSharedInts = 50000;       // counters and rows' notes that go i
                                            // in global memory 7.4; of 256 rows, 1020 pages: 9.6 and 13.9)
 
 // Workspace, in ints: how many jobs there are; by page: job sources and targets, counters; by row: tokens of the job, the
-// row's notes.  The copies read the jobs; counters and notes are used only where shared memory does not hold them.
+// row's notes.  The copies read the jobs (and callers a compaction's, from SLIM_PAGES_MOVED_OFFSET on); counters and notes are
+// used only where shared memory does not hold them.
 struct PagesWork {
     int *n_jobs, *source, *target, *part, *notes;
 };
-constexpr int kPgHead = 4;
+constexpr int kPgHead = SLIM_PAGES_MOVED_OFFSET / (int)sizeof(int);
 constexpr int kPgNotes = 4;   // notes per row
 static PagesWork pages_work(void *workspace, int num_pages, int rows)
 {

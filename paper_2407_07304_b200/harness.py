@@ -292,7 +292,7 @@ class SampledRun:
         self.counts = [0] * self.rows
 
     def compact(self):
-        """Moves the pages in use together; returns how many there are."""
+        """Moves the pages in use together; returns how many there are.  (Pages kept beside the rows: slim.pages_moved on ws_pages.)"""
         slim.slim_pages_compact(self.layers, self.pages, self.pages, self.result, self.ws_pages)
         return int(self.result[0])
 
