@@ -221,6 +221,7 @@ class _BlockTable:
         if block_table.dtype is not torch.int32 or block_table.dim() != 2 or not block_table.is_contiguous() or block_table.device != self.codes.device:
             raise TypeError("block tables must be contiguous int32 [rows, pages] on the cache's device")
         self.B, self.max_pages_per_seq = block_table.shape
+        self.rows = self.B
         self.block_table = block_table
         held = self.held_struct
         held.block_table, held.max_pages_per_seq = block_table.data_ptr(), self.max_pages_per_seq
@@ -521,6 +522,9 @@ class SlimCache4(_BlockTable):
         self.held_struct = SlimCacheStruct(self.codes.data_ptr(), self.scales.data_ptr(), self.block_table.data_ptr(),
                                            self.num_pages, PAGE_TOKENS, num_kv_heads, HEAD_DIM, max_pages_per_seq)
         self.ref = ctypes.byref(self.held_struct)
+        if self.block_table.dim() != 2 or self.block_table.shape[1] != max_pages_per_seq:
+            raise TypeError("block tables must be [rows, max_pages_per_seq]")
+        self.rows, self.at = self.block_table.shape[0], self.codes.get_device()
 
     @property
     def struct(self):
@@ -536,31 +540,79 @@ class SlimCache4(_BlockTable):
         return self.scales.view(self.num_pages, self.Hkv, 2, PAGE_TOKENS, 2)
 
 
-def _cache4(cache, where):
+# Every call checks sizes, types and places of what it is given: a kernel would read past the end of what is too short.  Single
+# tokens go through here too, where the host's time is the step's, so the checks are few calls and their words are put
+# together only when they fail.  get_device() is -1 for what no GPU can read.
+_BF16, _INT = torch.bfloat16, torch.int32
+_device, _raw_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
+
+
+def _refuse(where, what):
+    raise SlimError(SLIM_ERR_INVALID_ARG, f"{where}: {what}")
+
+
+def _cache4(where, cache, B):
     if type(cache) is not SlimCache4 and not isinstance(cache, SlimCache4):
-        raise SlimError(SLIM_ERR_INVALID_ARG, f"{where}: needs a SlimCache4")
+        _refuse(where, "needs a SlimCache4")
+    if B > cache.rows:
+        _refuse(where, f"{B} sequences on a block table of {cache.rows} rows")
     return cache.ref
 
 
-def _rows4(where, Hkv, k, v):
+def _rows4(where, cache, n, k, v):
+    """Rows of keys and values, n at least."""
     shape = k.shape
-    if k.dtype is not torch.bfloat16 or v.dtype is not torch.bfloat16 or v.shape != shape or len(shape) != 3 or shape[1] != Hkv or \
+    if k.dtype is not _BF16 or v.dtype is not _BF16 or v.shape != shape or len(shape) != 3 or shape[0] < n or shape[1] != cache.Hkv or \
             shape[2] != HEAD_DIM or not k.is_contiguous() or not v.is_contiguous():
-        raise SlimError(SLIM_ERR_INVALID_ARG, f"{where}: rows must be contiguous bfloat16 [tokens, kv heads, 128], K's and V's alike")
+        _refuse(where, f"rows must be contiguous bfloat16 [tokens, kv heads, 128], K's and V's alike, {n} tokens at least")
+    if k.get_device() != cache.at or v.get_device() != cache.at:
+        _refuse(where, "rows and cache lie on different devices")
 
 
-def _queries4(where, rows, q, out):
-    for t in (q, out):
-        if t.dtype is not torch.bfloat16 or not t.is_contiguous() or t.numel() < rows * HEAD_DIM:
-            raise SlimError(SLIM_ERR_INVALID_ARG, f"{where}: q and out must be contiguous bfloat16 [rows, heads, 128]")
+def _queries4(where, cache, n, q, out):
+    """Query rows, n at least, and room for as many results; how many there are."""
+    size = q.numel()
+    if q.dtype is not _BF16 or out.dtype is not _BF16 or not q.is_contiguous() or not out.is_contiguous() or size < n * HEAD_DIM or \
+            out.numel() < size:
+        _refuse(where, f"q and out must be contiguous bfloat16 [rows, heads, 128] of one size, {n} rows of heads at least")
+    if q.get_device() != cache.at or out.get_device() != cache.at:
+        _refuse(where, "q, out and cache lie on different devices")
+    return size // HEAD_DIM
+
+
+def _lens4(where, cache, B, lens, cu=None):
+    """A length or position per sequence, and offsets (one more)."""
+    if lens.dtype is not _INT or lens.numel() < B or not lens.is_contiguous() or lens.get_device() != cache.at or \
+            (cu is not None and (cu.dtype is not _INT or cu.numel() <= B or not cu.is_contiguous() or cu.get_device() != cache.at)):
+        _refuse(where, "lengths and positions must be contiguous int32, one per sequence (offsets one more), on the cache's device")
+
+
+def _scratch4(where, cache, t):
+    """Address and size of a workspace."""
+    if t is None:
+        return None, 0
+    if t.get_device() != cache.at:
+        _refuse(where, "workspace and cache lie on different devices")
+    return t.data_ptr(), t.nbytes
+
+
+def _stream_at(where, at, stream):
+    """The stream's address; the memory has to be the current device's."""
+    if at < 0:
+        _refuse(where, "the memory is not a GPU's")
+    if _device() != at:
+        _refuse(where, f"memory of device {at}, which is not the current one")
+    return _raw_stream(at) if stream is None else stream.cuda_stream
 
 
 def slim_kv4_append(cache, k_new, v_new, cu_new, start_pos, B, max_new, stream=None):
     """slim_kv_append into the 4-bit cache."""
     where = "slim_kv4_append"
-    ref = _cache4(cache, where)
-    _rows4(where, cache.Hkv, k_new, v_new)
-    rc = (_lib or lib()).slim_kv4_append(ref, k_new.data_ptr(), v_new.data_ptr(), cu_new.data_ptr(), start_pos.data_ptr(), B, max_new, _cuda_stream(stream))
+    ref = _cache4(where, cache, B)
+    _rows4(where, cache, 0, k_new, v_new)
+    _lens4(where, cache, B, start_pos, cu_new)
+    rc = (_lib or lib()).slim_kv4_append(ref, k_new.data_ptr(), v_new.data_ptr(), cu_new.data_ptr(), start_pos.data_ptr(), B, max_new,
+                                         _stream_at(where, cache.at, stream))
     if rc:
         _check(rc, where)
 
@@ -568,37 +620,49 @@ def slim_kv4_append(cache, k_new, v_new, cu_new, start_pos, B, max_new, stream=N
 def slim_kv4_read(cache, k_out, v_out, cu, start_pos, B, max_rows, stream=None):
     """The values held for positions start_pos[b] .. of every sequence, as bf16 rows cu[b] .. cu[b + 1] - 1 of k_out and v_out."""
     where = "slim_kv4_read"
-    ref = _cache4(cache, where)
-    _rows4(where, cache.Hkv, k_out, v_out)
-    rc = (_lib or lib()).slim_kv4_read(ref, k_out.data_ptr(), v_out.data_ptr(), cu.data_ptr(), start_pos.data_ptr(), B, max_rows, _cuda_stream(stream))
+    ref = _cache4(where, cache, B)
+    _rows4(where, cache, 0, k_out, v_out)
+    _lens4(where, cache, B, start_pos, cu)
+    rc = (_lib or lib()).slim_kv4_read(ref, k_out.data_ptr(), v_out.data_ptr(), cu.data_ptr(), start_pos.data_ptr(), B, max_rows,
+                                       _stream_at(where, cache.at, stream))
     if rc:
         _check(rc, where)
 
 
 def slim_attn4_prefill(cache, q, out, cu_q, kv_len, B, max_q, max_kv, Hq, sm_scale, workspace, stream=None):
-    _queries4("slim_attn4_prefill", 0, q, out)
-    rc = lib().slim_attn4_prefill(_cache4(cache, "slim_attn4_prefill"), _addr(q), _addr(out), _addr(cu_q), _addr(kv_len), B, max_q, max_kv, Hq,
-                                  sm_scale, _addr(workspace), _nbytes(workspace), _cuda_stream(stream))
-    _check(rc, "slim_attn4_prefill")
+    where = "slim_attn4_prefill"
+    ref = _cache4(where, cache, B)
+    _queries4(where, cache, 0, q, out)
+    _lens4(where, cache, B, kv_len, cu_q)
+    rc = (_lib or lib()).slim_attn4_prefill(ref, q.data_ptr(), out.data_ptr(), cu_q.data_ptr(), kv_len.data_ptr(), B, max_q, max_kv, Hq, sm_scale,
+                                            *_scratch4(where, cache, workspace), _stream_at(where, cache.at, stream))
+    _check(rc, where)
 
 
 def slim_prefill4_step(cache, q, k_new, v_new, out, cu_q, kv_len, B, max_q, max_kv, Hq, sm_scale, workspace, stream=None):
-    _queries4("slim_prefill4_step", 0, q, out)
-    _rows4("slim_prefill4_step", cache.Hkv, k_new, v_new)
-    rc = lib().slim_prefill4_step(_cache4(cache, "slim_prefill4_step"), _addr(q), _addr(k_new), _addr(v_new), _addr(out), _addr(cu_q), _addr(kv_len),
-                                  B, max_q, max_kv, Hq, sm_scale, _addr(workspace), _nbytes(workspace), _cuda_stream(stream))
-    _check(rc, "slim_prefill4_step")
+    where = "slim_prefill4_step"
+    ref = _cache4(where, cache, B)
+    rows = _queries4(where, cache, 0, q, out)
+    _rows4(where, cache, -(-rows // max(Hq, 1)), k_new, v_new)   # (every query token has a new key and value)
+    _lens4(where, cache, B, kv_len, cu_q)
+    rc = (_lib or lib()).slim_prefill4_step(ref, q.data_ptr(), k_new.data_ptr(), v_new.data_ptr(), out.data_ptr(), cu_q.data_ptr(), kv_len.data_ptr(), B,
+                                            max_q, max_kv, Hq, sm_scale, *_scratch4(where, cache, workspace),
+                                            _stream_at(where, cache.at, stream))
+    _check(rc, where)
 
 
 def slim_attn4_decode(cache, q, out, kv_len, B, max_kv, Hq, sm_scale, workspace, stream=None, k_new=None, v_new=None):
     """Decode attention over the 4-bit cache; with k_new and v_new the new tokens go into position kv_len - 1 in the same call."""
-    _queries4("slim_attn4_decode", B * Hq, q, out)
+    where = "slim_attn4_decode"
+    ref = _cache4(where, cache, B)
+    _queries4(where, cache, B * Hq, q, out)
     if k_new is not None and v_new is not None:
-        _rows4("slim_attn4_decode", cache.Hkv, k_new, v_new)
-    rc = (_lib or lib()).slim_attn4_decode(_cache4(cache, "slim_attn4_decode"), _addr(q), _addr(k_new), _addr(v_new), _addr(out), _addr(kv_len), B, max_kv, Hq,
-                                 sm_scale, _addr(workspace), _nbytes(workspace), _cuda_stream(stream))
+        _rows4(where, cache, B, k_new, v_new)
+    _lens4(where, cache, B, kv_len)
+    rc = (_lib or lib()).slim_attn4_decode(ref, q.data_ptr(), _addr(k_new), _addr(v_new), out.data_ptr(), kv_len.data_ptr(), B, max_kv, Hq, sm_scale,
+                                           *_scratch4(where, cache, workspace), _stream_at(where, cache.at, stream))
     if rc:
-        _check(rc, "slim_attn4_decode")
+        _check(rc, where)
 
 
 def decode4_workspace(B, Hq, Hkv, max_kv, device="cuda"):
