@@ -676,12 +676,12 @@ class SlimPages:
 
     def __init__(self, refs, table, held):
         for t in (refs, table, held):
-            if t.dtype is not torch.int32 or not t.is_contiguous():
-                raise TypeError("page tables, counters and counts must be contiguous int32")
+            if t.dtype is not torch.int32 or not t.is_contiguous() or t.device != refs.device:
+                raise TypeError("page tables, counters and counts must be contiguous int32 on one device")
         if refs.dim() != 1 or table.dim() != 2 or held.shape != table.shape[:1]:
             raise TypeError("refs [num_pages], table [rows, stride], held [rows]")
         self.refs, self.table, self.held = refs, table, held   # kept here because the struct holds bare addresses
-        self.num_pages, self.rows = refs.numel(), table.shape[0]
+        self.num_pages, self.rows, self.at = refs.numel(), table.shape[0], refs.get_device()
         self.struct = SlimPagesStruct(refs.data_ptr(), table.data_ptr(), held.data_ptr(), refs.numel(), table.shape[0], table.shape[1])
         self.ref = ctypes.byref(self.struct)
 
@@ -699,7 +699,9 @@ class PageLayers:
         self.caches = list(caches)
         if len({c.num_pages for c in self.caches}) > 1:
             raise ValueError("the layers' pools must have the same number of pages")
-        self.num_pages = self.caches[0].num_pages if self.caches else None
+        if len({c.codes.device for c in self.caches}) > 1:
+            raise ValueError("the layers' pools must lie on one device")
+        self.num_pages, self.at = (self.caches[0].num_pages, self.caches[0].codes.get_device()) if self.caches else (None, None)
         rows = [HEAD_DIM // 2 if isinstance(c, SlimCache4) else HEAD_DIM for c in self.caches]
         self.array = (SlimLayerStruct * max(1, len(self.caches)))(
             *[SlimLayerStruct(c.codes.data_ptr(), c.scales.data_ptr(), c.Hkv, n) for c, n in zip(self.caches, rows)])
@@ -708,34 +710,48 @@ class PageLayers:
 def _layers(where, layers, pages):
     if layers is None:
         return None, 0
-    if layers.num_pages != pages.num_pages and layers.caches:
-        raise SlimError(SLIM_ERR_INVALID_ARG, f"{where}: a layer's pool and the page counters differ in size")
+    if layers.caches and (layers.num_pages != pages.num_pages or layers.at != pages.at):
+        _refuse(where, "a layer's pool and the page counters differ in size, or in where they lie")
     return layers.array, len(layers.caches)
 
 
-def _i32(where, t, n):
+def _i32(where, at, t, n):
     """The address of n numbers at least."""
-    if t.dtype is not torch.int32 or t.numel() < n or not t.is_contiguous():
-        raise SlimError(SLIM_ERR_INVALID_ARG, f"{where}: lengths, parents and results must be contiguous int32, one per row (two results)")
+    if t.dtype is not _INT or t.numel() < n or not t.is_contiguous() or t.get_device() != at:
+        _refuse(where, "lengths, parents and results must be contiguous int32, one per row (two results), on the tables' device")
     return t.data_ptr()
+
+
+def _scratch_at(where, at, t):
+    if t.get_device() != at:
+        _refuse(where, "workspace and tables lie on different devices")
+    return t.data_ptr(), t.nbytes
+
+
+def _two_tables(where, src, dst):
+    if src.at != dst.at:
+        _refuse(where, "the two tables lie on different devices")
+    return src.at
 
 
 def slim_pages_fork(layers, src, dst, parent, kv_len, len_out, result, workspace, stream=None):
     """Row i of dst continues row parent[i] of src (-1: an empty row): the first child takes the row over, others share its full
     pages and get a copy of the last one, rows without children are freed.  layers: PageLayers, or None for the tables alone."""
     where = "slim_pages_fork"
+    at = _two_tables(where, src, dst)
     array, n = _layers(where, layers, src)
-    rc = (_lib or lib()).slim_pages_fork(src.ref, dst.ref, _i32(where, parent, dst.rows), _i32(where, kv_len, src.rows), _i32(where, len_out, dst.rows),
-                                         array, n, _i32(where, result, 2), workspace.data_ptr(), _nbytes(workspace), _cuda_stream(stream))
+    rc = (_lib or lib()).slim_pages_fork(src.ref, dst.ref, _i32(where, at, parent, dst.rows), _i32(where, at, kv_len, src.rows),
+                                         _i32(where, at, len_out, dst.rows), array, n, _i32(where, at, result, 2), *_scratch_at(where, at, workspace),
+                                         _stream_at(where, at, stream))
     if rc:
         _check(rc, where)
 
 
 def slim_pages_grow(pages, kv_len, room, result, workspace, stream=None):
     """Pages for kv_len + room tokens in every row of length 0 or more."""
-    where = "slim_pages_grow"
-    rc = (_lib or lib()).slim_pages_grow(pages.ref, _i32(where, kv_len, pages.rows), room, _i32(where, result, 2), workspace.data_ptr(),
-                                         _nbytes(workspace), _cuda_stream(stream))
+    where, at = "slim_pages_grow", pages.at
+    rc = (_lib or lib()).slim_pages_grow(pages.ref, _i32(where, at, kv_len, pages.rows), room, _i32(where, at, result, 2),
+                                         *_scratch_at(where, at, workspace), _stream_at(where, at, stream))
     if rc:
         _check(rc, where)
 
@@ -744,9 +760,10 @@ def slim_pages_compact(layers, src, dst, result, workspace, stream=None):
     """The pages in use move to the lowest ids, in every layer; dst (may be src) holds the tables afterwards.  Pages that others
     hold too move with them: see pages_moved."""
     where = "slim_pages_compact"
+    at = _two_tables(where, src, dst)
     array, n = _layers(where, layers, src)
-    rc = (_lib or lib()).slim_pages_compact(src.ref, dst.ref, array, n, _i32(where, result, 2), workspace.data_ptr(), _nbytes(workspace),
-                                            _cuda_stream(stream))
+    rc = (_lib or lib()).slim_pages_compact(src.ref, dst.ref, array, n, _i32(where, at, result, 2), *_scratch_at(where, at, workspace),
+                                            _stream_at(where, at, stream))
     if rc:
         _check(rc, where)
 
