@@ -213,6 +213,10 @@ def _check(rc, where):
         raise SlimError(rc, where)
 
 
+def _refuse(where, what):
+    raise SlimError(SLIM_ERR_INVALID_ARG, f"{where}: {what}")
+
+
 class _BlockTable:
     """What both caches do with their block table."""
 
@@ -247,6 +251,7 @@ class SlimCache(_BlockTable):
         self.struct = SlimCacheStruct(self.codes.data_ptr(), self.scales.data_ptr(), self.block_table.data_ptr(),
                                       self.num_pages, PAGE_TOKENS, num_kv_heads, HEAD_DIM, max_pages_per_seq)
         self.held_struct = self.struct
+        self.rows = self.block_table.numel() // max_pages_per_seq
 
     def codes_view(self):
         """int8 [num_pages, Hkv, 2, 128, 128]"""
@@ -257,29 +262,37 @@ class SlimCache(_BlockTable):
         return self.scales.view(self.num_pages, self.Hkv, 2, PAGE_TOKENS)
 
 
+def _cache8(where, cache, B):
+    """The struct's address, where its block table has a row for every sequence (tables may change: set_block_table)."""
+    struct, rows = cache.struct, getattr(cache, "rows", B)   # (any object with a struct serves as a cache)
+    if B > rows:
+        _refuse(where, f"{B} sequences on a block table of {rows} rows")
+    return ctypes.byref(struct)
+
+
 def slim_kv_append(cache, k_new, v_new, cu_new, start_pos, B, max_new, stream=None):
-    rc = lib().slim_kv_append(ctypes.byref(cache.struct), _ptr(k_new), _ptr(v_new), _ptr(cu_new), _ptr(start_pos),
+    rc = lib().slim_kv_append(_cache8("slim_kv_append", cache, B), _ptr(k_new), _ptr(v_new), _ptr(cu_new), _ptr(start_pos),
                               B, max_new, _stream(stream))
     _check(rc, "slim_kv_append")
 
 
 def slim_attn_prefill(cache, q, out, cu_q, kv_len, B, max_q, max_kv, Hq, sm_scale, workspace=None, stream=None):
     ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    rc = lib().slim_attn_prefill(ctypes.byref(cache.struct), _ptr(q), _ptr(out), _ptr(cu_q), _ptr(kv_len),
+    rc = lib().slim_attn_prefill(_cache8("slim_attn_prefill", cache, B), _ptr(q), _ptr(out), _ptr(cu_q), _ptr(kv_len),
                                  B, max_q, max_kv, Hq, sm_scale, _ptr(workspace), ws_bytes, _stream(stream))
     _check(rc, "slim_attn_prefill")
 
 
 def slim_prefill_step(cache, q, k_new, v_new, out, cu_q, kv_len, B, max_q, max_kv, Hq, sm_scale, workspace=None, stream=None):
     ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    rc = lib().slim_prefill_step(ctypes.byref(cache.struct), _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(out), _ptr(cu_q), _ptr(kv_len),
+    rc = lib().slim_prefill_step(_cache8("slim_prefill_step", cache, B), _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(out), _ptr(cu_q), _ptr(kv_len),
                                  B, max_q, max_kv, Hq, sm_scale, _ptr(workspace), ws_bytes, _stream(stream))
     _check(rc, "slim_prefill_step")
 
 
 def slim_attn_prefill_two_pass(cache, q, out, cu_q, kv_len, B, max_q, max_kv, Hq, sm_scale, workspace=None, stream=None):
     ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    rc = lib().slim_attn_prefill_two_pass(ctypes.byref(cache.struct), _ptr(q), _ptr(out), _ptr(cu_q), _ptr(kv_len),
+    rc = lib().slim_attn_prefill_two_pass(_cache8("slim_attn_prefill_two_pass", cache, B), _ptr(q), _ptr(out), _ptr(cu_q), _ptr(kv_len),
                                           B, max_q, max_kv, Hq, sm_scale, _ptr(workspace), ws_bytes, _stream(stream))
     _check(rc, "slim_attn_prefill_two_pass")
 
@@ -290,26 +303,26 @@ FULL_ROW_MAX_KEYS = 256
 def slim_attn_prefill_full_row(cache, q, out, cu_q, kv_len, B, max_q, max_kv, Hq, sm_scale, workspace=None, stream=None):
     """Prefill with the whole score row on chip (caches of at most FULL_ROW_MAX_KEYS tokens)."""
     ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    rc = lib().slim_attn_prefill_full_row(ctypes.byref(cache.struct), _ptr(q), _ptr(out), _ptr(cu_q), _ptr(kv_len),
+    rc = lib().slim_attn_prefill_full_row(_cache8("slim_attn_prefill_full_row", cache, B), _ptr(q), _ptr(out), _ptr(cu_q), _ptr(kv_len),
                                           B, max_q, max_kv, Hq, sm_scale, _ptr(workspace), ws_bytes, _stream(stream))
     _check(rc, "slim_attn_prefill_full_row")
 
 
 def slim_attn_decode(cache, q, out, kv_len, B, max_kv, Hq, sm_scale, workspace, stream=None):
     ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    rc = lib().slim_attn_decode(ctypes.byref(cache.struct), _ptr(q), _ptr(out), _ptr(kv_len), B, max_kv, Hq,
+    rc = lib().slim_attn_decode(_cache8("slim_attn_decode", cache, B), _ptr(q), _ptr(out), _ptr(kv_len), B, max_kv, Hq,
                                 sm_scale, _ptr(workspace), ws_bytes, _stream(stream))
     _check(rc, "slim_attn_decode")
 
 
 def slim_attn_decode_split(cache, q, kv_len, B, max_kv, Hq, sm_scale, workspace, stream=None, k_new=None, v_new=None):
-    rc = lib().slim_attn_decode_split(ctypes.byref(cache.struct), _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(kv_len), B, max_kv,
+    rc = lib().slim_attn_decode_split(_cache8("slim_attn_decode_split", cache, B), _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(kv_len), B, max_kv,
                                       Hq, sm_scale, _ptr(workspace), _nbytes(workspace), _stream(stream))
     _check(rc, "slim_attn_decode_split")
 
 
 def slim_attn_decode_merge(cache, out, kv_len, B, max_kv, Hq, workspace, stream=None):
-    rc = lib().slim_attn_decode_merge(ctypes.byref(cache.struct), _ptr(out), _ptr(kv_len), B, max_kv, Hq,
+    rc = lib().slim_attn_decode_merge(_cache8("slim_attn_decode_merge", cache, B), _ptr(out), _ptr(kv_len), B, max_kv, Hq,
                                       _ptr(workspace), _nbytes(workspace), _stream(stream))
     _check(rc, "slim_attn_decode_merge")
 
@@ -322,7 +335,7 @@ def slim_attn_decode_static(cache, q, out, kv_len, B, max_kv, Hq, sm_scale, stre
     """slim_attn_decode without a workspace argument: partials go to the library's built-in
     8 MiB device array, for callers that may not allocate.  Calls sharing a device must not
     overlap on the GPU."""
-    rc = lib().slim_attn_decode_static(ctypes.byref(cache.struct), _ptr(q), _ptr(out), _ptr(kv_len), B, max_kv, Hq,
+    rc = lib().slim_attn_decode_static(_cache8("slim_attn_decode_static", cache, B), _ptr(q), _ptr(out), _ptr(kv_len), B, max_kv, Hq,
                                        sm_scale, _stream(stream))
     _check(rc, "slim_attn_decode_static")
 
@@ -333,7 +346,7 @@ PARTIAL_FLOATS = 132   # fp32 per (sequence, query head) row of slim_attn_decode
 def slim_attn_decode_partial(cache, q, partial, kv_len, B, max_kv, Hq, sm_scale, workspace, stream=None):
     """slim_attn_decode over the part of the keys this device holds, without the final normalisation:
     partial fp32 [B, Hq, PARTIAL_FLOATS] receives every row's merged (O, M, l)."""
-    rc = lib().slim_attn_decode_partial(ctypes.byref(cache.struct), _ptr(q), _ptr(partial), _ptr(kv_len), B, max_kv, Hq,
+    rc = lib().slim_attn_decode_partial(_cache8("slim_attn_decode_partial", cache, B), _ptr(q), _ptr(partial), _ptr(kv_len), B, max_kv, Hq,
                                         sm_scale, _ptr(workspace), _nbytes(workspace), _stream(stream))
     _check(rc, "slim_attn_decode_partial")
 
@@ -360,7 +373,7 @@ def slim_static_selftest_timeout(stream=None):
 
 def slim_decode_step(cache, q, k_new, v_new, out, kv_len, B, max_kv, Hq, sm_scale, workspace, stream=None):
     """Appends one token per sequence at position kv_len - 1 and attends over kv_len tokens, in one kernel."""
-    rc = lib().slim_decode_step(ctypes.byref(cache.struct), _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(out), _ptr(kv_len),
+    rc = lib().slim_decode_step(_cache8("slim_decode_step", cache, B), _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(out), _ptr(kv_len),
                                 B, max_kv, Hq, sm_scale, _ptr(workspace), _nbytes(workspace), _stream(stream))
     _check(rc, "slim_decode_step")
 
@@ -368,7 +381,7 @@ def slim_decode_step(cache, q, k_new, v_new, out, kv_len, B, max_kv, Hq, sm_scal
 def slim_decode_step_host(cache, q_host, k_new_host, v_new_host, out_host, staging, kv_len, B, max_kv, Hq, sm_scale,
                           workspace, stream=None):
     """q_host / k_new_host / v_new_host / out_host are CPU (pinned) bf16 tensors."""
-    rc = lib().slim_decode_step_host(ctypes.byref(cache.struct), _ptr(q_host), _ptr(k_new_host), _ptr(v_new_host),
+    rc = lib().slim_decode_step_host(_cache8("slim_decode_step_host", cache, B), _ptr(q_host), _ptr(k_new_host), _ptr(v_new_host),
                                      _ptr(out_host), _ptr(staging), _nbytes(staging), _ptr(kv_len), B, max_kv, Hq,
                                      sm_scale, _ptr(workspace), _nbytes(workspace), _stream(stream))
     _check(rc, "slim_decode_step_host")
@@ -460,7 +473,7 @@ def slim_norm_rope_append(cache, nr, q, q_out, k, v, positions, cu_new, start_po
         _bad_rows(where + " (q, k, v and the cache differ in tokens or kv heads)")
     if positions is not None and (positions.dtype is not torch.int32 or positions.numel() != nr.n_axes * n or not positions.is_contiguous()):
         _bad_rows(where)
-    rc = lib().slim_norm_rope_append(ctypes.byref(cache.struct), nr.ref, _addr(q), qs, _addr(q_out), k.data_ptr(), ks, v.data_ptr(), vs,
+    rc = lib().slim_norm_rope_append(_cache8("slim_norm_rope_append", cache, B), nr.ref, _addr(q), qs, _addr(q_out), k.data_ptr(), ks, v.data_ptr(), vs,
                                      _addr(positions), cu_new.data_ptr(), start_pos.data_ptr(), B, n, hq, _cuda_stream(stream))
     _check(rc, where)
 
@@ -468,7 +481,7 @@ def slim_norm_rope_append(cache, nr, q, q_out, k, v, positions, cu_new, start_po
 def slim_attn_decode_shared(cache, q, out, cu_group, shared_len, kv_len, n_groups, B, max_group, max_shared, max_tail, Hq, sm_scale,
                             workspace, stream=None, k_new=None, v_new=None):
     """Decode attention of a batch whose groups of sequences share a prefix of shared_len tokens (the same pages)."""
-    rc = lib().slim_attn_decode_shared(ctypes.byref(cache.struct), _addr(q), _addr(k_new), _addr(v_new), _addr(out), _addr(cu_group),
+    rc = lib().slim_attn_decode_shared(_cache8("slim_attn_decode_shared", cache, B), _addr(q), _addr(k_new), _addr(v_new), _addr(out), _addr(cu_group),
                                        _addr(shared_len), _addr(kv_len), n_groups, B, max_group, max_shared, max_tail, Hq, sm_scale,
                                        _addr(workspace), _nbytes(workspace), _cuda_stream(stream))
     _check(rc, "slim_attn_decode_shared")
@@ -489,7 +502,7 @@ def slim_attn_decode_weights(cache, q, out, weight_in, weight_out, weighed, kv_l
                              k_new=None, v_new=None):
     """slim_attn_decode that also accumulates attention weights: fp32 [B, Hkv, stride], weight_in may be weight_out or None."""
     stride = _slots("slim_attn_decode_weights", B, cache.Hkv, weight_out, (weight_in, torch.float32))
-    rc = lib().slim_attn_decode_weights(ctypes.byref(cache.struct), _addr(q), _addr(k_new), _addr(v_new), _addr(out), _addr(weight_in),
+    rc = lib().slim_attn_decode_weights(_cache8("slim_attn_decode_weights", cache, B), _addr(q), _addr(k_new), _addr(v_new), _addr(out), _addr(weight_in),
                                         _addr(weight_out), stride, _addr(weighed), _addr(kv_len), B, max_kv, Hq, sm_scale, decay,
                                         _addr(workspace), _nbytes(workspace), _cuda_stream(stream))
     _check(rc, "slim_attn_decode_weights")
@@ -500,7 +513,7 @@ def slim_kv_evict(cache, weight_in, weight_out, pos_in, pos_out, kv_len, placed,
     """Keeps `budget` tokens of every (sequence, kv head); weights fp32 and positions int32 [B, Hkv, stride] follow them.
     The lengths afterwards are min(kv_len, budget)."""
     stride = _slots("slim_kv_evict", B, cache.Hkv, weight_out, (weight_in, torch.float32), (pos_in, torch.int32), (pos_out, torch.int32))
-    rc = lib().slim_kv_evict(ctypes.byref(cache.struct), _addr(weight_in), _addr(weight_out), _addr(pos_in), _addr(pos_out), stride,
+    rc = lib().slim_kv_evict(_cache8("slim_kv_evict", cache, B), _addr(weight_in), _addr(weight_out), _addr(pos_in), _addr(pos_out), stride,
                              _addr(kv_len), _addr(placed), _addr(seen), B, max_kv, budget, n_sink, n_recent, _addr(workspace),
                              _nbytes(workspace), _cuda_stream(stream))
     _check(rc, "slim_kv_evict")
@@ -545,10 +558,6 @@ class SlimCache4(_BlockTable):
 # together only when they fail.  get_device() is -1 for what no GPU can read.
 _BF16, _INT = torch.bfloat16, torch.int32
 _device, _raw_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
-
-
-def _refuse(where, what):
-    raise SlimError(SLIM_ERR_INVALID_ARG, f"{where}: {what}")
 
 
 def _cache4(where, cache, B):

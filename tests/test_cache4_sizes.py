@@ -95,3 +95,32 @@ def test_one_tensor_on_the_host(which):
                 fn()
         else:
             fn()
+
+
+WS = torch.zeros(1 << 20, dtype=torch.uint8)
+ONE, LENS = rows(B, HQ), i32(B)
+INT8 = {
+    "slim_kv_append": lambda c: slim.slim_kv_append(c, rows(B, HKV), rows(B, HKV), i32(B + 1), LENS, B, 1, STREAM),
+    "slim_attn_prefill": lambda c: slim.slim_attn_prefill(c, ONE, ONE, i32(B + 1), LENS, B, 1, 256, HQ, 0.1, WS, STREAM),
+    "slim_prefill_step": lambda c: slim.slim_prefill_step(c, ONE, rows(B, HKV), rows(B, HKV), ONE, i32(B + 1), LENS, B, 1, 256, HQ, 0.1, WS, STREAM),
+    "slim_attn_prefill_two_pass": lambda c: slim.slim_attn_prefill_two_pass(c, ONE, ONE, i32(B + 1), LENS, B, 1, 256, HQ, 0.1, WS, STREAM),
+    "slim_attn_prefill_full_row": lambda c: slim.slim_attn_prefill_full_row(c, ONE, ONE, i32(B + 1), LENS, B, 1, 256, HQ, 0.1, WS, STREAM),
+    "slim_attn_decode": lambda c: slim.slim_attn_decode(c, ONE, ONE, LENS, B, 256, HQ, 0.1, WS, STREAM),
+    "slim_attn_decode_split": lambda c: slim.slim_attn_decode_split(c, ONE, LENS, B, 256, HQ, 0.1, WS, STREAM),
+    "slim_attn_decode_static": lambda c: slim.slim_attn_decode_static(c, ONE, ONE, LENS, B, 256, HQ, 0.1, STREAM),
+    "slim_attn_decode_partial": lambda c: slim.slim_attn_decode_partial(c, ONE, WS, LENS, B, 256, HQ, 0.1, WS, STREAM),
+    "slim_decode_step": lambda c: slim.slim_decode_step(c, ONE, rows(B, HKV), rows(B, HKV), ONE, LENS, B, 256, HQ, 0.1, WS, STREAM),
+}
+
+
+class STREAM:
+    cuda_stream = 0
+
+
+@pytest.mark.parametrize("name", INT8)
+def test_int8_calls_on_a_smaller_table(name):
+    cache = slim.SlimCache(B, HKV, 2, device="cpu")
+    cache.set_block_table(i32(B - 1, 2))
+    with pytest.raises(slim.SlimError, match="block table") as e:
+        INT8[name](cache)
+    assert e.value.code == slim.SLIM_ERR_INVALID_ARG
