@@ -540,7 +540,12 @@ int slim_kv4_append(const slim_cache4_t *cache, const void *k_new, const void *v
 int slim_kv4_read(const slim_cache4_t *cache, void *k_out, void *v_out, const int32_t *cu, const int32_t *start_pos,
                   int32_t B, int32_t max_rows, void *stream);
 
-/* slim_attn_prefill and slim_prefill_step over the 4-bit cache: arguments, workspace and errors are theirs. */
+/*
+ * slim_attn_prefill and slim_prefill_step over the 4-bit cache: arguments, workspace and errors are theirs.
+ * The values held, z + u s, are rounded to fp16 before they are multiplied: 2^-11 of each, or 17 x 2^-25 of the largest in the
+ * page's 128 tokens where that is more; so are the weights, as in slim_attn_prefill.  Decode multiplies the codes themselves and
+ * has no such rounding of keys and values.  It is more than the 4-bit code loses where |z| is beyond 1000 to 2000 s.
+ */
 int slim_attn4_prefill(const slim_cache4_t *cache, const void *q, void *out,
                        const int32_t *cu_q, const int32_t *kv_len,
                        int32_t B, int32_t max_q, int32_t max_kv, int32_t Hq, float sm_scale,
@@ -559,9 +564,10 @@ int slim_prefill4_step(const slim_cache4_t *cache, const void *q, const void *k_
  *              appends nothing and attends over the tokens that fit
  *   workspace  device, 16-byte aligned, at least slim_attn4_workspace_bytes(Hq, Hkv) bytes, whatever the batch and lengths;
  *              header as for slim_attn_decode.  Two calls that can overlap need one each
- * Scores are exact to fp32; the products of a token's weight and its scale are rounded to fp16 (2^-11 of each of a result's
- * terms).  The copies read whole halves of a page (64 slots), whatever the length; what lies behind it is ignored.  B *
- * num_kv_heads * max_kv / 64 beyond 31 bits is SLIM_ERR_UNSUPPORTED.
+ * Scores are exact to fp32; the products of a token's weight and its V scale are rounded to fp16: 2^-11 of each, or, where that
+ * is more, 2^-34 of the sequence's largest scale.  Query and value rows may have magnitudes up to 2^100.  The copies read whole
+ * halves of a page (64 slots), whatever the length; what lies behind it is ignored.  B * num_kv_heads * max_kv / 64 beyond 31
+ * bits is SLIM_ERR_UNSUPPORTED.
  */
 int slim_attn4_decode(const slim_cache4_t *cache, const void *q, const void *k_new, const void *v_new, void *out,
                       const int32_t *kv_len, int32_t B, int32_t max_kv, int32_t Hq, float sm_scale,
@@ -612,7 +618,8 @@ typedef struct slim_layer {
  *   layers     host array of n_layers pools (0: tables only)
  *   result     device int32 [2]: pages that are missing, pages free afterwards.  Where pages are missing nothing else is
  *              written: free some and call again
- *   workspace  device, 16-byte aligned, at least slim_pages_workspace_bytes(num_pages, most rows) bytes; no initialisation
+ *   workspace  device, 16-byte aligned, at least slim_pages_workspace_bytes(num_pages, most rows) bytes; no initialisation.  Two
+ *              calls that can overlap need one each
  */
 int slim_pages_fork(const slim_pages_t *from, const slim_pages_t *to, const int32_t *parent, const int32_t *kv_len,
                     int32_t *len_out, const slim_layer_t *layers, int32_t n_layers, int32_t *result,

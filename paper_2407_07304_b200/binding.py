@@ -557,7 +557,7 @@ class SlimCache4(_BlockTable):
 # tokens go through here too, where the host's time is the step's, so the checks are few calls and their words are put
 # together only when they fail.  get_device() is -1 for what no GPU can read.
 _BF16, _INT = torch.bfloat16, torch.int32
-_device, _raw_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
+_device, _raw_stream = (getattr(torch._C, n, None) for n in ("_cuda_getDevice", "_cuda_getCurrentRawStream"))
 
 
 def _cache4(where, cache, B):

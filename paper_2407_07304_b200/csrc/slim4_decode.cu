@@ -35,7 +35,8 @@
 // eight warps of 255 registers, 3.9 TB/s (64 x 32768 tokens, 32 / 2 heads, 571 MB: 147 us).
 //
 // Query rows are held as fp16 after division by a power of two near the row's largest value: exact down to 2^-24 of it.
-// The weights p_j s_j are rounded to fp16 (2^-11 of each), p_j itself, its sum and the offset's sum stay fp32.
+// The weights p_j s_j are rounded to fp16 (2^-11 of each, 2^-34 of the largest scale at least), p_j itself, its sum and the offset's
+// sum stay fp32.
 // Every wait is bounded; a wait that runs out raises the status word and the warp writes nothing more.
 #include <cuda.h>
 
@@ -924,9 +925,11 @@ static int launch_d4(const slim_cache4_t *c, const Decode4Params &p, int max_kv,
     if (rc != SLIM_OK) return rc;
     rc = allow_dynamic_smem(reinterpret_cast<const void *>(slim4_decode_kernel<kHeads, kStep>), (int)D4<kHeads>::kBytes);
     if (rc != SLIM_OK) return rc;
-    // Few pairs on many blocks (one sequence of 32768 tokens on two kv heads: 74 blocks each): a second kernel merges them,
-    // 17.5 us against 20.7 with the last blocks doing it in two steps; for more pairs its launch costs more than it saves (32
-    // ragged sequences, 64 / 8 heads: 32.5 us against 28.3).
+    // Few pairs on many blocks: a second kernel merges them.  In us, the last block merging / the second kernel, with one, eight
+    // and sixteen query heads per kv head, one sequence of 32768 tokens: 74 blocks per pair 20.8 / 13.0, 23.4 / 15.6, 37.2 / 17.6;
+    // 18.5 blocks 17.9 / 18.0, 20.2 / 18.1, 27.1 / 21.9; 9.2 blocks 22.2 / 23.4, 25.3 / 24.0, 35.7 / 29.9; 4.6 blocks 33.2 / 35.0 and
+    // 36.4 / 36.5 (four sequences of 8192: 19.0 / 18.7).  With more pairs its launch costs more than it saves (32 ragged
+    // sequences, 64 / 8 heads, 0.6 blocks: 28.3 / 32.5).
     const bool defer = blocks > kD4Few * pairs;
     Decode4Params q = p;
     if (defer) q.counters = nullptr;

@@ -533,7 +533,8 @@ slim_prefill_tc_kernel(const __grid_constant__ CUtensorMap codes_map, const Pref
                     const int r = gr * 8 + (lane >> 2);
                     const uint4 w4 = *reinterpret_cast<const uint4 *>(raw + gr * 512 + lane * 16);
                     const uint32_t row_scale = (r < n_valid) ? scales[r] : 0u;
-                    // scale and offset are bf16, over a power of two not far from the larger one: exact in fp16 down to 2^-14 of it
+                    // scale and offset are bf16, over a power of two not far from the tile's largest value: exact in fp16 down to 2^-17 of
+                    // it, 2^-25 off below; the value is rounded once, to fp16 (2^-11, or 2^-25), as every operand of these products is
                     const float f = pair_scale(row_scale) * rex, z = pair_offset(row_scale) * rex;
                     const uint32_t fac2 = pack_half2(f, f), off2 = pack_half2(z, z);
                     unsigned char *dstb = dst_tile + r * 128;
